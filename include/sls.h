@@ -418,6 +418,132 @@ int sls_lanczos_topr_noalloc(const float* Phi, int64_t N, int D, int r,
                              double* beta, void* stream);
 
 /*
+ * ---------------------------------------------------------------------------
+ * Attention over the macro-tokens (what follows the pass: prefill of the
+ * compressed prompt, Sec. 3.1 and Fig. 1, at the macro-tokens' positions,
+ * Sec. 3.4, and decoding behind it).  Three calls share one paged cache of
+ * keys and values:
+ *   sls_qkv_append         norm and rotate the new queries and keys, append
+ *                          keys and values to the cache
+ *   sls_attention_prefill  packed prompts of new tokens over the cache
+ *   sls_attention_decode   one new token per sequence over the cache
+ *
+ * A batch has B sequences; sequence s has n_s new tokens, packed one sequence
+ * after the other (cu_seqlens: B + 1 ascending int32 offsets), and kv_lens[s]
+ * tokens in the cache, the new ones included: new token i of s has cache
+ * index x = kv_lens[s] - n_s + i.  Cache index x of s lives in slot
+ * x % page_size of page page_table[s * table_ld + x / page_size].  Slots that
+ * no sequence's length covers are never used: they may hold anything, NaN
+ * included.  Lengths are cut to what the table holds (max_pages pages); a page
+ * number outside [0, num_pages) reads as zeros and is not written.
+ * ---------------------------------------------------------------------------
+ */
+typedef struct sls_kv_cache {
+  void* k;                   /* num_pages x page_size x kv_heads x head_dim    */
+  void* v;                   /* the same layout and strides                    */
+  int dtype;                 /* SLS_BF16 or SLS_F16                            */
+  int kv_heads;
+  int head_dim;              /* multiple of 8, 8..SLS_MAX_HEAD_DIM             */
+  int page_size;             /* power of two, 16..1024                         */
+  int64_t num_pages;
+  int64_t page_stride;       /* strides in elements, multiples of 8; a head's  */
+  int64_t slot_stride;       /* head_dim elements are contiguous               */
+  int64_t head_stride;
+  const int32_t* page_table; /* B rows of max_pages page numbers               */
+  int64_t table_ld;          /* row stride of the table, >= max_pages          */
+  int max_pages;
+  const int32_t* kv_lens;    /* B                                              */
+  int64_t batch;             /* B                                              */
+} sls_kv_cache_t;
+
+/* Packed rows (token, head) of head_dim contiguous elements; strides in
+ * elements, multiples of 8 (16-byte aligned rows). */
+typedef struct sls_rows {
+  void* data;
+  int64_t token_stride;
+  int64_t head_stride;
+} sls_rows_t;
+
+/*
+ * Rotation of the first 2 * pairs elements of a head by the token's position
+ * p: pair i (elements i and pairs + i, or 2 i and 2 i + 1 when interleaved)
+ * turns by the angle p * inv_freq[i] and is scaled by `scale`:
+ *   a' = scale (a cos t - b sin t),  b' = scale (b cos t + a sin t).
+ * inv_freq: `pairs` floats, so any scaling for long contexts is a choice of
+ * frequencies.  The angle is reduced from the exact product p * inv_freq[i].
+ */
+typedef struct sls_rope {
+  const float* inv_freq;
+  int pairs;                 /* 0..head_dim / 2 */
+  int interleaved;
+  float scale;
+} sls_rope_t;
+
+#define SLS_F16 2             /* cache and query dtype of the attention calls */
+#define SLS_MAX_HEAD_DIM 128
+#define SLS_MAX_HEAD_GROUP 128 /* query heads per key head */
+
+/*
+ * Appends T new tokens to the cache and rotates their queries.  For every
+ * (token, head) row x of q and k, in float32 and rounded once at the end:
+ *   y = weight * x / sqrt(mean(x^2) + eps)   (skipped when the weight is NULL)
+ *   the rotation of `rope`                   (skipped when rope is NULL)
+ * y goes to q_out for queries and to the cache for keys; values are copied.
+ * q, q_out: T x q_heads rows (q_out may be q itself); k, v: T x kv_heads rows;
+ * q_weight, k_weight: head_dim elements of the cache's dtype, or NULL;
+ * cu_seqlens: B + 1 offsets, or NULL for one token per sequence (T = B);
+ * positions: T int32, or NULL for the cache index.  kv_lens counts the new
+ * tokens.  A token outside every sequence, or whose cache index is negative or
+ * past the table, is not appended (its query is still written).  Two sequences
+ * must not append to the same slot.
+ * Errors: INVALID_ARG (sizes, NULL pointers, strides or pointers that break
+ * the 16-byte rule), UNSUPPORTED (dtype, head_dim, page_size, head ratio).
+ */
+int sls_qkv_append(const sls_rows_t* q, const sls_rows_t* k, const sls_rows_t* v, int64_t T,
+                   int q_heads, const sls_kv_cache_t* cache, const int32_t* cu_seqlens,
+                   const int32_t* positions, const void* q_weight, const void* k_weight,
+                   float eps, const sls_rope_t* rope, const sls_rows_t* q_out, void* stream);
+
+/*
+ * Attention of packed new tokens over the cache (their own keys and values
+ * appended before):
+ *   out_i = sum_j softmax_j(scale q_i . k_j) v_j
+ * over the cache indices j <= x_i of the token's sequence (causal), or all
+ * j < kv_lens[s]; query head h reads key head h / (q_heads / kv_heads).  A row
+ * with no keys is zero.  A key or value that a row does not see does not
+ * change it, whatever it holds.  q, out: T x q_heads rows in the cache's dtype;
+ * a token outside every sequence is not written.
+ * workspace: sls_attention_prefill_workspace_size() bytes (may be 0), holding
+ * nothing between calls.
+ * Errors: as sls_qkv_append, and WORKSPACE.
+ */
+size_t sls_attention_prefill_workspace_size(int64_t T, int q_heads, const sls_kv_cache_t* cache);
+int sls_attention_prefill(const sls_rows_t* q, int64_t T, int q_heads,
+                          const sls_kv_cache_t* cache, const int32_t* cu_seqlens, int causal,
+                          float scale, const sls_rows_t* out, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/*
+ * The single-token form: row s of q (B x q_heads rows) attends to all
+ * kv_lens[s] tokens of sequence s; a sequence of length 0 gives zeros.  The
+ * work of all sequences is cut into equal parts along the cached tokens, and
+ * the parts of a row are joined in a fixed order.  workspace:
+ * sls_attention_decode_workspace_size() bytes, holding nothing between calls.
+ * Errors: as sls_qkv_append, and WORKSPACE.
+ */
+size_t sls_attention_decode_workspace_size(int q_heads, const sls_kv_cache_t* cache);
+int sls_attention_decode(const sls_rows_t* q, int q_heads, const sls_kv_cache_t* cache,
+                         float scale, const sls_rows_t* out, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
+/*
+ * Reads (synchronously, on `stream`) and clears the current device's status
+ * word of the attention kernels: SLS_OK, or SLS_ERR_TIMEOUT when a device-side
+ * wait of one of them gave up since the last reading.
+ */
+int sls_attention_status(void* stream);
+
+/*
  * Optional per-phase timing of sls_compress.  `events` is a host array of
  * 2 * SLS_NUM_PHASES cudaEvent_t handles (passed as void*) owned by the
  * caller; while set, every sls_compress call records events[2p] on its

@@ -8,7 +8,9 @@ library is not built, importing the functions works but every call raises.
 
 The same names as the C entry points are exported:
 ``feature_map``, ``lanczos_topr``, ``simhash``, ``aggregate``, ``compress``,
-``embed_gather``, ``compress_tokens``.
+``embed_gather``, ``compress_tokens``; the attention calls behind the pass
+(``qkv_append``, ``attention_prefill``, ``attention_decode``) are in
+``attention.py``.
 """
 from __future__ import annotations
 
@@ -593,3 +595,10 @@ def workspace_status(workspace: Workspace) -> int:
     """Device status word of a compress workspace (0 = ok, 5 = timeout)."""
     return int(lib().sls_workspace_status(_ptr(workspace.buf),
                                           _stream(workspace.buf)))
+
+
+from . import attention as _attention  # noqa: E402  (needs the names above)
+from .attention import *  # noqa: E402,F401,F403
+
+EXPORTED.update(_attention.EXPORTED)
+__all__ += _attention.__all__
