@@ -445,7 +445,7 @@ typedef struct sls_kv_cache {
   int kv_heads;
   int head_dim;              /* multiple of 8, 8..SLS_MAX_HEAD_DIM             */
   int page_size;             /* power of two, 16..1024                         */
-  int64_t num_pages;
+  int64_t num_pages;         /* >= 1                                           */
   int64_t page_stride;       /* strides in elements, multiples of 8; a head's  */
   int64_t slot_stride;       /* head_dim elements are contiguous               */
   int64_t head_stride;
@@ -512,7 +512,7 @@ int sls_qkv_append(const sls_rows_t* q, const sls_rows_t* k, const sls_rows_t* v
  * j < kv_lens[s]; query head h reads key head h / (q_heads / kv_heads).  A row
  * with no keys is zero.  A key or value that a row does not see does not
  * change it, whatever it holds.  q, out: T x q_heads rows in the cache's dtype;
- * a token outside every sequence is not written.
+ * a token outside every sequence is not written.  scale > 0, finite.
  * workspace: sls_attention_prefill_workspace_size() bytes (may be 0), holding
  * nothing between calls.
  * Errors: as sls_qkv_append, and WORKSPACE.

@@ -108,5 +108,8 @@ struct AttnArgs {
   float scale;
 };
 int launch_attention(const AttnArgs& a, int dtype, cudaStream_t stream);
+int launch_attention_prefill(const AttnArgs& a, int dtype, cudaStream_t stream);
+// Device address of the current device's status word.
+int attention_status_word(int** word);
 
 }  // namespace sls

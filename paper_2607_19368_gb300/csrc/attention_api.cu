@@ -8,6 +8,9 @@ namespace {
 
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;
 
+// The running maximum is taken of unscaled scores.
+bool scale_ok(float s) { return s > 0.f && s <= 3.402823466e38f; }
+
 bool aligned16(const void* p) { return p != nullptr && (uintptr_t)p % 16 == 0; }
 
 // A packed-rows argument of T tokens; the pointer may be NULL when there are none.
@@ -25,7 +28,7 @@ int rows_view(const sls_rows_t* r, int64_t T, int head_dim, RowsView* out) {
 
 int cache_view(const sls_kv_cache_t* c, int q_heads, CacheView* v) {
   if (!c || q_heads < 1 || c->kv_heads < 1) return SLS_ERR_INVALID_ARG;
-  if (c->batch < 0 || c->max_pages < 0 || c->num_pages < 0 || c->table_ld < c->max_pages)
+  if (c->batch < 0 || c->max_pages < 0 || c->num_pages < 1 || c->table_ld < c->max_pages)
     return SLS_ERR_INVALID_ARG;
   if (q_heads % c->kv_heads != 0) return SLS_ERR_INVALID_ARG;
   if (c->dtype != SLS_BF16 && c->dtype != SLS_F16) return SLS_ERR_UNSUPPORTED;
@@ -38,7 +41,7 @@ int cache_view(const sls_kv_cache_t* c, int q_heads, CacheView* v) {
   if (c->page_stride < 0 || c->page_stride % 8 || c->slot_stride % 8 || c->head_stride % 8 ||
       c->slot_stride < c->head_dim || c->head_stride < c->head_dim)
     return SLS_ERR_INVALID_ARG;
-  if (c->num_pages > 0 && (!aligned16(c->k) || !aligned16(c->v))) return SLS_ERR_INVALID_ARG;
+  if (!aligned16(c->k) || !aligned16(c->v)) return SLS_ERR_INVALID_ARG;
   if (c->batch > 0 && (!c->kv_lens || (c->max_pages > 0 && !c->page_table)))
     return SLS_ERR_INVALID_ARG;
   v->k = (char*)c->k;
@@ -108,7 +111,7 @@ int sls_attention_prefill(const sls_rows_t* q, int64_t T, int q_heads,
   AttnArgs a{};
   int st = cache_view(cache, q_heads, &a.c);
   if (st != SLS_OK) return st;
-  if (T < 0 || T > kMaxTokens || !cu_seqlens) return SLS_ERR_INVALID_ARG;
+  if (T < 0 || T > kMaxTokens || !cu_seqlens || !scale_ok(scale)) return SLS_ERR_INVALID_ARG;
   if ((st = rows_view(q, T, cache->head_dim, &a.q)) != SLS_OK ||
       (st = rows_view(out, T, cache->head_dim, &a.out)) != SLS_OK)
     return st;
@@ -117,7 +120,7 @@ int sls_attention_prefill(const sls_rows_t* q, int64_t T, int q_heads,
   a.cu = cu_seqlens;
   a.causal = causal != 0;
   a.scale = scale;
-  return launch_attention(a, cache->dtype, (cudaStream_t)stream);
+  return launch_attention_prefill(a, cache->dtype, (cudaStream_t)stream);
 }
 
 size_t sls_attention_decode_workspace_size(int q_heads, const sls_kv_cache_t* cache) {
@@ -131,6 +134,7 @@ int sls_attention_decode(const sls_rows_t* q, int q_heads, const sls_kv_cache_t*
   AttnArgs a{};
   int st = cache_view(cache, q_heads, &a.c);
   if (st != SLS_OK) return st;
+  if (!scale_ok(scale)) return SLS_ERR_INVALID_ARG;
   a.T = cache->batch;
   if ((st = rows_view(q, a.T, cache->head_dim, &a.q)) != SLS_OK ||
       (st = rows_view(out, a.T, cache->head_dim, &a.out)) != SLS_OK)
@@ -141,8 +145,9 @@ int sls_attention_decode(const sls_rows_t* q, int q_heads, const sls_kv_cache_t*
 }
 
 int sls_attention_status(void* stream) {
-  (void)stream;
-  return SLS_OK;
+  int* word = nullptr;
+  int st = attention_status_word(&word);
+  return st != SLS_OK ? st : sls_workspace_status(word, stream);
 }
 
 }  // extern "C"

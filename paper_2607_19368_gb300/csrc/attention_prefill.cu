@@ -1,0 +1,825 @@
+// Attention of packed new tokens over the paged cache on the 5th-generation tensor
+// cores (sm_103a):  O = softmax(scale Q K^T + mask) V.
+#include <cuda.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "attention.cuh"
+
+namespace sls {
+
+namespace {
+
+constexpr int AP_BM = 128;             // rows of a query tile: (token, head of the group)
+constexpr int AP_BN = 128;             // keys of a step
+constexpr int AP_SOFT_WARPS = 8;       // two warpgroups, one per query tile
+constexpr int AP_THREADS = 384;        // and one warpgroup of which two warps work
+constexpr int AP_LOAD_WARP = AP_SOFT_WARPS, AP_MMA_WARP = AP_SOFT_WARPS + 1;
+constexpr int AP_ITEMS = 2;            // item slots
+constexpr float AP_LAZY = 8.f;         // log2 of the growth of the maximum that is let pass
+
+__device__ int g_attn_status;
+
+template <int HD>
+struct ApShape {
+  static constexpr int HALVES = HD / 64;
+  static constexpr int HALF_BYTES = 128 * 128;          // 128 rows of 64 16-bit elements
+  static constexpr int TILE_BYTES = HALVES * HALF_BYTES;
+  static constexpr int STAGES = HD == 128 ? 5 : 8;
+  static constexpr size_t SMEM = (size_t)(2 + STAGES) * TILE_BYTES + 1024;
+};
+
+struct ApItem {
+  int seq;            // -1: no more items
+  int head;           // key head
+  int tok0;           // first packed token of the pair of tiles
+  int ntok;           // tokens of the pair
+  int tiles[2];       // key steps of each query tile
+  int len;            // cached tokens of the sequence
+  int lim0;           // keys that the pair's first token sees, before cutting to [0, len]
+  int causal;
+};
+
+// ---- tcgen05 / TMA wrappers ------------------------------------------------------
+
+// 128-byte swizzle matrix descriptor; lbo: bytes between 64-element blocks along M
+// or N for an operand whose M or N runs along the rows (unused otherwise).
+SLS_DEV uint64_t ap_desc(uint32_t smem_addr, uint32_t lbo) {
+  uint64_t d = 0;
+  d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
+  d |= (uint64_t)(lbo >> 4) << 16;
+  d |= (uint64_t)(1024u >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+
+SLS_DEV void ap_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(acc)
+      : "memory");
+}
+SLS_DEV void ap_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(acc)
+      : "memory");
+}
+SLS_DEV void ap_commit(uint64_t* bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
+          smem_u32(bar))
+      : "memory");
+}
+SLS_DEV void ap_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+SLS_DEV void ap_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+SLS_DEV void ap_ld32(uint32_t addr, float* v) {
+  uint32_t* u = reinterpret_cast<uint32_t*>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]),
+        "=r"(u[7]), "=r"(u[8]), "=r"(u[9]), "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]),
+        "=r"(u[14]), "=r"(u[15]), "=r"(u[16]), "=r"(u[17]), "=r"(u[18]), "=r"(u[19]),
+        "=r"(u[20]), "=r"(u[21]), "=r"(u[22]), "=r"(u[23]), "=r"(u[24]), "=r"(u[25]),
+        "=r"(u[26]), "=r"(u[27]), "=r"(u[28]), "=r"(u[29]), "=r"(u[30]), "=r"(u[31])
+      : "r"(addr));
+}
+SLS_DEV void ap_st32(uint32_t addr, const float* v) {
+  const uint32_t* u = reinterpret_cast<const uint32_t*>(v);
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(
+          addr),
+      "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]),
+      "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]),
+      "r"(u[15]), "r"(u[16]), "r"(u[17]), "r"(u[18]), "r"(u[19]), "r"(u[20]), "r"(u[21]),
+      "r"(u[22]), "r"(u[23]), "r"(u[24]), "r"(u[25]), "r"(u[26]), "r"(u[27]), "r"(u[28]),
+      "r"(u[29]), "r"(u[30]), "r"(u[31])
+      : "memory");
+}
+SLS_DEV void ap_st16(uint32_t addr, const uint32_t* u) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(addr),
+      "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]),
+      "r"(u[8]), "r"(u[9]), "r"(u[10]), "r"(u[11]), "r"(u[12]), "r"(u[13]), "r"(u[14]),
+      "r"(u[15])
+      : "memory");
+}
+// Loads before this are in their registers after it; the empty statements keep
+// the compiler from using a register earlier.
+template <int N>
+SLS_DEV void ap_wait_ld(float* v) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+f"(v[i]));
+}
+SLS_DEV void ap_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+SLS_DEV void ap_tma3(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+      : "memory");
+}
+SLS_DEV void ap_tma4(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w,
+                     uint64_t* bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+      : "memory");
+}
+
+SLS_DEV float ap_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Bounded wait of a whole warp; false when the time is up or another role gave up.
+SLS_DEV bool ap_wait(uint64_t* bar, unsigned parity, volatile int* abort_flag) {
+  bool ok = mbar_try_wait(bar, parity);
+  if (!ok) {
+    const long long t0 = clock64();
+    for (unsigned it = 0;; ++it) {
+      ok = mbar_try_wait(bar, parity);
+      if (ok || ((it & 63) == 63 && (*abort_flag || clock64() - t0 > SLS_WAIT_CYCLES))) break;
+    }
+  }
+  return __all_sync(0xffffffffu, ok);
+}
+
+// ---- the order of the work ---------------------------------------------------------
+// An item is a pair of query tiles (2 * tpt tokens of one sequence, all query heads
+// of one key head).  Items go from the longest (most keys) to the shortest, and CTA
+// b of g takes numbers b, 2g-1-b, 2g+b, ...: neighbours in the order cost about the
+// same, so turning the direction every round evens the sums out.  An item is found
+// from its number by a warp without any table: the number of blocks with at least c
+// key steps is a closed form per sequence, summed over the sequences by the lanes,
+// and a search over c narrows to the item's level.
+struct ApOrder {
+  const int32_t* cu;
+  CacheView c;
+  int64_t T;
+  int qb;       // tokens of a block
+  int causal;
+  int level;    // an upper bound of the next item's level
+  int total;    // blocks of all sequences
+};
+
+SLS_DEV void ap_lens(const ApOrder& o, int s, int& n, int& m) {
+  int64_t q0, q1;
+  seq_rows(o.cu, s, o.T, q0, q1);
+  n = (int)(q1 - q0);
+  m = max(o.c.kv_lens[s], 0);
+}
+
+// blocks of a sequence whose key steps number at least c
+SLS_DEV int ap_count(const ApOrder& o, int n, int m, int c) {
+  const int nb = (n + o.qb - 1) / o.qb;
+  if (c <= 0) return nb;
+  const int x = (c - 1) * AP_BN;  // more than x keys
+  if (m <= x) return 0;
+  if (!o.causal) return nb;
+  const int e = x - (m - n) + 1;  // the block's last token is number e or later
+  return e <= 0 ? nb : nb - min(nb, (e + o.qb - 1) / o.qb - 1);
+}
+
+SLS_DEV int ap_count_all(const ApOrder& o, int c) {
+  int sum = 0;
+  for (int s = threadIdx.x & 31; s < o.c.B; s += 32) {
+    int n, m;
+    ap_lens(o, s, n, m);
+    sum += ap_count(o, n, m, c);
+  }
+  return __reduce_add_sync(0xffffffffu, sum);
+}
+
+SLS_DEV void ap_order_init(ApOrder& o) {
+  int top = 0;
+  for (int s = threadIdx.x & 31; s < o.c.B; s += 32) top = max(top, max(o.c.kv_lens[s], 0));
+  o.level = (__reduce_max_sync(0xffffffffu, top) + AP_BN - 1) / AP_BN;
+  o.total = ap_count_all(o, 0);
+}
+
+// the item number i; false when there is none
+SLS_DEV bool ap_find(ApOrder& o, int64_t i, int tpt, ApItem& it) {
+  const int heads = o.c.kv_heads;
+  if (i >= (int64_t)o.total * heads) return false;
+  const int j = (int)(i / heads);
+  // the highest level with more than j blocks at or above it
+  int lo = 0, hi = o.level;
+  int above = 0;  // blocks above the level
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    const int cnt = ap_count_all(o, mid);
+    if (cnt > j) {
+      lo = mid;
+    } else {
+      hi = mid - 1;
+      above = cnt;
+    }
+  }
+  o.level = lo;
+  if (hi == o.level && above == 0) above = ap_count_all(o, lo + 1);
+  int left = j - above;
+  const int lane = threadIdx.x & 31;
+  for (int s0 = 0; s0 < o.c.B; s0 += 32) {
+    const int s = s0 + lane;
+    int n = 0, m = 0, mine = 0, b0 = 0;
+    if (s < o.c.B) {
+      ap_lens(o, s, n, m);
+      const int ge = ap_count(o, n, m, lo), gt = ap_count(o, n, m, lo + 1);
+      mine = ge - gt;
+      b0 = (n + o.qb - 1) / o.qb - ge;  // the level's first block
+      if (!o.causal) b0 = 0;
+    }
+    int pre = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int x = __shfl_up_sync(0xffffffffu, pre, d);
+      if (lane >= d) pre += x;
+    }
+    const int all = __shfl_sync(0xffffffffu, pre, 31);
+    if (left < all) {
+      const unsigned hit = __ballot_sync(0xffffffffu, left < pre);
+      const int src = __ffs(hit) - 1;
+      const int b = __shfl_sync(0xffffffffu, b0 + left - (pre - mine), src);
+      n = __shfl_sync(0xffffffffu, n, src);
+      m = __shfl_sync(0xffffffffu, m, src);
+      it.seq = s0 + src;
+      int64_t q0, q1;
+      seq_rows(o.cu, it.seq, o.T, q0, q1);
+      it.head = (int)(i - (int64_t)j * heads);
+      it.tok0 = (int)q0 + b * o.qb;
+      it.ntok = min(o.qb, n - b * o.qb);
+      it.len = (int)cache_len(o.c, it.seq);
+      it.causal = o.causal;
+      it.lim0 = o.causal ? m - n + b * o.qb + 1 : it.len;
+      for (int t = 0; t < 2; ++t) {
+        const int nt = min(tpt, it.ntok - t * tpt);  // tokens of the tile
+        const int lim = o.causal ? it.lim0 + t * tpt + nt - 1 : it.len;
+        it.tiles[t] = nt > 0 ? (max(0, min(lim, it.len)) + AP_BN - 1) / AP_BN : 0;
+      }
+      return true;
+    }
+    left -= all;
+  }
+  return false;
+}
+
+// ---- a row by itself -----------------------------------------------------------------
+// The tensor cores multiply a hidden key's weight 0 with its value, and 0 times
+// infinity or NaN is NaN: a row whose result is not finite is computed again by one
+// warp over the keys that it sees and no others (lanes hold four elements each).
+template <typename E>
+SLS_DEV void ap_row(const CacheView& c, const char* q, char* out, int seq,
+                                    int head, int keys, float scale) {
+  const int lane = threadIdx.x & 31, e0 = 4 * lane;
+  const bool on = e0 < c.head_dim;
+  float x[4] = {0.f, 0.f, 0.f, 0.f}, o[4] = {0.f, 0.f, 0.f, 0.f};
+  if (on) {
+    const uint2 u = *reinterpret_cast<const uint2*>(q + 2 * e0);
+    const float2 a = Half2<E>::widen(u.x), b = Half2<E>::widen(u.y);
+    x[0] = a.x * scale, x[1] = a.y * scale, x[2] = b.x * scale, x[3] = b.y * scale;
+  }
+  float mx = -INFINITY, l = 0.f;
+  for (int j = 0; j < keys; ++j) {
+    const int64_t page = c.table[seq * c.table_ld + (j >> c.page_shift)];
+    float k[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (on && page >= 0 && page < c.num_pages) {
+      const int64_t off = page * c.page_b + (j & ((1 << c.page_shift) - 1)) * c.slot_b +
+                          head * c.head_b + 2 * e0;
+      const uint2 ku = *reinterpret_cast<const uint2*>(c.k + off);
+      const uint2 vu = *reinterpret_cast<const uint2*>(c.v + off);
+      const float2 k0 = Half2<E>::widen(ku.x), k1 = Half2<E>::widen(ku.y);
+      const float2 v0 = Half2<E>::widen(vu.x), v1 = Half2<E>::widen(vu.y);
+      k[0] = k0.x, k[1] = k0.y, k[2] = k1.x, k[3] = k1.y;
+      v[0] = v0.x, v[1] = v0.y, v[2] = v1.x, v[3] = v1.y;
+    }
+    float d = x[0] * k[0] + x[1] * k[1] + x[2] * k[2] + x[3] * k[3];
+#pragma unroll
+    for (int s = 16; s > 0; s >>= 1) d += __shfl_xor_sync(0xffffffffu, d, s);
+    const float mn = fmaxf(mx, d);
+    const float base = mn == -INFINITY ? 0.f : mn;
+    const float corr = __expf(mx - base), p = __expf(d - base);
+    l = l * corr + p;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = o[e] * corr + p * v[e];
+    mx = mn;
+  }
+  const float inv = keys > 0 ? 1.f / l : 0.f;
+  if (on)
+    *reinterpret_cast<uint2*>(out + 2 * e0) = make_uint2(
+        Half2<E>::narrow(o[0] * inv, o[1] * inv), Half2<E>::narrow(o[2] * inv, o[3] * inv));
+}
+
+// ---- the kernel --------------------------------------------------------------------
+template <typename E, int HD>
+__global__ void __launch_bounds__(AP_THREADS, 1)
+attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
+                         const __grid_constant__ CUtensorMap tmK,
+                         const __grid_constant__ CUtensorMap tmV,
+                         const __grid_constant__ AttnArgs a) {
+  using S = ApShape<HD>;
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  __shared__ uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], done_bar;
+  __shared__ uint64_t kv_full[S::STAGES], kv_empty[S::STAGES];
+  __shared__ uint64_t item_full[AP_ITEMS], item_empty[AP_ITEMS];
+  __shared__ ApItem s_item[AP_ITEMS];
+  __shared__ uint32_t tmem_holder;
+  __shared__ volatile int s_abort;
+
+  unsigned char* smem = reinterpret_cast<unsigned char*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  const uint32_t q_smem = smem_u32(smem);
+  const uint32_t kv_smem = q_smem + 2 * S::TILE_BYTES;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int group = a.q_heads / a.c.kv_heads;
+  const int tpt = AP_BM / group;  // tokens of a query tile
+
+  if (threadIdx.x == 0) {
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&q_full[t], 1);
+      mbar_init(&q_empty[t], 1);
+      mbar_init(&s_full[t], 1);
+      mbar_init(&p_full[t], AP_SOFT_WARPS / 2);
+      mbar_init(&o_full[t], 1);
+    }
+    for (int s = 0; s < S::STAGES; ++s) {
+      mbar_init(&kv_full[s], 1);
+      mbar_init(&kv_empty[s], 1);
+    }
+    for (int s = 0; s < AP_ITEMS; ++s) {
+      mbar_init(&item_full[s], 1);
+      mbar_init(&item_empty[s], AP_SOFT_WARPS + 1);
+    }
+    mbar_init(&done_bar, 1);
+    mbar_fence_init();
+    s_abort = 0;
+  }
+  if (warp == AP_MMA_WARP) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                     smem_u32(&tmem_holder)),
+                 "r"(512)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  ap_fence_before();
+  __syncthreads();
+  ap_fence_after();
+  const uint32_t tmem = tmem_holder;
+  // columns: scores (and, over them, weights) of the two tiles, then their outputs
+  const uint32_t tm_s[2] = {tmem, tmem + AP_BN};
+  const uint32_t tm_o[2] = {tmem + 2 * AP_BN, tmem + 2 * AP_BN + HD};
+
+  auto fail = [&]() {
+    s_abort = 1;
+    atomicExch(&g_attn_status, SLS_ERR_TIMEOUT);
+  };
+
+  // registers: 384 x 168 at launch, 2 x 128 x 208 + 128 x 88 from here
+  if (warp >= AP_SOFT_WARPS) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+
+  if (warp == AP_LOAD_WARP) {
+    // ------------------------------ items and copies ------------------------------
+    ApOrder o{a.cu, a.c, a.T, 2 * tpt, a.causal, 0, 0};
+    ap_order_init(o);
+    unsigned stage = 0, q_used[2] = {0, 0};
+    const int box = min(AP_BN, 1 << a.c.page_shift);  // slots of one copy
+    const int per_tile = AP_BN / box;
+    const int col_shift = min(7, a.c.page_shift);
+    bool ok = true;
+    for (unsigned k = 0; ok; ++k) {
+      const int64_t i = (int64_t)k * gridDim.x + ((k & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+      ApItem it;
+      it.seq = -1;
+      const bool any = ap_find(o, i, tpt, it);
+      const unsigned slot = k % AP_ITEMS, use = k / AP_ITEMS;
+      if (!ap_wait(&item_empty[slot], (use & 1) ^ 1, &s_abort)) {
+        if (lane == 0) fail();
+        break;
+      }
+      if (lane == 0) {
+        s_item[slot] = it;
+        mbar_arrive(&item_full[slot]);
+      }
+      if (!any) break;
+      const int nk = max(it.tiles[0], it.tiles[1]);
+      const int32_t* table = a.c.table + it.seq * a.c.table_ld;
+      // page numbers of the first key step: lane l holds that of copy l of the step
+      auto page_of = [&](int j) {
+        const int x = j * AP_BN + (lane << col_shift);
+        return (lane < per_tile && j < nk && x < it.len) ? table[x >> a.c.page_shift] : -1;
+      };
+      int page = page_of(0);
+      for (int j = 0; j < nk && ok; ++j) {
+        const int next = page_of(j + 1);
+        const int here = min(AP_BN, it.len - j * AP_BN);
+        const int copies = (here + box - 1) / box;  // of each half
+        const int slot0 = (j * AP_BN) & ((1 << a.c.page_shift) - 1);
+        for (int kv = 0; kv < 2 && ok; ++kv) {
+          if (j == 0) {
+            // the query tiles of the item: the first before the first keys, the
+            // second after them
+            const int t = kv;
+            if (it.tiles[t] > 0) {
+              if (!ap_wait(&q_empty[t], (q_used[t] & 1) ^ 1, &s_abort)) {
+                if (lane == 0) fail();
+                ok = false;
+                break;
+              }
+              ++q_used[t];
+              if (lane == 0) {
+                mbar_expect_tx(&q_full[t], S::HALVES * group * tpt * 128);
+                for (int h = 0; h < S::HALVES; ++h)
+                  ap_tma3(q_smem + t * S::TILE_BYTES + h * S::HALF_BYTES, &tmQ, 64 * h,
+                          it.head * group, it.tok0 + t * tpt, &q_full[t]);
+              }
+            }
+          }
+          const unsigned st = stage % S::STAGES;
+          if (!ap_wait(&kv_empty[st], ((stage / S::STAGES) & 1) ^ 1, &s_abort)) {
+            if (lane == 0) fail();
+            ok = false;
+            break;
+          }
+          if (lane == 0) mbar_expect_tx(&kv_full[st], S::HALVES * copies * box * 128);
+          __syncwarp();
+          if (lane < copies) {
+            const uint32_t dst = kv_smem + st * S::TILE_BYTES + lane * box * 128;
+#pragma unroll
+            for (int h = 0; h < S::HALVES; ++h)
+              ap_tma4(dst + h * S::HALF_BYTES, kv ? &tmV : &tmK, 64 * h, slot0, it.head, page,
+                      &kv_full[st]);
+          }
+          ++stage;
+        }
+        page = next;
+      }
+    }
+    // every copy has landed before the CTA may exit
+    for (unsigned s = stage > S::STAGES ? stage - S::STAGES : 0; s < stage; ++s)
+      for (unsigned w = 0; w < (1u << 25); ++w)
+        if (mbar_try_wait(&kv_full[s % S::STAGES], (s / S::STAGES) & 1)) break;
+    for (int t = 0; t < 2; ++t)
+      if (q_used[t] > 0)
+        for (unsigned w = 0; w < (1u << 25); ++w)
+          if (mbar_try_wait(&q_full[t], (q_used[t] - 1) & 1)) break;
+  } else if (warp == AP_MMA_WARP) {
+    // ------------------------------ products -----------------------------------------
+    constexpr uint32_t fmt = std::is_same<E, __nv_bfloat16>::value ? 1u : 0u;
+    constexpr uint32_t id_common = (1u << 4) | (fmt << 7) | (fmt << 10) |
+                                   ((uint32_t)(AP_BM >> 4) << 24);
+    constexpr uint32_t id_s = id_common | ((uint32_t)(AP_BN >> 3) << 17);
+    constexpr uint32_t id_o = id_common | (1u << 16) | ((uint32_t)(HD >> 3) << 17);
+    unsigned stage = 0, q_used[2] = {0, 0}, p_used[2] = {0, 0};
+    bool ok = true;
+    // S_t = Q_t K^T from ring stage st
+    auto scores = [&](int t, unsigned st) {
+      if (lane == 0) {
+        const uint32_t qa = q_smem + t * S::TILE_BYTES, ka = kv_smem + st * S::TILE_BYTES;
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk) {
+          const uint32_t off = (kk >> 2) * S::HALF_BYTES + (kk & 3) * 32;
+          ap_mma_ss(tm_s[t], ap_desc(qa + off, 16), ap_desc(ka + off, 16), id_s, kk > 0);
+        }
+        ap_commit(&s_full[t]);
+      }
+    };
+    // O_t (+)= P_t V
+    auto values = [&](int t, unsigned st, bool acc) {
+      if (lane == 0) {
+        const uint32_t va = kv_smem + st * S::TILE_BYTES;
+#pragma unroll
+        for (int kk = 0; kk < AP_BN / 16; ++kk)
+          ap_mma_ts(tm_o[t], tm_s[t] + 8 * kk, ap_desc(va + 2048 * kk, S::HALF_BYTES), id_o,
+                    acc || kk > 0);
+      }
+    };
+    auto wait = [&](uint64_t* bar, unsigned parity) {
+      if (ok && !ap_wait(bar, parity, &s_abort)) {
+        if (lane == 0) fail();
+        ok = false;
+      }
+      ap_fence_after();
+      return ok;
+    };
+    for (unsigned k = 0; ok; ++k) {
+      const unsigned slot = k % AP_ITEMS;
+      if (!wait(&item_full[slot], (k / AP_ITEMS) & 1)) break;
+      const ApItem it = s_item[slot];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&item_empty[slot]);
+      if (it.seq < 0) break;
+      const int nk = max(it.tiles[0], it.tiles[1]);
+      if (nk == 0) continue;
+      const unsigned first = stage;  // the item's ring stages: K_0 V_0 K_1 V_1 ...
+      if (!wait(&kv_full[first % S::STAGES], (first / S::STAGES) & 1)) break;
+      for (int t = 0; t < 2; ++t) {
+        if (it.tiles[t] == 0) continue;
+        if (!wait(&q_full[t], q_used[t] & 1)) break;
+        ++q_used[t];
+        scores(t, first % S::STAGES);
+        if (it.tiles[t] == 1 && lane == 0) ap_commit(&q_empty[t]);
+      }
+      if (!ok) break;
+      if (lane == 0) ap_commit(&kv_empty[first % S::STAGES]);
+      for (int j = 0; j < nk && ok; ++j) {
+        const unsigned sv = first + 2 * j + 1, sk = sv + 1;
+        if (!wait(&kv_full[sv % S::STAGES], (sv / S::STAGES) & 1)) break;
+        if ((j + 1) * AP_BN > it.len) {
+          // values past the sequence's end: whatever their slots hold, zero here
+          const int r0 = it.len - j * AP_BN;
+          unsigned char* va = smem + (2 + sv % S::STAGES) * S::TILE_BYTES;
+          for (int x = r0 * 8 + lane; x < AP_BN * 8; x += 32)
+#pragma unroll
+            for (int h = 0; h < S::HALVES; ++h)
+              reinterpret_cast<uint4*>(va + h * S::HALF_BYTES)[x] = make_uint4(0, 0, 0, 0);
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+        }
+        for (int t = 0; t < 2; ++t) {
+          if (j >= it.tiles[t]) continue;
+          if (!wait(&p_full[t], p_used[t] & 1)) break;
+          ++p_used[t];
+          values(t, sv % S::STAGES, j > 0);
+          if (j + 1 < it.tiles[t]) {
+            if (!wait(&kv_full[sk % S::STAGES], (sk / S::STAGES) & 1)) break;
+            scores(t, sk % S::STAGES);
+            if (j + 2 == it.tiles[t] && lane == 0) ap_commit(&q_empty[t]);
+          } else if (lane == 0) {
+            ap_commit(&o_full[t]);
+          }
+        }
+        if (!ok) break;
+        if (lane == 0) {
+          ap_commit(&kv_empty[sv % S::STAGES]);
+          if (j + 1 < nk) ap_commit(&kv_empty[sk % S::STAGES]);
+        }
+      }
+      stage += 2 * nk;
+    }
+    // every product issued has completed before tensor memory is freed
+    if (lane == 0) ap_commit(&done_bar);
+    for (unsigned w = 0; w < (1u << 25); ++w)
+      if (mbar_try_wait(&done_bar, 0)) break;
+  }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    // ------------------------------ softmax, a row per thread --------------------------
+    const int t = warp >> 2;
+    const int row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t ts = tm_s[t] + lanes, to = tm_o[t] + lanes;
+    const int tok_in = row / group, head_in = row - tok_in * group;
+    const float c = a.scale * 1.4426950408889634f;
+    unsigned s_used = 0, o_used = 0;
+    bool ok = true;
+    for (unsigned k = 0; ok; ++k) {
+      const unsigned slot = k % AP_ITEMS;
+      if (!ap_wait(&item_full[slot], (k / AP_ITEMS) & 1, &s_abort)) {
+        if (lane == 0) fail();
+        break;
+      }
+      const ApItem it = s_item[slot];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&item_empty[slot]);
+      if (it.seq < 0) break;
+      const int tok = t * tpt + tok_in;  // within the pair
+      const bool live = row < group * tpt && tok < it.ntok;
+      const int keys = live ? max(0, min(it.len, it.causal ? it.lim0 + tok : it.len)) : 0;
+      const int nk = it.tiles[t];
+      // key steps before this one are seen whole by every live row of the warp
+      const int whole = __reduce_min_sync(0xffffffffu, live ? keys : 0x7fffffff) / AP_BN;
+      float mx = -INFINITY, l = 0.f;  // the maximum in use, the sum of weights under it
+      for (int j = 0; j < nk; ++j) {
+        if (!ap_wait(&s_full[t], s_used & 1, &s_abort)) {
+          if (lane == 0) fail();
+          ok = false;
+          break;
+        }
+        ++s_used;
+        ap_fence_after();
+        float s[AP_BN];
+#pragma unroll
+        for (int q = 0; q < AP_BN / 32; ++q) ap_ld32(ts + 32 * q, s + 32 * q);
+        ap_wait_ld<AP_BN>(s);
+        if (j >= whole) {
+          const int lim = keys - j * AP_BN;
+#pragma unroll
+          for (int e = 0; e < AP_BN; ++e) s[e] = e < lim ? s[e] : -INFINITY;
+        }
+        float top = fmaxf(s[0], s[1]);
+#pragma unroll
+        for (int e = 2; e < AP_BN; e += 2) top = fmaxf(fmaxf(top, s[e]), s[e + 1]);
+        if (j == 0) {
+          mx = top;
+        } else {
+          const float to_mx = fmaxf(mx, top);
+          // the output is brought to a new maximum only where the old one lets
+          // weights grow past 2^AP_LAZY
+          const bool grow = mx == -INFINITY ? to_mx > -INFINITY : (to_mx - mx) * c > AP_LAZY;
+          if (__any_sync(0xffffffffu, grow)) {
+            const float f = grow ? ap_exp2((mx - to_mx) * c) : 1.f;
+            if (grow) mx = to_mx;
+            l *= f;
+#pragma unroll 1
+            for (int q = 0; q < HD / 32; ++q) {
+              float o[32];
+              ap_ld32(to + 32 * q, o);
+              ap_wait_ld<32>(o);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] *= f;
+              ap_st32(to + 32 * q, o);
+            }
+          }
+        }
+        const float base = mx == -INFINITY ? 0.f : -mx * c;
+        const f32x2_t c2 = pk2(c, c), b2 = pk2(base, base);
+        f32x2_t sum = pk2(0.f, 0.f);
+#pragma unroll
+        for (int q = 0; q < AP_BN / 32; ++q) {
+          uint32_t p[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            float x, y;
+            upk2(fma2(pk2(s[32 * q + 2 * e], s[32 * q + 2 * e + 1]), c2, b2), x, y);
+            x = ap_exp2(x);
+            y = ap_exp2(y);
+            sum = add2(sum, pk2(x, y));
+            p[e] = Half2<E>::narrow(x, y);
+          }
+          ap_st16(ts + 16 * q, p);
+        }
+        ap_wait_st();
+        ap_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&p_full[t]);
+        float sx, sy;
+        upk2(sum, sx, sy);
+        l += sx + sy;
+      }
+      if (!ok) break;
+      const int64_t gt = it.tok0 + tok;
+      const int h = it.head * group + head_in;
+      char* out = a.out.data + gt * a.out.token_b + h * a.out.head_b;
+      const float inv = 1.f / l;
+      float odd = 0.f;  // NaN once any element is not finite
+      if (nk > 0) {
+        if (!ap_wait(&o_full[t], o_used & 1, &s_abort)) {
+          if (lane == 0) fail();
+          break;
+        }
+        ++o_used;
+        ap_fence_after();
+      }
+#pragma unroll
+      for (int q = 0; q < HD / 32; ++q) {
+        float o[32];
+        if (nk > 0) {
+          ap_ld32(to + 32 * q, o);
+          ap_wait_ld<32>(o);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) o[e] = 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < 32; e += 8) {
+          float x[8];
+#pragma unroll
+          for (int d = 0; d < 8; ++d) {
+            x[d] = keys > 0 ? o[e + d] * inv : 0.f;
+            odd = __fmaf_rn(x[d], 0.f, odd);
+          }
+          if (live && 32 * q + e < a.c.head_dim)
+            *reinterpret_cast<uint4*>(out + 2 * (32 * q + e)) = narrow8<E>(x);
+        }
+      }
+      ap_fence_before();
+      unsigned bad = __ballot_sync(0xffffffffu, live && !(odd == 0.f));
+      while (bad) {
+        const int src = __ffs(bad) - 1;
+        bad &= bad - 1;
+        const int64_t bt = __shfl_sync(0xffffffffu, (long long)gt, src);
+        const int bh = __shfl_sync(0xffffffffu, h, src);
+        const int bk = __shfl_sync(0xffffffffu, keys, src);
+        __syncwarp();
+        ap_row<E>(a.c, a.q.data + bt * a.q.token_b + bh * a.q.head_b,
+                  a.out.data + bt * a.out.token_b + bh * a.out.head_b, it.seq, it.head, bk,
+                  a.scale);
+      }
+    }
+  }
+  ap_fence_before();
+  __syncthreads();
+  if (warp == AP_MMA_WARP) {
+    ap_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512)
+                 : "memory");
+  }
+}
+
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
+                             const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeFn encode_tiled() {
+  static const EncodeFn fn = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
+                                         &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      p = nullptr;
+    return reinterpret_cast<EncodeFn>(p);
+  }();
+  return fn;
+}
+
+bool map_of(CUtensorMap* map, int dtype, int rank, const void* base, const cuuint64_t* dims,
+            const cuuint64_t* strides, const cuuint32_t* box) {
+  const EncodeFn fn = encode_tiled();
+  if (!fn) return false;
+  const cuuint32_t one[5] = {1, 1, 1, 1, 1};
+  return fn(map, dtype == SLS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                   : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+            (cuuint32_t)rank, const_cast<void*>(base), dims, strides, box, one,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename E, int HD>
+int launch(const AttnArgs& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
+           int grid, cudaStream_t stream) {
+  static bool set[64] = {};  // per device
+  int dev = 0;
+  SLS_CUDA_TRY(cudaGetDevice(&dev));
+  auto kern = attention_prefill_kernel<E, HD>;
+  if (dev >= 64 || !set[dev]) {
+    SLS_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                      (int)ApShape<HD>::SMEM));
+    if (dev < 64) set[dev] = true;
+  }
+  kern<<<grid, AP_THREADS, ApShape<HD>::SMEM, stream>>>(q, k, v, a);
+  SLS_LAUNCH_CHECK();
+  return SLS_OK;
+}
+
+}  // namespace
+
+int launch_attention_prefill(const AttnArgs& a, int dtype, cudaStream_t stream) {
+  if (a.T == 0 || a.c.B == 0) return SLS_OK;
+  const CacheView& c = a.c;
+  const int group = a.q_heads / c.kv_heads, tpt = AP_BM / group;
+  int dev = 0, sms = 0;
+  SLS_CUDA_TRY(cudaGetDevice(&dev));
+  SLS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  const int64_t items = ((a.T + 2 * tpt - 1) / (2 * tpt) + std::min<int64_t>(c.B, a.T)) *
+                        c.kv_heads;
+  const int grid = (int)std::min<int64_t>(items, sms);
+  CUtensorMap q, k, v;
+  {
+    const cuuint64_t dims[3] = {(cuuint64_t)c.head_dim, (cuuint64_t)a.q_heads, (cuuint64_t)a.T};
+    const cuuint64_t strides[2] = {(cuuint64_t)a.q.head_b, (cuuint64_t)a.q.token_b};
+    const cuuint32_t box[3] = {64, (cuuint32_t)group, (cuuint32_t)tpt};
+    if (!map_of(&q, dtype, 3, a.q.data, dims, strides, box)) return SLS_ERR_UNSUPPORTED;
+  }
+  {
+    const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)1 << c.page_shift,
+                                (cuuint64_t)c.kv_heads, (cuuint64_t)std::max<int64_t>(c.num_pages, 1)};
+    const cuuint64_t strides[3] = {(cuuint64_t)c.slot_b, (cuuint64_t)c.head_b,
+                                   (cuuint64_t)c.page_b};
+    const cuuint32_t box[4] = {64, (cuuint32_t)std::min(128, 1 << c.page_shift), 1, 1};
+    if (!map_of(&k, dtype, 4, c.k, dims, strides, box) ||
+        !map_of(&v, dtype, 4, c.v, dims, strides, box))
+      return SLS_ERR_UNSUPPORTED;
+  }
+  const bool wide = c.head_dim > 64;
+  if (dtype == SLS_BF16)
+    return wide ? launch<__nv_bfloat16, 128>(a, q, k, v, grid, stream)
+                : launch<__nv_bfloat16, 64>(a, q, k, v, grid, stream);
+  return wide ? launch<__half, 128>(a, q, k, v, grid, stream)
+              : launch<__half, 64>(a, q, k, v, grid, stream);
+}
+
+int attention_status_word(int** word) {
+  void* p = nullptr;
+  SLS_CUDA_TRY(cudaGetSymbolAddress(&p, g_attn_status));
+  *word = (int*)p;
+  return SLS_OK;
+}
+
+}  // namespace sls
