@@ -107,9 +107,13 @@ struct AttnArgs {
   int causal;
   float scale;
 };
-int launch_attention(const AttnArgs& a, int dtype, cudaStream_t stream);
 int launch_attention_prefill(const AttnArgs& a, int dtype, cudaStream_t stream);
-// Device address of the current device's status word.
-int attention_status_word(int** word);
+// The single-token form (cu NULL); workspace: attention_decode_workspace() bytes.
+size_t attention_decode_workspace(const CacheView& c, int q_heads);
+int launch_attention_decode(const AttnArgs& a, int dtype, void* workspace, cudaStream_t stream);
+// Device addresses of the current device's status words, set when a device-side
+// wait of the kernel gives up.
+int prefill_status_word(int** word);
+int decode_status_word(int** word);
 
 }  // namespace sls

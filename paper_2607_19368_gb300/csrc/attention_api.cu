@@ -124,8 +124,8 @@ int sls_attention_prefill(const sls_rows_t* q, int64_t T, int q_heads,
 }
 
 size_t sls_attention_decode_workspace_size(int q_heads, const sls_kv_cache_t* cache) {
-  (void)q_heads, (void)cache;
-  return 0;
+  CacheView c;
+  return cache_view(cache, q_heads, &c) == SLS_OK ? attention_decode_workspace(c, q_heads) : 0;
 }
 
 int sls_attention_decode(const sls_rows_t* q, int q_heads, const sls_kv_cache_t* cache,
@@ -141,13 +141,17 @@ int sls_attention_decode(const sls_rows_t* q, int q_heads, const sls_kv_cache_t*
     return st;
   a.q_heads = q_heads;
   a.scale = scale;
-  return launch_attention(a, cache->dtype, (cudaStream_t)stream);
+  const size_t need = attention_decode_workspace(a.c, q_heads);
+  if (need > 0 && (!aligned16(workspace) || workspace_bytes < need)) return SLS_ERR_WORKSPACE;
+  return launch_attention_decode(a, cache->dtype, workspace, (cudaStream_t)stream);
 }
 
 int sls_attention_status(void* stream) {
-  int* word = nullptr;
-  int st = attention_status_word(&word);
-  return st != SLS_OK ? st : sls_workspace_status(word, stream);
+  int* word[2] = {nullptr, nullptr};
+  int st = prefill_status_word(&word[0]);
+  if (st == SLS_OK) st = decode_status_word(&word[1]);
+  for (int i = 0; i < 2 && st == SLS_OK; ++i) st = sls_workspace_status(word[i], stream);
+  return st;
 }
 
 }  // extern "C"

@@ -5,11 +5,13 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "attention.cuh"
+#include "attention_tma.cuh"
 
 namespace sls {
 
 namespace {
+
+__device__ int g_status;  // SLS_ERR_TIMEOUT once a wait gave up
 
 constexpr int AP_BM = 128;             // rows of a query tile: (token, head of the group)
 constexpr int AP_BN = 128;             // keys of a step
@@ -18,8 +20,6 @@ constexpr int AP_THREADS = 384;        // and one warpgroup of which two warps w
 constexpr int AP_LOAD_WARP = AP_SOFT_WARPS, AP_MMA_WARP = AP_SOFT_WARPS + 1;
 constexpr int AP_ITEMS = 2;            // item slots
 constexpr float AP_LAZY = 8.f;         // log2 of the growth of the maximum that is let pass
-
-__device__ int g_attn_status;
 
 template <int HD>
 struct ApShape {
@@ -123,28 +123,6 @@ SLS_DEV void ap_wait_ld(float* v) {
   for (int i = 0; i < N; ++i) asm volatile("" : "+f"(v[i]));
 }
 SLS_DEV void ap_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-SLS_DEV void ap_tma3(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
-      : "memory");
-}
-SLS_DEV void ap_tma4(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w,
-                     uint64_t* bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-      " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
-      : "memory");
-}
-
-SLS_DEV float ap_exp2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 
 // Bounded wait of a whole warp; false when the time is up or another role gave up.
 SLS_DEV bool ap_wait(uint64_t* bar, unsigned parity, volatile int* abort_flag) {
@@ -385,7 +363,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
 
   auto fail = [&]() {
     s_abort = 1;
-    atomicExch(&g_attn_status, SLS_ERR_TIMEOUT);
+    atomicExch(&g_status, SLS_ERR_TIMEOUT);
   };
 
   // registers: 384 x 168 at launch, 2 x 128 x 208 + 128 x 88 from here
@@ -444,7 +422,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
               if (lane == 0) {
                 mbar_expect_tx(&q_full[t], S::HALVES * group * tpt * 128);
                 for (int h = 0; h < S::HALVES; ++h)
-                  ap_tma3(q_smem + t * S::TILE_BYTES + h * S::HALF_BYTES, &tmQ, 64 * h,
+                  at_tma3(q_smem + t * S::TILE_BYTES + h * S::HALF_BYTES, &tmQ, 64 * h,
                           it.head * group, it.tok0 + t * tpt, &q_full[t]);
               }
             }
@@ -461,7 +439,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
             const uint32_t dst = kv_smem + st * S::TILE_BYTES + lane * box * 128;
 #pragma unroll
             for (int h = 0; h < S::HALVES; ++h)
-              ap_tma4(dst + h * S::HALF_BYTES, kv ? &tmV : &tmK, 64 * h, slot0, it.head, page,
+              at_tma4(dst + h * S::HALF_BYTES, kv ? &tmV : &tmK, 64 * h, slot0, it.head, page,
                       &kv_full[st]);
           }
           ++stage;
@@ -632,7 +610,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
           // weights grow past 2^AP_LAZY
           const bool grow = mx == -INFINITY ? to_mx > -INFINITY : (to_mx - mx) * c > AP_LAZY;
           if (__any_sync(0xffffffffu, grow)) {
-            const float f = grow ? ap_exp2((mx - to_mx) * c) : 1.f;
+            const float f = grow ? at_exp2((mx - to_mx) * c) : 1.f;
             if (grow) mx = to_mx;
             l *= f;
 #pragma unroll 1
@@ -656,8 +634,8 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
           for (int e = 0; e < 16; ++e) {
             float x, y;
             upk2(fma2(pk2(s[32 * q + 2 * e], s[32 * q + 2 * e + 1]), c2, b2), x, y);
-            x = ap_exp2(x);
-            y = ap_exp2(y);
+            x = at_exp2(x);
+            y = at_exp2(y);
             sum = add2(sum, pk2(x, y));
             p[e] = Half2<E>::narrow(x, y);
           }
@@ -731,36 +709,6 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
   }
 }
 
-typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
-                             const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeFn encode_tiled() {
-  static const EncodeFn fn = [] {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault,
-                                         &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess)
-      p = nullptr;
-    return reinterpret_cast<EncodeFn>(p);
-  }();
-  return fn;
-}
-
-bool map_of(CUtensorMap* map, int dtype, int rank, const void* base, const cuuint64_t* dims,
-            const cuuint64_t* strides, const cuuint32_t* box) {
-  const EncodeFn fn = encode_tiled();
-  if (!fn) return false;
-  const cuuint32_t one[5] = {1, 1, 1, 1, 1};
-  return fn(map, dtype == SLS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
-                                   : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
-            (cuuint32_t)rank, const_cast<void*>(base), dims, strides, box, one,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <typename E, int HD>
 int launch(const AttnArgs& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
            int grid, cudaStream_t stream) {
@@ -795,16 +743,11 @@ int launch_attention_prefill(const AttnArgs& a, int dtype, cudaStream_t stream) 
     const cuuint64_t dims[3] = {(cuuint64_t)c.head_dim, (cuuint64_t)a.q_heads, (cuuint64_t)a.T};
     const cuuint64_t strides[2] = {(cuuint64_t)a.q.head_b, (cuuint64_t)a.q.token_b};
     const cuuint32_t box[3] = {64, (cuuint32_t)group, (cuuint32_t)tpt};
-    if (!map_of(&q, dtype, 3, a.q.data, dims, strides, box)) return SLS_ERR_UNSUPPORTED;
+    if (!at_map(&q, dtype, 3, a.q.data, dims, strides, box)) return SLS_ERR_UNSUPPORTED;
   }
   {
-    const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)1 << c.page_shift,
-                                (cuuint64_t)c.kv_heads, (cuuint64_t)std::max<int64_t>(c.num_pages, 1)};
-    const cuuint64_t strides[3] = {(cuuint64_t)c.slot_b, (cuuint64_t)c.head_b,
-                                   (cuuint64_t)c.page_b};
-    const cuuint32_t box[4] = {64, (cuuint32_t)std::min(128, 1 << c.page_shift), 1, 1};
-    if (!map_of(&k, dtype, 4, c.k, dims, strides, box) ||
-        !map_of(&v, dtype, 4, c.v, dims, strides, box))
+    const int slots = std::min(AP_BN, 1 << c.page_shift);
+    if (!at_cache_map(&k, dtype, c, c.k, slots) || !at_cache_map(&v, dtype, c, c.v, slots))
       return SLS_ERR_UNSUPPORTED;
   }
   const bool wide = c.head_dim > 64;
@@ -815,9 +758,9 @@ int launch_attention_prefill(const AttnArgs& a, int dtype, cudaStream_t stream) 
               : launch<__half, 64>(a, q, k, v, grid, stream);
 }
 
-int attention_status_word(int** word) {
+int prefill_status_word(int** word) {
   void* p = nullptr;
-  SLS_CUDA_TRY(cudaGetSymbolAddress(&p, g_attn_status));
+  SLS_CUDA_TRY(cudaGetSymbolAddress(&p, g_status));
   *word = (int*)p;
   return SLS_OK;
 }
