@@ -16,8 +16,9 @@ __device__ int g_status;  // SLS_ERR_TIMEOUT once a wait gave up
 constexpr int AP_BM = 128;             // rows of a query tile: (token, head of the group)
 constexpr int AP_BN = 128;             // keys of a step
 constexpr int AP_SOFT_WARPS = 8;       // two warpgroups, one per query tile
-constexpr int AP_THREADS = 384;        // and one warpgroup of which two warps work
-constexpr int AP_LOAD_WARP = AP_SOFT_WARPS, AP_MMA_WARP = AP_SOFT_WARPS + 1;
+constexpr int AP_THREADS = 384;        // and one warpgroup of single warps
+constexpr int AP_LOAD_WARP = AP_SOFT_WARPS, AP_MMA_WARP = AP_SOFT_WARPS + 1,
+              AP_RING_WARP = AP_SOFT_WARPS + 2;  // and the next
 constexpr int AP_ITEMS = 2;            // item slots
 constexpr float AP_LAZY = 8.f;         // log2 of the growth of the maximum that is let pass
 
@@ -26,8 +27,9 @@ struct ApShape {
   static constexpr int HALVES = HD / 64;
   static constexpr int HALF_BYTES = 128 * 128;          // 128 rows of 64 16-bit elements
   static constexpr int TILE_BYTES = HALVES * HALF_BYTES;
-  static constexpr int STAGES = HD == 128 ? 5 : 8;
-  static constexpr size_t SMEM = (size_t)(2 + STAGES) * TILE_BYTES + 1024;
+  static constexpr int STAGES = HD == 128 ? 4 : 8;
+  static constexpr int OUT_BYTES = 32 * 128;            // 64 elements of a warp's 32 rows
+  static constexpr size_t SMEM = (size_t)(2 + STAGES) * TILE_BYTES + AP_SOFT_WARPS * OUT_BYTES + 1024;
 };
 
 struct ApItem {
@@ -43,37 +45,43 @@ struct ApItem {
 
 // ---- tcgen05 / TMA wrappers ------------------------------------------------------
 
-// 128-byte swizzle matrix descriptor; lbo: bytes between 64-element blocks along M
-// or N for an operand whose M or N runs along the rows (unused otherwise).
-SLS_DEV uint64_t ap_desc(uint32_t smem_addr, uint32_t lbo) {
-  uint64_t d = 0;
-  d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
-  d |= (uint64_t)(lbo >> 4) << 16;
-  d |= (uint64_t)(1024u >> 4) << 32;
-  d |= (uint64_t)1 << 46;
-  d |= (uint64_t)2 << 61;
-  return d;
+// 128-byte swizzle matrix descriptor (stride between eight-row groups 1024 bytes):
+// the high word is fixed, the low word holds the address and the leading offset, the
+// bytes between 64-element blocks along N for an operand whose N runs along the rows
+// (unused otherwise), both in units of 16 bytes.
+constexpr uint32_t AP_DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);
+SLS_DEV uint32_t ap_desc(uint32_t smem_addr, uint32_t lead) {
+  return ((smem_addr & 0x3FFFFu) >> 4) | ((lead >> 4) << 16);
 }
 
-SLS_DEV void ap_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+// D (+)= A B with A in shared memory / in tensor memory
+SLS_DEV void ap_mma_ss(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(acc)
+      "{\n .reg .pred p, q;\n .reg .b64 x, y;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %6, 0;\n"
+      " mov.b64 x, {%1, %5};\n mov.b64 y, {%2, %5};\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(acc), "n"(AP_DESC_HI), "r"(lead)
       : "memory");
 }
-SLS_DEV void ap_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+SLS_DEV void ap_mma_ts(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(acc)
+      "{\n .reg .pred p, q;\n .reg .b64 y;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %6, 0;\n"
+      " mov.b64 y, {%2, %5};\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(acc), "n"(AP_DESC_HI), "r"(lead)
       : "memory");
 }
-SLS_DEV void ap_commit(uint64_t* bar) {
+SLS_DEV void ap_commit(uint32_t lead, uint64_t* bar) {
   asm volatile(
-      "tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(
-          smem_u32(bar))
+      "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
+      " @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(
+          smem_u32(bar)), "r"(lead)
       : "memory");
+}
+SLS_DEV uint32_t ap_elect() {
+  uint32_t r;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
+  return r;
 }
 SLS_DEV void ap_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 SLS_DEV void ap_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -123,6 +131,12 @@ SLS_DEV void ap_wait_ld(float* v) {
   for (int i = 0; i < N; ++i) asm volatile("" : "+f"(v[i]));
 }
 SLS_DEV void ap_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+SLS_DEV float ap_max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
 
 // Bounded wait of a whole warp; false when the time is up or another role gave up.
 SLS_DEV bool ap_wait(uint64_t* bar, unsigned parity, volatile int* abort_flag) {
@@ -249,6 +263,8 @@ SLS_DEV bool ap_find(ApOrder& o, int64_t i, int tpt, ApItem& it) {
         const int lim = o.causal ? it.lim0 + t * tpt + nt - 1 : it.len;
         it.tiles[t] = nt > 0 ? (max(0, min(lim, it.len)) + AP_BN - 1) / AP_BN : 0;
       }
+      // the second tile, unless empty, has the item's last step
+      if (it.tiles[1] > 0) it.tiles[1] = max(it.tiles[0], it.tiles[1]);
       return true;
     }
     left -= all;
@@ -311,7 +327,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
                          const __grid_constant__ AttnArgs a) {
   using S = ApShape<HD>;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
-  __shared__ uint64_t q_full[2], q_empty[2], s_full[2], p_full[2], o_full[2], done_bar;
+  __shared__ uint64_t q_full[2], q_empty[2], s_full[2], p_half[2], p_full[2], o_full[2], done_bar;
   __shared__ uint64_t kv_full[S::STAGES], kv_empty[S::STAGES];
   __shared__ uint64_t item_full[AP_ITEMS], item_empty[AP_ITEMS];
   __shared__ ApItem s_item[AP_ITEMS];
@@ -331,6 +347,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
       mbar_init(&q_full[t], 1);
       mbar_init(&q_empty[t], 1);
       mbar_init(&s_full[t], 1);
+      mbar_init(&p_half[t], AP_SOFT_WARPS / 2 + 1);
       mbar_init(&p_full[t], AP_SOFT_WARPS / 2);
       mbar_init(&o_full[t], 1);
     }
@@ -340,7 +357,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
     }
     for (int s = 0; s < AP_ITEMS; ++s) {
       mbar_init(&item_full[s], 1);
-      mbar_init(&item_empty[s], AP_SOFT_WARPS + 1);
+      mbar_init(&item_empty[s], AP_SOFT_WARPS + 3);
     }
     mbar_init(&done_bar, 1);
     mbar_fence_init();
@@ -357,9 +374,8 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
   __syncthreads();
   ap_fence_after();
   const uint32_t tmem = tmem_holder;
-  // columns: scores (and, over them, weights) of the two tiles, then their outputs
-  const uint32_t tm_s[2] = {tmem, tmem + AP_BN};
-  const uint32_t tm_o[2] = {tmem + 2 * AP_BN, tmem + 2 * AP_BN + HD};
+  // columns of tensor memory: scores (and, over them, weights) of the two tiles, then
+  // their outputs
 
   auto fail = [&]() {
     s_abort = 1;
@@ -379,11 +395,15 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
     const int per_tile = AP_BN / box;
     const int col_shift = min(7, a.c.page_shift);
     bool ok = true;
-    for (unsigned k = 0; ok; ++k) {
-      const int64_t i = (int64_t)k * gridDim.x + ((k & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-      ApItem it;
+    auto find = [&](unsigned k, ApItem& it) {
       it.seq = -1;
-      const bool any = ap_find(o, i, tpt, it);
+      ap_find(o, (int64_t)k * gridDim.x + ((k & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x), tpt,
+              it);
+    };
+    ApItem following;
+    find(0, following);
+    for (unsigned k = 0; ok; ++k) {
+      const ApItem it = following;
       const unsigned slot = k % AP_ITEMS, use = k / AP_ITEMS;
       if (!ap_wait(&item_empty[slot], (use & 1) ^ 1, &s_abort)) {
         if (lane == 0) fail();
@@ -393,7 +413,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         s_item[slot] = it;
         mbar_arrive(&item_full[slot]);
       }
-      if (!any) break;
+      if (it.seq < 0) break;
       const int nk = max(it.tiles[0], it.tiles[1]);
       const int32_t* table = a.c.table + it.seq * a.c.table_ld;
       // page numbers of the first key step: lane l holds that of copy l of the step
@@ -402,6 +422,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         return (lane < per_tile && j < nk && x < it.len) ? table[x >> a.c.page_shift] : -1;
       };
       int page = page_of(0);
+      if (nk == 0) find(k + 1, following);
       for (int j = 0; j < nk && ok; ++j) {
         const int next = page_of(j + 1);
         const int here = min(AP_BN, it.len - j * AP_BN);
@@ -445,6 +466,8 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
           ++stage;
         }
         page = next;
+        // the next item is looked for while the ring is full
+        if (j == min(nk - 1, 1)) find(k + 1, following);
       }
     }
     // every copy has landed before the CTA may exit
@@ -456,71 +479,131 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         for (unsigned w = 0; w < (1u << 25); ++w)
           if (mbar_try_wait(&q_full[t], (q_used[t] - 1) & 1)) break;
   } else if (warp == AP_MMA_WARP) {
-    // ------------------------------ products -----------------------------------------
+    // ------------------------------ products -------------------------------------------
+    // One thread for both tiles, so that their turns alternate: while one tile's weights
+    // form, the other's products run (a thread for each tile lets both fall into step,
+    // and the products wait for the softmax and the softmax for the products).  Little
+    // code: its instructions come from beyond the caches that the softmax loops fill.
+    const uint32_t lead = ap_elect();
     constexpr uint32_t fmt = std::is_same<E, __nv_bfloat16>::value ? 1u : 0u;
     constexpr uint32_t id_common = (1u << 4) | (fmt << 7) | (fmt << 10) |
                                    ((uint32_t)(AP_BM >> 4) << 24);
     constexpr uint32_t id_s = id_common | ((uint32_t)(AP_BN >> 3) << 17);
     constexpr uint32_t id_o = id_common | (1u << 16) | ((uint32_t)(HD >> 3) << 17);
-    unsigned stage = 0, q_used[2] = {0, 0}, p_used[2] = {0, 0};
+    const uint32_t qd = ap_desc(q_smem, 16);
+    const uint32_t kd = ap_desc(kv_smem, 16), vd = ap_desc(kv_smem, S::HALF_BYTES);
+    unsigned stage = 0, q_par = 0, p_par = 0;  // ring stages used; a bit for each tile
     bool ok = true;
-    // S_t = Q_t K^T from ring stage st
-    auto scores = [&](int t, unsigned st) {
-      if (lane == 0) {
-        const uint32_t qa = q_smem + t * S::TILE_BYTES, ka = kv_smem + st * S::TILE_BYTES;
-#pragma unroll
-        for (int kk = 0; kk < HD / 16; ++kk) {
-          const uint32_t off = (kk >> 2) * S::HALF_BYTES + (kk & 3) * 32;
-          ap_mma_ss(tm_s[t], ap_desc(qa + off, 16), ap_desc(ka + off, 16), id_s, kk > 0);
-        }
-        ap_commit(&s_full[t]);
-      }
-    };
-    // O_t (+)= P_t V
-    auto values = [&](int t, unsigned st, bool acc) {
-      if (lane == 0) {
-        const uint32_t va = kv_smem + st * S::TILE_BYTES;
-#pragma unroll
-        for (int kk = 0; kk < AP_BN / 16; ++kk)
-          ap_mma_ts(tm_o[t], tm_s[t] + 8 * kk, ap_desc(va + 2048 * kk, S::HALF_BYTES), id_o,
-                    acc || kk > 0);
-      }
-    };
     auto wait = [&](uint64_t* bar, unsigned parity) {
-      if (ok && !ap_wait(bar, parity, &s_abort)) {
-        if (lane == 0) fail();
-        ok = false;
-      }
-      ap_fence_after();
+      ok = ap_wait(bar, parity, &s_abort);
+      if (!ok && lead) fail();
       return ok;
     };
-    for (unsigned k = 0; ok; ++k) {
+    // S = Q K^T of a tile from a ring stage
+    auto scores = [&](int t, unsigned st) {
+      const uint32_t k = kd + st * (S::TILE_BYTES >> 4), q = qd + t * (S::TILE_BYTES >> 4);
+#pragma unroll
+      for (int kk = 0; kk < HD / 16; ++kk) {
+        const uint32_t off = ((kk >> 2) * S::HALF_BYTES + (kk & 3) * 32) >> 4;
+        ap_mma_ss(lead, t * AP_BN, q + off, k + off, id_s, kk > 0);
+      }
+      ap_commit(lead, &s_full[t]);
+    };
+    for (unsigned k = 0;; ++k) {
       const unsigned slot = k % AP_ITEMS;
       if (!wait(&item_full[slot], (k / AP_ITEMS) & 1)) break;
-      const ApItem it = s_item[slot];
+      const int seq = __shfl_sync(0xffffffffu, s_item[slot].seq, 0);
+      const int n0 = __shfl_sync(0xffffffffu, s_item[slot].tiles[0], 0);
+      const int n1 = __shfl_sync(0xffffffffu, s_item[slot].tiles[1], 0);
+      const int nk = max(n0, n1);
       __syncwarp();
-      if (lane == 0) mbar_arrive(&item_empty[slot]);
-      if (it.seq < 0) break;
-      const int nk = max(it.tiles[0], it.tiles[1]);
+      if (lead) mbar_arrive(&item_empty[slot]);
+      if (seq < 0) break;
       if (nk == 0) continue;
-      const unsigned first = stage;  // the item's ring stages: K_0 V_0 K_1 V_1 ...
-      if (!wait(&kv_full[first % S::STAGES], (first / S::STAGES) & 1)) break;
+      // the item's ring stages: K_0 V_0 K_1 V_1 ...
+      if (!wait(&kv_full[stage % S::STAGES], (stage / S::STAGES) & 1)) break;
+#pragma unroll
       for (int t = 0; t < 2; ++t) {
-        if (it.tiles[t] == 0) continue;
-        if (!wait(&q_full[t], q_used[t] & 1)) break;
-        ++q_used[t];
-        scores(t, first % S::STAGES);
-        if (it.tiles[t] == 1 && lane == 0) ap_commit(&q_empty[t]);
+        if ((t ? n1 : n0) == 0) continue;
+        if (!wait(&q_full[t], (q_par >> t) & 1)) break;
+        q_par ^= 1u << t;
+        ap_fence_after();
+        scores(t, stage % S::STAGES);
       }
       if (!ok) break;
-      if (lane == 0) ap_commit(&kv_empty[first % S::STAGES]);
-      for (int j = 0; j < nk && ok; ++j) {
-        const unsigned sv = first + 2 * j + 1, sk = sv + 1;
-        if (!wait(&kv_full[sv % S::STAGES], (sv / S::STAGES) & 1)) break;
-        if ((j + 1) * AP_BN > it.len) {
-          // values past the sequence's end: whatever their slots hold, zero here
-          const int r0 = it.len - j * AP_BN;
-          unsigned char* va = smem + (2 + sv % S::STAGES) * S::TILE_BYTES;
+#pragma unroll 1
+      for (int j = 0; j < nk; ++j) {
+        const unsigned sv = (stage + 2 * j + 1) % S::STAGES, sk = (stage + 2 * j + 2) % S::STAGES;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const int mine = t ? n1 : n0;
+          if (j >= mine) continue;
+          // O (+)= P V: the first half of the keys while the weights of the second form
+          const uint32_t v = vd + sv * (S::TILE_BYTES >> 4);
+          const uint32_t o = 2 * AP_BN + t * HD, w = t * AP_BN;
+          if (!wait(&p_half[t], (p_par >> t) & 1)) break;
+          ap_fence_after();
+#pragma unroll
+          for (int kk = 0; kk < AP_BN / 32; ++kk)
+            ap_mma_ts(lead, o, w + 8 * kk, v + (2048 >> 4) * kk, id_o, kk > 0 || j > 0);
+          if (!wait(&p_full[t], (p_par >> t) & 1)) break;
+          p_par ^= 1u << t;
+          ap_fence_after();
+#pragma unroll
+          for (int kk = AP_BN / 32; kk < AP_BN / 16; ++kk)
+            ap_mma_ts(lead, o, w + 8 * kk, v + (2048 >> 4) * kk, id_o, 1);
+          if (j + 1 < mine) scores(t, sk);
+          else ap_commit(lead, &o_full[t]);
+        }
+        if (!ok) break;
+      }
+      if (!ok) break;
+      stage += 2 * nk;
+    }
+    // every product issued has completed before tensor memory is freed
+    ap_commit(lead, &done_bar);
+    for (unsigned w = 0; w < (1u << 25); ++w)
+      if (mbar_try_wait(&done_bar, 0)) break;
+  } else {
+    // ------------------------------ the ring, for query tile t ---------------------------
+    // Waits for the keys and values that the products of a step will read, as one more
+    // arrival at the weights' barrier, and frees what finished products have read (the
+    // second tile's scores of a step come after everything else of it, and speak for
+    // both): the product warp waits for nothing but weights, the softmax for nothing but
+    // scores.
+    const int t = warp - AP_RING_WARP;
+    unsigned stage = 0, s_used = 0, o_used = 0;
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, unsigned parity) {
+      ok = ap_wait(bar, parity, &s_abort);
+      if (!ok && lane == 0) fail();
+      return ok;
+    };
+    for (unsigned k = 0;; ++k) {
+      const unsigned slot = k % AP_ITEMS;
+      if (!wait(&item_full[slot], (k / AP_ITEMS) & 1)) break;
+      const int seq = s_item[slot].seq, len = s_item[slot].len;
+      const int nk = s_item[slot].tiles[t], other = s_item[slot].tiles[t ^ 1];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&item_empty[slot]);
+      if (seq < 0) break;
+      const bool frees = lane == 0 && (t == 1 || other == 0);
+      for (int j = 0; j < nk; ++j) {
+        // the scores of step j are there: its keys, and the step before, are done with
+        const unsigned kst = stage + 2 * j, vst = kst + 1;
+        if (!wait(&s_full[t], s_used & 1)) break;
+        ++s_used;
+        if (frees) {
+          if (j > 0) mbar_arrive(&kv_empty[(kst - 1) % S::STAGES]);
+          mbar_arrive(&kv_empty[kst % S::STAGES]);
+        }
+        if (lane == 0 && j + 1 == nk) mbar_arrive(&q_empty[t]);
+        if (!wait(&kv_full[vst % S::STAGES], (vst / S::STAGES) & 1)) break;
+        if ((j + 1) * AP_BN > len) {
+          // values past the sequence's end: whatever their slots hold, zero here (by the
+          // warps of both tiles, the same zeros)
+          const int r0 = len - j * AP_BN;
+          unsigned char* va = smem + (2 + vst % S::STAGES) * S::TILE_BYTES;
           for (int x = r0 * 8 + lane; x < AP_BN * 8; x += 32)
 #pragma unroll
             for (int h = 0; h < S::HALVES; ++h)
@@ -528,31 +611,18 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
         }
-        for (int t = 0; t < 2; ++t) {
-          if (j >= it.tiles[t]) continue;
-          if (!wait(&p_full[t], p_used[t] & 1)) break;
-          ++p_used[t];
-          values(t, sv % S::STAGES, j > 0);
-          if (j + 1 < it.tiles[t]) {
-            if (!wait(&kv_full[sk % S::STAGES], (sk / S::STAGES) & 1)) break;
-            scores(t, sk % S::STAGES);
-            if (j + 2 == it.tiles[t] && lane == 0) ap_commit(&q_empty[t]);
-          } else if (lane == 0) {
-            ap_commit(&o_full[t]);
-          }
-        }
-        if (!ok) break;
-        if (lane == 0) {
-          ap_commit(&kv_empty[sv % S::STAGES]);
-          if (j + 1 < nk) ap_commit(&kv_empty[sk % S::STAGES]);
-        }
+        if (j + 1 < nk && !wait(&kv_full[(vst + 1) % S::STAGES], ((vst + 1) / S::STAGES) & 1))
+          break;
+        if (lane == 0) mbar_arrive(&p_half[t]);
       }
-      stage += 2 * nk;
+      if (!ok) break;
+      if (nk > 0) {
+        if (!wait(&o_full[t], o_used & 1)) break;
+        ++o_used;
+        if (frees) mbar_arrive(&kv_empty[(stage + 2 * nk - 1) % S::STAGES]);
+      }
+      stage += 2 * max(nk, other);
     }
-    // every product issued has completed before tensor memory is freed
-    if (lane == 0) ap_commit(&done_bar);
-    for (unsigned w = 0; w < (1u << 25); ++w)
-      if (mbar_try_wait(&done_bar, 0)) break;
   }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
@@ -560,7 +630,8 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
     const int t = warp >> 2;
     const int row = (warp & 3) * 32 + lane;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t ts = tm_s[t] + lanes, to = tm_o[t] + lanes;
+    const uint32_t ts = tmem + t * AP_BN + lanes, to = tmem + 2 * AP_BN + t * HD + lanes;
+    unsigned char* stage_out = smem + (2 + S::STAGES) * S::TILE_BYTES + warp * S::OUT_BYTES;
     const int tok_in = row / group, head_in = row - tok_in * group;
     const float c = a.scale * 1.4426950408889634f;
     unsigned s_used = 0, o_used = 0;
@@ -582,37 +653,33 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
       // key steps before this one are seen whole by every live row of the warp
       const int whole = __reduce_min_sync(0xffffffffu, live ? keys : 0x7fffffff) / AP_BN;
       float mx = -INFINITY, l = 0.f;  // the maximum in use, the sum of weights under it
-      for (int j = 0; j < nk; ++j) {
-        if (!ap_wait(&s_full[t], s_used & 1, &s_abort)) {
-          if (lane == 0) fail();
-          ok = false;
-          break;
-        }
+      auto step = [&](int j, auto hidden) {
+        if (!ap_wait(&s_full[t], s_used & 1, &s_abort)) return false;
         ++s_used;
         ap_fence_after();
         float s[AP_BN];
 #pragma unroll
         for (int q = 0; q < AP_BN / 32; ++q) ap_ld32(ts + 32 * q, s + 32 * q);
         ap_wait_ld<AP_BN>(s);
-        if (j >= whole) {
+        if constexpr (decltype(hidden)::value) {
           const int lim = keys - j * AP_BN;
 #pragma unroll
           for (int e = 0; e < AP_BN; ++e) s[e] = e < lim ? s[e] : -INFINITY;
         }
-        float top = fmaxf(s[0], s[1]);
+        float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int e = 2; e < AP_BN; e += 2) top = fmaxf(fmaxf(top, s[e]), s[e + 1]);
-        if (j == 0) {
-          mx = top;
-        } else {
-          const float to_mx = fmaxf(mx, top);
-          // the output is brought to a new maximum only where the old one lets
-          // weights grow past 2^AP_LAZY
-          const bool grow = mx == -INFINITY ? to_mx > -INFINITY : (to_mx - mx) * c > AP_LAZY;
-          if (__any_sync(0xffffffffu, grow)) {
-            const float f = grow ? at_exp2((mx - to_mx) * c) : 1.f;
-            if (grow) mx = to_mx;
-            l *= f;
+        for (int e = 0; e < AP_BN; e += 8)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) tops[i] = ap_max3(tops[i], s[e + 2 * i], s[e + 2 * i + 1]);
+        const float to_mx = fmaxf(mx, fmaxf(ap_max3(tops[0], tops[1], tops[2]), tops[3]));
+        // the output is brought to a new maximum only where the old one lets weights
+        // grow past 2^AP_LAZY
+        const bool grow = mx == -INFINITY ? to_mx > -INFINITY : (to_mx - mx) * c > AP_LAZY;
+        if (__any_sync(0xffffffffu, grow)) {
+          const float f = grow ? at_exp2((mx - to_mx) * c) : 1.f;
+          if (grow) mx = to_mx;
+          l *= f;
+          if (j > 0) {
 #pragma unroll 1
             for (int q = 0; q < HD / 32; ++q) {
               float o[32];
@@ -626,7 +693,8 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         }
         const float base = mx == -INFINITY ? 0.f : -mx * c;
         const f32x2_t c2 = pk2(c, c), b2 = pk2(base, base);
-        f32x2_t sum = pk2(0.f, 0.f);
+        f32x2_t sum[2] = {pk2(0.f, 0.f), pk2(0.f, 0.f)};
+        // weights 2^(c (s - mx)) as 16-bit pairs over the scores' columns
 #pragma unroll
         for (int q = 0; q < AP_BN / 32; ++q) {
           uint32_t p[16];
@@ -636,19 +704,29 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
             upk2(fma2(pk2(s[32 * q + 2 * e], s[32 * q + 2 * e + 1]), c2, b2), x, y);
             x = at_exp2(x);
             y = at_exp2(y);
-            sum = add2(sum, pk2(x, y));
+            sum[e & 1] = add2(sum[e & 1], pk2(x, y));
             p[e] = Half2<E>::narrow(x, y);
           }
           ap_st16(ts + 16 * q, p);
+          if (q == AP_BN / 64 - 1 || q == AP_BN / 32 - 1) {
+            ap_wait_st();
+            ap_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q == AP_BN / 64 - 1 ? &p_half[t] : &p_full[t]);
+          }
         }
-        ap_wait_st();
-        ap_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&p_full[t]);
         float sx, sy;
-        upk2(sum, sx, sy);
+        upk2(add2(sum[0], sum[1]), sx, sy);
         l += sx + sy;
-      }
+        return true;
+      };
+      // steps that every live row of the warp sees whole, then the others
+      int j = 0;
+#pragma unroll 1
+      for (; ok && j < min(nk, whole); ++j) ok = step(j, std::false_type());
+#pragma unroll 1
+      for (; ok && j < nk; ++j) ok = step(j, std::true_type());
+      if (!ok && lane == 0) fail();
       if (!ok) break;
       const int64_t gt = it.tok0 + tok;
       const int h = it.head * group + head_in;
@@ -663,27 +741,46 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         ++o_used;
         ap_fence_after();
       }
+      // 64 elements at a time through shared memory, so that a store instruction writes
+      // whole 128-byte pieces of four rows
 #pragma unroll
-      for (int q = 0; q < HD / 32; ++q) {
-        float o[32];
-        if (nk > 0) {
-          ap_ld32(to + 32 * q, o);
-          ap_wait_ld<32>(o);
-        } else {
+      for (int hf = 0; hf < S::HALVES; ++hf) {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) o[e] = 0.f;
-        }
+        for (int q = 0; q < 2; ++q) {
+          float o[32];
+          if (nk > 0) {
+            ap_ld32(to + 64 * hf + 32 * q, o);
+            ap_wait_ld<32>(o);
+          } else {
 #pragma unroll
-        for (int e = 0; e < 32; e += 8) {
-          float x[8];
-#pragma unroll
-          for (int d = 0; d < 8; ++d) {
-            x[d] = keys > 0 ? o[e + d] * inv : 0.f;
-            odd = __fmaf_rn(x[d], 0.f, odd);
+            for (int e = 0; e < 32; ++e) o[e] = 0.f;
           }
-          if (live && 32 * q + e < a.c.head_dim)
-            *reinterpret_cast<uint4*>(out + 2 * (32 * q + e)) = narrow8<E>(x);
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+            float x[8];
+#pragma unroll
+            for (int d = 0; d < 8; ++d) {
+              x[d] = keys > 0 ? o[e + d] * inv : 0.f;
+              odd = __fmaf_rn(x[d], 0.f, odd);
+            }
+            const int ch = 4 * q + (e >> 3);
+            *reinterpret_cast<uint4*>(stage_out + lane * 128 + ((ch ^ (lane & 7)) << 4)) =
+                narrow8<E>(x);
+          }
         }
+        __syncwarp();
+        const int ch = lane & 7;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int rr = 4 * i + (lane >> 3);
+          char* dst = reinterpret_cast<char*>(
+              __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(live ? out : nullptr), rr));
+          const uint4 v =
+              *reinterpret_cast<const uint4*>(stage_out + rr * 128 + ((ch ^ (rr & 7)) << 4));
+          if (dst && 64 * hf + 8 * ch < a.c.head_dim)
+            *reinterpret_cast<uint4*>(dst + 128 * hf + 16 * ch) = v;
+        }
+        __syncwarp();
       }
       ap_fence_before();
       unsigned bad = __ballot_sync(0xffffffffu, live && !(odd == 0.f));
