@@ -167,9 +167,15 @@ struct ApOrder {
   int causal;
   int level;    // an upper bound of the next item's level
   int total;    // blocks of all sequences
+  int n0, m0;   // this lane's first sequence: new tokens, cached tokens
 };
 
+// new and cached tokens of a sequence, one of this lane's (s % 32 is the lane)
 SLS_DEV void ap_lens(const ApOrder& o, int s, int& n, int& m) {
+  if (s < 32) {
+    n = o.n0, m = o.m0;
+    return;
+  }
   int64_t q0, q1;
   seq_rows(o.cu, s, o.T, q0, q1);
   n = (int)(q1 - q0);
@@ -198,9 +204,17 @@ SLS_DEV int ap_count_all(const ApOrder& o, int c) {
 }
 
 SLS_DEV void ap_order_init(ApOrder& o) {
-  int top = 0;
-  for (int s = threadIdx.x & 31; s < o.c.B; s += 32) top = max(top, max(o.c.kv_lens[s], 0));
-  o.level = (__reduce_max_sync(0xffffffffu, top) + AP_BN - 1) / AP_BN;
+  const int lane = threadIdx.x & 31;
+  o.n0 = o.m0 = 0;
+  if (lane < o.c.B) {
+    int64_t q0, q1;
+    seq_rows(o.cu, lane, o.T, q0, q1);
+    o.n0 = (int)(q1 - q0);
+    o.m0 = max(o.c.kv_lens[lane], 0);
+  }
+  int top = o.m0;
+  for (int s = 32 + lane; s < o.c.B; s += 32) top = max(top, max(o.c.kv_lens[s], 0));
+  o.level = (int)(((unsigned)__reduce_max_sync(0xffffffffu, top) + AP_BN - 1) / AP_BN);
   o.total = ap_count_all(o, 0);
 }
 
@@ -209,8 +223,9 @@ SLS_DEV bool ap_find(ApOrder& o, int64_t i, int tpt, ApItem& it) {
   const int heads = o.c.kv_heads;
   if (i >= (int64_t)o.total * heads) return false;
   const int j = (int)(i / heads);
-  // the highest level with more than j blocks at or above it
-  int lo = 0, hi = o.level;
+  // the highest level with more than j blocks at or above it (one sequence: its blocks
+  // from the last to the first, which needs no levels)
+  int lo = 0, hi = o.c.B == 1 ? 0 : o.level;
   int above = 0;  // blocks above the level
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -223,7 +238,7 @@ SLS_DEV bool ap_find(ApOrder& o, int64_t i, int tpt, ApItem& it) {
     }
   }
   o.level = lo;
-  if (hi == o.level && above == 0) above = ap_count_all(o, lo + 1);
+  if (above == 0 && o.c.B > 1) above = ap_count_all(o, lo + 1);
   int left = j - above;
   const int lane = threadIdx.x & 31;
   for (int s0 = 0; s0 < o.c.B; s0 += 32) {
@@ -231,10 +246,11 @@ SLS_DEV bool ap_find(ApOrder& o, int64_t i, int tpt, ApItem& it) {
     int n = 0, m = 0, mine = 0, b0 = 0;
     if (s < o.c.B) {
       ap_lens(o, s, n, m);
-      const int ge = ap_count(o, n, m, lo), gt = ap_count(o, n, m, lo + 1);
+      const int ge = ap_count(o, n, m, lo), gt = o.c.B > 1 ? ap_count(o, n, m, lo + 1) : 0;
       mine = ge - gt;
       b0 = (n + o.qb - 1) / o.qb - ge;  // the level's first block
       if (!o.causal) b0 = 0;
+      if (o.c.B == 1) b0 = mine - 1 - 2 * left;  // b0 + left is the block
     }
     int pre = mine;
 #pragma unroll
@@ -363,6 +379,18 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
     mbar_fence_init();
     s_abort = 0;
   }
+  ApOrder o;
+  ApItem following;
+  auto find = [&](unsigned k) {
+    following.seq = -1;
+    ap_find(o, (int64_t)k * gridDim.x + ((k & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x), tpt,
+            following);
+  };
+  if (warp == AP_LOAD_WARP) {
+    o.cu = a.cu, o.c = a.c, o.T = a.T, o.qb = 2 * tpt, o.causal = a.causal;
+    ap_order_init(o);
+    find(0);
+  }
   if (warp == AP_MMA_WARP) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
                      smem_u32(&tmem_holder)),
@@ -388,20 +416,11 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
 
   if (warp == AP_LOAD_WARP) {
     // ------------------------------ items and copies ------------------------------
-    ApOrder o{a.cu, a.c, a.T, 2 * tpt, a.causal, 0, 0};
-    ap_order_init(o);
     unsigned stage = 0, q_used[2] = {0, 0};
     const int box = min(AP_BN, 1 << a.c.page_shift);  // slots of one copy
     const int per_tile = AP_BN / box;
     const int col_shift = min(7, a.c.page_shift);
     bool ok = true;
-    auto find = [&](unsigned k, ApItem& it) {
-      it.seq = -1;
-      ap_find(o, (int64_t)k * gridDim.x + ((k & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x), tpt,
-              it);
-    };
-    ApItem following;
-    find(0, following);
     for (unsigned k = 0; ok; ++k) {
       const ApItem it = following;
       const unsigned slot = k % AP_ITEMS, use = k / AP_ITEMS;
@@ -422,7 +441,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         return (lane < per_tile && j < nk && x < it.len) ? table[x >> a.c.page_shift] : -1;
       };
       int page = page_of(0);
-      if (nk == 0) find(k + 1, following);
+      if (nk == 0) find(k + 1);
       for (int j = 0; j < nk && ok; ++j) {
         const int next = page_of(j + 1);
         const int here = min(AP_BN, it.len - j * AP_BN);
@@ -467,7 +486,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         }
         page = next;
         // the next item is looked for while the ring is full
-        if (j == min(nk - 1, 1)) find(k + 1, following);
+        if (j == min(nk - 1, 1)) find(k + 1);
       }
     }
     // every copy has landed before the CTA may exit
@@ -731,8 +750,15 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
       const int64_t gt = it.tok0 + tok;
       const int h = it.head * group + head_in;
       char* out = a.out.data + gt * a.out.token_b + h * a.out.head_b;
-      const float inv = 1.f / l;
-      float odd = 0.f;  // NaN once any element is not finite
+      const float inv = keys > 0 ? 1.f / l : 0.f;
+      // rows 4 i + lane / 8 of the warp, of which this lane will store 16-byte pieces
+      char* dst[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        dst[i] = reinterpret_cast<char*>(__shfl_sync(
+            0xffffffffu, reinterpret_cast<unsigned long long>(live ? out : nullptr),
+            4 * i + (lane >> 3)));
+      float o[HD];
       if (nk > 0) {
         if (!ap_wait(&o_full[t], o_used & 1, &s_abort)) {
           if (lane == 0) fail();
@@ -740,50 +766,48 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         }
         ++o_used;
         ap_fence_after();
+#pragma unroll
+        for (int q = 0; q < HD / 32; ++q) ap_ld32(to + 32 * q, o + 32 * q);
+        ap_wait_ld<HD>(o);
+      } else {
+#pragma unroll
+        for (int e = 0; e < HD; ++e) o[e] = 0.f;
       }
       // 64 elements at a time through shared memory, so that a store instruction writes
       // whole 128-byte pieces of four rows
+      f32x2_t odd = pk2(0.f, 0.f);  // NaN once any element is not finite
+      const f32x2_t inv2 = pk2(inv, inv), zero2 = pk2(0.f, 0.f);
+      const int ch = lane & 7;
 #pragma unroll
       for (int hf = 0; hf < S::HALVES; ++hf) {
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          float o[32];
-          if (nk > 0) {
-            ap_ld32(to + 64 * hf + 32 * q, o);
-            ap_wait_ld<32>(o);
-          } else {
+        for (int q = 0; q < 8; ++q) {
+          float x[8];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = 0.f;
+          for (int d = 0; d < 4; ++d) {
+            const int e = 64 * hf + 8 * q + 2 * d;
+            const f32x2_t v = mul2(pk2(o[e], o[e + 1]), inv2);
+            odd = fma2(v, zero2, odd);
+            upk2(v, x[2 * d], x[2 * d + 1]);
           }
-#pragma unroll
-          for (int e = 0; e < 32; e += 8) {
-            float x[8];
-#pragma unroll
-            for (int d = 0; d < 8; ++d) {
-              x[d] = keys > 0 ? o[e + d] * inv : 0.f;
-              odd = __fmaf_rn(x[d], 0.f, odd);
-            }
-            const int ch = 4 * q + (e >> 3);
-            *reinterpret_cast<uint4*>(stage_out + lane * 128 + ((ch ^ (lane & 7)) << 4)) =
-                narrow8<E>(x);
-          }
+          *reinterpret_cast<uint4*>(stage_out + lane * 128 + ((q ^ (lane & 7)) << 4)) =
+              narrow8<E>(x);
         }
         __syncwarp();
-        const int ch = lane & 7;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int rr = 4 * i + (lane >> 3);
-          char* dst = reinterpret_cast<char*>(
-              __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(live ? out : nullptr), rr));
           const uint4 v =
               *reinterpret_cast<const uint4*>(stage_out + rr * 128 + ((ch ^ (rr & 7)) << 4));
-          if (dst && 64 * hf + 8 * ch < a.c.head_dim)
-            *reinterpret_cast<uint4*>(dst + 128 * hf + 16 * ch) = v;
+          if (dst[i] && 64 * hf + 8 * ch < a.c.head_dim)
+            *reinterpret_cast<uint4*>(dst[i] + 128 * hf + 16 * ch) = v;
         }
         __syncwarp();
       }
+      float odd_x, odd_y;
+      upk2(odd, odd_x, odd_y);
       ap_fence_before();
-      unsigned bad = __ballot_sync(0xffffffffu, live && !(odd == 0.f));
+      unsigned bad = __ballot_sync(0xffffffffu, live && !(odd_x + odd_y == 0.f));
       while (bad) {
         const int src = __ffs(bad) - 1;
         bad &= bad - 1;
