@@ -182,6 +182,7 @@ attention_decode_kernel(const __grid_constant__ CUtensorMap tmK,
   int64_t left = t1 - t0;  // steps still to issue
   int batch0 = -1, page = -1;  // lane l: the page of tokens 16 l of the batch of 16 steps
   unsigned issued = 0;
+  const uint32_t lead = at_elect();
   auto issue = [&]() {
     if (left == 0) return;
     if (ij * AD_KEYS >= ilen) {
@@ -200,15 +201,20 @@ attention_decode_kernel(const __grid_constant__ CUtensorMap tmK,
     const unsigned st = issued % S::STAGES;
     const int here = min(AD_KEYS, ilen - ij * AD_KEYS);
     const int copies = (here + box - 1) / box;
-    // lane: copy, K or V, half
-    const int cp = lane / (2 * S::HALVES), kv = (lane / S::HALVES) & 1, h = lane % S::HALVES;
-    const int pg = __shfl_sync(0xffffffffu, page, 2 * (ij - batch0) + (cp & 1));
-    if (lane == 0) mbar_expect_tx(&bars[st], 2 * S::HALVES * copies * box * 128);
+    const int slot0 = (ij * AD_KEYS) & ((1 << c.page_shift) - 1);
+    if (lead) mbar_expect_tx(&bars[st], 2 * S::HALVES * copies * box * 128);
     __syncwarp();
-    if (cp < copies)
-      at_tma4(ring_s + st * S::STAGE_BYTES + kv * S::MAT_BYTES + h * S::HALF_BYTES + cp * box * 128,
-              kv ? &tmV : &tmK, 64 * h, (ij * AD_KEYS) & ((1 << c.page_shift) - 1), kvh, pg,
-              &bars[st]);
+#pragma unroll 1
+    for (int cp = 0; cp < copies; ++cp) {
+      const int pg = __shfl_sync(0xffffffffu, page, 2 * (ij - batch0) + cp);
+      const uint32_t dst = ring_s + st * S::STAGE_BYTES + cp * box * 128;
+#pragma unroll
+      for (int h = 0; h < S::HALVES; ++h) {
+        at_tma4(lead, dst + h * S::HALF_BYTES, &tmK, 64 * h, slot0, kvh, pg, &bars[st]);
+        at_tma4(lead, dst + S::MAT_BYTES + h * S::HALF_BYTES, &tmV, 64 * h, slot0, kvh, pg,
+                &bars[st]);
+      }
+    }
     ++ij;
     ++issued;
     --left;

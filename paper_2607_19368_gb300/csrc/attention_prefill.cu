@@ -78,11 +78,6 @@ SLS_DEV void ap_commit(uint32_t lead, uint64_t* bar) {
           smem_u32(bar)), "r"(lead)
       : "memory");
 }
-SLS_DEV uint32_t ap_elect() {
-  uint32_t r;
-  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
-  return r;
-}
 SLS_DEV void ap_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 SLS_DEV void ap_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
@@ -157,133 +152,155 @@ SLS_DEV bool ap_wait(uint64_t* bar, unsigned parity, volatile int* abort_flag) {
 // b of g takes numbers b, 2g-1-b, 2g+b, ...: neighbours in the order cost about the
 // same, so turning the direction every round evens the sums out.  An item is found
 // from its number by a warp without any table: the number of blocks with at least c
-// key steps is a closed form per sequence, summed over the sequences by the lanes,
-// and a search over c narrows to the item's level.
+// key steps (the level c and above) is a closed form per sequence, summed over the
+// sequences by the lanes; a CTA's numbers rise, so its level falls, most often not at
+// all or by one.
 struct ApOrder {
   const int32_t* cu;
   CacheView c;
   int64_t T;
-  int qb;       // tokens of a block
+  int qb;               // tokens of a block
+  unsigned qb_mul, qb_shift;  // x / qb = mulhi(x, qb_mul) >> qb_shift for 0 <= x < 2^31
   int causal;
-  int level;    // an upper bound of the next item's level
-  int total;    // blocks of all sequences
-  int n0, m0;   // this lane's first sequence: new tokens, cached tokens
+  int level;            // the last item's level
+  int at_level, above;  // blocks at the level or above, blocks above it
+  int total;            // blocks of all sequences
+  int q0, n0, m0;       // this lane's first sequence: first row, new tokens, cached tokens
 };
 
-// new and cached tokens of a sequence, one of this lane's (s % 32 is the lane)
-SLS_DEV void ap_lens(const ApOrder& o, int s, int& n, int& m) {
+SLS_DEV int ap_div(const ApOrder& o, int x) {
+  return (int)(__umulhi((unsigned)x, o.qb_mul) >> o.qb_shift);
+}
+
+// first row, new and cached tokens of a sequence, one of this lane's (s % 32 is the lane)
+SLS_DEV void ap_lens(const ApOrder& o, int s, int& q0, int& n, int& m) {
   if (s < 32) {
-    n = o.n0, m = o.m0;
+    q0 = o.q0, n = o.n0, m = o.m0;
     return;
   }
-  int64_t q0, q1;
-  seq_rows(o.cu, s, o.T, q0, q1);
-  n = (int)(q1 - q0);
+  int64_t r0, r1;
+  seq_rows(o.cu, s, o.T, r0, r1);
+  q0 = (int)r0;
+  n = (int)(r1 - r0);
   m = max(o.c.kv_lens[s], 0);
 }
 
 // blocks of a sequence whose key steps number at least c
 SLS_DEV int ap_count(const ApOrder& o, int n, int m, int c) {
-  const int nb = (n + o.qb - 1) / o.qb;
+  const int nb = ap_div(o, n + o.qb - 1);
   if (c <= 0) return nb;
   const int x = (c - 1) * AP_BN;  // more than x keys
   if (m <= x) return 0;
   if (!o.causal) return nb;
   const int e = x - (m - n) + 1;  // the block's last token is number e or later
-  return e <= 0 ? nb : nb - min(nb, (e + o.qb - 1) / o.qb - 1);
+  return e <= 0 ? nb : nb - min(nb, ap_div(o, e + o.qb - 1) - 1);
 }
 
 SLS_DEV int ap_count_all(const ApOrder& o, int c) {
   int sum = 0;
   for (int s = threadIdx.x & 31; s < o.c.B; s += 32) {
-    int n, m;
-    ap_lens(o, s, n, m);
+    int q0, n, m;
+    ap_lens(o, s, q0, n, m);
     sum += ap_count(o, n, m, c);
   }
   return __reduce_add_sync(0xffffffffu, sum);
 }
 
-SLS_DEV void ap_order_init(ApOrder& o) {
+SLS_DEV void ap_order_init(ApOrder& o, const AttnArgs& a, int qb) {
   const int lane = threadIdx.x & 31;
-  o.n0 = o.m0 = 0;
+  o.cu = a.cu, o.c = a.c, o.T = a.T, o.qb = qb, o.causal = a.causal;
+  // T. Granlund and P. L. Montgomery, "Division by Invariant Integers using
+  // Multiplication", 1994: with 2^(l-1) < d <= 2^l, x / d = (x ceil(2^(31+l) / d)) >> (31+l)
+  // for x < 2^31 (qb is even, so l >= 1)
+  const int l = 32 - __clz(qb - 1);
+  o.qb_mul = (unsigned)(((1ull << (31 + l)) + qb - 1) / qb);
+  o.qb_shift = l - 1;
+  o.q0 = o.n0 = o.m0 = 0;
   if (lane < o.c.B) {
-    int64_t q0, q1;
-    seq_rows(o.cu, lane, o.T, q0, q1);
-    o.n0 = (int)(q1 - q0);
+    int64_t r0, r1;
+    seq_rows(o.cu, lane, o.T, r0, r1);
+    o.q0 = (int)r0;
+    o.n0 = (int)(r1 - r0);
     o.m0 = max(o.c.kv_lens[lane], 0);
   }
   int top = o.m0;
   for (int s = 32 + lane; s < o.c.B; s += 32) top = max(top, max(o.c.kv_lens[s], 0));
-  o.level = (int)(((unsigned)__reduce_max_sync(0xffffffffu, top) + AP_BN - 1) / AP_BN);
-  o.total = ap_count_all(o, 0);
+  // one sequence needs no levels: its blocks go from the last to the first
+  o.level = o.c.B == 1 ? 0
+                       : (int)(((unsigned)__reduce_max_sync(0xffffffffu, top) + AP_BN - 1) / AP_BN);
+  o.above = 0;
+  o.at_level = ap_count_all(o, o.level);
+  o.total = o.level == 0 ? o.at_level : ap_count_all(o, 0);
 }
 
 // the item number i; false when there is none
 SLS_DEV bool ap_find(ApOrder& o, int64_t i, int tpt, ApItem& it) {
   const int heads = o.c.kv_heads;
   if (i >= (int64_t)o.total * heads) return false;
-  const int j = (int)(i / heads);
-  // the highest level with more than j blocks at or above it (one sequence: its blocks
-  // from the last to the first, which needs no levels)
-  int lo = 0, hi = o.c.B == 1 ? 0 : o.level;
-  int above = 0;  // blocks above the level
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    const int cnt = ap_count_all(o, mid);
-    if (cnt > j) {
-      lo = mid;
-    } else {
-      hi = mid - 1;
-      above = cnt;
+  const int j = (int)i / heads;  // total * heads is below 2^31
+  // the highest level with more than j blocks at or above it: down in doubling steps,
+  // then halved
+  if (j >= o.at_level) {
+    int hi = o.level, lo = o.level;  // at hi there are not enough, at lo there will be
+    int at_hi = o.at_level, at_lo = o.at_level;
+    for (int step = 1; at_lo <= j; step *= 2) {
+      hi = lo, at_hi = at_lo;
+      lo = max(0, lo - step);
+      at_lo = ap_count_all(o, lo);
     }
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1, cnt = ap_count_all(o, mid);
+      if (cnt > j) lo = mid, at_lo = cnt;
+      else hi = mid, at_hi = cnt;
+    }
+    o.level = lo, o.at_level = at_lo, o.above = at_hi;
   }
-  o.level = lo;
-  if (above == 0 && o.c.B > 1) above = ap_count_all(o, lo + 1);
-  int left = j - above;
+  int left = j - o.above;
   const int lane = threadIdx.x & 31;
   for (int s0 = 0; s0 < o.c.B; s0 += 32) {
     const int s = s0 + lane;
-    int n = 0, m = 0, mine = 0, b0 = 0;
+    int q0 = 0, n = 0, m = 0, mine = 0, b0 = 0;
     if (s < o.c.B) {
-      ap_lens(o, s, n, m);
-      const int ge = ap_count(o, n, m, lo), gt = o.c.B > 1 ? ap_count(o, n, m, lo + 1) : 0;
-      mine = ge - gt;
-      b0 = (n + o.qb - 1) / o.qb - ge;  // the level's first block
-      if (!o.causal) b0 = 0;
-      if (o.c.B == 1) b0 = mine - 1 - 2 * left;  // b0 + left is the block
+      ap_lens(o, s, q0, n, m);
+      const int ge = ap_count(o, n, m, o.level);
+      mine = o.c.B > 1 ? ge - ap_count(o, n, m, o.level + 1) : ge;
+      b0 = o.causal ? ap_div(o, n + o.qb - 1) - ge : 0;  // the level's first block
+      if (o.c.B == 1) b0 = mine - 1 - 2 * left;          // b0 + left is the block
     }
     int pre = mine;
+    if (o.c.B > 1) {
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int x = __shfl_up_sync(0xffffffffu, pre, d);
-      if (lane >= d) pre += x;
+      for (int d = 1; d < 32; d <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, pre, d);
+        if (lane >= d) pre += x;
+      }
     }
-    const int all = __shfl_sync(0xffffffffu, pre, 31);
-    if (left < all) {
-      const unsigned hit = __ballot_sync(0xffffffffu, left < pre);
+    const unsigned hit = __ballot_sync(0xffffffffu, mine > 0 && left < pre);
+    if (hit) {
       const int src = __ffs(hit) - 1;
       const int b = __shfl_sync(0xffffffffu, b0 + left - (pre - mine), src);
+      q0 = __shfl_sync(0xffffffffu, q0, src);
       n = __shfl_sync(0xffffffffu, n, src);
       m = __shfl_sync(0xffffffffu, m, src);
       it.seq = s0 + src;
-      int64_t q0, q1;
-      seq_rows(o.cu, it.seq, o.T, q0, q1);
-      it.head = (int)(i - (int64_t)j * heads);
-      it.tok0 = (int)q0 + b * o.qb;
+      it.head = (int)i - j * heads;
+      it.tok0 = q0 + b * o.qb;
       it.ntok = min(o.qb, n - b * o.qb);
-      it.len = (int)cache_len(o.c, it.seq);
+      it.len = (int)min((int64_t)m, (int64_t)o.c.max_pages << o.c.page_shift);
       it.causal = o.causal;
       it.lim0 = o.causal ? m - n + b * o.qb + 1 : it.len;
+#pragma unroll
       for (int t = 0; t < 2; ++t) {
         const int nt = min(tpt, it.ntok - t * tpt);  // tokens of the tile
         const int lim = o.causal ? it.lim0 + t * tpt + nt - 1 : it.len;
-        it.tiles[t] = nt > 0 ? (max(0, min(lim, it.len)) + AP_BN - 1) / AP_BN : 0;
+        it.tiles[t] =
+            nt > 0 ? (int)(((unsigned)max(0, min(lim, it.len)) + AP_BN - 1) / AP_BN) : 0;
       }
       // the second tile, unless empty, has the item's last step
       if (it.tiles[1] > 0) it.tiles[1] = max(it.tiles[0], it.tiles[1]);
       return true;
     }
-    left -= all;
+    left -= __shfl_sync(0xffffffffu, pre, 31);
   }
   return false;
 }
@@ -387,8 +404,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
             following);
   };
   if (warp == AP_LOAD_WARP) {
-    o.cu = a.cu, o.c = a.c, o.T = a.T, o.qb = 2 * tpt, o.causal = a.causal;
-    ap_order_init(o);
+    ap_order_init(o, a, 2 * tpt);
     find(0);
   }
   if (warp == AP_MMA_WARP) {
@@ -416,6 +432,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
 
   if (warp == AP_LOAD_WARP) {
     // ------------------------------ items and copies ------------------------------
+    const uint32_t lead = at_elect();
     unsigned stage = 0, q_used[2] = {0, 0};
     const int box = min(AP_BN, 1 << a.c.page_shift);  // slots of one copy
     const int per_tile = AP_BN / box;
@@ -459,10 +476,12 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
                 break;
               }
               ++q_used[t];
-              if (lane == 0) {
-                mbar_expect_tx(&q_full[t], S::HALVES * group * tpt * 128);
+              if (lead) mbar_expect_tx(&q_full[t], S::HALVES * group * tpt * 128);
+              __syncwarp();
+              {
+#pragma unroll
                 for (int h = 0; h < S::HALVES; ++h)
-                  at_tma3(q_smem + t * S::TILE_BYTES + h * S::HALF_BYTES, &tmQ, 64 * h,
+                  at_tma3(lead, q_smem + t * S::TILE_BYTES + h * S::HALF_BYTES, &tmQ, 64 * h,
                           it.head * group, it.tok0 + t * tpt, &q_full[t]);
               }
             }
@@ -473,13 +492,15 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
             ok = false;
             break;
           }
-          if (lane == 0) mbar_expect_tx(&kv_full[st], S::HALVES * copies * box * 128);
+          if (lead) mbar_expect_tx(&kv_full[st], S::HALVES * copies * box * 128);
           __syncwarp();
-          if (lane < copies) {
-            const uint32_t dst = kv_smem + st * S::TILE_BYTES + lane * box * 128;
+#pragma unroll 1
+          for (int i = 0; i < copies; ++i) {
+            const uint32_t dst = kv_smem + st * S::TILE_BYTES + i * box * 128;
+            const int pg = __shfl_sync(0xffffffffu, page, i);
 #pragma unroll
             for (int h = 0; h < S::HALVES; ++h)
-              at_tma4(dst + h * S::HALF_BYTES, kv ? &tmV : &tmK, 64 * h, slot0, it.head, page,
+              at_tma4(lead, dst + h * S::HALF_BYTES, kv ? &tmV : &tmK, 64 * h, slot0, it.head, pg,
                       &kv_full[st]);
           }
           ++stage;
@@ -503,7 +524,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
     // form, the other's products run (a thread for each tile lets both fall into step,
     // and the products wait for the softmax and the softmax for the products).  Little
     // code: its instructions come from beyond the caches that the softmax loops fill.
-    const uint32_t lead = ap_elect();
+    const uint32_t lead = at_elect();
     constexpr uint32_t fmt = std::is_same<E, __nv_bfloat16>::value ? 1u : 0u;
     constexpr uint32_t id_common = (1u << 4) | (fmt << 7) | (fmt << 10) |
                                    ((uint32_t)(AP_BM >> 4) << 24);
@@ -670,7 +691,8 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
       const int keys = live ? max(0, min(it.len, it.causal ? it.lim0 + tok : it.len)) : 0;
       const int nk = it.tiles[t];
       // key steps before this one are seen whole by every live row of the warp
-      const int whole = __reduce_min_sync(0xffffffffu, live ? keys : 0x7fffffff) / AP_BN;
+      const int least = __reduce_min_sync(0xffffffffu, live ? keys : 0x7fffffff);
+      const int whole = least / AP_BN;
       float mx = -INFINITY, l = 0.f;  // the maximum in use, the sum of weights under it
       auto step = [&](int j, auto hidden) {
         if (!ap_wait(&s_full[t], s_used & 1, &s_abort)) return false;
@@ -681,9 +703,14 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         for (int q = 0; q < AP_BN / 32; ++q) ap_ld32(ts + 32 * q, s + 32 * q);
         ap_wait_ld<AP_BN>(s);
         if constexpr (decltype(hidden)::value) {
-          const int lim = keys - j * AP_BN;
+          const int lim = keys - j * AP_BN, sure = least - j * AP_BN;
 #pragma unroll
-          for (int e = 0; e < AP_BN; ++e) s[e] = e < lim ? s[e] : -INFINITY;
+          for (int q = 0; q < AP_BN / 32; ++q) {
+            if (32 * (q + 1) <= sure) continue;  // every row sees these
+            asm volatile("" ::: "memory");       // a branch, not 32 predicates
+#pragma unroll
+            for (int e = 32 * q; e < 32 * q + 32; ++e) s[e] = e < lim ? s[e] : -INFINITY;
+          }
         }
         float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -758,7 +785,6 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         dst[i] = reinterpret_cast<char*>(__shfl_sync(
             0xffffffffu, reinterpret_cast<unsigned long long>(live ? out : nullptr),
             4 * i + (lane >> 3)));
-      float o[HD];
       if (nk > 0) {
         if (!ap_wait(&o_full[t], o_used & 1, &s_abort)) {
           if (lane == 0) fail();
@@ -766,41 +792,46 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         }
         ++o_used;
         ap_fence_after();
-#pragma unroll
-        for (int q = 0; q < HD / 32; ++q) ap_ld32(to + 32 * q, o + 32 * q);
-        ap_wait_ld<HD>(o);
-      } else {
-#pragma unroll
-        for (int e = 0; e < HD; ++e) o[e] = 0.f;
       }
       // 64 elements at a time through shared memory, so that a store instruction writes
-      // whole 128-byte pieces of four rows
+      // whole 128-byte pieces of four rows (loops, not straight code: it runs once an
+      // item, from beyond the instruction caches)
       f32x2_t odd = pk2(0.f, 0.f);  // NaN once any element is not finite
       const f32x2_t inv2 = pk2(inv, inv), zero2 = pk2(0.f, 0.f);
       const int ch = lane & 7;
-#pragma unroll
+#pragma unroll 1
       for (int hf = 0; hf < S::HALVES; ++hf) {
+#pragma unroll 1
+        for (int q = 0; q < 2; ++q) {
+          float o[32];
+          if (nk > 0) {
+            ap_ld32(to + 64 * hf + 32 * q, o);
+            ap_wait_ld<32>(o);
+          } else {
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          float x[8];
-#pragma unroll
-          for (int d = 0; d < 4; ++d) {
-            const int e = 64 * hf + 8 * q + 2 * d;
-            const f32x2_t v = mul2(pk2(o[e], o[e + 1]), inv2);
-            odd = fma2(v, zero2, odd);
-            upk2(v, x[2 * d], x[2 * d + 1]);
+            for (int e = 0; e < 32; ++e) o[e] = 0.f;
           }
-          *reinterpret_cast<uint4*>(stage_out + lane * 128 + ((q ^ (lane & 7)) << 4)) =
-              narrow8<E>(x);
+#pragma unroll
+          for (int e = 0; e < 32; e += 8) {
+            float x[8];
+#pragma unroll
+            for (int d = 0; d < 8; d += 2) {
+              const f32x2_t v = mul2(pk2(o[e + d], o[e + d + 1]), inv2);
+              odd = fma2(v, zero2, odd);
+              upk2(v, x[d], x[d + 1]);
+            }
+            *reinterpret_cast<uint4*>(stage_out + lane * 128 +
+                                      (((4 * q + (e >> 3)) ^ (lane & 7)) << 4)) = narrow8<E>(x);
+          }
         }
         __syncwarp();
+        const bool on = 64 * hf + 8 * ch < a.c.head_dim;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int rr = 4 * i + (lane >> 3);
           const uint4 v =
               *reinterpret_cast<const uint4*>(stage_out + rr * 128 + ((ch ^ (rr & 7)) << 4));
-          if (dst[i] && 64 * hf + 8 * ch < a.c.head_dim)
-            *reinterpret_cast<uint4*>(dst[i] + 128 * hf + 16 * ch) = v;
+          if (dst[i] && on) *reinterpret_cast<uint4*>(dst[i] + 128 * hf + 16 * ch) = v;
         }
         __syncwarp();
       }
@@ -858,6 +889,7 @@ int launch_attention_prefill(const AttnArgs& a, int dtype, cudaStream_t stream) 
   SLS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   const int64_t items = ((a.T + 2 * tpt - 1) / (2 * tpt) + std::min<int64_t>(c.B, a.T)) *
                         c.kv_heads;
+  if (items > 0x7fffffff) return SLS_ERR_UNSUPPORTED;
   const int grid = (int)std::min<int64_t>(items, sms);
   CUtensorMap q, k, v;
   {
