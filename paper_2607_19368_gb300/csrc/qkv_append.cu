@@ -2,14 +2,14 @@
 // keys and values appended to the paged cache, in one pass:
 //   y = w x / sqrt(mean(x^2) + eps);  pair (a, b) of y turned by t = p f_i.
 //
-// A copy bound by HBM bandwidth with ten operations an element on the way.  A
-// CTA takes a few tokens and all (or, for few tokens, a share) of their heads:
-// the cosines and sines of a token are formed once in shared memory and serve
-// all of its heads.  A (token, head) row is 16 lanes of one 16-byte vector each
-// (8 lanes for heads of up to 64), four rows in flight per lane; the sum of
-// squares stays within the row's lanes, and the partner of an element is in the
-// lane half a rotation away (a shuffle), or, where the halves are no multiple of
-// a vector, read again from the row.
+// A copy bound by HBM bandwidth with some ten operations an element on the way.  A CTA
+// takes a few tokens and all (or, for few tokens, a share) of their heads: the cosines
+// and sines of a token are formed once and serve all of its heads.  A row (token, head)
+// is 8 lanes of two 16-byte vectors (4 lanes for heads of up to 64), the vectors chosen
+// so that a lane holds both halves of its rotated pairs; weight, cosine and sine are
+// multiplied together once and stay in registers while the lane goes from head to head
+// of its token, so that an element costs one multiplication, one fused
+// multiply-add and the product with the norm.
 #include <algorithm>
 
 #include "attention.cuh"
@@ -18,10 +18,13 @@ namespace sls {
 
 namespace {
 
-constexpr int QA_T = 256;
-constexpr int QA_TOKENS = 8;   // tokens of a CTA
-constexpr int QA_ROWS = 4;     // rows in flight per lane group
+constexpr int QA_T = 128;
+constexpr int QA_ROWS = 4;     // rows in flight per lane
+constexpr int QA_MAX_TOKENS = 8;
 constexpr int QA_MAX_PAIRS = SLS_MAX_HEAD_DIM / 2;
+
+enum { QA_PAIRED, QA_INTERLEAVED, QA_ODD };  // halves of whole vectors (or no rotation); pairs
+                                             // side by side; halves that split vectors
 
 // cos and sin of p * f.  The product is held as a rounded float32 and its exact
 // remainder (one fused multiply-add); Cody and Waite's reduction (W. J. Cody and
@@ -43,34 +46,77 @@ SLS_DEV float2 turn(float p, float f) {
   return make_float2(c, s);
 }
 
-// L lanes per row
-template <typename E, int L>
-__global__ void __launch_bounds__(QA_T)
-qkv_append_kernel(const __grid_constant__ AppendArgs a, int heads_per_cta) {
-  __shared__ float2 s_turn[QA_TOKENS][QA_MAX_PAIRS];  // (cos, sin) * scale
-  __shared__ int64_t s_slot[QA_TOKENS];               // byte offset of the token's slot, or -1
-  __shared__ float s_pos[QA_TOKENS];
+// The factors of a lane's two vectors for rows of queries or of keys: element e of the
+// first becomes f (x c0[e] - x' s0[e]), of the second f (x' c1[e] + x s1[e]), with x and
+// x' the elements e of the two vectors and f the row's norm.
+struct QaFactors {
+  f32x2_t c0[4], s0[4], c1[4], s1[4];
+};
+
+// L lanes per row; heads of one token are shared by QA_T / (L tokens) groups of lanes
+template <typename E, int L, int MODE>
+__global__ void __launch_bounds__(QA_T, 4)
+qkv_append_kernel(const __grid_constant__ AppendArgs a, int tokens, int heads_per_cta) {
+  __shared__ float2 s_turn[QA_MAX_TOKENS][QA_MAX_PAIRS];  // (cos, sin) * scale
+  __shared__ int64_t s_slot[QA_MAX_TOKENS];               // byte offset of the token's slot, or -1
+  __shared__ float s_pos[QA_MAX_TOKENS];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t t0 = (int64_t)blockIdx.x * QA_TOKENS;
-  const int nt = (int)min((int64_t)QA_TOKENS, a.T - t0);
+  const int64_t t0 = (int64_t)blockIdx.x * tokens;
+  const int nt = (int)min((int64_t)tokens, a.T - t0);
   const CacheView& c = a.c;
 
-  // where each token goes: its sequence is the number of sequences that end at
-  // or before it
+  // this lane's token, first head and vectors
+  const int groups = QA_T / L;             // a multiple of tokens
+  const int per_token = groups / tokens;
+  const int grp = threadIdx.x / L, l = threadIdx.x & (L - 1);
+  const int tok = grp / per_token, sub = grp - tok * per_token;
+  const int64_t t = t0 + tok;
+  const int h_first = blockIdx.y * heads_per_cta;
+  const int h_end = min(h_first + heads_per_cta, a.q_heads + 2 * c.kv_heads);
+  const int nv = c.head_dim >> 3;
+  const int half = MODE == QA_PAIRED ? a.pairs >> 3 : 0;
+  const bool rotated = l < half;           // QA_PAIRED: the lane holds a rotated pair
+  const int v0 = MODE == QA_PAIRED && !rotated ? 2 * l : l;
+  const int v1 = MODE == QA_PAIRED ? (rotated ? l + half : 2 * l + 1) : l + L;
+  const bool on0 = v0 < nv, on1 = v1 < nv;
+
+  auto row_of = [&](int h) -> const char* {
+    const bool is_q = h < a.q_heads, is_k = h < a.q_heads + c.kv_heads;
+    const RowsView& v = is_q ? a.q : (is_k ? a.k : a.v);
+    const int hh = is_q ? h : (is_k ? h - a.q_heads : h - a.q_heads - c.kv_heads);
+    return v.data + t * v.token_b + hh * v.head_b;
+  };
+  uint4 x0[QA_ROWS], x1[QA_ROWS];
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int u = 0; u < QA_ROWS; ++u) {
+      const int h = h0 + u * per_token;
+      x0[u] = x1[u] = make_uint4(0, 0, 0, 0);
+      if (tok < nt && h < h_end) {
+        const char* p = row_of(h);
+        if (on0) x0[u] = *reinterpret_cast<const uint4*>(p + 16 * v0);
+        if (on1) x1[u] = *reinterpret_cast<const uint4*>(p + 16 * v1);
+      }
+    }
+  };
+  load(h_first + sub);  // under way while the tokens are looked up
+
+  // where each token goes: its sequence is the number of sequences that end at or
+  // before it
   for (int i = warp; i < nt; i += QA_T / 32) {
-    const int64_t t = t0 + i;
-    int s = (int)t;
+    const int64_t tt = t0 + i;
+    int s = (int)tt;
     if (a.cu) {
       int ended = 0;
-      for (int b = lane; b < c.B; b += 32) ended += (a.cu[b + 1] <= t);
+      for (int b = lane; b < c.B; b += 32) ended += (a.cu[b + 1] <= tt);
       s = __reduce_add_sync(0xffffffffu, ended);
     }
     if (lane == 0) {
       int64_t idx = -1, slot = -1;
       if (s < c.B) {
         const int64_t m = c.kv_lens[s];
-        idx = a.cu ? m - (int64_t)a.cu[s + 1] + t : m - 1;
-        if (a.cu && t < a.cu[s]) idx = -1;  // before the first sequence
+        idx = a.cu ? m - (int64_t)a.cu[s + 1] + tt : m - 1;
+        if (a.cu && tt < a.cu[s]) idx = -1;  // before the first sequence
         const int64_t col = idx >> c.page_shift;
         if (idx >= 0 && col < c.max_pages) {
           const int64_t page = c.table[s * c.table_ld + col];
@@ -79,163 +125,181 @@ qkv_append_kernel(const __grid_constant__ AppendArgs a, int heads_per_cta) {
         }
       }
       s_slot[i] = slot;
-      s_pos[i] = a.positions ? (float)a.positions[t] : (float)idx;
+      s_pos[i] = a.positions ? (float)a.positions[tt] : (float)idx;
     }
   }
   __syncthreads();
   for (int i = threadIdx.x; i < nt * a.pairs; i += QA_T) {
-    const int tok = i / a.pairs, pr = i - tok * a.pairs;
-    const float2 cs = turn(s_pos[tok], a.inv_freq[pr]);
-    s_turn[tok][pr] = make_float2(cs.x * a.rope_scale, cs.y * a.rope_scale);
+    const int k = i / a.pairs, pr = i - k * a.pairs;
+    const float2 cs = turn(s_pos[k], a.inv_freq[pr]);
+    s_turn[k][pr] = make_float2(cs.x * a.rope_scale, cs.y * a.rope_scale);
   }
   __syncthreads();
-
-  const int heads = a.q_heads + 2 * c.kv_heads;  // queries, keys, values
-  const int h0 = blockIdx.y * heads_per_cta;
-  const int nh = min(heads_per_cta, heads - h0);
-  const int rows = nt * nh;
-  const int l = threadIdx.x & (L - 1), grp = threadIdx.x / L;
-  constexpr int GROUPS = QA_T / L;
-  const int e0 = 8 * l;
-  const bool on = e0 < c.head_dim;
+  if (tok >= nt) return;  // whole groups; no barrier follows
+  const unsigned mates = (L == 32 ? 0xffffffffu : ((1u << L) - 1)) << (lane & ~(L - 1));
+  const int64_t slot = s_slot[tok];
   const float inv_n = 1.f / (float)c.head_dim;
 
-  for (int r0 = grp; r0 - grp < rows; r0 += GROUPS * QA_ROWS) {
-    uint4 raw[QA_ROWS];
-    const char* src[QA_ROWS];
+  // weights and turns of this lane's vectors, multiplied together
+  auto factors = [&](const E* w, QaFactors& f) {
+    float w0[8], w1[8];
 #pragma unroll
-    for (int u = 0; u < QA_ROWS; ++u) {
-      const int r = r0 + u * GROUPS;
-      raw[u] = make_uint4(0, 0, 0, 0);
-      src[u] = nullptr;
-      if (r < rows) {
-        const int tok = r / nh;
-        const int h = h0 + r - tok * nh;
-        const int64_t t = t0 + tok;
-        const RowsView& v = h < a.q_heads ? a.q : (h < a.q_heads + c.kv_heads ? a.k : a.v);
-        const int hh = h < a.q_heads
-                           ? h
-                           : (h < a.q_heads + c.kv_heads ? h - a.q_heads
-                                                         : h - a.q_heads - c.kv_heads);
-        src[u] = v.data + t * v.token_b + hh * v.head_b;
-        if (on) raw[u] = *reinterpret_cast<const uint4*>(src[u] + 2 * e0);
+    for (int e = 0; e < 8; ++e) w0[e] = w1[e] = 1.f;
+    if (w && on0) widen8<E>(*reinterpret_cast<const uint4*>(w + 8 * v0), w0);
+    if (w && on1) widen8<E>(*reinterpret_cast<const uint4*>(w + 8 * v1), w1);
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      if (MODE == QA_PAIRED) {
+        float2 ca = make_float2(1.f, 0.f), cb = ca;
+        if (rotated) ca = s_turn[tok][8 * l + e], cb = s_turn[tok][8 * l + e + 1];
+        f.c0[e >> 1] = pk2(w0[e] * ca.x, w0[e + 1] * cb.x);
+        f.s0[e >> 1] = pk2(-w1[e] * ca.y, -w1[e + 1] * cb.y);
+        f.c1[e >> 1] = pk2(w1[e] * ca.x, w1[e + 1] * cb.x);
+        f.s1[e >> 1] = pk2(w0[e] * ca.y, w0[e + 1] * cb.y);
+      } else if (MODE == QA_INTERLEAVED) {
+        // the pair (e, e + 1) of a vector: y_e = c w_e x_e - s w_{e+1} x_{e+1}
+        const int p0 = 4 * v0 + (e >> 1), p1 = 4 * v1 + (e >> 1);
+        const float2 ca = p0 < a.pairs ? s_turn[tok][p0] : make_float2(1.f, 0.f);
+        const float2 cb = p1 < a.pairs ? s_turn[tok][p1] : make_float2(1.f, 0.f);
+        f.c0[e >> 1] = pk2(w0[e] * ca.x, w0[e + 1] * ca.x);
+        f.s0[e >> 1] = pk2(-w0[e + 1] * ca.y, w0[e] * ca.y);
+        f.c1[e >> 1] = pk2(w1[e] * cb.x, w1[e + 1] * cb.x);
+        f.s1[e >> 1] = pk2(-w1[e + 1] * cb.y, w1[e] * cb.y);
+      } else {
+        f.c0[e >> 1] = pk2(w0[e], w0[e + 1]);
+        f.c1[e >> 1] = pk2(w1[e], w1[e + 1]);
       }
     }
+  };
+  // one row of queries or keys: norm, rotation, rounding
+  auto row = [&](uint4& r0, uint4& r1, const E* w, const QaFactors& f, const char* src) {
+    float x[8], y[8];
+    widen8<E>(r0, x);
+    widen8<E>(r1, y);
+    f32x2_t a2[4], b2[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) a2[e] = pk2(x[2 * e], x[2 * e + 1]), b2[e] = pk2(y[2 * e], y[2 * e + 1]);
+    float norm = 1.f;
+    if (w) {
+      f32x2_t q = mul2(a2[0], a2[0]), r = mul2(b2[0], b2[0]);
+#pragma unroll
+      for (int e = 1; e < 4; ++e) q = fma2(a2[e], a2[e], q), r = fma2(b2[e], b2[e], r);
+      float u, v;
+      upk2(add2(q, r), u, v);
+      float ss = u + v;
+#pragma unroll
+      for (int o = L / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(mates, ss, o);
+      norm = rsqrtf(__fmaf_rn(ss, inv_n, a.eps));
+    }
+    const f32x2_t n2 = pk2(norm, norm);
+    f32x2_t u2[4], v2[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      u2[e] = mul2(a2[e], f.c0[e]);
+      v2[e] = mul2(b2[e], f.c1[e]);
+      if (MODE == QA_PAIRED) {
+        if (rotated) {
+          u2[e] = fma2(b2[e], f.s0[e], u2[e]);
+          v2[e] = fma2(a2[e], f.s1[e], v2[e]);
+        }
+      } else if (MODE == QA_INTERLEAVED) {
+        if (4 * v0 + e < a.pairs) u2[e] = fma2(pk2(x[2 * e + 1], x[2 * e]), f.s0[e], u2[e]);
+        if (4 * v1 + e < a.pairs) v2[e] = fma2(pk2(y[2 * e + 1], y[2 * e]), f.s1[e], v2[e]);
+      }
+      upk2(mul2(u2[e], n2), x[2 * e], x[2 * e + 1]);
+      upk2(mul2(v2[e], n2), y[2 * e], y[2 * e + 1]);
+    }
+    if (MODE == QA_ODD) {
+      // x and y are weighed and normalised; partners are read from the row
+      const E* xs = reinterpret_cast<const E*>(src);
+#pragma unroll 1
+      for (int k = 0; k < 2; ++k) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int i = 8 * (k ? v1 : v0) + e;
+          if (i >= 2 * a.pairs) continue;
+          const int j = i < a.pairs ? i + a.pairs : i - a.pairs;
+          float p = (float)xs[j];
+          if (w) p *= norm * (float)w[j];
+          const float2 cs = s_turn[tok][min(i, j)];
+          float& z = k ? y[e] : x[e];
+          z = i < a.pairs ? z * cs.x - p * cs.y : z * cs.x + p * cs.y;
+        }
+      }
+      __syncwarp(mates);  // partners are read before a row is written in place
+    }
+    r0 = narrow8<E>(x);
+    r1 = narrow8<E>(y);
+  };
+
+  QaFactors f;
+  int of = -1;  // what the factors are for: 0 queries, 1 keys
+  for (int h0 = h_first + sub;; ) {
 #pragma unroll
     for (int u = 0; u < QA_ROWS; ++u) {
-      const int r = r0 + u * GROUPS;
-      const bool live = r < rows;
-      const int tok = live ? r / nh : 0;
-      const int h = live ? h0 + r - tok * nh : 0;
-      const bool is_q = h < a.q_heads, is_v = h >= a.q_heads + c.kv_heads;
-      uint4 res = raw[u];
-      float x[8], y[8];
-      widen8<E>(raw[u], x);
-      float ss = 0.f;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) ss = __fmaf_rn(x[e], x[e], ss);
-#pragma unroll
-      for (int o = L / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      const E* w = reinterpret_cast<const E*>(is_q ? a.q_weight : a.k_weight);
-      const float f = w ? rsqrtf(__fmaf_rn(ss, inv_n, a.eps)) : 1.f;
-      // the partner elements, raw: half a rotation away
-      const bool first = e0 < a.pairs;
-      const bool whole = (a.pairs & 7) == 0;
-      uint4 other = raw[u];
-      if (!a.interleaved && a.pairs > 0 && whole) {
-        const int from = (lane & ~(L - 1)) + ((first ? l + (a.pairs >> 3) : l - (a.pairs >> 3)) &
-                                              (L - 1));
-        other.x = __shfl_sync(0xffffffffu, raw[u].x, from);
-        other.y = __shfl_sync(0xffffffffu, raw[u].y, from);
-        other.z = __shfl_sync(0xffffffffu, raw[u].z, from);
-        other.w = __shfl_sync(0xffffffffu, raw[u].w, from);
+      const int h = h0 + u * per_token;
+      if (h >= h_end) break;
+      const bool is_q = h < a.q_heads, is_k = !is_q && h < a.q_heads + c.kv_heads;
+      if (is_q || is_k) {
+        const E* w = reinterpret_cast<const E*>(is_q ? a.q_weight : a.k_weight);
+        if (of != (int)is_k) {
+          factors(w, f);
+          of = is_k;
+        }
+        row(x0[u], x1[u], w, f, MODE == QA_ODD ? row_of(h) : nullptr);
       }
-      if (live && on && !is_v) {
-        if (w) {
-          float g[8];
-          widen8<E>(*reinterpret_cast<const uint4*>(w + e0), g);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] *= f * g[e];
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = x[e];
-        if (e0 < 2 * a.pairs) {
-          if (a.interleaved) {
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-              const int pr = (e0 + e) >> 1;
-              if (pr < a.pairs) {
-                const float2 cs = s_turn[tok][pr];
-                y[e] = x[e] * cs.x - x[e + 1] * cs.y;
-                y[e + 1] = x[e + 1] * cs.x + x[e] * cs.y;
-              }
-            }
-          } else if (whole) {
-            float p[8];
-            widen8<E>(other, p);
-            const int pe = first ? e0 + a.pairs : e0 - a.pairs;
-            if (w) {
-              float g[8];
-              widen8<E>(*reinterpret_cast<const uint4*>(w + pe), g);
-#pragma unroll
-              for (int e = 0; e < 8; ++e) p[e] *= f * g[e];
-            }
-            const int pr = first ? e0 : pe;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float2 cs = s_turn[tok][pr + e];
-              y[e] = first ? x[e] * cs.x - p[e] * cs.y : x[e] * cs.x + p[e] * cs.y;
-            }
-          } else {
-            for (int e = 0; e < 8; ++e) {
-              const int i = e0 + e;
-              if (i >= 2 * a.pairs) break;
-              const int j = i < a.pairs ? i + a.pairs : i - a.pairs;
-              float p = (float)reinterpret_cast<const E*>(src[u])[j];
-              if (w) p *= f * (float)w[j];
-              const float2 cs = s_turn[tok][min(i, j)];
-              y[e] = i < a.pairs ? x[e] * cs.x - p * cs.y : x[e] * cs.x + p * cs.y;
-            }
-          }
-        }
-        res = narrow8<E>(y);
-      }
-      __syncwarp();  // partners are read before a row is written in place
-      if (live && on) {
-        if (is_q) {
-          *reinterpret_cast<uint4*>(a.out.data + (t0 + tok) * a.out.token_b + h * a.out.head_b +
-                                    2 * e0) = res;
-        } else if (s_slot[tok] >= 0) {
-          const int hh = h - a.q_heads - (is_v ? c.kv_heads : 0);
-          *reinterpret_cast<uint4*>((is_v ? c.v : c.k) + s_slot[tok] + hh * c.head_b + 2 * e0) =
-              res;
-        }
+      char* dst = nullptr;
+      if (is_q) dst = a.out.data + t * a.out.token_b + h * a.out.head_b;
+      else if (slot >= 0)
+        dst = (is_k ? c.k : c.v) + slot +
+              (h - a.q_heads - (is_k ? 0 : c.kv_heads)) * c.head_b;
+      if (dst) {
+        if (on0) *reinterpret_cast<uint4*>(dst + 16 * v0) = x0[u];
+        if (on1) *reinterpret_cast<uint4*>(dst + 16 * v1) = x1[u];
       }
     }
+    h0 += QA_ROWS * per_token;
+    if (h0 >= h_end) break;
+    load(h0);
   }
+}
+
+template <typename E>
+int launch(const AppendArgs& a, cudaStream_t stream) {
+  const int heads = a.q_heads + 2 * a.c.kv_heads;
+  const bool narrow = a.c.head_dim <= 64;
+  const int groups = QA_T / (narrow ? 4 : 8);
+  // tokens of a CTA: as many as give every lane several heads to keep its factors for,
+  // fewer where the GPU would not fill (152 SMs of 4 CTAs each), down to one whose heads
+  // are shared out
+  int tokens = QA_MAX_TOKENS;
+  while (tokens > 1 && (a.T + tokens - 1) / tokens < 608) tokens /= 2;
+  const int64_t tiles = (a.T + tokens - 1) / tokens;
+  const int share = (int)std::max<int64_t>(1, std::min<int64_t>(608 / tiles, heads));
+  const int least = groups / tokens;  // heads that one pass of a CTA takes
+  const int per = std::max((heads + share - 1) / share, std::min(heads, least));
+  const dim3 grid((unsigned)tiles, (unsigned)((heads + per - 1) / per));
+  const int mode = a.interleaved ? QA_INTERLEAVED : (a.pairs & 7) ? QA_ODD : QA_PAIRED;
+#define QA_LAUNCH(L, MODE) qkv_append_kernel<E, L, MODE><<<grid, QA_T, 0, stream>>>(a, tokens, per)
+  if (narrow) {
+    if (mode == QA_PAIRED) QA_LAUNCH(4, QA_PAIRED);
+    else if (mode == QA_INTERLEAVED) QA_LAUNCH(4, QA_INTERLEAVED);
+    else QA_LAUNCH(4, QA_ODD);
+  } else {
+    if (mode == QA_PAIRED) QA_LAUNCH(8, QA_PAIRED);
+    else if (mode == QA_INTERLEAVED) QA_LAUNCH(8, QA_INTERLEAVED);
+    else QA_LAUNCH(8, QA_ODD);
+  }
+#undef QA_LAUNCH
+  SLS_LAUNCH_CHECK();
+  return SLS_OK;
 }
 
 }  // namespace
 
 int launch_qkv_append(const AppendArgs& a, int dtype, cudaStream_t stream) {
   if (a.T == 0) return SLS_OK;
-  const int heads = a.q_heads + 2 * a.c.kv_heads;
-  const int64_t tiles = (a.T + QA_TOKENS - 1) / QA_TOKENS;
-  if (tiles > 0x7fffffff) return SLS_ERR_UNSUPPORTED;
-  // few tokens: their heads are spread over more CTAs
-  const int share = tiles >= 256 ? 1 : (int)std::min<int64_t>((256 + tiles - 1) / tiles, heads);
-  const int per = (heads + share - 1) / share;
-  const dim3 grid((unsigned)tiles, (unsigned)((heads + per - 1) / per));
-  const bool narrow = a.c.head_dim <= 64;
-  if (dtype == SLS_BF16) {
-    if (narrow) qkv_append_kernel<__nv_bfloat16, 8><<<grid, QA_T, 0, stream>>>(a, per);
-    else qkv_append_kernel<__nv_bfloat16, 16><<<grid, QA_T, 0, stream>>>(a, per);
-  } else {
-    if (narrow) qkv_append_kernel<__half, 8><<<grid, QA_T, 0, stream>>>(a, per);
-    else qkv_append_kernel<__half, 16><<<grid, QA_T, 0, stream>>>(a, per);
-  }
-  SLS_LAUNCH_CHECK();
-  return SLS_OK;
+  return dtype == SLS_BF16 ? launch<__nv_bfloat16>(a, stream) : launch<__half>(a, stream);
 }
 
 }  // namespace sls
