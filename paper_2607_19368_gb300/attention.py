@@ -14,7 +14,9 @@ or float16); ``page_table`` (B x max_pages int32) lists every sequence's pages a
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
+import struct
 from typing import Optional
 
 import torch
@@ -29,38 +31,28 @@ SLS_F16 = 2
 _vp, _i64, _i32, _f32, _sz = (ctypes.c_void_p, ctypes.c_int64, ctypes.c_int, ctypes.c_float,
                               ctypes.c_size_t)
 
-
-class _Cache(ctypes.Structure):
-    _fields_ = [("k", _vp), ("v", _vp), ("dtype", _i32), ("kv_heads", _i32), ("head_dim", _i32),
-                ("page_size", _i32), ("num_pages", _i64), ("page_stride", _i64),
-                ("slot_stride", _i64), ("head_stride", _i64), ("page_table", _vp),
-                ("table_ld", _i64), ("max_pages", _i32), ("kv_lens", _vp), ("batch", _i64)]
-
-
-class _Rows(ctypes.Structure):
-    _fields_ = [("data", _vp), ("token_stride", _i64), ("head_stride", _i64)]
-
-
-class _Rope(ctypes.Structure):
-    _fields_ = [("inv_freq", _vp), ("pairs", _i32), ("interleaved", _i32), ("scale", _f32)]
-
-
-_P = ctypes.POINTER
-
-# name -> (restype, argtypes); the attention part of include/sls.h
+# name -> (restype, argtypes); the attention part of include/sls.h.  Structures go as
+# packed bytes (or byref of a ctypes structure).
 EXPORTED = {
-    "sls_qkv_append": (_i32, [_P(_Rows), _P(_Rows), _P(_Rows), _i64, _i32, _P(_Cache), _vp, _vp,
-                              _vp, _vp, _f32, _P(_Rope), _P(_Rows), _vp]),
-    "sls_attention_prefill_workspace_size": (_sz, [_i64, _i32, _P(_Cache)]),
-    "sls_attention_prefill": (_i32, [_P(_Rows), _i64, _i32, _P(_Cache), _vp, _i32, _f32,
-                                     _P(_Rows), _vp, _sz, _vp]),
-    "sls_attention_decode_workspace_size": (_sz, [_i32, _P(_Cache)]),
-    "sls_attention_decode": (_i32, [_P(_Rows), _i32, _P(_Cache), _f32, _P(_Rows), _vp, _sz,
-                                    _vp]),
+    "sls_qkv_append": (_i32, [_vp, _vp, _vp, _i64, _i32, _vp, _vp, _vp, _vp, _vp, _f32, _vp, _vp,
+                              _vp]),
+    "sls_attention_prefill_workspace_size": (_sz, [_i64, _i32, _vp]),
+    "sls_attention_prefill": (_i32, [_vp, _i64, _i32, _vp, _vp, _i32, _f32, _vp, _vp, _sz, _vp]),
+    "sls_attention_decode_workspace_size": (_sz, [_i32, _vp]),
+    "sls_attention_decode": (_i32, [_vp, _i32, _vp, _f32, _vp, _vp, _sz, _vp]),
     "sls_attention_status": (_i32, [_vp]),
 }
 
 _CODES = {torch.bfloat16: 1, torch.float16: SLS_F16}
+
+# sls_kv_cache_t, sls_rows_t and sls_rope_t in native layout: the calls are a few
+# microseconds of work on the GPU at their smallest, and packing is the cheapest way to
+# hand a structure over
+_CACHE = struct.Struct("@PPiiiiqqqqPqiPq")
+_ROWS = struct.Struct("@Pqq")
+_ROPE = struct.Struct("@Piif")
+_pack_cache, _pack_rows = _CACHE.pack, _ROWS.pack
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 class Rope:
@@ -76,8 +68,8 @@ class Rope:
         self.inv_freq = inv_freq.contiguous()
         self.interleaved = bool(interleaved)
         self.scale = float(scale)
-        self._c = _Rope(self.inv_freq.data_ptr(), self.inv_freq.numel(), int(self.interleaved),
-                        self.scale)
+        self._c = _ROPE.pack(self.inv_freq.data_ptr(), self.inv_freq.numel(),
+                             int(self.interleaved), self.scale)
 
     @classmethod
     def make(cls, rot_dim: int, base: float = 10000.0, interleaved: bool = False,
@@ -104,73 +96,74 @@ class Rope:
         return cls(f.float().to(device), interleaved=interleaved, scale=scale)
 
 
-def _code(t: torch.Tensor) -> int:
-    c = _CODES.get(t.dtype)
-    if c is None:
-        raise TypeError(f"unsupported attention dtype {t.dtype} (bfloat16 or float16)")
-    return c
-
-
-def _rows(name: str, t: torch.Tensor, dtype, head_dim: int) -> _Rows:
-    if t.dim() != 3 or t.shape[2] != head_dim or t.dtype != dtype or not t.is_cuda:
-        raise ValueError(f"{name}: tokens x heads x {head_dim} of {dtype} on the GPU")
+def _rows(name: str, t: torch.Tensor, dtype, heads: int, head_dim: int, dev: int) -> bytes:
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != head_dim or t.dtype != dtype or t.get_device() != dev \
+            or (heads and shape[1] != heads):
+        raise ValueError(f"{name}: tokens x {heads or 'heads'} x {head_dim} of {dtype} on the "
+                         "cache's device")
     st, sh, se = t.stride()
     if se != 1:
         raise ValueError(f"{name}: the elements of a head must be contiguous")
     # the stride of a dimension of one entry says nothing
-    if t.shape[1] == 1:
+    if shape[1] == 1:
         sh = head_dim
-    if t.shape[0] <= 1:
-        st = sh * t.shape[1]
-    return _Rows(t.data_ptr(), st, sh)
+    if shape[0] <= 1:
+        st = sh * shape[1]
+    return _pack_rows(t.data_ptr(), st, sh)
 
 
-def _ints(name: str, t: torch.Tensor, n: Optional[int] = None) -> torch.Tensor:
-    if t.dtype != torch.int32 or not t.is_cuda or t.dim() != 1 or not t.is_contiguous() \
-            or (n is not None and t.shape[0] != n):
-        raise ValueError(f"{name}: a contiguous int32 CUDA tensor"
-                         + (f" of {n} entries" if n is not None else ""))
-    return t
+def _ints(name: str, t: torch.Tensor, n: int, dev: int) -> int:
+    if t.dtype != torch.int32 or t.shape != (n,) or not t.is_contiguous() \
+            or t.get_device() != dev:
+        raise ValueError(f"{name}: {n} contiguous int32 entries on the cache's device")
+    return t.data_ptr()
 
 
-def _cache(cache_k, cache_v, page_table, kv_lens) -> _Cache:
-    code = _code(cache_k)
-    if cache_k.dim() != 4 or cache_v.shape != cache_k.shape or cache_v.dtype != cache_k.dtype \
-            or not cache_k.is_cuda or not cache_v.is_cuda:
-        raise ValueError("cache_k, cache_v: pages x page_size x kv_heads x head_dim, alike, on "
-                         "the GPU")
-    sp, ss, sh, se = cache_k.stride()
-    if se != 1 or cache_v.stride() != cache_k.stride():
-        raise ValueError("cache_k, cache_v: equal strides, contiguous heads")
-    _ints("kv_lens", kv_lens)
-    B = kv_lens.shape[0]
-    if page_table.dim() != 2 or page_table.shape[0] != B or page_table.dtype != torch.int32 \
-            or not page_table.is_cuda or page_table.stride(1) != 1:
-        raise ValueError("page_table: B x max_pages int32 on the GPU, contiguous rows")
-    n, ps, H, hd = cache_k.shape
+def _cache(cache_k, cache_v, page_table, kv_lens):
+    """(packed sls_kv_cache_t, shape, dtype, device index, batch, page table columns)"""
+    dt, shape, dev = cache_k.dtype, cache_k.shape, cache_k.get_device()
+    code = _CODES.get(dt)
+    if code is None:
+        raise TypeError(f"unsupported attention dtype {dt} (bfloat16 or float16)")
+    strides = cache_k.stride()
+    if dev < 0 or len(shape) != 4 or cache_v.shape != shape or cache_v.dtype != dt \
+            or cache_v.get_device() != dev or strides[3] != 1 or cache_v.stride() != strides:
+        raise ValueError("cache_k, cache_v: pages x page_size x kv_heads x head_dim on one GPU, "
+                         "of equal strides, the elements of a head contiguous")
+    table = page_table.shape
+    if len(table) != 2 or page_table.dtype != torch.int32 or page_table.get_device() != dev:
+        raise ValueError("page_table: B x max_pages int32 on the cache's device")
+    B, cols = table
+    ld, se = page_table.stride()
+    if se != 1 and cols > 1:
+        raise ValueError("page_table: contiguous rows")
+    lens = _ints("kv_lens", kv_lens, B, dev)
+    n, ps, H, hd = shape
+    sp, ss, sh, _ = strides
     if H == 1:
         sh = hd
-    if n <= 1:
+    if n == 1:
         sp = ps * max(ss, sh * H)
-    cols = page_table.shape[1]
-    return _Cache(cache_k.data_ptr(), cache_v.data_ptr(), code, H, hd, ps, n, sp, ss, sh,
-                  page_table.data_ptr(), max(page_table.stride(0), cols), cols,
-                  kv_lens.data_ptr(), B)
+    return (_pack_cache(cache_k.data_ptr(), cache_v.data_ptr(), code, H, hd, ps, n, sp, ss, sh,
+                        page_table.data_ptr(), ld if ld > cols else cols, cols, lens, B),
+            shape, dt, dev, B, cols)
 
 
-def _weight(name: str, w: Optional[torch.Tensor], dtype, head_dim: int):
+def _weight(name: str, w: Optional[torch.Tensor], dtype, head_dim: int, dev: int):
     if w is None:
         return None
-    if w.dtype != dtype or w.shape != (head_dim,) or not w.is_contiguous() or not w.is_cuda:
-        raise ValueError(f"{name}: {head_dim} contiguous elements of {dtype} on the GPU")
+    if w.dtype != dtype or w.shape != (head_dim,) or not w.is_contiguous() \
+            or w.get_device() != dev:
+        raise ValueError(f"{name}: {head_dim} contiguous elements of {dtype} on the cache's device")
     return w.data_ptr()
 
 
-def _done(fn: str, st: int, t: torch.Tensor):
-    _sls._check(fn, st)
+def _done(fn: str, st: int, dev: int):
+    if st != 0:
+        _sls._check(fn, st)
     if _sls._CHECK_STATUS:
-        with torch.cuda.device(t.device):
-            st = int(_sls.lib().sls_attention_status(_sls._stream(t)))
+        st = attention_status(dev)
         if st != 0:
             raise _sls.SLSError(fn + " (device status)", st,
                                 _sls.lib().sls_status_string(st).decode())
@@ -190,51 +183,69 @@ def qkv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_k: torch
     T x kv_heads x head_dim (any token and head strides that are multiples of 8);
     cu_seqlens packs the new tokens (B + 1 int32; None: one token per sequence).
     kv_lens counts the new tokens.  Returns the queries (`out`, which may be q)."""
-    c = _cache(cache_k, cache_v, page_table, kv_lens)
-    dt, hd = cache_k.dtype, cache_k.shape[3]
-    T, Hq = q.shape[0], q.shape[1]
+    c, (_, _, H, hd), dt, dev, B, _ = _cache(cache_k, cache_v, page_table, kv_lens)
+    shape = q.shape
     if out is None:
-        out = torch.empty((T, Hq, hd), dtype=q.dtype, device=q.device)
-    rq, rk, rv, ro = (_rows("q", q, dt, hd), _rows("k", k, dt, hd), _rows("v", v, dt, hd),
-                      _rows("out", out, dt, hd))
-    want = (T, c.kv_heads, hd)
-    if tuple(k.shape) != want or tuple(v.shape) != want or out.shape != q.shape:
-        raise ValueError("k and v: one row per token of q and key head; out: the shape of q")
+        out = q.new_empty(shape)
+    elif out.shape != shape:
+        raise ValueError("out: the shape of q")
+    T = shape[0]
+    if k.shape[0] != T or v.shape[0] != T:
+        raise ValueError("k and v: one row per token of q and key head")
+    rq, ro = _rows("q", q, dt, 0, hd, dev), _rows("out", out, dt, 0, hd, dev)
+    rk, rv = _rows("k", k, dt, H, hd, dev), _rows("v", v, dt, H, hd, dev)
     if cu_seqlens is not None:
-        _ints("cu_seqlens", cu_seqlens, c.batch + 1)
-    elif T != c.batch:
+        cu_seqlens = _ints("cu_seqlens", cu_seqlens, B + 1, dev)
+    elif T != B:
         raise ValueError("without cu_seqlens q has one token per sequence")
     if positions is not None:
-        _ints("positions", positions, T)
-    st = _sls.lib().sls_qkv_append(
-        rq, rk, rv, T, Hq, c, None if cu_seqlens is None else cu_seqlens.data_ptr(),
-        None if positions is None else positions.data_ptr(),
-        _weight("q_weight", q_weight, dt, hd), _weight("k_weight", k_weight, dt, hd), eps,
-        None if rope is None else rope._c, ro, _sls._stream(q))
-    _done("sls_qkv_append", st, q)
+        positions = _ints("positions", positions, T, dev)
+    if q_weight is not None:
+        q_weight = _weight("q_weight", q_weight, dt, hd, dev)
+    if k_weight is not None:
+        k_weight = _weight("k_weight", k_weight, dt, hd, dev)
+    st = (_sls._lib or _sls.lib()).sls_qkv_append(
+        rq, rk, rv, T, shape[1], c, cu_seqlens, positions, q_weight, k_weight, eps,
+        None if rope is None else rope._c, ro, _raw_stream(dev))
+    _done("sls_qkv_append", st, dev)
     return out
 
 
-def _attention_args(q, cache_k, out, scale):
-    dt, hd = cache_k.dtype, cache_k.shape[3]
+def _attention_rows(q, out, scale, dt, hd, dev):
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = q.new_empty(q.shape)
     elif out.shape != q.shape:
         raise ValueError("out: the shape of q")
-    return (_rows("q", q, dt, hd), _rows("out", out, dt, hd), out,
-            1.0 / math.sqrt(hd) if scale is None else float(scale))
+    return (_rows("q", q, dt, 0, hd, dev), _rows("out", out, dt, 0, hd, dev), out,
+            hd ** -0.5 if scale is None else float(scale))
 
 
-def _scratch(nbytes: int, workspace: Optional[torch.Tensor], device):
-    """(pointer, bytes, tensor) of a caller's workspace (a uint8 tensor) or of one
-    for this call."""
+def _scratch(nbytes: int, workspace: Optional[torch.Tensor], q: torch.Tensor):
+    """A caller's workspace (a uint8 tensor) or one for this call."""
     if workspace is None:
-        if nbytes == 0:
-            return None, 0, None
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    elif not workspace.is_cuda or workspace.dtype != torch.uint8:
+        return q.new_empty(nbytes, dtype=torch.uint8)
+    if not workspace.is_cuda or workspace.dtype != torch.uint8:
         raise ValueError("workspace: a uint8 CUDA tensor")
-    return workspace.data_ptr(), workspace.numel(), workspace
+    return workspace
+
+
+# a workspace's size depends on these numbers alone (pointers that are never read stand
+# in for the cache's)
+def _size_args(code, H, hd, ps, n, B, cols):
+    return _pack_cache(256, 256, code, H, hd, ps, n, ps * H * hd, H * hd, hd, 256, cols, cols,
+                       256, B)
+
+
+@functools.lru_cache(maxsize=256)
+def _decode_bytes(dev, Hq, *cache) -> int:
+    with torch.cuda.device(dev):
+        return int(_sls.lib().sls_attention_decode_workspace_size(Hq, _size_args(*cache)))
+
+
+@functools.lru_cache(maxsize=256)
+def _prefill_bytes(dev, T, Hq, *cache) -> int:
+    with torch.cuda.device(dev):
+        return int(_sls.lib().sls_attention_prefill_workspace_size(T, Hq, _size_args(*cache)))
 
 
 def attention_prefill(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tensor,
@@ -247,15 +258,18 @@ def attention_prefill(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Ten
     sequence with n new and kv_lens tokens sees the cache up to its own index
     kv_lens - n + i (causal) or all of it.  scale defaults to head_dim^-0.5.
     Returns q's shape; rows that see no key are zero."""
-    c = _cache(cache_k, cache_v, page_table, kv_lens)
-    rq, ro, out, scale = _attention_args(q, cache_k, out, scale)
-    _ints("cu_seqlens", cu_seqlens, c.batch + 1)
-    T, Hq = q.shape[0], q.shape[1]
-    L = _sls.lib()
-    wp, wn, keep = _scratch(L.sls_attention_prefill_workspace_size(T, Hq, c), workspace, q.device)
-    st = L.sls_attention_prefill(rq, T, Hq, c, cu_seqlens.data_ptr(), int(causal), scale, ro, wp,
-                                 wn, _sls._stream(q))
-    _done("sls_attention_prefill", st, q)
+    c, (n, ps, H, hd), dt, dev, B, cols = _cache(cache_k, cache_v, page_table, kv_lens)
+    rq, ro, out, scale = _attention_rows(q, out, scale, dt, hd, dev)
+    cu = _ints("cu_seqlens", cu_seqlens, B + 1, dev)
+    T, Hq, _ = q.shape
+    nbytes = _prefill_bytes(dev, T, Hq, _CODES[dt], H, hd, ps, n, B, cols)
+    wp = 0
+    if nbytes:
+        workspace = _scratch(nbytes, workspace, q)
+        wp, nbytes = workspace.data_ptr(), workspace.numel()
+    st = (_sls._lib or _sls.lib()).sls_attention_prefill(rq, T, Hq, c, cu, causal, scale, ro, wp,
+                                                         nbytes, _raw_stream(dev))
+    _done("sls_attention_prefill", st, dev)
     return out
 
 
@@ -265,15 +279,19 @@ def attention_decode(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tens
                      out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """One token per sequence (q: B x q_heads x head_dim) over all kv_lens tokens of
     its sequence.  Returns q's shape; a sequence of length 0 gives zeros."""
-    c = _cache(cache_k, cache_v, page_table, kv_lens)
-    rq, ro, out, scale = _attention_args(q, cache_k, out, scale)
-    if q.shape[0] != c.batch:
+    c, (n, ps, H, hd), dt, dev, B, cols = _cache(cache_k, cache_v, page_table, kv_lens)
+    rq, ro, out, scale = _attention_rows(q, out, scale, dt, hd, dev)
+    T, Hq, _ = q.shape
+    if T != B:
         raise ValueError("q: one token per sequence")
-    Hq = q.shape[1]
-    L = _sls.lib()
-    wp, wn, keep = _scratch(L.sls_attention_decode_workspace_size(Hq, c), workspace, q.device)
-    st = L.sls_attention_decode(rq, Hq, c, scale, ro, wp, wn, _sls._stream(q))
-    _done("sls_attention_decode", st, q)
+    nbytes = _decode_bytes(dev, Hq, _CODES[dt], H, hd, ps, n, B, cols)
+    wp = 0
+    if nbytes:
+        workspace = _scratch(nbytes, workspace, q)
+        wp, nbytes = workspace.data_ptr(), workspace.numel()
+    st = (_sls._lib or _sls.lib()).sls_attention_decode(rq, Hq, c, scale, ro, wp, nbytes,
+                                                        _raw_stream(dev))
+    _done("sls_attention_decode", st, dev)
     return out
 
 

@@ -19,7 +19,7 @@ namespace sls {
 namespace {
 
 constexpr int QA_T = 128;
-constexpr int QA_ROWS = 4;     // rows in flight per lane
+constexpr int QA_ROWS = 2;     // rows in flight per lane
 constexpr int QA_MAX_TOKENS = 8;
 constexpr int QA_MAX_PAIRS = SLS_MAX_HEAD_DIM / 2;
 
@@ -55,7 +55,7 @@ struct QaFactors {
 
 // L lanes per row; heads of one token are shared by QA_T / (L tokens) groups of lanes
 template <typename E, int L, int MODE>
-__global__ void __launch_bounds__(QA_T, 4)
+__global__ void __launch_bounds__(QA_T, 6)
 qkv_append_kernel(const __grid_constant__ AppendArgs a, int tokens, int heads_per_cta) {
   __shared__ float2 s_turn[QA_MAX_TOKENS][QA_MAX_PAIRS];  // (cos, sin) * scale
   __shared__ int64_t s_slot[QA_MAX_TOKENS];               // byte offset of the token's slot, or -1

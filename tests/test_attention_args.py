@@ -14,18 +14,46 @@ def sls():
     return sls
 
 
+class _Cache(ctypes.Structure):
+    """sls_kv_cache_t as the header declares it."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_int),
+                ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("page_size", ctypes.c_int), ("num_pages", ctypes.c_int64),
+                ("page_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("page_table", ctypes.c_void_p),
+                ("table_ld", ctypes.c_int64), ("max_pages", ctypes.c_int),
+                ("kv_lens", ctypes.c_void_p), ("batch", ctypes.c_int64)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("pairs", ctypes.c_int),
+                ("interleaved", ctypes.c_int), ("scale", ctypes.c_float)]
+
+
+def test_packed_layouts_are_the_structures(sls):
+    from paper_2607_19368_gb300 import attention as A
+    for packed, kind in ((A._CACHE, _Cache), (A._ROWS, _Rows), (A._ROPE, _Rope)):
+        # one odd value per field, in the header's order
+        vals = [float(i + 1) if f[1] is ctypes.c_float else 1001 + i
+                for i, f in enumerate(kind._fields_)]
+        assert packed.pack(*vals).ljust(ctypes.sizeof(kind), b"\0") == bytes(kind(*vals))
+
+
 def cache(sls, **kw):
-    from paper_2607_19368_gb300.attention import _Cache
     a = dict(k=256, v=256, dtype=1, kv_heads=2, head_dim=64, page_size=16, num_pages=4,
              page_stride=16 * 128, slot_stride=128, head_stride=64, page_table=256, table_ld=2,
              max_pages=2, kv_lens=256, batch=2)
     a.update(kw)
-    return _Cache(**a)
+    return ctypes.byref(_Cache(**a))
 
 
 def rows(data=256, token=512, head=64):
-    from paper_2607_19368_gb300.attention import _Rows
-    return _Rows(data, token, head)
+    return ctypes.byref(_Rows(data, token, head))
 
 
 BAD_CACHE = [
@@ -53,8 +81,10 @@ def test_caches_that_are_refused(sls, change, status):
 
 
 def test_rows_and_options_that_are_refused(sls):
-    from paper_2607_19368_gb300.attention import _Rope
     L, c, r = sls.lib(), cache(sls), rows()
+
+    def rope(inv_freq, pairs):
+        return ctypes.byref(_Rope(inv_freq, pairs, 0, 1.0))
 
     def append(q=r, k=r, v=r, T=3, cu=256, qw=None, eps=1e-6, rope=None, out=r, Hq=4):
         return L.sls_qkv_append(q, k, v, T, Hq, c, cu, None, qw, None, eps, rope, out, None)
@@ -68,8 +98,8 @@ def test_rows_and_options_that_are_refused(sls):
     assert append(T=-1) == 1 and append(T=3, cu=None) == 1 and append(qw=8) == 1
     assert append(eps=-1.0) == 1 and append(eps=math.nan) == 1 and append(Hq=3) == 1
     assert append(Hq=0) == 1
-    assert append(rope=_Rope(256, 33, 0, 1.0)) == 1 and append(rope=_Rope(None, 8, 0, 1.0)) == 1
-    assert append(rope=_Rope(256, -1, 0, 1.0)) == 1
+    assert append(rope=rope(256, 33)) == 1 and append(rope=rope(None, 8)) == 1
+    assert append(rope=rope(256, -1)) == 1
     assert L.sls_attention_prefill(r, 3, 4, c, None, 1, 1.0, r, None, 0, None) == 1
     assert L.sls_attention_prefill(r, 3, 4, None, 256, 1, 1.0, r, None, 0, None) == 1
     # nothing to do is no error
