@@ -186,7 +186,7 @@ def qkv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_k: torch
     c, (_, _, H, hd), dt, dev, B, _ = _cache(cache_k, cache_v, page_table, kv_lens)
     shape = q.shape
     if out is None:
-        out = q.new_empty(shape)
+        out = torch.empty_like(q)
     elif out.shape != shape:
         raise ValueError("out: the shape of q")
     T = shape[0]
@@ -213,7 +213,7 @@ def qkv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_k: torch
 
 def _attention_rows(q, out, scale, dt, hd, dev):
     if out is None:
-        out = q.new_empty(q.shape)
+        out = torch.empty_like(q)
     elif out.shape != q.shape:
         raise ValueError("out: the shape of q")
     return (_rows("q", q, dt, 0, hd, dev), _rows("out", out, dt, 0, hd, dev), out,

@@ -29,8 +29,6 @@ namespace {
 
 __device__ int g_status;  // SLS_ERR_TIMEOUT once a wait gave up
 
-constexpr int AD_WARPS = 4;
-constexpr int AD_T = 32 * AD_WARPS;
 constexpr int AD_KEYS = 32;       // tokens of a step
 constexpr int AD_MIN_STEPS = 2;   // a part holds at least so many steps where there are as many
 constexpr int AD_ROWS = 16;       // query heads of a tile
@@ -42,8 +40,12 @@ struct AdShape {
   static constexpr int HALF_BYTES = AD_KEYS * 128;
   static constexpr int MAT_BYTES = HALVES * HALF_BYTES;  // K or V of a step
   static constexpr int STAGE_BYTES = 2 * MAT_BYTES;
-  static constexpr int STAGES = HD == 128 ? 3 : 6;
-  static constexpr size_t SMEM = (size_t)AD_WARPS * STAGES * STAGE_BYTES + 1024;
+  // narrow heads have half the bytes a step and nearly the same instructions: twice the
+  // warps
+  static constexpr int WARPS = HD == 128 ? 4 : 8;
+  static constexpr int THREADS = 32 * WARPS;
+  static constexpr int STAGES = 3;
+  static constexpr size_t SMEM = (size_t)WARPS * STAGES * STAGE_BYTES + 1024;
 };
 
 // Parts, their groups of warps and the pieces in the workspace.
@@ -94,15 +96,16 @@ SLS_DEV void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32
 }
 
 template <typename E, int HD>
-__global__ void __launch_bounds__(AD_T, 1)
+__global__ void __launch_bounds__(AdShape<HD>::THREADS, 1)
 attention_decode_kernel(const __grid_constant__ CUtensorMap tmK,
                         const __grid_constant__ CUtensorMap tmV,
                         const __grid_constant__ AttnArgs a, const __grid_constant__ AdPlan p) {
   using S = AdShape<HD>;
+  constexpr int AD_T = S::THREADS;
   constexpr int KS = HD / 16;  // 16-element slices of a head
   constexpr int NB = HD / 8;   // 8-element blocks of a head
   extern __shared__ __align__(1024) unsigned char smem_raw[];
-  __shared__ uint64_t full_bar[AD_WARPS][S::STAGES];
+  __shared__ uint64_t full_bar[S::WARPS][S::STAGES];
   __shared__ int64_t s_pre[AD_T + 1];
   const CacheView& c = a.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -141,7 +144,7 @@ attention_decode_kernel(const __grid_constant__ CUtensorMap tmK,
   }
   const int64_t total = s_pre[AD_T];
   const int parts = ad_parts(total, p.groups);
-  const int gw = blockIdx.x * AD_WARPS + warp;
+  const int gw = blockIdx.x * S::WARPS + warp;
   const int g = gw / p.vheads, vh = gw - g * p.vheads;
   if (g >= parts) return;
   const int64_t t0 = total * g / parts, t1 = total * (g + 1) / parts;
@@ -468,13 +471,14 @@ int ad_host(const CacheView& c, int q_heads, AdHost* h) {
   int dev = 0, sms = 0;
   SLS_CUDA_TRY(cudaGetDevice(&dev));
   SLS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  const int warps = c.head_dim > 64 ? AdShape<128>::WARPS : AdShape<64>::WARPS;
   const int group = q_heads / c.kv_heads, blocks = (group + AD_ROWS - 1) / AD_ROWS;
   h->vheads = c.kv_heads * blocks;
-  h->groups = std::max(1, sms * AD_WARPS / h->vheads);
+  h->groups = std::max(1, sms * warps / h->vheads);
   // no more parts than the page tables can hold steps for
   const int64_t most = (int64_t)c.B * (((int64_t)c.max_pages << c.page_shift) / AD_KEYS + 1);
   h->groups = (int)std::min<int64_t>(h->groups, (most + AD_MIN_STEPS - 1) / AD_MIN_STEPS);
-  h->grid = (h->groups * h->vheads + AD_WARPS - 1) / AD_WARPS;
+  h->grid = (h->groups * h->vheads + warps - 1) / warps;
   h->hd_pad = c.head_dim;
   h->prefix_b = sls_align256(((size_t)c.B + 1) * 8);
   const size_t rows = (size_t)h->groups * 2 * h->vheads * AD_ROWS;
@@ -495,7 +499,7 @@ int launch(const AttnArgs& a, const AdPlan& p, int grid, const CUtensorMap& k,
                                       (int)AdShape<HD>::SMEM));
     if (dev < 64) set[dev] = true;
   }
-  kern<<<grid, AD_T, AdShape<HD>::SMEM, stream>>>(k, v, a, p);
+  kern<<<grid, AdShape<HD>::THREADS, AdShape<HD>::SMEM, stream>>>(k, v, a, p);
   SLS_LAUNCH_CHECK();
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((int64_t)a.c.B * a.q_heads));
