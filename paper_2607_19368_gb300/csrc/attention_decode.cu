@@ -95,98 +95,31 @@ SLS_DEV void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-template <typename E, int HD>
-__global__ void __launch_bounds__(AdShape<HD>::THREADS, 1)
-attention_decode_kernel(const __grid_constant__ CUtensorMap tmK,
-                        const __grid_constant__ CUtensorMap tmV,
-                        const __grid_constant__ AttnArgs a, const __grid_constant__ AdPlan p) {
+// A warp's ring: its next steps are copied ahead, from sequence to sequence.
+template <int HD>
+struct AdRing {
   using S = AdShape<HD>;
-  constexpr int AD_T = S::THREADS;
-  constexpr int KS = HD / 16;  // 16-element slices of a head
-  constexpr int NB = HD / 8;   // 8-element blocks of a head
-  extern __shared__ __align__(1024) unsigned char smem_raw[];
-  __shared__ uint64_t full_bar[S::WARPS][S::STAGES];
-  __shared__ int64_t s_pre[AD_T + 1];
-  const CacheView& c = a.c;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const CacheView& c;
+  const CUtensorMap* tmK;
+  const CUtensorMap* tmV;
+  unsigned char* mem;
+  uint64_t* bars;
+  int kvh;
+  uint32_t lead;
+  int is, ij, ilen;  // the step to issue next: its sequence, its number there, the length
+  int64_t left;      // steps still to issue
+  int batch0, page;  // lane l: the page of tokens 16 l of the batch of 16 steps from batch0 on
+  unsigned issued, used;
 
-  // the next launch may start its preamble
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  // steps before every chunk of R sequences
-  const int R = (c.B + AD_T - 1) / AD_T;
-  {
-    int64_t mine = 0;
-    const int s0 = min(c.B, (int)threadIdx.x * R), s1 = min(c.B, s0 + R);
-    for (int s = s0; s < s1; ++s) mine += ad_steps(c, s);
-    int64_t pre = mine;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const int64_t x = __shfl_up_sync(0xffffffffu, pre, d);
-      if (lane >= d) pre += x;
-    }
-    if (lane == 31) s_pre[warp] = pre;
-    if (lane < S::STAGES) mbar_init(&full_bar[warp][lane], 1);
-    mbar_fence_init();
-    __syncthreads();
-    for (int w = 0; w < warp; ++w) pre += s_pre[w];
-    __syncthreads();
-    s_pre[threadIdx.x + 1] = pre;
-    if (threadIdx.x == 0) s_pre[0] = 0;
-    if (blockIdx.x == 0) {
-      int64_t at = pre - mine;
-      for (int s = s0; s < s1; ++s) {
-        p.prefix[s] = at;
-        at += ad_steps(c, s);
-      }
-      if (threadIdx.x == AD_T - 1) p.prefix[c.B] = pre;
-    }
-    __syncthreads();
-  }
-  const int64_t total = s_pre[AD_T];
-  const int parts = ad_parts(total, p.groups);
-  const int gw = blockIdx.x * S::WARPS + warp;
-  const int g = gw / p.vheads, vh = gw - g * p.vheads;
-  if (g >= parts) return;
-  const int64_t t0 = total * g / parts, t1 = total * (g + 1) / parts;
-  const int group = a.q_heads / c.kv_heads;
-  const int blocks = (group + AD_ROWS - 1) / AD_ROWS;
-  const int kvh = vh / blocks, row0 = (vh - kvh * blocks) * AD_ROWS;
-  const int rows = min(AD_ROWS, group - row0);
-  const int head0 = kvh * group + row0;
-
-  // the sequence of step t0
-  int seq;
-  int64_t before;  // steps before seq
-  {
-    int lo = 0, hi = AD_T - 1;  // the last chunk that starts at or before t0
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (s_pre[mid] <= t0) lo = mid;
-      else hi = mid - 1;
-    }
-    seq = lo * R;
-    before = s_pre[lo];
-    for (;;) {
-      const int n = ad_steps(c, seq);
-      if (t0 < before + n) break;
-      before += n;
-      ++seq;
-    }
+  SLS_DEV AdRing(const CacheView& cache, const CUtensorMap* k, const CUtensorMap* v,
+                 unsigned char* ring, uint64_t* b, int head, int seq, int step, int len, int64_t n)
+      : c(cache), tmK(k), tmV(v), mem(ring), bars(b), kvh(head), lead(at_elect()), is(seq),
+        ij(step), ilen(len), left(n), batch0(-1), page(-1), issued(0), used(0) {
+#pragma unroll 1
+    for (int i = 0; i < S::STAGES; ++i) issue();
   }
 
-  // ---- the ring: step `issued` of this warp goes to stage issued % STAGES ----
-  unsigned char* smem = reinterpret_cast<unsigned char*>(
-      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-  unsigned char* ring = smem + warp * S::STAGES * S::STAGE_BYTES;
-  const uint32_t ring_s = smem_u32(ring);
-  uint64_t* bars = full_bar[warp];
-  const int box = min(AD_KEYS, 1 << c.page_shift);  // 16 or 32 slots of one copy
-  int is = seq, ij = (int)(t0 - before), ilen = (int)cache_len(c, seq);
-  int64_t left = t1 - t0;  // steps still to issue
-  int batch0 = -1, page = -1;  // lane l: the page of tokens 16 l of the batch of 16 steps
-  unsigned issued = 0;
-  const uint32_t lead = at_elect();
-  auto issue = [&]() {
+  SLS_DEV void issue() {
     if (left == 0) return;
     if (ij * AD_KEYS >= ilen) {
       do {
@@ -196,80 +129,87 @@ attention_decode_kernel(const __grid_constant__ CUtensorMap tmK,
       ij = 0;
       batch0 = -1;
     }
+    const int lane = threadIdx.x & 31;
     if (batch0 < 0 || ij - batch0 == 16) {
       batch0 = ij;
       const int x = ij * AD_KEYS + 16 * lane;
       page = x < ilen ? c.table[is * c.table_ld + (x >> c.page_shift)] : -1;
     }
     const unsigned st = issued % S::STAGES;
-    const int here = min(AD_KEYS, ilen - ij * AD_KEYS);
-    const int copies = (here + box - 1) / box;
+    const int box = min(AD_KEYS, 1 << c.page_shift);  // 16 or 32 slots of one copy
+    const int copies = (min(AD_KEYS, ilen - ij * AD_KEYS) + box - 1) / box;
     const int slot0 = (ij * AD_KEYS) & ((1 << c.page_shift) - 1);
     if (lead) mbar_expect_tx(&bars[st], 2 * S::HALVES * copies * box * 128);
     __syncwarp();
 #pragma unroll 1
     for (int cp = 0; cp < copies; ++cp) {
       const int pg = __shfl_sync(0xffffffffu, page, 2 * (ij - batch0) + cp);
-      const uint32_t dst = ring_s + st * S::STAGE_BYTES + cp * box * 128;
+      const uint32_t dst = smem_u32(mem) + st * S::STAGE_BYTES + cp * box * 128;
 #pragma unroll
       for (int h = 0; h < S::HALVES; ++h) {
-        at_tma4(lead, dst + h * S::HALF_BYTES, &tmK, 64 * h, slot0, kvh, pg, &bars[st]);
-        at_tma4(lead, dst + S::MAT_BYTES + h * S::HALF_BYTES, &tmV, 64 * h, slot0, kvh, pg,
+        at_tma4(lead, dst + h * S::HALF_BYTES, tmK, 64 * h, slot0, kvh, pg, &bars[st]);
+        at_tma4(lead, dst + S::MAT_BYTES + h * S::HALF_BYTES, tmV, 64 * h, slot0, kvh, pg,
                 &bars[st]);
       }
     }
     ++ij;
     ++issued;
     --left;
-  };
-#pragma unroll 1
-  for (int i = 0; i < S::STAGES; ++i) issue();
+  }
 
-  const float cs = a.scale * 1.4426950408889634f;
-  const int r = lane >> 2, cq = 2 * (lane & 3);
-  unsigned used = 0;
-  int64_t t = t0;
-  while (t < t1) {
-    // ---- a piece: steps [j0, j1) of sequence seq ----
-    const int len = (int)cache_len(c, seq);
-    const int n = (len + AD_KEYS - 1) / AD_KEYS;
-    if (n == 0) {
-      ++seq;
-      continue;
-    }
-    const int j0 = (int)(t - before);
-    const int j1 = (int)min((int64_t)n, t1 - before);
-    uint32_t q[KS][4];
-    {
-      const char* qp = a.q.data + seq * a.q.token_b + head0 * a.q.head_b;
+  // Waits for the next step; false when the time is up, after the other copies in
+  // flight have landed or run out of time too.
+  SLS_DEV bool wait() {
+    if (__all_sync(0xffffffffu, mbar_wait(&bars[used % S::STAGES], (used / S::STAGES) & 1)))
+      return true;
+    if ((threadIdx.x & 31) == 0) atomicExch(&g_status, SLS_ERR_TIMEOUT);
+    for (unsigned x = used + 1; x < issued; ++x)
+      mbar_wait(&bars[x % S::STAGES], (x / S::STAGES) & 1);
+    return false;
+  }
+};
+
+// The rows of a piece: queries as A fragments, unnormalised outputs, the maximum in use
+// and this lane's part of the sum of weights, for rows lane / 4 and lane / 4 + 8.
+template <typename E, int HD>
+struct AdRows {
+  using S = AdShape<HD>;
+  static constexpr int KS = HD / 16;  // 16-element slices of a head
+  static constexpr int NB = HD / 8;   // 8-element blocks of a head
+  uint32_t q[KS][4];
+  float o[NB][4];
+  float mx[2], l[2];
+
+  SLS_DEV void start(const AttnArgs& a, int seq, int head0, int rows) {
+    const int lane = threadIdx.x & 31, r = lane >> 2, cq = 2 * (lane & 3);
+    const char* qp = a.q.data + seq * a.q.token_b + head0 * a.q.head_b;
 #pragma unroll
-      for (int k = 0; k < KS; ++k)
+    for (int k = 0; k < KS; ++k)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int rr = r + 8 * (i & 1), e = 16 * k + cq + 8 * (i >> 1);
-          q[k][i] = (rr < rows && e < c.head_dim)
-                        ? *reinterpret_cast<const uint32_t*>(qp + rr * a.q.head_b + 2 * e)
-                        : 0u;
-        }
-    }
-    float o[NB][4];
+      for (int i = 0; i < 4; ++i) {
+        const int rr = r + 8 * (i & 1), e = 16 * k + cq + 8 * (i >> 1);
+        q[k][i] = (rr < rows && e < a.c.head_dim)
+                      ? *reinterpret_cast<const uint32_t*>(qp + rr * a.q.head_b + 2 * e)
+                      : 0u;
+      }
 #pragma unroll
     for (int b = 0; b < NB; ++b) o[b][0] = o[b][1] = o[b][2] = o[b][3] = 0.f;
-    float mx[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-    for (int j = j0; j < j1; ++j, ++used) {
-      const unsigned st = used % S::STAGES;
-      if (!__all_sync(0xffffffffu, mbar_wait(&bars[st], (used / S::STAGES) & 1))) {
-        // the other copies of the warp land, or run out of time too, before it leaves
-        if (lane == 0) atomicExch(&g_status, SLS_ERR_TIMEOUT);
-        for (unsigned x = used + 1; x < issued; ++x)
-          mbar_wait(&bars[x % S::STAGES], (x / S::STAGES) & 1);
-        return;
-      }
-      const uint32_t kb = ring_s + st * S::STAGE_BYTES, vb = kb + S::MAT_BYTES;
+    mx[0] = mx[1] = -INFINITY;
+    l[0] = l[1] = 0.f;
+  }
+
+  // steps [j0, j1) of a sequence of `len` tokens; cs: scale log2(e)
+  SLS_DEV bool run(AdRing<HD>& ring, int len, int j0, int j1, float cs) {
+    const int lane = threadIdx.x & 31, cq = 2 * (lane & 3);
+#pragma unroll 1
+    for (int j = j0; j < j1; ++j) {
+      if (!ring.wait()) return false;
+      unsigned char* stage = ring.mem + (ring.used % S::STAGES) * S::STAGE_BYTES;
+      const uint32_t kb = smem_u32(stage), vb = kb + S::MAT_BYTES;
       const int lim = len - j * AD_KEYS;
       if (lim < AD_KEYS) {
         // values past the end: whatever their slots hold, zero here
-        unsigned char* v = ring + st * S::STAGE_BYTES + S::MAT_BYTES;
+        unsigned char* v = stage + S::MAT_BYTES;
         for (int x = lim * 8 + lane; x < AD_KEYS * 8; x += 32)
 #pragma unroll
           for (int h = 0; h < S::HALVES; ++h)
@@ -349,13 +289,119 @@ attention_decode_kernel(const __grid_constant__ CUtensorMap tmK,
         }
       }
       __syncwarp();
-      issue();
+      ++ring.used;
+      ring.issue();
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       l[x] += __shfl_xor_sync(0xffffffffu, l[x], 1);
       l[x] += __shfl_xor_sync(0xffffffffu, l[x], 2);
     }
+    return true;
+  }
+};
+
+template <typename E, int HD>
+__global__ void __launch_bounds__(AdShape<HD>::THREADS, 1)
+attention_decode_kernel(const __grid_constant__ CUtensorMap tmK,
+                        const __grid_constant__ CUtensorMap tmV,
+                        const __grid_constant__ AttnArgs a, const __grid_constant__ AdPlan p) {
+  using S = AdShape<HD>;
+  constexpr int AD_T = S::THREADS;
+  constexpr int NB = HD / 8;  // 8-element blocks of a head
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  __shared__ uint64_t full_bar[S::WARPS][S::STAGES];
+  __shared__ int64_t s_pre[AD_T + 1];
+  const CacheView& c = a.c;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  // the next launch may start its preamble
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  // steps before every chunk of R sequences
+  const int R = (c.B + AD_T - 1) / AD_T;
+  {
+    int64_t mine = 0;
+    const int s0 = min(c.B, (int)threadIdx.x * R), s1 = min(c.B, s0 + R);
+    for (int s = s0; s < s1; ++s) mine += ad_steps(c, s);
+    int64_t pre = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t x = __shfl_up_sync(0xffffffffu, pre, d);
+      if (lane >= d) pre += x;
+    }
+    if (lane == 31) s_pre[warp] = pre;
+    if (lane < S::STAGES) mbar_init(&full_bar[warp][lane], 1);
+    mbar_fence_init();
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) pre += s_pre[w];
+    __syncthreads();
+    s_pre[threadIdx.x + 1] = pre;
+    if (threadIdx.x == 0) s_pre[0] = 0;
+    if (blockIdx.x == 0) {
+      int64_t at = pre - mine;
+      for (int s = s0; s < s1; ++s) {
+        p.prefix[s] = at;
+        at += ad_steps(c, s);
+      }
+      if (threadIdx.x == AD_T - 1) p.prefix[c.B] = pre;
+    }
+    __syncthreads();
+  }
+  const int64_t total = s_pre[AD_T];
+  const int parts = ad_parts(total, p.groups);
+  const int gw = blockIdx.x * S::WARPS + warp;
+  const int g = gw / p.vheads, vh = gw - g * p.vheads;
+  if (g >= parts) return;
+  const int64_t t0 = total * g / parts, t1 = total * (g + 1) / parts;
+  const int group = a.q_heads / c.kv_heads;
+  const int blocks = (group + AD_ROWS - 1) / AD_ROWS;
+  const int kvh = vh / blocks, row0 = (vh - kvh * blocks) * AD_ROWS;
+  const int rows = min(AD_ROWS, group - row0);
+  const int head0 = kvh * group + row0;
+
+  // the sequence of step t0
+  int seq;
+  int64_t before;  // steps before seq
+  {
+    int lo = 0, hi = AD_T - 1;  // the last chunk that starts at or before t0
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (s_pre[mid] <= t0) lo = mid;
+      else hi = mid - 1;
+    }
+    seq = lo * R;
+    before = s_pre[lo];
+    for (;;) {
+      const int n = ad_steps(c, seq);
+      if (t0 < before + n) break;
+      before += n;
+      ++seq;
+    }
+  }
+
+  unsigned char* smem = reinterpret_cast<unsigned char*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  AdRing<HD> ring(c, &tmK, &tmV, smem + warp * S::STAGES * S::STAGE_BYTES, full_bar[warp], kvh,
+                  seq, (int)(t0 - before), (int)cache_len(c, seq), t1 - t0);
+
+  const float cs = a.scale * 1.4426950408889634f;
+  const int r = lane >> 2, cq = 2 * (lane & 3);
+  int64_t t = t0;
+  while (t < t1) {
+    // ---- a piece: steps [j0, j1) of sequence seq ----
+    const int len = (int)cache_len(c, seq);
+    const int n = (len + AD_KEYS - 1) / AD_KEYS;
+    if (n == 0) {
+      ++seq;
+      continue;
+    }
+    const int j0 = (int)(t - before);
+    const int j1 = (int)min((int64_t)n, t1 - before);
+    AdRows<E, HD> w;
+    w.start(a, seq, head0, rows);
+    if (!w.run(ring, len, j0, j1, cs)) return;
+    const auto& o = w.o;
+    const float(&mx)[2] = w.mx, (&l)[2] = w.l;
     if (j0 == 0 && j1 == n) {
       const float inv[2] = {1.f / l[0], 1.f / l[1]};
 #pragma unroll
@@ -391,6 +437,138 @@ attention_decode_kernel(const __grid_constant__ CUtensorMap tmK,
       ++seq;
     }
   }
+}
+
+// Few rows: a cluster of CTAs owns a (sequence, key head, block of rows), its warps take
+// equal pieces of the sequence, leave maximum, sum and unnormalised output in shared
+// memory, and the CTAs join the rows among themselves (row r by CTA r mod size) reading
+// one another's shared memory: one launch, no workspace.
+template <typename E, int HD>
+__global__ void __launch_bounds__(AdShape<HD>::THREADS, 1)
+attention_decode_cluster_kernel(const __grid_constant__ CUtensorMap tmK,
+                                const __grid_constant__ CUtensorMap tmV,
+                                const __grid_constant__ AttnArgs a, int vheads) {
+  using S = AdShape<HD>;
+  constexpr int NB = HD / 8;
+  constexpr int W = S::WARPS;
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  __shared__ uint64_t full_bar[W][S::STAGES];
+  __shared__ float s_m[W][AD_ROWS], s_l[W][AD_ROWS];
+  __shared__ float s_join[W][HD + 2];
+  const CacheView& c = a.c;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint32_t rank, size;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(size));
+  const int unit = blockIdx.x / size;
+  const int seq = unit / vheads, vh = unit - seq * vheads;
+  const int group = a.q_heads / c.kv_heads;
+  const int blocks = (group + AD_ROWS - 1) / AD_ROWS;
+  const int kvh = vh / blocks, row0 = (vh - kvh * blocks) * AD_ROWS;
+  const int rows = min(AD_ROWS, group - row0);
+  const int head0 = kvh * group + row0;
+  if (lane < S::STAGES) mbar_init(&full_bar[warp][lane], 1);
+  mbar_fence_init();
+  __syncwarp();
+
+  unsigned char* smem = reinterpret_cast<unsigned char*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  unsigned char* mine = smem + warp * S::STAGES * S::STAGE_BYTES;
+  const int len = (int)cache_len(c, seq);
+  const int n = (len + AD_KEYS - 1) / AD_KEYS;
+  const int me = rank * W + warp, all = size * W;
+  const int j0 = (int)((int64_t)n * me / all), j1 = (int)((int64_t)n * (me + 1) / all);
+  AdRing<HD> ring(c, &tmK, &tmV, mine, full_bar[warp], kvh, seq, j0, len, j1 - j0);
+  AdRows<E, HD> w;
+  w.start(a, seq, head0, rows);
+  const float cs = a.scale * 1.4426950408889634f;
+  const bool ok = w.run(ring, len, j0, j1, cs);
+  // the outputs go where the warp's ring was: 16 rows of HD floats
+  static_assert(S::STAGES * S::STAGE_BYTES >= AD_ROWS * HD * 4, "a ring holds a piece");
+  const int r = lane >> 2, cq = 2 * (lane & 3);
+  float* out_s = reinterpret_cast<float*>(mine);
+  __syncwarp();
+#pragma unroll
+  for (int x = 0; x < 2; ++x) {
+    const int rr = r + 8 * x;
+    if (cq == 0) {
+      s_m[warp][rr] = w.mx[x] == -INFINITY ? -INFINITY : w.mx[x] * cs;
+      s_l[warp][rr] = ok ? w.l[x] : 0.f;
+    }
+    if (rr < rows) {
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        *reinterpret_cast<float2*>(out_s + rr * HD + 8 * b + cq) =
+            make_float2(w.o[b][2 * x], w.o[b][2 * x + 1]);
+    }
+  }
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  // rows rank, rank + size, ...: the warps of this CTA take the warps of the cluster in
+  // turn, in order, then their sums are joined in order
+  auto peer = [](const void* p, uint32_t cta) {
+    uint32_t x;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(x) : "r"(smem_u32(p)), "r"(cta));
+    return x;
+  };
+  auto ld = [](uint32_t x) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(x) : "memory");
+    return v;
+  };
+  auto ld4 = [](uint32_t x) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(x)
+                 : "memory");
+    return v;
+  };
+  const int e0 = 4 * lane;
+  for (int rr = rank; rr < rows; rr += size) {
+    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (uint32_t p = 0; p < size; ++p) {
+      // warp `warp` of every CTA's W, CTA by CTA
+      const float pm = ld(peer(&s_m[warp][rr], p)), pl = ld(peer(&s_l[warp][rr], p));
+      const float4 v =
+          e0 < HD ? ld4(peer(out_s + rr * HD + e0, p)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      const float mn = fmaxf(m, pm), base = mn == -INFINITY ? 0.f : mn;
+      const float f = at_exp2(m - base), g = at_exp2(pm - base);
+      l = l * f + pl * g;
+      o[0] = o[0] * f + v.x * g, o[1] = o[1] * f + v.y * g;
+      o[2] = o[2] * f + v.z * g, o[3] = o[3] * f + v.w * g;
+      m = mn;
+    }
+    if (lane == 0) s_join[warp][HD] = m, s_join[warp][HD + 1] = l;
+    if (e0 < HD) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s_join[warp][e0 + i] = o[i];
+    }
+    __syncthreads();
+    const int e = 2 * threadIdx.x;
+    if (e < c.head_dim) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < W; ++x) top = fmaxf(top, s_join[x][HD]);
+      const float base = top == -INFINITY ? 0.f : top;
+      float sum = 0.f, y = 0.f, z = 0.f;
+#pragma unroll
+      for (int x = 0; x < W; ++x) {
+        const float f = at_exp2(s_join[x][HD] - base);
+        sum += s_join[x][HD + 1] * f;
+        y += s_join[x][e] * f;
+        z += s_join[x][e + 1] * f;
+      }
+      const float inv = n > 0 ? 1.f / sum : 0.f;
+      *reinterpret_cast<uint32_t*>(a.out.data + seq * a.out.token_b +
+                                   (head0 + rr) * a.out.head_b + 2 * e) =
+          Half2<E>::narrow(y * inv, z * inv);
+    }
+    __syncthreads();
+  }
+  // no CTA leaves while another reads its shared memory
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // A CTA per (sequence, query head): the pieces of the row, in the order of the
@@ -463,6 +641,7 @@ attention_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant_
 
 // Parts, and the workspace's layout.
 struct AdHost {
+  int cluster;  // CTAs of a cluster; 0: parts and pieces
   int groups, vheads, grid, hd_pad;
   size_t prefix_b, ml_b, o_b;
 };
@@ -474,6 +653,14 @@ int ad_host(const CacheView& c, int q_heads, AdHost* h) {
   const int warps = c.head_dim > 64 ? AdShape<128>::WARPS : AdShape<64>::WARPS;
   const int group = q_heads / c.kv_heads, blocks = (group + AD_ROWS - 1) / AD_ROWS;
   h->vheads = c.kv_heads * blocks;
+  // A cluster for each (sequence, key head) where they and their CTAs fit the GPU at once
+  // and no warp gets more than 16 steps; up to 16 query heads a key head, so that a key is
+  // read once.
+  h->cluster = 0;
+  const int64_t units = (int64_t)c.B * h->vheads, room = (int64_t)c.max_pages << c.page_shift;
+  if (blocks == 1)
+    for (int n = 8; n >= 2 && h->cluster == 0; n /= 2)
+      if (units * n <= sms && room <= (int64_t)16 * AD_KEYS * n * warps) h->cluster = n;
   h->groups = std::max(1, sms * warps / h->vheads);
   // no more parts than the page tables can hold steps for
   const int64_t most = (int64_t)c.B * (((int64_t)c.max_pages << c.page_shift) / AD_KEYS + 1);
@@ -484,6 +671,35 @@ int ad_host(const CacheView& c, int q_heads, AdHost* h) {
   const size_t rows = (size_t)h->groups * 2 * h->vheads * AD_ROWS;
   h->ml_b = sls_align256(rows * 8);
   h->o_b = sls_align256(rows * h->hd_pad * 4);
+  return SLS_OK;
+}
+
+template <typename E, int HD>
+int launch_cluster(const AttnArgs& a, const AdHost& h, const CUtensorMap& k, const CUtensorMap& v,
+                   cudaStream_t stream) {
+  static bool set[64] = {};  // per device
+  int dev = 0;
+  SLS_CUDA_TRY(cudaGetDevice(&dev));
+  auto kern = attention_decode_cluster_kernel<E, HD>;
+  if (dev >= 64 || !set[dev]) {
+    SLS_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                      (int)AdShape<HD>::SMEM));
+    if (dev < 64) set[dev] = true;
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(a.c.B * h.vheads * h.cluster));
+  cfg.blockDim = dim3(AdShape<HD>::THREADS);
+  cfg.dynamicSmemBytes = AdShape<HD>::SMEM;
+  cfg.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)h.cluster;
+  at[0].val.clusterDim.y = 1;
+  at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  SLS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, k, v, a, h.vheads));
+  SLS_LAUNCH_CHECK();
   return SLS_OK;
 }
 
@@ -519,7 +735,7 @@ int launch(const AttnArgs& a, const AdPlan& p, int grid, const CUtensorMap& k,
 
 size_t attention_decode_workspace(const CacheView& c, int q_heads) {
   AdHost h;
-  if (c.B == 0 || ad_host(c, q_heads, &h) != SLS_OK) return 0;
+  if (c.B == 0 || ad_host(c, q_heads, &h) != SLS_OK || h.cluster > 0) return 0;
   return h.prefix_b + h.ml_b + h.o_b;
 }
 
@@ -542,6 +758,13 @@ int launch_attention_decode(const AttnArgs& a, int dtype, void* workspace, cudaS
       !at_cache_map(&v, dtype, c, c.v, std::min(AD_KEYS, 1 << c.page_shift)))
     return SLS_ERR_UNSUPPORTED;
   const bool wide = c.head_dim > 64;
+  if (h.cluster > 0) {
+    if (dtype == SLS_BF16)
+      return wide ? launch_cluster<__nv_bfloat16, 128>(a, h, k, v, stream)
+                  : launch_cluster<__nv_bfloat16, 64>(a, h, k, v, stream);
+    return wide ? launch_cluster<__half, 128>(a, h, k, v, stream)
+                : launch_cluster<__half, 64>(a, h, k, v, stream);
+  }
   if (dtype == SLS_BF16)
     return wide ? launch<__nv_bfloat16, 128>(a, p, h.grid, k, v, stream)
                 : launch<__nv_bfloat16, 64>(a, p, h.grid, k, v, stream);
