@@ -107,7 +107,9 @@ struct AttnArgs {
   int causal;
   float scale;
 };
-int launch_attention_prefill(const AttnArgs& a, int dtype, cudaStream_t stream);
+// Prefill; workspace: attention_prefill_workspace() bytes.
+size_t attention_prefill_workspace(const CacheView& c, int64_t T, int q_heads);
+int launch_attention_prefill(const AttnArgs& a, int dtype, void* workspace, cudaStream_t stream);
 // The single-token form (cu NULL); workspace: attention_decode_workspace() bytes.
 size_t attention_decode_workspace(const CacheView& c, int q_heads);
 int launch_attention_decode(const AttnArgs& a, int dtype, void* workspace, cudaStream_t stream);

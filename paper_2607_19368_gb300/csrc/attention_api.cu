@@ -100,8 +100,9 @@ int sls_qkv_append(const sls_rows_t* q, const sls_rows_t* k, const sls_rows_t* v
 }
 
 size_t sls_attention_prefill_workspace_size(int64_t T, int q_heads, const sls_kv_cache_t* cache) {
-  (void)T, (void)q_heads, (void)cache;
-  return 0;
+  CacheView c;
+  if (T < 0 || T > kMaxTokens || cache_view(cache, q_heads, &c) != SLS_OK) return 0;
+  return attention_prefill_workspace(c, T, q_heads);
 }
 
 int sls_attention_prefill(const sls_rows_t* q, int64_t T, int q_heads,
@@ -120,7 +121,9 @@ int sls_attention_prefill(const sls_rows_t* q, int64_t T, int q_heads,
   a.cu = cu_seqlens;
   a.causal = causal != 0;
   a.scale = scale;
-  return launch_attention_prefill(a, cache->dtype, (cudaStream_t)stream);
+  const size_t need = attention_prefill_workspace(a.c, T, q_heads);
+  if (need > 0 && (!aligned16(workspace) || workspace_bytes < need)) return SLS_ERR_WORKSPACE;
+  return launch_attention_prefill(a, cache->dtype, workspace, (cudaStream_t)stream);
 }
 
 size_t sls_attention_decode_workspace_size(int q_heads, const sls_kv_cache_t* cache) {

@@ -32,6 +32,7 @@ struct ApShape {
   static constexpr size_t SMEM = (size_t)(2 + STAGES) * TILE_BYTES + AP_SOFT_WARPS * OUT_BYTES + 1024;
 };
 
+// An item, or a piece of one: key steps, keys and limits count from key k0.
 struct ApItem {
   int seq;            // -1: no more items
   int head;           // key head
@@ -41,6 +42,16 @@ struct ApItem {
   int len;            // cached tokens of the sequence
   int lim0;           // keys that the pair's first token sees, before cutting to [0, len]
   int causal;
+  int k0;             // a multiple of AP_BN
+  int slot;           // where a piece leaves its sums; -1: the item is whole
+};
+
+// Few items with many keys: the steps of all items form one list that the CTAs share
+// evenly; an item that falls to several CTAs is left in pieces, at most two a CTA (its
+// first and its last), and joined by a second launch.
+struct ApSplit {
+  float2* ml;   // (slot, row of the pair): maximum (log2 units), sum of weights
+  float4* o;    // (slot, element / 4, row of the pair): unnormalised output
 };
 
 // ---- tcgen05 / TMA wrappers ------------------------------------------------------
@@ -233,6 +244,47 @@ SLS_DEV void ap_order_init(ApOrder& o, const AttnArgs& a, int qb) {
   o.total = o.level == 0 ? o.at_level : ap_count_all(o, 0);
 }
 
+// a sequence: first row, new tokens, cached tokens, those that the page table can hold
+struct ApSeq {
+  int q0, n, m, len;
+};
+SLS_DEV ApSeq ap_seq(const AttnArgs& a, int s) {
+  int64_t r0, r1;
+  seq_rows(a.cu, s, a.T, r0, r1);
+  ApSeq q;
+  q.q0 = (int)r0, q.n = (int)(r1 - r0), q.m = max(a.c.kv_lens[s], 0);
+  q.len = (int)cache_len(a.c, s);
+  return q;
+}
+// key steps of block b
+SLS_DEV int ap_steps(const ApSeq& q, int b, int qb, int causal) {
+  const int keys = causal ? q.m - q.n + min((b + 1) * qb, q.n) : q.len;
+  return (int)(((unsigned)max(0, min(keys, q.len)) + AP_BN - 1) / AP_BN);
+}
+// key steps [j0, j1) of block b and a key head, as far as they go
+SLS_DEV void ap_item_of(const ApSeq& q, int seq, int b, int head, int j0, int j1, int tpt,
+                        int causal, ApItem& it) {
+  const int qb = 2 * tpt;
+  it.seq = seq, it.head = head, it.causal = causal;
+  it.tok0 = q.q0 + b * qb;
+  it.ntok = min(qb, q.n - b * qb);
+  const int lim0 = causal ? q.m - q.n + b * qb + 1 : q.len;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int nt = min(tpt, it.ntok - t * tpt);  // tokens of the tile
+    const int lim = causal ? lim0 + t * tpt + nt - 1 : q.len;
+    it.tiles[t] = nt > 0 ? (int)(((unsigned)max(0, min(lim, q.len)) + AP_BN - 1) / AP_BN) : 0;
+  }
+  // the second tile, unless empty, has the item's last step
+  if (it.tiles[1] > 0) it.tiles[1] = max(it.tiles[0], it.tiles[1]);
+#pragma unroll
+  for (int t = 0; t < 2; ++t) it.tiles[t] = max(0, min(it.tiles[t], j1) - j0);
+  it.k0 = j0 * AP_BN;
+  it.len = q.len - it.k0;
+  it.lim0 = lim0 - it.k0;
+  it.slot = -1;
+}
+
 // the item number i; false when there is none
 SLS_DEV bool ap_find(ApOrder& o, int64_t i, int tpt, ApItem& it) {
   const int heads = o.c.kv_heads;
@@ -282,22 +334,10 @@ SLS_DEV bool ap_find(ApOrder& o, int64_t i, int tpt, ApItem& it) {
       q0 = __shfl_sync(0xffffffffu, q0, src);
       n = __shfl_sync(0xffffffffu, n, src);
       m = __shfl_sync(0xffffffffu, m, src);
-      it.seq = s0 + src;
-      it.head = (int)i - j * heads;
-      it.tok0 = q0 + b * o.qb;
-      it.ntok = min(o.qb, n - b * o.qb);
-      it.len = (int)min((int64_t)m, (int64_t)o.c.max_pages << o.c.page_shift);
-      it.causal = o.causal;
-      it.lim0 = o.causal ? m - n + b * o.qb + 1 : it.len;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int nt = min(tpt, it.ntok - t * tpt);  // tokens of the tile
-        const int lim = o.causal ? it.lim0 + t * tpt + nt - 1 : it.len;
-        it.tiles[t] =
-            nt > 0 ? (int)(((unsigned)max(0, min(lim, it.len)) + AP_BN - 1) / AP_BN) : 0;
-      }
-      // the second tile, unless empty, has the item's last step
-      if (it.tiles[1] > 0) it.tiles[1] = max(it.tiles[0], it.tiles[1]);
+      ApSeq sq;
+      sq.q0 = q0, sq.n = n, sq.m = m;
+      sq.len = (int)min((int64_t)m, (int64_t)o.c.max_pages << o.c.page_shift);
+      ap_item_of(sq, s0 + src, b, (int)i - j * heads, 0, 0x7fffffff, tpt, o.causal, it);
       return true;
     }
     left -= __shfl_sync(0xffffffffu, pre, 31);
@@ -305,13 +345,132 @@ SLS_DEV bool ap_find(ApOrder& o, int64_t i, int tpt, ApItem& it) {
   return false;
 }
 
+// ---- the order of the work in split launches ---------------------------------------
+// blocks in the order of the tokens, the key heads of a block one after the other
+
+constexpr int AP_LEAST = 4;   // a CTA takes at least so many steps where there are as many
+constexpr int AP_GAIN = 10;   // steps that cutting has to save, about what joining costs
+// CTAs that share `total` steps, the longest item having `longest`; 0: no item is cut
+SLS_DEV int ap_parts(int64_t total, int longest, int most) {
+  const int64_t n = (total + AP_LEAST - 1) / AP_LEAST;
+  const int parts = (int)(n < most ? n : most);
+  return (int64_t)(longest - AP_GAIN) * parts > total ? parts : 0;
+}
+
+struct ApWalk {
+  ApSeq q;
+  int seq, b, head, j;  // the next step
+  int64_t left;         // steps still to take
+  int taken;            // pieces so far
+};
+
+// The warp's first step: number total * cta / parts of the list; false when no item is
+// to be cut.
+SLS_DEV bool ap_walk_init(ApWalk& w, const AttnArgs& a, int qb) {
+  const int lane = threadIdx.x & 31, heads = a.c.kv_heads;
+  // steps of one head's items of a sequence
+  int longest = 0;
+  auto sum_of = [&](int s) {
+    int64_t sum = 0;
+    if (s < a.c.B) {
+      const ApSeq q = ap_seq(a, s);
+      for (int b = 0; b * qb < q.n; ++b) {
+        const int n = ap_steps(q, b, qb, a.causal);
+        sum += n;
+        longest = max(longest, n);
+      }
+    }
+    return sum;
+  };
+  auto scan = [&](int64_t& x) {  // inclusive; returns the warp's sum
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const int64_t y = __shfl_up_sync(0xffffffffu, x, d);
+      if (lane >= d) x += y;
+    }
+    return __shfl_sync(0xffffffffu, x, 31);
+  };
+  int64_t total = 0;
+  for (int s0 = 0; s0 < a.c.B; s0 += 32) {
+    int64_t x = sum_of(s0 + lane);
+    total += scan(x);
+  }
+  total *= heads;
+  longest = __reduce_max_sync(0xffffffffu, longest);
+  const int parts = ap_parts(total, longest, gridDim.x);
+  if (parts == 0) return false;
+  w.left = 0, w.taken = 0, w.seq = 0;
+  if ((int)blockIdx.x >= parts) return true;
+  int64_t at = total * blockIdx.x / parts;
+  w.left = total * (blockIdx.x + 1) / parts - at;
+  for (int s0 = 0;; s0 += 32) {
+    const int64_t mine = sum_of(s0 + lane) * heads;
+    int64_t x = mine;
+    const int64_t all = scan(x);
+    if (at < all) {
+      const int src = __ffs(__ballot_sync(0xffffffffu, at < x)) - 1;
+      at -= __shfl_sync(0xffffffffu, x - mine, src);
+      w.seq = s0 + src;
+      break;
+    }
+    at -= all;
+  }
+  w.q = ap_seq(a, w.seq);
+  for (int b0 = 0;; b0 += 32) {
+    const int b = b0 + lane;
+    const int64_t mine = b * qb < w.q.n ? (int64_t)ap_steps(w.q, b, qb, a.causal) * heads : 0;
+    int64_t x = mine;
+    const int64_t all = scan(x);
+    if (at < all) {
+      const int src = __ffs(__ballot_sync(0xffffffffu, at < x)) - 1;
+      at -= __shfl_sync(0xffffffffu, x - mine, src);
+      w.b = b0 + src;
+      break;
+    }
+    at -= all;
+  }
+  const int n = ap_steps(w.q, w.b, qb, a.causal);
+  w.head = (int)(at / n);
+  w.j = (int)(at - (int64_t)w.head * n);
+  return true;
+}
+
+// the next item or piece; false when the CTA's share is done
+SLS_DEV bool ap_walk(ApWalk& w, const AttnArgs& a, int tpt, ApItem& it) {
+  if (w.left == 0) return false;
+  const int qb = 2 * tpt;
+  int n = ap_steps(w.q, w.b, qb, a.causal);
+  if (w.j == n) {  // the next item that has keys
+    w.j = 0;
+    if (++w.head == a.c.kv_heads) {
+      w.head = 0;
+      do {
+        ++w.b;
+        while (w.b * qb >= w.q.n) {
+          w.b = 0;
+          w.q = ap_seq(a, ++w.seq);
+        }
+        n = ap_steps(w.q, w.b, qb, a.causal);
+      } while (n == 0);
+    }
+  }
+  const int take = (int)min((int64_t)(n - w.j), w.left);
+  ap_item_of(w.q, w.seq, w.b, w.head, w.j, w.j + take, tpt, a.causal, it);
+  if (take < n) it.slot = 2 * blockIdx.x + (w.taken > 0);
+  w.j += take;
+  w.left -= take;
+  ++w.taken;
+  return true;
+}
+
 // ---- a row by itself -----------------------------------------------------------------
 // The tensor cores multiply a hidden key's weight 0 with its value, and 0 times
 // infinity or NaN is NaN: a row whose result is not finite is computed again by one
-// warp over the keys that it sees and no others (lanes hold four elements each).
+// warp over the keys that it sees and no others (lanes hold four elements each), its
+// elements [d0, d1) written.
 template <typename E>
 SLS_DEV void ap_row(const CacheView& c, const char* q, char* out, int seq,
-                                    int head, int keys, float scale) {
+                                    int head, int keys, float scale, int d0, int d1) {
   const int lane = threadIdx.x & 31, e0 = 4 * lane;
   const bool on = e0 < c.head_dim;
   float x[4] = {0.f, 0.f, 0.f, 0.f}, o[4] = {0.f, 0.f, 0.f, 0.f};
@@ -346,18 +505,20 @@ SLS_DEV void ap_row(const CacheView& c, const char* q, char* out, int seq,
     mx = mn;
   }
   const float inv = keys > 0 ? 1.f / l : 0.f;
-  if (on)
+  if (on && e0 >= d0 && e0 < d1)
     *reinterpret_cast<uint2*>(out + 2 * e0) = make_uint2(
         Half2<E>::narrow(o[0] * inv, o[1] * inv), Half2<E>::narrow(o[2] * inv, o[3] * inv));
 }
 
 // ---- the kernel --------------------------------------------------------------------
-template <typename E, int HD>
+// CUT: items may be cut (a kernel of its own: the search for items is code that runs once an
+// item, from beyond the instruction caches)
+template <typename E, int HD, bool CUT>
 __global__ void __launch_bounds__(AP_THREADS, 1)
 attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
                          const __grid_constant__ CUtensorMap tmK,
                          const __grid_constant__ CUtensorMap tmV,
-                         const __grid_constant__ AttnArgs a) {
+                         const __grid_constant__ AttnArgs a, const __grid_constant__ ApSplit sp) {
   using S = ApShape<HD>;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   __shared__ uint64_t q_full[2], q_empty[2], s_full[2], p_half[2], p_full[2], o_full[2], done_bar;
@@ -375,6 +536,8 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
   const int group = a.q_heads / a.c.kv_heads;
   const int tpt = AP_BM / group;  // tokens of a query tile
 
+  // the joining launch may start its preamble
+  if constexpr (CUT) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (threadIdx.x == 0) {
     for (int t = 0; t < 2; ++t) {
       mbar_init(&q_full[t], 1);
@@ -397,14 +560,23 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
     s_abort = 0;
   }
   ApOrder o;
+  ApWalk walk;
+  bool cut = false;
   ApItem following;
   auto find = [&](unsigned k) {
     following.seq = -1;
+    if constexpr (CUT) {
+      if (cut) {
+        ap_walk(walk, a, tpt, following);
+        return;
+      }
+    }
     ap_find(o, (int64_t)k * gridDim.x + ((k & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x), tpt,
             following);
   };
   if (warp == AP_LOAD_WARP) {
-    ap_order_init(o, a, 2 * tpt);
+    if constexpr (CUT) cut = ap_walk_init(walk, a, 2 * tpt);
+    if (!cut) ap_order_init(o, a, 2 * tpt);
     find(0);
   }
   if (warp == AP_MMA_WARP) {
@@ -455,16 +627,17 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
       // page numbers of the first key step: lane l holds that of copy l of the step
       auto page_of = [&](int j) {
         const int x = j * AP_BN + (lane << col_shift);
-        return (lane < per_tile && j < nk && x < it.len) ? table[x >> a.c.page_shift] : -1;
+        return (lane < per_tile && j < nk && x < it.len) ? table[(it.k0 + x) >> a.c.page_shift]
+                                                         : -1;
       };
       int page = page_of(0);
-      if (nk == 0) find(k + 1);
-      for (int j = 0; j < nk && ok; ++j) {
+      const int turns = max(nk, 1), copied = nk > 0 ? 2 : 0;
+      for (int j = 0; j < turns && ok; ++j) {
         const int next = page_of(j + 1);
         const int here = min(AP_BN, it.len - j * AP_BN);
         const int copies = (here + box - 1) / box;  // of each half
-        const int slot0 = (j * AP_BN) & ((1 << a.c.page_shift) - 1);
-        for (int kv = 0; kv < 2 && ok; ++kv) {
+        const int slot0 = (it.k0 + j * AP_BN) & ((1 << a.c.page_shift) - 1);
+        for (int kv = 0; kv < copied && ok; ++kv) {
           if (j == 0) {
             // the query tiles of the item: the first before the first keys, the
             // second after them
@@ -507,7 +680,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         }
         page = next;
         // the next item is looked for while the ring is full
-        if (j == min(nk - 1, 1)) find(k + 1);
+        if (j == min(turns - 1, 1)) find(k + 1);
       }
     }
     // every copy has landed before the CTA may exit
@@ -793,6 +966,28 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         ++o_used;
         ap_fence_after();
       }
+      if (CUT && it.slot >= 0) {
+        // a piece: rows next to one another for every four elements
+        const int64_t at = (int64_t)it.slot * 2 * AP_BM + t * AP_BM + row;
+        sp.ml[at] = make_float2(mx == -INFINITY ? -INFINITY : mx * c, l);
+        float4* po = sp.o + (int64_t)it.slot * (HD / 4) * 2 * AP_BM + t * AP_BM + row;
+#pragma unroll 1
+        for (int q = 0; q < HD / 32; ++q) {
+          float o[32];
+          if (nk > 0) {
+            ap_ld32(to + 32 * q, o);
+            ap_wait_ld<32>(o);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = 0.f;
+          }
+#pragma unroll
+          for (int e = 0; e < 32; e += 4)
+            po[(8 * q + e / 4) * 2 * AP_BM] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+        }
+        ap_fence_before();
+        continue;
+      }
       // 64 elements at a time through shared memory, so that a store instruction writes
       // whole 128-byte pieces of four rows (loops, not straight code: it runs once an
       // item, from beyond the instruction caches)
@@ -848,7 +1043,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         __syncwarp();
         ap_row<E>(a.c, a.q.data + bt * a.q.token_b + bh * a.q.head_b,
                   a.out.data + bt * a.out.token_b + bh * a.out.head_b, it.seq, it.head, bk,
-                  a.scale);
+                  a.scale, 0, HD);
       }
     }
   }
@@ -861,36 +1056,230 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
   }
 }
 
+// Joins the pieces of the items that were cut: a CTA per item and 8 elements, a
+// thread per row, the pieces in the order of the keys.  Rows of items that were not cut
+// are there already; rows of items without keys become zero here.
+constexpr int AP_JOIN = 8;   // elements of a thread
+constexpr int AP_FLIGHT = 4;  // pieces in flight
 template <typename E, int HD>
-int launch(const AttnArgs& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
-           int grid, cudaStream_t stream) {
+__global__ void __launch_bounds__(2 * AP_BM)
+attention_prefill_join_kernel(const __grid_constant__ AttnArgs a,
+                              const __grid_constant__ ApSplit sp, int ctas) {
+  __shared__ int64_t s_sum[2][2 * AP_BM / 32];
+  __shared__ int s_longest[2 * AP_BM / 32];
+  const int heads = a.c.kv_heads, group = a.q_heads / heads, tpt = AP_BM / group, qb = 2 * tpt;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  int b = blockIdx.x / heads;
+  const int head = blockIdx.x - b * heads;
+  // this block's sequence, the steps before it and of all blocks (from the lengths alone,
+  // while the first launch still runs)
+  int seq = -1, first = b;
+  int64_t before = 0, total = 0;
+  int longest = 0;
+  for (int s = 0, at = 0; s < a.c.B; ++s) {
+    const ApSeq q = ap_seq(a, s);
+    const int nb = (q.n + qb - 1) / qb;
+    if (seq < 0 && b < at + nb) seq = s, first = b - at;
+    for (int x = tid; x < nb; x += 2 * AP_BM) {
+      const int n = ap_steps(q, x, qb, a.causal);
+      total += n;
+      longest = max(longest, n);
+      if (at + x < b) before += n;
+    }
+    at += nb;
+  }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) {
+    before += __shfl_xor_sync(0xffffffffu, before, d);
+    total += __shfl_xor_sync(0xffffffffu, total, d);
+  }
+  longest = __reduce_max_sync(0xffffffffu, longest);
+  if (lane == 0) s_sum[0][warp] = before, s_sum[1][warp] = total, s_longest[warp] = longest;
+  __syncthreads();
+  before = total = 0;
+#pragma unroll
+  for (int w = 0; w < 2 * AP_BM / 32; ++w) {
+    before += s_sum[0][w], total += s_sum[1][w];
+    longest = max(longest, s_longest[w]);
+  }
+  total *= heads;
+  const int parts = ap_parts(total, longest, ctas);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (seq < 0 || parts == 0) return;
+  b = first;
+  const ApSeq q = ap_seq(a, seq);
+  const int n = ap_steps(q, b, qb, a.causal);
+  const int t = tid / AP_BM, row = tid - t * AP_BM;
+  const int tok = t * tpt + row / group;  // within the pair
+  const bool live = row < group * tpt && b * qb + tok < q.n;
+  const int d0 = AP_JOIN * blockIdx.y;
+  if (d0 >= a.c.head_dim) return;
+  const int64_t gt = q.q0 + b * qb + tok;
+  const int h = head * group + row - (row / group) * group;
+  char* out = a.out.data + gt * a.out.token_b + h * a.out.head_b;
+  if (n == 0) {
+    if (live) {
+#pragma unroll
+      for (int e = 0; e < AP_JOIN; e += 8)
+        if (d0 + e < a.c.head_dim)
+          *reinterpret_cast<uint4*>(out + 2 * (d0 + e)) = make_uint4(0, 0, 0, 0);
+    }
+    return;
+  }
+  const int64_t x0 = before * heads + (int64_t)head * n, x1 = x0 + n;
+  // the CTA of step x is the last whose start total * g / parts is at most x
+  const int g0 = (int)(((x0 + 1) * parts - 1) / total), g1 = (int)((x1 * parts - 1) / total);
+  if (g0 == g1) return;
+  // the first piece is its CTA's last unless the CTA starts with it
+  const int late = total * g0 / parts < x0;
+  const int keys = live ? max(0, min(q.len, a.causal ? q.m - q.n + b * qb + tok + 1 : q.len)) : 0;
+  float top = -INFINITY, sum = 0.f, o[AP_JOIN];
+#pragma unroll
+  for (int e = 0; e < AP_JOIN; ++e) o[e] = 0.f;
+  for (int g = g0; g <= g1; g += AP_FLIGHT) {
+    float2 ml[AP_FLIGHT];
+    float4 v[AP_FLIGHT][AP_JOIN / 4];
+#pragma unroll
+    for (int u = 0; u < AP_FLIGHT; ++u) {
+      const int64_t slot = 2 * (g + u) + (g + u == g0 ? late : 0);
+      ml[u] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int x = 0; x < AP_JOIN / 4; ++x) v[u][x] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (g + u <= g1 && live) {
+        ml[u] = sp.ml[slot * 2 * AP_BM + tid];
+#pragma unroll
+        for (int x = 0; x < AP_JOIN / 4; ++x)
+          v[u][x] = sp.o[(slot * (HD / 4) + d0 / 4 + x) * 2 * AP_BM + tid];
+      }
+    }
+    float to = top;
+#pragma unroll
+    for (int u = 0; u < AP_FLIGHT; ++u) to = fmaxf(to, ml[u].x);
+    const float base = to == -INFINITY ? 0.f : to, f = at_exp2(top - base);
+    top = to;
+    sum *= f;
+#pragma unroll
+    for (int e = 0; e < AP_JOIN; ++e) o[e] *= f;
+#pragma unroll
+    for (int u = 0; u < AP_FLIGHT; ++u) {
+      const float w = at_exp2(ml[u].x - base);
+      sum += ml[u].y * w;
+#pragma unroll
+      for (int x = 0; x < AP_JOIN / 4; ++x) {
+        o[4 * x] += v[u][x].x * w, o[4 * x + 1] += v[u][x].y * w;
+        o[4 * x + 2] += v[u][x].z * w, o[4 * x + 3] += v[u][x].w * w;
+      }
+    }
+  }
+  const float inv = keys > 0 ? 1.f / sum : 0.f;
+  float odd = 0.f;
+#pragma unroll
+  for (int e = 0; e < AP_JOIN; e += 8) {
+    float x[8];
+#pragma unroll
+    for (int d = 0; d < 8; ++d) {
+      x[d] = o[e + d] * inv;
+      odd = __fmaf_rn(x[d], 0.f, odd);
+    }
+    if (live && d0 + e < a.c.head_dim)
+      *reinterpret_cast<uint4*>(out + 2 * (d0 + e)) = narrow8<E>(x);
+  }
+  unsigned bad = __ballot_sync(0xffffffffu, live && !(odd == 0.f));
+  while (bad) {
+    const int src = __ffs(bad) - 1;
+    bad &= bad - 1;
+    const int64_t bt = __shfl_sync(0xffffffffu, (long long)gt, src);
+    const int bh = __shfl_sync(0xffffffffu, h, src);
+    const int bk = __shfl_sync(0xffffffffu, keys, src);
+    __syncwarp();
+    ap_row<E>(a.c, a.q.data + bt * a.q.token_b + bh * a.q.head_b,
+              a.out.data + bt * a.out.token_b + bh * a.out.head_b, seq, head, bk, a.scale, d0,
+              d0 + AP_JOIN);
+  }
+}
+
+// Items of a launch at most, its CTAs, and whether it may cut items: where there are no more
+// items than SMs and the page tables have room for AP_ROOM steps (the lengths decide on the
+// device).  Device time, whole / cut: 50 tokens behind 10000 of 28 + 4 heads 108 / 30 us, 2 x 500
+// behind 7001 of 24 + 8 heads of 64 73.4 / 59; 1000 tokens alone 20 / 36, which stay whole.
+constexpr int AP_ROOM = 16;
+struct ApHost {
+  int64_t items;
+  int grid;
+  bool split;
+  size_t ml_b, o_b;
+};
+int ap_host(const CacheView& c, int64_t T, int q_heads, ApHost* h) {
+  int dev = 0, sms = 0;
+  SLS_CUDA_TRY(cudaGetDevice(&dev));
+  SLS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  const int qb = 2 * (AP_BM / (q_heads / c.kv_heads));
+  h->items = ((T + qb - 1) / qb + std::min<int64_t>(c.B, T)) * c.kv_heads;
+  const int64_t room = (int64_t)c.max_pages << c.page_shift;
+  h->split = h->items <= sms && room >= AP_ROOM * AP_BN;
+  h->grid = (int)(h->split ? sms : std::min<int64_t>(h->items, sms));
+  const size_t rows = (size_t)h->grid * 2 * 2 * AP_BM;
+  const int hd = c.head_dim > 64 ? 128 : 64;
+  h->ml_b = h->split ? sls_align256(rows * 8) : 0;
+  h->o_b = h->split ? sls_align256(rows * hd * 4) : 0;
+  return SLS_OK;
+}
+
+template <typename E, int HD, bool CUT>
+int launch_as(const AttnArgs& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
+           const ApHost& h, const ApSplit& sp, cudaStream_t stream) {
   static bool set[64] = {};  // per device
   int dev = 0;
   SLS_CUDA_TRY(cudaGetDevice(&dev));
-  auto kern = attention_prefill_kernel<E, HD>;
+  auto kern = attention_prefill_kernel<E, HD, CUT>;
   if (dev >= 64 || !set[dev]) {
     SLS_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                       (int)ApShape<HD>::SMEM));
     if (dev < 64) set[dev] = true;
   }
-  kern<<<grid, AP_THREADS, ApShape<HD>::SMEM, stream>>>(q, k, v, a);
+  kern<<<h.grid, AP_THREADS, ApShape<HD>::SMEM, stream>>>(q, k, v, a, sp);
+  SLS_LAUNCH_CHECK();
+  if constexpr (!CUT) return SLS_OK;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)h.items, HD / AP_JOIN);
+  cfg.blockDim = dim3(2 * AP_BM);
+  cfg.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  SLS_CUDA_TRY(cudaLaunchKernelEx(&cfg, attention_prefill_join_kernel<E, HD>, a, sp, h.grid));
   SLS_LAUNCH_CHECK();
   return SLS_OK;
 }
 
+template <typename E, int HD>
+int launch(const AttnArgs& a, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
+           const ApHost& h, const ApSplit& sp, cudaStream_t stream) {
+  return h.split ? launch_as<E, HD, true>(a, q, k, v, h, sp, stream)
+                 : launch_as<E, HD, false>(a, q, k, v, h, sp, stream);
+}
+
 }  // namespace
 
-int launch_attention_prefill(const AttnArgs& a, int dtype, cudaStream_t stream) {
+size_t attention_prefill_workspace(const CacheView& c, int64_t T, int q_heads) {
+  ApHost h;
+  if (T == 0 || c.B == 0 || ap_host(c, T, q_heads, &h) != SLS_OK) return 0;
+  return h.ml_b + h.o_b;
+}
+
+int launch_attention_prefill(const AttnArgs& a, int dtype, void* workspace, cudaStream_t stream) {
   if (a.T == 0 || a.c.B == 0) return SLS_OK;
   const CacheView& c = a.c;
   const int group = a.q_heads / c.kv_heads, tpt = AP_BM / group;
-  int dev = 0, sms = 0;
-  SLS_CUDA_TRY(cudaGetDevice(&dev));
-  SLS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-  const int64_t items = ((a.T + 2 * tpt - 1) / (2 * tpt) + std::min<int64_t>(c.B, a.T)) *
-                        c.kv_heads;
-  if (items > 0x7fffffff) return SLS_ERR_UNSUPPORTED;
-  const int grid = (int)std::min<int64_t>(items, sms);
+  ApHost h;
+  const int st = ap_host(c, a.T, a.q_heads, &h);
+  if (st != SLS_OK) return st;
+  if (h.items > 0x7fffffff) return SLS_ERR_UNSUPPORTED;
+  ApSplit sp;
+  sp.ml = (float2*)workspace;
+  sp.o = (float4*)((char*)workspace + h.ml_b);
   CUtensorMap q, k, v;
   {
     const cuuint64_t dims[3] = {(cuuint64_t)c.head_dim, (cuuint64_t)a.q_heads, (cuuint64_t)a.T};
@@ -905,10 +1294,10 @@ int launch_attention_prefill(const AttnArgs& a, int dtype, cudaStream_t stream) 
   }
   const bool wide = c.head_dim > 64;
   if (dtype == SLS_BF16)
-    return wide ? launch<__nv_bfloat16, 128>(a, q, k, v, grid, stream)
-                : launch<__nv_bfloat16, 64>(a, q, k, v, grid, stream);
-  return wide ? launch<__half, 128>(a, q, k, v, grid, stream)
-              : launch<__half, 64>(a, q, k, v, grid, stream);
+    return wide ? launch<__nv_bfloat16, 128>(a, q, k, v, h, sp, stream)
+                : launch<__nv_bfloat16, 64>(a, q, k, v, h, sp, stream);
+  return wide ? launch<__half, 128>(a, q, k, v, h, sp, stream)
+              : launch<__half, 64>(a, q, k, v, h, sp, stream);
 }
 
 int prefill_status_word(int** word) {

@@ -215,6 +215,57 @@ def test_prefill_large_and_low_scores(sls):
     R.check(prefill(sls, b), want, bound)
 
 
+CUT = [
+    # few rows against many cached tokens: items fall to several CTAs
+    ([1], [3000], 28, 4, 128, 64, True),
+    ([50], [10050], 28, 4, 128, 64, True),
+    ([3, 0, 200, 1], [2500, 40, 2300, 6000], 8, 2, 128, 16, True),
+    ([20, 5, 9], [4100, 0, 3], 6, 3, 96, 32, True),          # sequences without keys, rows before them
+    ([64], [5000], 10, 2, 64, 128, False),
+    ([100, 30], [7000, 2049], 24, 8, 40, 1024, True),
+    ([7], [2047], 66, 1, 128, 16, True),
+]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("case", CUT)
+def test_prefill_cut(sls, case, dtype):
+    new, m, Hq, Hkv, hd, page, causal = case
+    b = R.make_batch(new, m, Hq, Hkv, hd, page, dtype, seed=61)
+    want, bound = R.attention(b, causal)
+    got = prefill(sls, b, causal=causal)
+    R.check(got, want, bound, str(case))
+    assert torch.equal(got, prefill(sls, b, causal=causal))
+    # a workspace of the caller's, filled with anything
+    ws = torch.full((64 << 20,), 255, dtype=torch.uint8, device="cuda")
+    assert torch.equal(got, prefill(sls, b, causal=causal, workspace=ws))
+
+
+def test_prefill_cut_not_finite(sls):
+    """The same as whole items: what a row does not see does not reach it."""
+    b = R.make_batch([40], [5000], 4, 2, 64, 16, torch.bfloat16, seed=67)
+    want, bound = R.attention(b)
+    x = 4990                                      # seen from row 30 on
+    b["v"][b["table"][0, x // 16].long(), x % 16, :, 9] = float("inf")
+    got = prefill(sls, b)
+    R.check(got[:30], want[:30], bound[:30])
+    R.check(got[30:, :, :9], want[30:, :, :9], bound[30:, :, :9])
+    assert torch.isinf(got[30:, :, 9]).all()
+
+
+def test_workspaces_that_are_too_small(sls):
+    b = R.make_batch([50], [10050], 28, 4, 128, 64, torch.bfloat16, seed=71)
+    small = torch.empty(1024, dtype=torch.uint8, device="cuda")
+    with pytest.raises(sls.SLSError) as e:
+        prefill(sls, b, workspace=small)
+    assert e.value.status == 3
+    b = R.make_batch([1] * 70, [1000] * 70, 8, 8, 64, 16, torch.bfloat16, seed=73)
+    with pytest.raises(sls.SLSError) as e:
+        decode(sls, b, workspace=small)
+    assert e.value.status == 3
+    assert sls.attention_status() == 0
+
+
 def test_prefill_same_bits_twice(sls):
     b = R.make_batch([500, 90], [900, 90], 28, 4, 128, 64, torch.bfloat16, seed=19)
     assert torch.equal(prefill(sls, b), prefill(sls, b))
