@@ -668,13 +668,15 @@ int ad_host(const CacheView& c, int q_heads, AdHost* h) {
   const int group = q_heads / c.kv_heads, blocks = (group + AD_ROWS - 1) / AD_ROWS;
   h->vheads = c.kv_heads * blocks;
   // A cluster for each (sequence, key head) where they and their CTAs fit the GPU at once
-  // and no warp gets more than 16 steps; up to 16 query heads a key head, so that a key is
-  // read once.
+  // (a CTA each: twice) and no warp gets more than 16 steps; up to 16 query heads a key
+  // head, so that a key is read once.  Device time of parts and pieces / clusters, 28 + 4
+  // heads: 1 x 2061 tokens 9.8 / 6.9 us, 32 x 500 13.4 / 8.8 (a CTA each, as the next), 64 x
+  // 1000 25.4 / 23.6; 100 x 300, more than twice, 16.6 / 20.4.
   h->cluster = 0;
   const int64_t units = (int64_t)c.B * h->vheads, room = (int64_t)c.max_pages << c.page_shift;
   if (blocks == 1)
-    for (int n = 8; n >= 2 && h->cluster == 0; n /= 2)
-      if (units * n <= sms && room <= (int64_t)16 * AD_KEYS * n * warps) h->cluster = n;
+    for (int n = 8; n >= 1 && h->cluster == 0; n /= 2)
+      if (units * n <= (n == 1 ? 2 : 1) * sms && room <= (int64_t)16 * AD_KEYS * n * warps) h->cluster = n;
   h->groups = std::max(1, sms * warps / h->vheads);
   // no more parts than the page tables can hold steps for
   const int64_t most = (int64_t)c.B * (((int64_t)c.max_pages << c.page_shift) / AD_KEYS + 1);
