@@ -1,5 +1,33 @@
 // Attention of packed new tokens over the paged cache on the 5th-generation tensor
-// cores (sm_103a):  O = softmax(scale Q K^T + mask) V.
+// cores (sm_103a):  O = softmax(scale Q K^T + mask) V, one pass over the keys with the
+// running maximum and sum of a softmax.
+//
+// A query tile is 128 rows: 128 / G tokens of a sequence with all G query heads of a key
+// head, which the tensor map's box lays one after the other, so that keys and values are
+// read once for the group whatever G is.  A CTA has two query tiles (an item) and goes over
+// the keys in steps of 128:
+//   S = Q K^T   both operands in shared memory, float32 scores in tensor memory
+//   P = 2^(c (S - m))  a thread per row, scores and maximum in registers; 16-bit weights over
+//               the scores' columns of tensor memory; m is replaced only when weights would
+//               grow past 2^8, and the output scaled to it then (exact: the factor is common
+//               to a row's weights, their sum and its output)
+//   O += P V    weights from tensor memory, values from shared memory as they lie in
+//               the cache, float32 output in tensor memory
+// Warps: 0-3 and 4-7 the softmax of the two tiles, 8 finds items and copies queries, keys
+// and values (TMA, a ring of stages of 128 keys or values), 9 issues all products, 10 and 11
+// keep the ring for the two tiles.  The tiles take turns: while one's weights form, the
+// other's products run.
+//
+// Rounding: scores, maxima, sums and outputs are float32; the weights, which the tensor
+// cores take in 16 bits, are rounded once each (the sum is of the unrounded ones), the
+// output once at the end: the error against 64 bits is 1.4 times that of the output's
+// rounding alone.
+//
+// Bound by the chain softmax -> products -> softmax of a tile: a step of both tiles takes
+// 2730 cycles (the products 2112 of them, the exponentials 1024, the copies 8% of L2's
+// contention).  8192 tokens of 40 + 8 heads of 128: 450 us, 1.53 PFLOP/s, 79% of the
+// measured rate of a large matrix product; 2048 tokens of 28 + 4 heads: 33 us (16 steps of
+// the longest item, 6 us until the first scores, 2 us for the last output).
 #include <cuda.h>
 
 #include <algorithm>
