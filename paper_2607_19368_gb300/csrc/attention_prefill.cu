@@ -13,9 +13,9 @@
 //               to a row's weights, their sum and its output)
 //   O += P V    weights from tensor memory, values from shared memory as they lie in
 //               the cache, float32 output in tensor memory
-// Warps: 0-3 and 4-7 the softmax of the two tiles, 8 finds items and copies queries, keys
-// and values (TMA, a ring of stages of 128 keys or values), 9 issues all products, 10 and 11
-// keep the ring for the two tiles.  The tiles take turns: while one's weights form, the
+// Warps: 0-3 and 4-7 the softmax of the two tiles, 8 finds items and copies queries and
+// keys, 11 values (TMA, a ring of stages of 128 keys or values), 9 issues all products, 10
+// keeps the ring.  The tiles take turns: while one's weights form, the
 // other's products run.
 //
 // Rounding: scores, maxima, sums and outputs are float32; the weights, which the tensor
@@ -46,7 +46,7 @@ constexpr int AP_BN = 128;             // keys of a step
 constexpr int AP_SOFT_WARPS = 8;       // two warpgroups, one per query tile
 constexpr int AP_THREADS = 384;        // and one warpgroup of single warps
 constexpr int AP_LOAD_WARP = AP_SOFT_WARPS, AP_MMA_WARP = AP_SOFT_WARPS + 1,
-              AP_RING_WARP = AP_SOFT_WARPS + 2;  // and the next
+              AP_RING_WARP = AP_SOFT_WARPS + 2, AP_VALUE_WARP = AP_SOFT_WARPS + 3;
 constexpr int AP_ITEMS = 2;            // item slots
 constexpr float AP_LAZY = 8.f;         // log2 of the growth of the maximum that is let pass
 
@@ -538,6 +538,75 @@ SLS_DEV void ap_row(const CacheView& c, const char* q, char* out, int seq,
         Half2<E>::narrow(o[0] * inv, o[1] * inv), Half2<E>::narrow(o[2] * inv, o[3] * inv));
 }
 
+// ---- copies of keys or values ----------------------------------------------------------
+// One warp's copies into its stages of the ring: K_0 V_0 K_1 V_1 ... of an item, keys at
+// even places, values at odd ones.
+template <int HD>
+struct ApCopy {
+  using S = ApShape<HD>;
+  const CacheView& c;
+  const uint32_t ring;
+  uint64_t* full;
+  uint64_t* empty;
+  volatile int* abort_flag;
+  const uint32_t lead;
+  const int shift;  // log2 of the slots of one copy: a page, or 128 of them
+  const int32_t* table;
+  int head, len, k0, nk, page;
+  unsigned stage, issued;
+
+  SLS_DEV ApCopy(const CacheView& cache, uint32_t kv, uint64_t* f, uint64_t* e,
+                 volatile int* abort)
+      : c(cache), ring(kv), full(f), empty(e), abort_flag(abort), lead(at_elect()),
+        shift(min(7, cache.page_shift)), table(nullptr), head(0), len(0), k0(0), nk(0), page(-1),
+        stage(0), issued(0) {}
+
+  // page numbers of step j: lane l holds that of copy l
+  SLS_DEV int page_of(int j) const {
+    const int lane = threadIdx.x & 31;
+    const int x = j * AP_BN + (lane << shift);
+    return (lane < (AP_BN >> shift) && j < nk && x < len) ? table[(k0 + x) >> c.page_shift] : -1;
+  }
+  SLS_DEV void start(const ApItem& it, int steps) {
+    table = c.table + it.seq * c.table_ld;
+    head = it.head, len = it.len, k0 = it.k0, nk = steps;
+    page = page_of(0);
+  }
+  // step j of the item, which: 0 keys, 1 values; false when a wait gave up
+  SLS_DEV bool step(const CUtensorMap* map, int j, int which) {
+    const int next = page_of(j + 1);
+    const int copies = (min(AP_BN, len - j * AP_BN) + (1 << shift) - 1) >> shift;  // of each half
+    const int slot0 = (k0 + j * AP_BN) & ((1 << c.page_shift) - 1);
+    const unsigned at = stage + 2 * j + which, st = at % S::STAGES;
+    if (!ap_wait(&empty[st], ((at / S::STAGES) & 1) ^ 1, abort_flag)) return false;
+    if (lead) mbar_expect_tx(&full[st], S::HALVES * (copies << shift) * 128);
+    __syncwarp();
+    uint32_t dst = ring + st * S::TILE_BYTES;
+#pragma unroll 1
+    for (int i = 0; i < copies; ++i) {
+      const int pg = __shfl_sync(0xffffffffu, page, i);
+#pragma unroll
+      for (int h = 0; h < S::HALVES; ++h)
+        at_tma4(lead, dst + h * S::HALF_BYTES, map, 64 * h, slot0, head, pg, &full[st]);
+      dst += 128u << shift;
+    }
+    ++issued;
+    page = next;
+    return true;
+  }
+  SLS_DEV void end(int steps) { stage += 2 * steps; }
+  // the last copies into each of the warp's stages have landed (the place after the last
+  // one's is not known when a wait gave up; every stage's last fill is at most STAGES back)
+  SLS_DEV void drain(int which) {
+    for (unsigned i = 0; i < S::STAGES / 2; ++i) {
+      if (i >= issued) break;
+      const unsigned at = 2 * (issued - 1 - i) + which;
+      for (unsigned w = 0; w < (1u << 25); ++w)
+        if (mbar_try_wait(&full[at % S::STAGES], (at / S::STAGES) & 1)) break;
+    }
+  }
+};
+
 // ---- the kernel --------------------------------------------------------------------
 // CUT: items may be cut (a kernel of its own: the search for items is code that runs once an
 // item, from beyond the instruction caches)
@@ -626,17 +695,15 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
     atomicExch(&g_status, SLS_ERR_TIMEOUT);
   };
 
-  // registers: 384 x 168 at launch, 2 x 128 x 208 + 128 x 88 from here
+  // registers: 384 x 168 at launch, 2 x 128 x 200 + 128 x 104 from here (208 and 88: 450 us
+  // against 441 on 8192 tokens, the copy warp's registers spill)
   if (warp >= AP_SOFT_WARPS) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
 
   if (warp == AP_LOAD_WARP) {
-    // ------------------------------ items and copies ------------------------------
-    const uint32_t lead = at_elect();
-    unsigned stage = 0, q_used[2] = {0, 0};
-    const int box = min(AP_BN, 1 << a.c.page_shift);  // slots of one copy
-    const int per_tile = AP_BN / box;
-    const int col_shift = min(7, a.c.page_shift);
+    // ------------------------------ items, queries and keys ------------------------
+    ApCopy<HD> cp(a.c, kv_smem, kv_full, kv_empty, &s_abort);
+    unsigned q_used[2] = {0, 0};
     bool ok = true;
     for (unsigned k = 0; ok; ++k) {
       const ApItem it = following;
@@ -651,74 +718,63 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
       }
       if (it.seq < 0) break;
       const int nk = max(it.tiles[0], it.tiles[1]);
-      const int32_t* table = a.c.table + it.seq * a.c.table_ld;
-      // page numbers of the first key step: lane l holds that of copy l of the step
-      auto page_of = [&](int j) {
-        const int x = j * AP_BN + (lane << col_shift);
-        return (lane < per_tile && j < nk && x < it.len) ? table[(it.k0 + x) >> a.c.page_shift]
-                                                         : -1;
-      };
-      int page = page_of(0);
-      const int turns = max(nk, 1), copied = nk > 0 ? 2 : 0;
-      for (int j = 0; j < turns && ok; ++j) {
-        const int next = page_of(j + 1);
-        const int here = min(AP_BN, it.len - j * AP_BN);
-        const int copies = (here + box - 1) / box;  // of each half
-        const int slot0 = (it.k0 + j * AP_BN) & ((1 << a.c.page_shift) - 1);
-        for (int kv = 0; kv < copied && ok; ++kv) {
-          if (j == 0) {
-            // the query tiles of the item: the first before the first keys, the
-            // second after them
-            const int t = kv;
-            if (it.tiles[t] > 0) {
-              if (!ap_wait(&q_empty[t], (q_used[t] & 1) ^ 1, &s_abort)) {
-                if (lane == 0) fail();
-                ok = false;
-                break;
-              }
-              ++q_used[t];
-              if (lead) mbar_expect_tx(&q_full[t], S::HALVES * group * tpt * 128);
-              __syncwarp();
-              {
-#pragma unroll
-                for (int h = 0; h < S::HALVES; ++h)
-                  at_tma3(lead, q_smem + t * S::TILE_BYTES + h * S::HALF_BYTES, &tmQ, 64 * h,
-                          it.head * group, it.tok0 + t * tpt, &q_full[t]);
-              }
-            }
-          }
-          const unsigned st = stage % S::STAGES;
-          if (!ap_wait(&kv_empty[st], ((stage / S::STAGES) & 1) ^ 1, &s_abort)) {
-            if (lane == 0) fail();
-            ok = false;
-            break;
-          }
-          if (lead) mbar_expect_tx(&kv_full[st], S::HALVES * copies * box * 128);
-          __syncwarp();
-#pragma unroll 1
-          for (int i = 0; i < copies; ++i) {
-            const uint32_t dst = kv_smem + st * S::TILE_BYTES + i * box * 128;
-            const int pg = __shfl_sync(0xffffffffu, page, i);
-#pragma unroll
-            for (int h = 0; h < S::HALVES; ++h)
-              at_tma4(lead, dst + h * S::HALF_BYTES, kv ? &tmV : &tmK, 64 * h, slot0, it.head, pg,
-                      &kv_full[st]);
-          }
-          ++stage;
+      cp.start(it, nk);
+      for (int t = 0; t < 2 && ok; ++t) {
+        if (it.tiles[t] == 0) continue;
+        if (!ap_wait(&q_empty[t], (q_used[t] & 1) ^ 1, &s_abort)) {
+          ok = false;
+          break;
         }
-        page = next;
+        ++q_used[t];
+        if (cp.lead) mbar_expect_tx(&q_full[t], S::HALVES * group * tpt * 128);
+        __syncwarp();
+#pragma unroll
+        for (int h = 0; h < S::HALVES; ++h)
+          at_tma3(cp.lead, q_smem + t * S::TILE_BYTES + h * S::HALF_BYTES, &tmQ, 64 * h,
+                  it.head * group, it.tok0 + t * tpt, &q_full[t]);
+        if (t == 0 && nk > 0) ok = cp.step(&tmK, 0, 0);
+      }
+      // (a first tile without keys: its item's first keys are still to come)
+      const int begun = it.tiles[0] > 0 ? 1 : 0;
+      const int turns = max(nk, 1);
+      for (int j = 0; j < turns && ok; ++j) {
+        if (j >= begun && j < nk) ok = cp.step(&tmK, j, 0);
         // the next item is looked for while the ring is full
         if (j == min(turns - 1, 1)) find(k + 1);
       }
+      if (!ok && lane == 0) fail();
+      cp.end(nk);
     }
     // every copy has landed before the CTA may exit
-    for (unsigned s = stage > S::STAGES ? stage - S::STAGES : 0; s < stage; ++s)
-      for (unsigned w = 0; w < (1u << 25); ++w)
-        if (mbar_try_wait(&kv_full[s % S::STAGES], (s / S::STAGES) & 1)) break;
+    cp.drain(0);
     for (int t = 0; t < 2; ++t)
       if (q_used[t] > 0)
         for (unsigned w = 0; w < (1u << 25); ++w)
           if (mbar_try_wait(&q_full[t], (q_used[t] - 1) & 1)) break;
+  } else if (warp == AP_VALUE_WARP) {
+    // ------------------------------ values -----------------------------------------------
+    // a warp of their own: short pages make many copies of a step, and a warp issues one in
+    // about 100 cycles (a ragged batch in pages of 16: 164 us, 179 with one warp for both; in
+    // pages of 128 161 and 158)
+    ApCopy<HD> cp(a.c, kv_smem, kv_full, kv_empty, &s_abort);
+    bool ok = true;
+    for (unsigned k = 0; ok; ++k) {
+      const unsigned slot = k % AP_ITEMS;
+      if (!ap_wait(&item_full[slot], (k / AP_ITEMS) & 1, &s_abort)) {
+        if (lane == 0) fail();
+        break;
+      }
+      const ApItem it = s_item[slot];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&item_empty[slot]);
+      if (it.seq < 0) break;
+      const int nk = max(it.tiles[0], it.tiles[1]);
+      cp.start(it, nk);
+      for (int j = 0; j < nk && ok; ++j) ok = cp.step(&tmV, j, 1);
+      if (!ok && lane == 0) fail();
+      cp.end(nk);
+    }
+    cp.drain(1);
   } else if (warp == AP_MMA_WARP) {
     // ------------------------------ products -------------------------------------------
     // One thread for both tiles, so that their turns alternate: while one tile's weights
@@ -805,15 +861,14 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
     ap_commit(lead, &done_bar);
     for (unsigned w = 0; w < (1u << 25); ++w)
       if (mbar_try_wait(&done_bar, 0)) break;
-  } else {
-    // ------------------------------ the ring, for query tile t ---------------------------
+  } else if (warp == AP_RING_WARP) {
+    // ------------------------------ the ring ---------------------------------------------
     // Waits for the keys and values that the products of a step will read, as one more
     // arrival at the weights' barrier, and frees what finished products have read (the
     // second tile's scores of a step come after everything else of it, and speak for
     // both): the product warp waits for nothing but weights, the softmax for nothing but
     // scores.
-    const int t = warp - AP_RING_WARP;
-    unsigned stage = 0, s_used = 0, o_used = 0;
+    unsigned stage = 0, s_par = 0, o_par = 0;  // a bit for each tile
     bool ok = true;
     auto wait = [&](uint64_t* bar, unsigned parity) {
       ok = ap_wait(bar, parity, &s_abort);
@@ -824,49 +879,58 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
       const unsigned slot = k % AP_ITEMS;
       if (!wait(&item_full[slot], (k / AP_ITEMS) & 1)) break;
       const int seq = s_item[slot].seq, len = s_item[slot].len;
-      const int nk = s_item[slot].tiles[t], other = s_item[slot].tiles[t ^ 1];
+      const int n0 = s_item[slot].tiles[0], n1 = s_item[slot].tiles[1], nk = max(n0, n1);
       __syncwarp();
       if (lane == 0) mbar_arrive(&item_empty[slot]);
       if (seq < 0) break;
-      const bool frees = lane == 0 && (t == 1 || other == 0);
+      const int last = n1 > 0;  // the tile that speaks for both
       for (int j = 0; j < nk; ++j) {
-        // the scores of step j are there: its keys, and the step before, are done with
         const unsigned kst = stage + 2 * j, vst = kst + 1;
-        if (!wait(&s_full[t], s_used & 1)) break;
-        ++s_used;
-        if (frees) {
-          if (j > 0) mbar_arrive(&kv_empty[(kst - 1) % S::STAGES]);
-          mbar_arrive(&kv_empty[kst % S::STAGES]);
-        }
-        if (lane == 0 && j + 1 == nk) mbar_arrive(&q_empty[t]);
-        if (!wait(&kv_full[vst % S::STAGES], (vst / S::STAGES) & 1)) break;
-        if ((j + 1) * AP_BN > len) {
-          // values past the sequence's end: whatever their slots hold, zero here (by the
-          // warps of both tiles, the same zeros)
-          const int r0 = len - j * AP_BN;
-          unsigned char* va = smem + (2 + vst % S::STAGES) * S::TILE_BYTES;
-          for (int x = r0 * 8 + lane; x < AP_BN * 8; x += 32)
+#pragma unroll 1
+        for (int t = 0; t < 2; ++t) {
+          const int mine = t ? n1 : n0;
+          if (j >= mine) continue;
+          // the tile's scores of step j are there
+          if (!wait(&s_full[t], (s_par >> t) & 1)) break;
+          s_par ^= 1u << t;
+          if (lane == 0) {
+            if (t == last) {
+              if (j > 0) mbar_arrive(&kv_empty[(kst - 1) % S::STAGES]);
+              mbar_arrive(&kv_empty[kst % S::STAGES]);
+            }
+            if (j + 1 == mine) mbar_arrive(&q_empty[t]);
+          }
+          if (!wait(&kv_full[vst % S::STAGES], (vst / S::STAGES) & 1)) break;
+          if ((j + 1) * AP_BN > len && (t == 0 || j >= n0)) {
+            // values past the sequence's end: whatever their slots hold, zero here
+            const int r0 = len - j * AP_BN;
+            unsigned char* va = smem + (2 + vst % S::STAGES) * S::TILE_BYTES;
+            for (int x = r0 * 8 + lane; x < AP_BN * 8; x += 32)
 #pragma unroll
-            for (int h = 0; h < S::HALVES; ++h)
-              reinterpret_cast<uint4*>(va + h * S::HALF_BYTES)[x] = make_uint4(0, 0, 0, 0);
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          __syncwarp();
+              for (int h = 0; h < S::HALVES; ++h)
+                reinterpret_cast<uint4*>(va + h * S::HALF_BYTES)[x] = make_uint4(0, 0, 0, 0);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+          }
+          if (j + 1 < mine && !wait(&kv_full[(vst + 1) % S::STAGES], ((vst + 1) / S::STAGES) & 1))
+            break;
+          if (lane == 0) mbar_arrive(&p_half[t]);
         }
-        if (j + 1 < nk && !wait(&kv_full[(vst + 1) % S::STAGES], ((vst + 1) / S::STAGES) & 1))
-          break;
-        if (lane == 0) mbar_arrive(&p_half[t]);
+        if (!ok) break;
       }
       if (!ok) break;
+      // the last values: after the last tile's outputs
+      if (n0 > 0 && last == 1) o_par ^= 1u;  // the first tile's outputs, not waited for
       if (nk > 0) {
-        if (!wait(&o_full[t], o_used & 1)) break;
-        ++o_used;
-        if (frees) mbar_arrive(&kv_empty[(stage + 2 * nk - 1) % S::STAGES]);
+        if (!wait(&o_full[last], (o_par >> last) & 1)) break;
+        o_par ^= 1u << last;
+        if (lane == 0) mbar_arrive(&kv_empty[(stage + 2 * nk - 1) % S::STAGES]);
       }
-      stage += 2 * max(nk, other);
+      stage += 2 * nk;
     }
   }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     // ------------------------------ softmax, a row per thread --------------------------
     const int t = warp >> 2;
     const int row = (warp & 3) * 32 + lane;
