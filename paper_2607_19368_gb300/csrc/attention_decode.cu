@@ -315,8 +315,7 @@ attention_decode_kernel(const __grid_constant__ CUtensorMap tmK,
   const CacheView& c = a.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
-  // the next launch may start its preamble
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  at_wait_ahead();
   // steps before every chunk of R sequences
   const int R = (c.B + AD_T - 1) / AD_T;
   {
@@ -470,6 +469,8 @@ attention_decode_cluster_kernel(const __grid_constant__ CUtensorMap tmK,
   if (lane < S::STAGES) mbar_init(&full_bar[warp][lane], 1);
   mbar_fence_init();
   __syncwarp();
+  at_go();
+  at_wait_ahead();
 
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -593,7 +594,8 @@ attention_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant_
   const int vh = kvh * blocks + in / AD_ROWS, rr = in % AD_ROWS;
   char* out = a.out.data + seq * a.out.token_b + h * a.out.head_b;
   const int e0 = 4 * lane;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  at_go();
+  at_wait_ahead();
   const int64_t total = p.prefix[c.B], b0 = p.prefix[seq], b1 = p.prefix[seq + 1];
   if (b1 == b0) {
     if (warp == 0 && e0 < c.head_dim)
@@ -702,21 +704,8 @@ int launch_cluster(const AttnArgs& a, const AdHost& h, const CUtensorMap& k, con
                                       (int)AdShape<HD>::SMEM));
     if (dev < 64) set[dev] = true;
   }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(a.c.B * h.vheads * h.cluster));
-  cfg.blockDim = dim3(AdShape<HD>::THREADS);
-  cfg.dynamicSmemBytes = AdShape<HD>::SMEM;
-  cfg.stream = stream;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = (unsigned)h.cluster;
-  at[0].val.clusterDim.y = 1;
-  at[0].val.clusterDim.z = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  SLS_CUDA_TRY(cudaLaunchKernelEx(&cfg, kern, k, v, a, h.vheads));
-  SLS_LAUNCH_CHECK();
-  return SLS_OK;
+  return at_launch(kern, dim3((unsigned)(a.c.B * h.vheads * h.cluster)), AdShape<HD>::THREADS,
+                   AdShape<HD>::SMEM, h.cluster, stream, k, v, a, h.vheads);
 }
 
 template <typename E, int HD>
@@ -731,24 +720,15 @@ int launch(const AttnArgs& a, const AdPlan& p, int grid, const CUtensorMap& k,
                                       (int)AdShape<HD>::SMEM));
     if (dev < 64) set[dev] = true;
   }
-  kern<<<grid, AdShape<HD>::THREADS, AdShape<HD>::SMEM, stream>>>(k, v, a, p);
-  SLS_LAUNCH_CHECK();
-  cudaLaunchConfig_t cfg = {};
+  const int st = at_launch(kern, dim3((unsigned)grid), AdShape<HD>::THREADS, AdShape<HD>::SMEM, 1,
+                           stream, k, v, a, p);
+  if (st != SLS_OK) return st;
   // a sequence has 1 + groups / B pieces on average
   const bool few = p.groups <= 2 * (int64_t)a.c.B;
   const int64_t rows = (int64_t)a.c.B * a.q_heads;
-  cfg.gridDim = dim3((unsigned)(few ? (rows + AD_JOIN_WARPS - 1) / AD_JOIN_WARPS : rows));
-  cfg.blockDim = dim3(32 * AD_JOIN_WARPS);
-  cfg.stream = stream;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  SLS_CUDA_TRY(cudaLaunchKernelEx(
-      &cfg, few ? attention_join_kernel<E, 1> : attention_join_kernel<E, AD_JOIN_WARPS>, a, p));
-  SLS_LAUNCH_CHECK();
-  return SLS_OK;
+  return at_launch(few ? attention_join_kernel<E, 1> : attention_join_kernel<E, AD_JOIN_WARPS>,
+                   dim3((unsigned)(few ? (rows + AD_JOIN_WARPS - 1) / AD_JOIN_WARPS : rows)),
+                   32 * AD_JOIN_WARPS, 0, 1, stream, a, p);
 }
 
 }  // namespace

@@ -633,8 +633,6 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
   const int group = a.q_heads / a.c.kv_heads;
   const int tpt = AP_BM / group;  // tokens of a query tile
 
-  // the joining launch may start its preamble
-  if constexpr (CUT) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (threadIdx.x == 0) {
     for (int t = 0; t < 2; ++t) {
       mbar_init(&q_full[t], 1);
@@ -672,6 +670,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
             following);
   };
   if (warp == AP_LOAD_WARP) {
+    at_wait_ahead();
     if constexpr (CUT) cut = ap_walk_init(walk, a, 2 * tpt);
     if (!cut) ap_order_init(o, a, 2 * tpt);
     find(0);
@@ -686,6 +685,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
   ap_fence_before();
   __syncthreads();
   ap_fence_after();
+  at_wait_ahead();
   const uint32_t tmem = tmem_holder;
   // columns of tensor memory: scores (and, over them, weights) of the two tiles, then
   // their outputs
@@ -1163,8 +1163,9 @@ attention_prefill_join_kernel(const __grid_constant__ AttnArgs a,
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   int b = blockIdx.x / heads;
   const int head = blockIdx.x - b * heads;
-  // this block's sequence, the steps before it and of all blocks (from the lengths alone,
-  // while the first launch still runs)
+  at_go();
+  at_wait_ahead();
+  // this block's sequence, the steps before it and of all blocks
   int seq = -1, first = b;
   int64_t before = 0, total = 0;
   int longest = 0;
@@ -1196,7 +1197,6 @@ attention_prefill_join_kernel(const __grid_constant__ AttnArgs a,
   }
   total *= heads;
   const int parts = ap_parts(total, longest, ctas);
-  asm volatile("griddepcontrol.wait;" ::: "memory");
   if (seq < 0 || parts == 0) return;
   b = first;
   const ApSeq q = ap_seq(a, seq);
@@ -1329,21 +1329,15 @@ int launch_as(const AttnArgs& a, const CUtensorMap& q, const CUtensorMap& k, con
                                       (int)ApShape<HD>::SMEM));
     if (dev < 64) set[dev] = true;
   }
-  kern<<<h.grid, AP_THREADS, ApShape<HD>::SMEM, stream>>>(q, k, v, a, sp);
-  SLS_LAUNCH_CHECK();
-  if constexpr (!CUT) return SLS_OK;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)h.items, HD / AP_JOIN);
-  cfg.blockDim = dim3(2 * AP_BM);
-  cfg.stream = stream;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at;
-  cfg.numAttrs = 1;
-  SLS_CUDA_TRY(cudaLaunchKernelEx(&cfg, attention_prefill_join_kernel<E, HD>, a, sp, h.grid));
-  SLS_LAUNCH_CHECK();
-  return SLS_OK;
+  const int st = at_launch(kern, dim3((unsigned)h.grid), AP_THREADS, ApShape<HD>::SMEM, 1, stream,
+                           q, k, v, a, sp);
+  if constexpr (!CUT) {
+    return st;
+  } else {
+    if (st != SLS_OK) return st;
+    return at_launch(attention_prefill_join_kernel<E, HD>, dim3((unsigned)h.items, HD / AP_JOIN),
+                     2 * AP_BM, 0, 1, stream, a, sp, h.grid);
+  }
 }
 
 template <typename E, int HD>

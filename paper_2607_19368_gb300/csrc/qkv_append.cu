@@ -111,6 +111,8 @@ qkv_append_kernel(const __grid_constant__ AppendArgs a, int tokens, int heads_pe
       }
     }
   };
+  at_go();
+  at_wait_ahead();
   const char* q_src = a.q.data + t * a.q.token_b;
   load(q_src, a.q.head_b, sq.first, tok < nt ? sq.end : 0);  // while the tokens are looked up
 
@@ -301,7 +303,8 @@ int launch(const AppendArgs& a, cudaStream_t stream) {
   const int per = std::max((heads + share - 1) / share, std::min(heads, least));
   const dim3 grid((unsigned)tiles, (unsigned)((heads + per - 1) / per));
   const int mode = a.interleaved ? QA_INTERLEAVED : (a.pairs & 7) ? QA_ODD : QA_PAIRED;
-#define QA_LAUNCH(L, MODE) qkv_append_kernel<E, L, MODE><<<grid, QA_T, 0, stream>>>(a, tokens, per)
+#define QA_LAUNCH(L, MODE) \
+  return at_launch(qkv_append_kernel<E, L, MODE>, grid, QA_T, 0, 1, stream, a, tokens, per)
   if (narrow) {
     if (mode == QA_PAIRED) QA_LAUNCH(4, QA_PAIRED);
     else if (mode == QA_INTERLEAVED) QA_LAUNCH(4, QA_INTERLEAVED);
@@ -312,8 +315,6 @@ int launch(const AppendArgs& a, cudaStream_t stream) {
     else QA_LAUNCH(8, QA_ODD);
   }
 #undef QA_LAUNCH
-  SLS_LAUNCH_CHECK();
-  return SLS_OK;
 }
 
 }  // namespace
