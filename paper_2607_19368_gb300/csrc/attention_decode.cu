@@ -576,7 +576,8 @@ attention_decode_cluster_kernel(const __grid_constant__ CUtensorMap tmK,
 // sequence without tokens; nothing to do for one that was not cut.  WARPS warps share a
 // row, each a run of its pieces, and join their sums in order at the end; with WARPS = 1 a
 // CTA has a row for each of its warps (batches whose sequences have a few pieces each: the
-// whole call on 200 sequences of 12 heads 38.5 us with a CTA per row, 35.4 so).
+// whole call on 200 sequences of 12 heads 38.5 us with a CTA per row, 35.4 so; 34.9
+// since launches overlap).
 template <typename E, int WARPS>
 __global__ void __launch_bounds__(32 * AD_JOIN_WARPS)
 attention_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AdPlan p) {
@@ -672,8 +673,8 @@ int ad_host(const CacheView& c, int q_heads, AdHost* h) {
   // A cluster for each (sequence, key head) where they and their CTAs fit the GPU at once
   // (a CTA each: twice) and no warp gets more than 16 steps; up to 16 query heads a key
   // head, so that a key is read once.  Device time of parts and pieces / clusters, 28 + 4
-  // heads: 1 x 2061 tokens 9.8 / 6.9 us, 32 x 500 13.4 / 8.8 (a CTA each, as the next), 64 x
-  // 1000 25.4 / 23.6; 100 x 300, more than twice, 16.6 / 20.4.
+  // heads, before launches overlapped: 1 x 2061 tokens 9.8 / 6.9 us, 32 x 500 13.4 / 8.8
+  // (a CTA each, as the next), 64 x 1000 25.4 / 23.6; 100 x 300, more than twice, 16.6 / 20.4.
   h->cluster = 0;
   const int64_t units = (int64_t)c.B * h->vheads, room = (int64_t)c.max_pages << c.page_shift;
   if (blocks == 1)

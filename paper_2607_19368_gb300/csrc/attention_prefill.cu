@@ -25,9 +25,9 @@
 //
 // Bound by the chain softmax -> products -> softmax of a tile: a step of both tiles takes
 // 2730 cycles (the products 2112 of them, the exponentials 1024, the copies 8% of L2's
-// contention).  8192 tokens of 40 + 8 heads of 128: 450 us, 1.53 PFLOP/s, 79% of the
-// measured rate of a large matrix product; 2048 tokens of 28 + 4 heads: 33 us (16 steps of
-// the longest item, 6 us until the first scores, 2 us for the last output).
+// contention).  8192 tokens of 40 + 8 heads of 128: 446 us, 1.54 PFLOP/s, 79% of the
+// measured rate of a large matrix product; 2048 tokens of 28 + 4 heads: 32 us (16 steps of
+// the longest item, 4 us until the first scores, 2 us for the last output).
 #include <cuda.h>
 
 #include <algorithm>
@@ -1293,7 +1293,8 @@ attention_prefill_join_kernel(const __grid_constant__ AttnArgs a,
 // Items of a launch at most, its CTAs, and whether it may cut items: where there are no more
 // items than SMs and the page tables have room for AP_ROOM steps (the lengths decide on the
 // device).  Device time, whole / cut: 50 tokens behind 10000 of 28 + 4 heads 108 / 30 us, 2 x 500
-// behind 7001 of 24 + 8 heads of 64 73.4 / 59; 1000 tokens alone 20 / 36, which stay whole.
+// behind 7001 of 24 + 8 heads of 64 73.4 / 59; 1000 tokens alone 20 / 36, which stay whole
+// (both sides before launches overlapped: the cut ones' second launch costs less since).
 constexpr int AP_ROOM = 16;
 struct ApHost {
   int64_t items;
