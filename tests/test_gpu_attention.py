@@ -413,3 +413,32 @@ def test_graph_replay(sls):
     for a, c in zip(got, want):
         assert torch.equal(a, c)
     assert sls.attention_status() == 0
+
+
+# ---------------------------------------------------------------------------
+# nothing to do
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("sequences", [0, 3])
+def test_no_tokens(sls, sequences):
+    """No new tokens, of no sequence or of some: empty results, an untouched cache."""
+    b = R.make_batch([0] * sequences, [20] * sequences, 4, 2, 64, 16, torch.bfloat16, seed=83,
+                     fill=1.0)
+    k, v = b["k"].clone(), b["v"].clone()
+    rows = b["k"].new_empty(0, 2, 64)
+    out = sls.qkv_append(b["q"], rows, rows, b["k"], b["v"], b["table"], b["kv_lens"],
+                         cu_seqlens=b["cu"])
+    assert out.shape == (0, 4, 64) and prefill(sls, b).shape == (0, 4, 64)
+    if sequences == 0:
+        assert decode(sls, b).shape == (0, 4, 64)
+    assert torch.equal(b["k"], k) and torch.equal(b["v"], v)
+    assert sls.attention_status() == 0
+
+
+def test_page_table_without_columns(sls):
+    """Lengths are cut to what the table holds: rows without keys, which are zero."""
+    b = R.make_batch([1, 1], [20, 5], 4, 2, 64, 16, torch.float16, seed=89)
+    b["table"] = b["table"][:, :0].contiguous()
+    for got in (prefill(sls, b), decode(sls, b)):
+        assert torch.equal(got, torch.zeros_like(got))
+    assert sls.attention_status() == 0
