@@ -511,8 +511,11 @@ int sls_qkv_append(const sls_rows_t* q, const sls_rows_t* k, const sls_rows_t* v
  * over the cache indices j <= x_i of the token's sequence (causal), or all
  * j < kv_lens[s]; query head h reads key head h / (q_heads / kv_heads).  A row
  * with no keys is zero.  A key or value that a row does not see does not
- * change it, whatever it holds.  q, out: T x q_heads rows in the cache's dtype;
- * a token outside every sequence is not written.  scale > 0, finite.
+ * change it, whatever it holds.  An infinite value that a row sees makes its
+ * element infinite (or NaN where the weight falls below the 16-bit range that
+ * the products take) and leaves the others.  q, out: T x q_heads rows in the
+ * cache's dtype; a token outside every sequence is not written.  scale > 0,
+ * finite.
  * workspace: sls_attention_prefill_workspace_size() bytes (may be 0), holding
  * nothing between calls.
  * Errors: as sls_qkv_append, and WORKSPACE.

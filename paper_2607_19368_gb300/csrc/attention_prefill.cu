@@ -7,7 +7,7 @@
 // read once for the group whatever G is.  A CTA has two query tiles (an item) and goes over
 // the keys in steps of 128:
 //   S = Q K^T   both operands in shared memory, float32 scores in tensor memory
-//   P = 2^(c (S - m))  a thread per row, scores and maximum in registers; 16-bit weights over
+//   P = 2^(c (S - m) + a constant)  a thread per row, scores and maximum in registers; 16-bit weights over
 //               the scores' columns of tensor memory; m is replaced only when weights would
 //               grow past 2^8, and the output scaled to it then (exact: the factor is common
 //               to a row's weights, their sum and its output)
@@ -49,6 +49,13 @@ constexpr int AP_LOAD_WARP = AP_SOFT_WARPS, AP_MMA_WARP = AP_SOFT_WARPS + 1,
               AP_RING_WARP = AP_SOFT_WARPS + 2, AP_VALUE_WARP = AP_SOFT_WARPS + 3;
 constexpr int AP_ITEMS = 2;            // item slots
 constexpr float AP_LAZY = 8.f;         // log2 of the growth of the maximum that is let pass
+// log2 of a factor of all weights, which the division by their sum takes out again.  bf16 has
+// range to spare below: weights stay at most 1 with the growth that is let pass, so sums of
+// large values overflow no earlier than those of weights under the true maximum.
+template <typename E>
+struct ApShift {
+  static constexpr float value = std::is_same<E, __nv_bfloat16>::value ? -AP_LAZY : 0.f;
+};
 
 template <int HD>
 struct ApShape {
@@ -78,9 +85,15 @@ struct ApItem {
 // evenly; an item that falls to several CTAs is left in pieces, at most two a CTA (its
 // first and its last), and joined by a second launch.
 struct ApSplit {
-  float2* ml;   // (slot, row of the pair): maximum (log2 units), sum of weights
+  float2* ml;   // (slot, row of the pair): maximum of the scores, sum of weights
   float4* o;    // (slot, element / 4, row of the pair): unnormalised output
 };
+
+// Scores beyond this (in log2 units) are brought to their maximum before they are scaled: the
+// rounding of scale times maximum, common to a row's weights, would grow past the range of the
+// weights (and, where the maximum changes, past their precision).  Others are scaled and brought
+// to it in one fused step, whose share of that rounding is below 2^-14.
+constexpr float AP_FAR = 1024.f;
 
 // ---- tcgen05 / TMA wrappers ------------------------------------------------------
 
@@ -491,51 +504,79 @@ SLS_DEV bool ap_walk(ApWalk& w, const AttnArgs& a, int tpt, ApItem& it) {
   return true;
 }
 
-// ---- a row by itself -----------------------------------------------------------------
-// The tensor cores multiply a hidden key's weight 0 with its value, and 0 times
-// infinity or NaN is NaN: a row whose result is not finite is computed again by one
-// warp over the keys that it sees and no others (lanes hold four elements each), its
-// elements [d0, d1) written.
+// ---- values that are not finite -------------------------------------------------------
+// The tensor cores multiply a hidden key's weight 0 with its value, and 0 times infinity or
+// NaN is NaN.  Only the keys from the first token's limit on are hidden from some row of a
+// pair of tiles: there (less than 2 * tpt keys, in at most three steps) the ring warp puts 0
+// for elements that are not finite before the products read them (ap_clean), and the softmax
+// warps add those that a row does see to its finished output (ap_patch).  The rows cost
+// nothing of that where all values are finite.
+
+// exponents of all ones in either half of a word: bits 15 and 31
 template <typename E>
-SLS_DEV void ap_row(const CacheView& c, const char* q, char* out, int seq,
-                                    int head, int keys, float scale, int d0, int d1) {
+SLS_DEV uint32_t ap_odd(uint32_t w) {
+  constexpr bool BF = std::is_same<E, __nv_bfloat16>::value;
+  constexpr uint32_t all = BF ? 0x7f807f80u : 0x7c007c00u, one = BF ? 0x00800080u : 0x04000400u;
+  return ((w & all) + one) & 0x80008000u;
+}
+
+// Rows [r0, r1) of a tile of values in shared memory (128-byte rows, `halves` blocks of
+// them half_bytes apart): 0 for every element that is not finite; true when there was one.
+template <typename E, int HALVES>
+SLS_DEV bool ap_clean(unsigned char* tile, int half_bytes, int r0, int r1) {
+  const int lane = threadIdx.x & 31;
+  uint32_t odd = 0;
+#pragma unroll 1
+  for (int x = r0 * 8 + lane; x < r1 * 8; x += 32)
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h) {
+      const uint4 u = reinterpret_cast<const uint4*>(tile + h * half_bytes)[x];
+      odd |= ap_odd<E>(u.x) | ap_odd<E>(u.y) | ap_odd<E>(u.z) | ap_odd<E>(u.w);
+    }
+  if (!__any_sync(0xffffffffu, odd != 0)) return false;
+#pragma unroll 1
+  for (int h = 0; h < HALVES; ++h) {
+    uint32_t* v = reinterpret_cast<uint32_t*>(tile + h * half_bytes);
+#pragma unroll 1
+    for (int x = r0 * 32 + lane; x < r1 * 32; x += 32)
+      v[x] &= ~((ap_odd<E>(v[x]) >> 15) * 0xffffu);
+  }
+  return true;
+}
+
+// Adds to the finished rows of a warp the elements that ap_clean took out: element e of a
+// row that sees key h becomes infinite or NaN as value[h][e] is, and NaN where the key is
+// not finite either (its score is then NaN, or an infinity whose weight is NaN or 0).  This
+// lane's row sees `keys` keys, the values from h0 on were cleaned, those from h1 on are not
+// in this piece; add(row, x) adds x[0..3] to elements 4 lane ... of a row of the warp.
+template <typename E, typename Add>
+SLS_DEV void ap_patch(const CacheView& c, const ApItem& it, int keys, int h0, int h1, Add add) {
   const int lane = threadIdx.x & 31, e0 = 4 * lane;
   const bool on = e0 < c.head_dim;
-  float x[4] = {0.f, 0.f, 0.f, 0.f}, o[4] = {0.f, 0.f, 0.f, 0.f};
-  if (on) {
-    const uint2 u = *reinterpret_cast<const uint2*>(q + 2 * e0);
-    const float2 a = Half2<E>::widen(u.x), b = Half2<E>::widen(u.y);
-    x[0] = a.x * scale, x[1] = a.y * scale, x[2] = b.x * scale, x[3] = b.y * scale;
-  }
-  float mx = -INFINITY, l = 0.f;
-  for (int j = 0; j < keys; ++j) {
-    const int64_t page = c.table[seq * c.table_ld + (j >> c.page_shift)];
-    float k[4] = {0.f, 0.f, 0.f, 0.f}, v[4] = {0.f, 0.f, 0.f, 0.f};
+  const int mine = min(keys, h1);
+  float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int h = h0; h < h1; ++h) {
+    const int64_t at = (int64_t)it.k0 + h;
+    const int64_t page = c.table[it.seq * c.table_ld + (at >> c.page_shift)];
+    uint2 k = make_uint2(0, 0), v = k;
     if (on && page >= 0 && page < c.num_pages) {
-      const int64_t off = page * c.page_b + (j & ((1 << c.page_shift) - 1)) * c.slot_b +
-                          head * c.head_b + 2 * e0;
-      const uint2 ku = *reinterpret_cast<const uint2*>(c.k + off);
-      const uint2 vu = *reinterpret_cast<const uint2*>(c.v + off);
-      const float2 k0 = Half2<E>::widen(ku.x), k1 = Half2<E>::widen(ku.y);
-      const float2 v0 = Half2<E>::widen(vu.x), v1 = Half2<E>::widen(vu.y);
-      k[0] = k0.x, k[1] = k0.y, k[2] = k1.x, k[3] = k1.y;
-      v[0] = v0.x, v[1] = v0.y, v[2] = v1.x, v[3] = v1.y;
+      const int64_t off = page * c.page_b + (at & ((1 << c.page_shift) - 1)) * c.slot_b +
+                          it.head * c.head_b + 2 * e0;
+      k = *reinterpret_cast<const uint2*>(c.k + off);
+      v = *reinterpret_cast<const uint2*>(c.v + off);
     }
-    float d = x[0] * k[0] + x[1] * k[1] + x[2] * k[2] + x[3] * k[3];
+    const bool nan = __any_sync(0xffffffffu, (ap_odd<E>(k.x) | ap_odd<E>(k.y)) != 0);
+    const float2 a = Half2<E>::widen(v.x), b = Half2<E>::widen(v.y);
+    const float w[4] = {a.x, a.y, b.x, b.y};
 #pragma unroll
-    for (int s = 16; s > 0; s >>= 1) d += __shfl_xor_sync(0xffffffffu, d, s);
-    const float mn = fmaxf(mx, d);
-    const float base = mn == -INFINITY ? 0.f : mn;
-    const float corr = __expf(mx - base), p = __expf(d - base);
-    l = l * corr + p;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = o[e] * corr + p * v[e];
-    mx = mn;
+    for (int e = 0; e < 4; ++e)
+      if (!(fabsf(w[e]) < INFINITY)) x[e] += nan ? NAN : w[e];
+    unsigned rows = __ballot_sync(0xffffffffu, mine == h + 1);  // that see no further key
+    if (!__any_sync(0xffffffffu, !(x[0] == 0.f && x[1] == 0.f && x[2] == 0.f && x[3] == 0.f)))
+      continue;
+    for (; rows; rows &= rows - 1) add(__ffs(rows) - 1, x);
   }
-  const float inv = keys > 0 ? 1.f / l : 0.f;
-  if (on && e0 >= d0 && e0 < d1)
-    *reinterpret_cast<uint2*>(out + 2 * e0) = make_uint2(
-        Half2<E>::narrow(o[0] * inv, o[1] * inv), Half2<E>::narrow(o[2] * inv, o[3] * inv));
 }
 
 // ---- copies of keys or values ----------------------------------------------------------
@@ -622,6 +663,10 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
   __shared__ uint64_t kv_full[S::STAGES], kv_empty[S::STAGES];
   __shared__ uint64_t item_full[AP_ITEMS], item_empty[AP_ITEMS];
   __shared__ ApItem s_item[AP_ITEMS];
+  // of item k: whether values were cleaned.  A softmax warp may be at the end of an item when
+  // the ring warp is two items on (item_empty), so the places are four.
+  __shared__ uint64_t clean_full[4];
+  __shared__ int s_cleaned[4];
   __shared__ uint32_t tmem_holder;
   __shared__ volatile int s_abort;
 
@@ -650,6 +695,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
       mbar_init(&item_full[s], 1);
       mbar_init(&item_empty[s], AP_SOFT_WARPS + 3);
     }
+    for (int s = 0; s < 4; ++s) mbar_init(&clean_full[s], 1);
     mbar_init(&done_bar, 1);
     mbar_fence_init();
     s_abort = 0;
@@ -878,8 +924,12 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
     for (unsigned k = 0;; ++k) {
       const unsigned slot = k % AP_ITEMS;
       if (!wait(&item_full[slot], (k / AP_ITEMS) & 1)) break;
-      const int seq = s_item[slot].seq, len = s_item[slot].len;
+      const int seq = s_item[slot].seq, len = s_item[slot].len, lim0 = s_item[slot].lim0;
       const int n0 = s_item[slot].tiles[0], n1 = s_item[slot].tiles[1], nk = max(n0, n1);
+      // keys from `some` on are hidden from some row of the pair, those from `all` on from all
+      const int some = max(0, min(lim0, len));
+      const int all = s_item[slot].causal ? min(len, lim0 + s_item[slot].ntok - 1) : len;
+      bool cleaned = false;
       __syncwarp();
       if (lane == 0) mbar_arrive(&item_empty[slot]);
       if (seq < 0) break;
@@ -901,10 +951,13 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
             if (j + 1 == mine) mbar_arrive(&q_empty[t]);
           }
           if (!wait(&kv_full[vst % S::STAGES], (vst / S::STAGES) & 1)) break;
-          if ((j + 1) * AP_BN > len && (t == 0 || j >= n0)) {
-            // values past the sequence's end: whatever their slots hold, zero here
-            const int r0 = len - j * AP_BN;
+          if ((j + 1) * AP_BN > some && (t == 0 || j >= n0)) {
+            // hidden values: whatever their slots hold, zero past the pair's last limit,
+            // finite between the first token's and that
             unsigned char* va = smem + (2 + vst % S::STAGES) * S::TILE_BYTES;
+            const int r0 = min(AP_BN, all - j * AP_BN), first = max(0, some - j * AP_BN);
+            if (first < r0) cleaned |= ap_clean<E, S::HALVES>(va, S::HALF_BYTES, first, r0);
+#pragma unroll 1
             for (int x = r0 * 8 + lane; x < AP_BN * 8; x += 32)
 #pragma unroll
               for (int h = 0; h < S::HALVES; ++h)
@@ -919,6 +972,10 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         if (!ok) break;
       }
       if (!ok) break;
+      if (lane == 0) {
+        s_cleaned[k & 3] = cleaned;
+        mbar_arrive(&clean_full[k & 3]);
+      }
       // the last values: after the last tile's outputs
       if (n0 > 0 && last == 1) o_par ^= 1u;  // the first tile's outputs, not waited for
       if (nk > 0) {
@@ -959,6 +1016,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
       const int least = __reduce_min_sync(0xffffffffu, live ? keys : 0x7fffffff);
       const int whole = least / AP_BN;
       float mx = -INFINITY, l = 0.f;  // the maximum in use, the sum of weights under it
+      bool far = false;               // the maximum is beyond AP_FAR
       auto step = [&](int j, auto hidden) {
         if (!ap_wait(&s_full[t], s_used & 1, &s_abort)) return false;
         ++s_used;
@@ -986,9 +1044,10 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         // the output is brought to a new maximum only where the old one lets weights
         // grow past 2^AP_LAZY
         const bool grow = mx == -INFINITY ? to_mx > -INFINITY : (to_mx - mx) * c > AP_LAZY;
-        if (__any_sync(0xffffffffu, grow)) {
+        if (__any_sync(0xffffffffu, grow || far)) {
           const float f = grow ? at_exp2((mx - to_mx) * c) : 1.f;
           if (grow) mx = to_mx;
+          far = live && mx != -INFINITY && fabsf(mx * c) > AP_FAR;
           l *= f;
           if (j > 0) {
 #pragma unroll 1
@@ -1001,8 +1060,16 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
               ap_st32(to + 32 * q, o);
             }
           }
+          if (__any_sync(0xffffffffu, far)) {
+            const float m = far ? mx : 0.f;
+            const f32x2_t m2 = pk2(-m, -m);
+#pragma unroll
+            for (int e = 0; e < AP_BN; e += 2)
+              upk2(add2(pk2(s[e], s[e + 1]), m2), s[e], s[e + 1]);
+          }
         }
-        const float base = mx == -INFINITY ? 0.f : -mx * c;
+        const float base = mx == -INFINITY ? 0.f : far ? ApShift<E>::value
+                                                       : __fmaf_rn(-mx, c, ApShift<E>::value);
         const f32x2_t c2 = pk2(c, c), b2 = pk2(base, base);
         f32x2_t sum[2] = {pk2(0.f, 0.f), pk2(0.f, 0.f)};
         // weights 2^(c (s - mx)) as 16-bit pairs over the scores' columns
@@ -1058,10 +1125,18 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         ++o_used;
         ap_fence_after();
       }
+      if (!ap_wait(&clean_full[k & 3], (k >> 2) & 1, &s_abort)) {
+        if (lane == 0) fail();
+        break;
+      }
+      const bool cleaned = s_cleaned[k & 3];
+      // of the cleaned keys, the item's or piece's
+      const int h0 = max(0, min(it.lim0, it.len));
+      const int h1 = min(min(it.len, it.lim0 + it.ntok - 1), max(it.tiles[0], it.tiles[1]) * AP_BN);
       if (CUT && it.slot >= 0) {
         // a piece: rows next to one another for every four elements
         const int64_t at = (int64_t)it.slot * 2 * AP_BM + t * AP_BM + row;
-        sp.ml[at] = make_float2(mx == -INFINITY ? -INFINITY : mx * c, l);
+        sp.ml[at] = make_float2(mx, l);
         float4* po = sp.o + (int64_t)it.slot * (HD / 4) * 2 * AP_BM + t * AP_BM + row;
 #pragma unroll 1
         for (int q = 0; q < HD / 32; ++q) {
@@ -1078,13 +1153,22 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
             po[(8 * q + e / 4) * 2 * AP_BM] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
         }
         ap_fence_before();
+        if (cleaned) {
+          __syncwarp();
+          ap_patch<E>(a.c, it, keys, h0, h1, [&](int src, const float(&x)[4]) {
+            // element 4 lane of row src of the warp
+            float4* p = po + (int64_t)lane * 2 * AP_BM + (src - lane);
+            if (4 * lane >= a.c.head_dim) return;
+            const float4 v = *p;
+            *p = make_float4(v.x + x[0], v.y + x[1], v.z + x[2], v.w + x[3]);
+          });
+        }
         continue;
       }
       // 64 elements at a time through shared memory, so that a store instruction writes
       // whole 128-byte pieces of four rows (loops, not straight code: it runs once an
       // item, from beyond the instruction caches)
-      f32x2_t odd = pk2(0.f, 0.f);  // NaN once any element is not finite
-      const f32x2_t inv2 = pk2(inv, inv), zero2 = pk2(0.f, 0.f);
+      const f32x2_t inv2 = pk2(inv, inv);
       const int ch = lane & 7;
 #pragma unroll 1
       for (int hf = 0; hf < S::HALVES; ++hf) {
@@ -1103,9 +1187,7 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
             float x[8];
 #pragma unroll
             for (int d = 0; d < 8; d += 2) {
-              const f32x2_t v = mul2(pk2(o[e + d], o[e + d + 1]), inv2);
-              odd = fma2(v, zero2, odd);
-              upk2(v, x[d], x[d + 1]);
+              upk2(mul2(pk2(o[e + d], o[e + d + 1]), inv2), x[d], x[d + 1]);
             }
             *reinterpret_cast<uint4*>(stage_out + lane * 128 +
                                       (((4 * q + (e >> 3)) ^ (lane & 7)) << 4)) = narrow8<E>(x);
@@ -1122,20 +1204,18 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
         }
         __syncwarp();
       }
-      float odd_x, odd_y;
-      upk2(odd, odd_x, odd_y);
       ap_fence_before();
-      unsigned bad = __ballot_sync(0xffffffffu, live && !(odd_x + odd_y == 0.f));
-      while (bad) {
-        const int src = __ffs(bad) - 1;
-        bad &= bad - 1;
-        const int64_t bt = __shfl_sync(0xffffffffu, (long long)gt, src);
-        const int bh = __shfl_sync(0xffffffffu, h, src);
-        const int bk = __shfl_sync(0xffffffffu, keys, src);
-        __syncwarp();
-        ap_row<E>(a.c, a.q.data + bt * a.q.token_b + bh * a.q.head_b,
-                  a.out.data + bt * a.out.token_b + bh * a.out.head_b, it.seq, it.head, bk,
-                  a.scale, 0, HD);
+      if (cleaned) {
+        ap_patch<E>(a.c, it, keys, h0, h1, [&](int src, const float(&x)[4]) {
+          char* p = reinterpret_cast<char*>(__shfl_sync(
+              0xffffffffu, reinterpret_cast<unsigned long long>(out), src));
+          if (4 * lane >= a.c.head_dim) return;
+          uint2* u = reinterpret_cast<uint2*>(p + 8 * lane);
+          const uint2 w = *u;
+          const float2 y = Half2<E>::widen(w.x), z = Half2<E>::widen(w.y);
+          *u = make_uint2(Half2<E>::narrow(y.x + x[0], y.y + x[1]),
+                          Half2<E>::narrow(z.x + x[2], z.y + x[3]));
+        });
       }
     }
   }
@@ -1225,6 +1305,7 @@ attention_prefill_join_kernel(const __grid_constant__ AttnArgs a,
   // the first piece is its CTA's last unless the CTA starts with it
   const int late = total * g0 / parts < x0;
   const int keys = live ? max(0, min(q.len, a.causal ? q.m - q.n + b * qb + tok + 1 : q.len)) : 0;
+  const float c = a.scale * 1.4426950408889634f;
   float top = -INFINITY, sum = 0.f, o[AP_JOIN];
 #pragma unroll
   for (int e = 0; e < AP_JOIN; ++e) o[e] = 0.f;
@@ -1247,14 +1328,14 @@ attention_prefill_join_kernel(const __grid_constant__ AttnArgs a,
     float to = top;
 #pragma unroll
     for (int u = 0; u < AP_FLIGHT; ++u) to = fmaxf(to, ml[u].x);
-    const float base = to == -INFINITY ? 0.f : to, f = at_exp2(top - base);
+    const float base = to == -INFINITY ? 0.f : to, f = at_exp2((top - base) * c);
     top = to;
     sum *= f;
 #pragma unroll
     for (int e = 0; e < AP_JOIN; ++e) o[e] *= f;
 #pragma unroll
     for (int u = 0; u < AP_FLIGHT; ++u) {
-      const float w = at_exp2(ml[u].x - base);
+      const float w = at_exp2((ml[u].x - base) * c);
       sum += ml[u].y * w;
 #pragma unroll
       for (int x = 0; x < AP_JOIN / 4; ++x) {
@@ -1264,29 +1345,13 @@ attention_prefill_join_kernel(const __grid_constant__ AttnArgs a,
     }
   }
   const float inv = keys > 0 ? 1.f / sum : 0.f;
-  float odd = 0.f;
 #pragma unroll
   for (int e = 0; e < AP_JOIN; e += 8) {
     float x[8];
 #pragma unroll
-    for (int d = 0; d < 8; ++d) {
-      x[d] = o[e + d] * inv;
-      odd = __fmaf_rn(x[d], 0.f, odd);
-    }
+    for (int d = 0; d < 8; ++d) x[d] = o[e + d] * inv;
     if (live && d0 + e < a.c.head_dim)
       *reinterpret_cast<uint4*>(out + 2 * (d0 + e)) = narrow8<E>(x);
-  }
-  unsigned bad = __ballot_sync(0xffffffffu, live && !(odd == 0.f));
-  while (bad) {
-    const int src = __ffs(bad) - 1;
-    bad &= bad - 1;
-    const int64_t bt = __shfl_sync(0xffffffffu, (long long)gt, src);
-    const int bh = __shfl_sync(0xffffffffu, h, src);
-    const int bk = __shfl_sync(0xffffffffu, keys, src);
-    __syncwarp();
-    ap_row<E>(a.c, a.q.data + bt * a.q.token_b + bh * a.q.head_b,
-              a.out.data + bt * a.out.token_b + bh * a.out.head_b, seq, head, bk, a.scale, d0,
-              d0 + AP_JOIN);
   }
 }
 
