@@ -53,7 +53,7 @@ struct AdPlan {
   int groups;         // most parts
   int vheads;         // key heads times row blocks
   int64_t* prefix;    // B + 1: steps before every sequence
-  float2* ml;         // (part, first or last piece, vhead, row): maximum (log2 units), sum
+  float2* ml;         // (part, first or last piece, vhead, row): maximum of the scores, sum
   float* o;           // the same, hd_pad elements each
   int hd_pad;
 };
@@ -262,15 +262,16 @@ struct AdRows {
           o[b][2] *= f[1], o[b][3] *= f[1];
         }
       }
-      const float base[2] = {mx[0] == -INFINITY ? 0.f : -mx[0] * cs,
-                             mx[1] == -INFINITY ? 0.f : -mx[1] * cs};
+      // the distance from the maximum first, which is exact where it matters: scale times
+      // maximum would round by more than the weights' range where scores are large
+      const float base[2] = {mx[0] == -INFINITY ? 0.f : mx[0], mx[1] == -INFINITY ? 0.f : mx[1]};
       uint32_t w[2][4];
 #pragma unroll
       for (int nb = 0; nb < 4; ++nb) {
         float e[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          e[i] = at_exp2(__fmaf_rn(s[nb][i], cs, base[i >> 1]));
+          e[i] = at_exp2((s[nb][i] - base[i >> 1]) * cs);
           l[i >> 1] += e[i];
         }
         w[nb >> 1][2 * (nb & 1)] = Half2<E>::narrow(e[0], e[1]);
@@ -421,7 +422,7 @@ attention_decode_kernel(const __grid_constant__ CUtensorMap tmK,
         const int rr = r + 8 * x;
         if (rr >= rows) continue;
         if (cq == 0)
-          p.ml[slot + rr] = make_float2(mx[x] == -INFINITY ? -INFINITY : mx[x] * cs, l[x]);
+          p.ml[slot + rr] = make_float2(mx[x], l[x]);
         float* out = p.o + (slot + rr) * p.hd_pad;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -493,7 +494,7 @@ attention_decode_cluster_kernel(const __grid_constant__ CUtensorMap tmK,
   for (int x = 0; x < 2; ++x) {
     const int rr = r + 8 * x;
     if (cq == 0) {
-      s_m[warp][rr] = w.mx[x] == -INFINITY ? -INFINITY : w.mx[x] * cs;
+      s_m[warp][rr] = w.mx[x];
       s_l[warp][rr] = ok ? w.l[x] : 0.f;
     }
     if (rr < rows) {
@@ -534,7 +535,7 @@ attention_decode_cluster_kernel(const __grid_constant__ CUtensorMap tmK,
       const float4 v =
           e0 < HD ? ld4(peer(out_s + rr * HD + e0, p)) : make_float4(0.f, 0.f, 0.f, 0.f);
       const float mn = fmaxf(m, pm), base = mn == -INFINITY ? 0.f : mn;
-      const float f = at_exp2(m - base), g = at_exp2(pm - base);
+      const float f = at_exp2((m - base) * cs), g = at_exp2((pm - base) * cs);
       l = l * f + pl * g;
       o[0] = o[0] * f + v.x * g, o[1] = o[1] * f + v.y * g;
       o[2] = o[2] * f + v.z * g, o[3] = o[3] * f + v.w * g;
@@ -555,7 +556,7 @@ attention_decode_cluster_kernel(const __grid_constant__ CUtensorMap tmK,
       float sum = 0.f, y = 0.f, z = 0.f;
 #pragma unroll
       for (int x = 0; x < W; ++x) {
-        const float f = at_exp2(s_join[x][HD] - base);
+        const float f = at_exp2((s_join[x][HD] - base) * cs);
         sum += s_join[x][HD + 1] * f;
         y += s_join[x][e] * f;
         z += s_join[x][e + 1] * f;
@@ -604,6 +605,7 @@ attention_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant_
     return;
   }
   const int parts = ad_parts(total, p.groups);
+  const float cs = a.scale * 1.4426950408889634f;
   // the part of step t is the last whose start total * g / parts is at most t
   const int g0 = (int)(((b0 + 1) * parts - 1) / total), g1 = (int)((b1 * parts - 1) / total);
   if (g0 == g1) return;
@@ -621,7 +623,7 @@ attention_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant_
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     if (e0 < c.head_dim) v = *reinterpret_cast<const float4*>(p.o + slot * p.hd_pad + e0);
     const float mn = fmaxf(m, ml.x), base = mn == -INFINITY ? 0.f : mn;
-    const float f = at_exp2(m - base), w = at_exp2(ml.x - base);
+    const float f = at_exp2((m - base) * cs), w = at_exp2((ml.x - base) * cs);
     l = l * f + ml.y * w;
     o[0] = o[0] * f + v.x * w, o[1] = o[1] * f + v.y * w;
     o[2] = o[2] * f + v.z * w, o[3] = o[3] * f + v.w * w;
@@ -646,7 +648,7 @@ attention_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant_
     float sum = 0.f, x = 0.f, y = 0.f;
     for (int w = 0; w < WARPS; ++w) {
       if (w * per >= n) break;
-      const float f = at_exp2(s_m[w] - base);
+      const float f = at_exp2((s_m[w] - base) * cs);
       sum += s_l[w] * f;
       x += s_o[w][2 * e] * f;
       y += s_o[w][2 * e + 1] * f;
