@@ -33,6 +33,11 @@ constexpr int AD_KEYS = 32;       // tokens of a step
 constexpr int AD_MIN_STEPS = 2;   // a part holds at least so many steps where there are as many
 constexpr int AD_ROWS = 16;       // query heads of a tile
 constexpr int AD_JOIN_WARPS = 8;
+// log2 of a factor of all weights, which the division by their sum takes out again: float16
+// weights use the range above 1 too, so that many small ones next to a large one (2^-25 and
+// less of it, which would round to 0) reach the output as they reach the sum
+template <typename E>
+constexpr float AD_SHIFT = std::is_same<E, __nv_bfloat16>::value ? 0.f : 15.f;
 
 template <int HD>
 struct AdShape {
@@ -266,17 +271,20 @@ struct AdRows {
       // maximum would round by more than the weights' range where scores are large
       const float base[2] = {mx[0] == -INFINITY ? 0.f : mx[0], mx[1] == -INFINITY ? 0.f : mx[1]};
       uint32_t w[2][4];
+      float sum[2] = {0.f, 0.f};  // of the step: added to l one by one, small weights next to a
+                                  // large one would be below half of its last place
 #pragma unroll
       for (int nb = 0; nb < 4; ++nb) {
         float e[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          e[i] = at_exp2((s[nb][i] - base[i >> 1]) * cs);
-          l[i >> 1] += e[i];
+          e[i] = at_exp2(__fmaf_rn(s[nb][i] - base[i >> 1], cs, AD_SHIFT<E>));
+          sum[i >> 1] += e[i];
         }
         w[nb >> 1][2 * (nb & 1)] = Half2<E>::narrow(e[0], e[1]);
         w[nb >> 1][2 * (nb & 1) + 1] = Half2<E>::narrow(e[2], e[3]);
       }
+      l[0] += sum[0], l[1] += sum[1];
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks) {
         const int row = ks * 16 + (lane & 15);

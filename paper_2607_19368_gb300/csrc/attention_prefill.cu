@@ -51,11 +51,11 @@ constexpr int AP_ITEMS = 2;            // item slots
 constexpr float AP_LAZY = 8.f;         // log2 of the growth of the maximum that is let pass
 // log2 of a factor of all weights, which the division by their sum takes out again.  bf16 has
 // range to spare below: weights stay at most 1 with the growth that is let pass, so sums of
-// large values overflow no earlier than those of weights under the true maximum.
+// large values overflow no earlier than those of weights under the true maximum.  float16 uses
+// its range up to 2^15, so that many small weights next to a large one (2^-25 and less of it,
+// which would round to 0) reach the output as they reach the sum.
 template <typename E>
-struct ApShift {
-  static constexpr float value = std::is_same<E, __nv_bfloat16>::value ? -AP_LAZY : 0.f;
-};
+constexpr float AP_SHIFT = std::is_same<E, __nv_bfloat16>::value ? -AP_LAZY : 15.f - AP_LAZY;
 
 template <int HD>
 struct ApShape {
@@ -1068,8 +1068,9 @@ attention_prefill_kernel(const __grid_constant__ CUtensorMap tmQ,
               upk2(add2(pk2(s[e], s[e + 1]), m2), s[e], s[e + 1]);
           }
         }
-        const float base = mx == -INFINITY ? 0.f : far ? ApShift<E>::value
-                                                       : __fmaf_rn(-mx, c, ApShift<E>::value);
+        const float base = mx == -INFINITY ? 0.f
+                           : far           ? AP_SHIFT<E>
+                                           : __fmaf_rn(-mx, c, AP_SHIFT<E>);
         const f32x2_t c2 = pk2(c, c), b2 = pk2(base, base);
         f32x2_t sum[2] = {pk2(0.f, 0.f), pk2(0.f, 0.f)};
         // weights 2^(c (s - mx)) as 16-bit pairs over the scores' columns
