@@ -136,8 +136,10 @@ def _cache(cache_k, cache_v, page_table, kv_lens):
         raise ValueError("page_table: B x max_pages int32 on the cache's device")
     B, cols = table
     ld, se = page_table.stride()
-    if se != 1 and cols > 1:
-        raise ValueError("page_table: contiguous rows")
+    if B <= 1:
+        ld = cols
+    if (se != 1 and cols > 1) or ld < cols:
+        raise ValueError("page_table: contiguous rows that do not overlap")
     lens = _ints("kv_lens", kv_lens, B, dev)
     n, ps, H, hd = shape
     sp, ss, sh, _ = strides
@@ -146,7 +148,7 @@ def _cache(cache_k, cache_v, page_table, kv_lens):
     if n == 1:
         sp = ps * max(ss, sh * H)
     return (_pack_cache(cache_k.data_ptr(), cache_v.data_ptr(), code, H, hd, ps, n, sp, ss, sh,
-                        page_table.data_ptr(), ld if ld > cols else cols, cols, lens, B),
+                        page_table.data_ptr(), ld, cols, lens, B),
             shape, dt, dev, B, cols)
 
 
