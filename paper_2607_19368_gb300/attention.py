@@ -53,6 +53,7 @@ _ROWS = struct.Struct("@Pqq")
 _ROPE = struct.Struct("@Piif")
 _pack_cache, _pack_rows = _CACHE.pack, _ROWS.pack
 _raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
 
 
 class Rope:
@@ -161,7 +162,13 @@ def _weight(name: str, w: Optional[torch.Tensor], dtype, head_dim: int, dev: int
     return w.data_ptr()
 
 
-def _done(fn: str, st: int, dev: int):
+def _call(fn: str, dev: int, *args):
+    """A C call on the current stream of the tensors' device, which is made current: the
+    library launches on the current one."""
+    if _current_device() != dev:
+        with torch.cuda.device(dev):
+            return _call(fn, dev, *args)
+    st = getattr(_sls._lib or _sls.lib(), fn)(*args, _raw_stream(dev))
     if st != 0:
         _sls._check(fn, st)
     if _sls._CHECK_STATUS:
@@ -206,10 +213,10 @@ def qkv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_k: torch
         q_weight = _weight("q_weight", q_weight, dt, hd, dev)
     if k_weight is not None:
         k_weight = _weight("k_weight", k_weight, dt, hd, dev)
-    st = (_sls._lib or _sls.lib()).sls_qkv_append(
-        rq, rk, rv, T, shape[1], c, cu_seqlens, positions, q_weight, k_weight, eps,
-        None if rope is None else rope._c, ro, _raw_stream(dev))
-    _done("sls_qkv_append", st, dev)
+    if rope is not None and rope.inv_freq.get_device() != dev:
+        raise ValueError("rope: frequencies on the cache's device")
+    _call("sls_qkv_append", dev, rq, rk, rv, T, shape[1], c, cu_seqlens, positions, q_weight,
+          k_weight, eps, None if rope is None else rope._c, ro)
     return out
 
 
@@ -222,12 +229,13 @@ def _attention_rows(q, out, scale, dt, hd, dev):
             hd ** -0.5 if scale is None else float(scale))
 
 
-def _scratch(nbytes: int, workspace: Optional[torch.Tensor], q: torch.Tensor):
+def _scratch(nbytes: int, workspace: Optional[torch.Tensor], q: torch.Tensor, dev: int):
     """A caller's workspace (a uint8 tensor) or one for this call."""
     if workspace is None:
         return q.new_empty(nbytes, dtype=torch.uint8)
-    if not workspace.is_cuda or workspace.dtype != torch.uint8:
-        raise ValueError("workspace: a uint8 CUDA tensor")
+    if workspace.get_device() != dev or workspace.dtype != torch.uint8 \
+            or not workspace.is_contiguous():
+        raise ValueError("workspace: a contiguous uint8 tensor on the cache's device")
     return workspace
 
 
@@ -267,11 +275,9 @@ def attention_prefill(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Ten
     nbytes = _prefill_bytes(dev, T, Hq, _CODES[dt], H, hd, ps, n, B, cols)
     wp = 0
     if nbytes:
-        workspace = _scratch(nbytes, workspace, q)
+        workspace = _scratch(nbytes, workspace, q, dev)
         wp, nbytes = workspace.data_ptr(), workspace.numel()
-    st = (_sls._lib or _sls.lib()).sls_attention_prefill(rq, T, Hq, c, cu, causal, scale, ro, wp,
-                                                         nbytes, _raw_stream(dev))
-    _done("sls_attention_prefill", st, dev)
+    _call("sls_attention_prefill", dev, rq, T, Hq, c, cu, causal, scale, ro, wp, nbytes)
     return out
 
 
@@ -289,11 +295,9 @@ def attention_decode(q: torch.Tensor, cache_k: torch.Tensor, cache_v: torch.Tens
     nbytes = _decode_bytes(dev, Hq, _CODES[dt], H, hd, ps, n, B, cols)
     wp = 0
     if nbytes:
-        workspace = _scratch(nbytes, workspace, q)
+        workspace = _scratch(nbytes, workspace, q, dev)
         wp, nbytes = workspace.data_ptr(), workspace.numel()
-    st = (_sls._lib or _sls.lib()).sls_attention_decode(rq, Hq, c, scale, ro, wp, nbytes,
-                                                        _raw_stream(dev))
-    _done("sls_attention_decode", st, dev)
+    _call("sls_attention_decode", dev, rq, Hq, c, scale, ro, wp, nbytes)
     return out
 
 
