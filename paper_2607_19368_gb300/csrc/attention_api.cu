@@ -153,8 +153,11 @@ int sls_attention_status(void* stream) {
   int* word[2] = {nullptr, nullptr};
   int st = prefill_status_word(&word[0]);
   if (st == SLS_OK) st = decode_status_word(&word[1]);
-  for (int i = 0; i < 2 && st == SLS_OK; ++i) st = sls_workspace_status(word[i], stream);
-  return st;
+  if (st != SLS_OK) return st;
+  // both are read and cleared, whatever the first one holds
+  const int prefill = sls_workspace_status(word[0], stream);
+  const int decode = sls_workspace_status(word[1], stream);
+  return prefill != SLS_OK ? prefill : decode;
 }
 
 }  // extern "C"
