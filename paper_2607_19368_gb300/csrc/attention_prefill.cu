@@ -241,10 +241,10 @@ SLS_DEV void ap_lens(const ApOrder& o, int s, int& q0, int& n, int& m) {
 SLS_DEV int ap_count(const ApOrder& o, int n, int m, int c) {
   const int nb = ap_div(o, n + o.qb - 1);
   if (c <= 0) return nb;
-  const int x = (c - 1) * AP_BN;  // more than x keys
-  if (m <= x) return 0;
+  const unsigned x = (unsigned)(c - 1) * AP_BN;  // more than x keys; up to 2^31
+  if ((unsigned)m <= x) return 0;
   if (!o.causal) return nb;
-  const int e = x - (m - n) + 1;  // the block's last token is number e or later
+  const int e = (int)x - (m - n) + 1;  // the block's last token is number e or later
   return e <= 0 ? nb : nb - min(nb, ap_div(o, e + o.qb - 1) - 1);
 }
 

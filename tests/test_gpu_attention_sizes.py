@@ -126,3 +126,23 @@ def test_append_of_one_token_per_sequence(sls, B, mode, given):
     b = R.make_batch([1] * B, m, 4, 2, mode[0], 64, torch.bfloat16, seed=43)
     x, pos = projected(B, 4, 2, mode[0], torch.bfloat16)
     appended(sls, b, x, 4, 2, pos if given else None, mode, torch.bfloat16, None)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_lengths_up_to_the_largest_integer(sls, causal):
+    """A length is cut to what the page table holds, whatever it says: rows of new tokens
+    past the table see all of it, and the batch's other sequences theirs."""
+    table_tokens = 512
+    for n in (30, 300):
+        b = R.make_batch([n, 200, 33], [table_tokens, 200, 77], 4, 2, 64, 16, torch.bfloat16, seed=47)
+        b["table"] = b["table"][:, :table_tokens // 16].contiguous()
+        b["kv_lens"][0] = (1 << 31) - 1
+        all_of_it = dict(b, q=b["q"][:n], new=[n], m=[table_tokens])
+        want, bound = R.attention(all_of_it, False)
+        rest = dict(b, q=b["q"][n:], new=[200, 33], m=[200, 77], table=b["table"][1:])
+        want2, bound2 = R.attention(rest, causal)
+        out = torch.full_like(b["q"], float("nan"))
+        sls.attention_prefill(b["q"], b["k"], b["v"], b["table"], b["kv_lens"], b["cu"],
+                              causal=causal, out=out)
+        R.check(out, torch.cat([want, want2]), torch.cat([bound, bound2]))
+        assert sls.attention_status() == 0
