@@ -451,7 +451,7 @@ typedef struct sls_kv_cache {
   int64_t head_stride;
   const int32_t* page_table; /* B rows of max_pages page numbers               */
   int64_t table_ld;          /* row stride of the table, >= max_pages          */
-  int max_pages;
+  int max_pages;             /* max_pages * page_size at most 2^31 - 1024      */
   const int32_t* kv_lens;    /* B                                              */
   int64_t batch;             /* B                                              */
 } sls_kv_cache_t;

@@ -7,6 +7,8 @@ using namespace sls;
 namespace {
 
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;
+// the kernels count cached tokens, and up to a step's or a batch of pages' more, in 32 bits
+constexpr int64_t kMaxCached = ((int64_t)1 << 31) - 1024;
 
 // The running maximum is taken of unscaled scores.
 bool scale_ok(float s) { return s > 0.f && s <= 3.402823466e38f; }
@@ -38,6 +40,7 @@ int cache_view(const sls_kv_cache_t* c, int q_heads, CacheView* v) {
     return SLS_ERR_UNSUPPORTED;
   if (q_heads / c->kv_heads > SLS_MAX_HEAD_GROUP) return SLS_ERR_UNSUPPORTED;
   if (c->batch > kMaxTokens || c->num_pages > 0x7fffffff) return SLS_ERR_UNSUPPORTED;
+  if ((int64_t)c->max_pages * c->page_size > kMaxCached) return SLS_ERR_UNSUPPORTED;
   if (c->page_stride < 0 || c->page_stride % 8 || c->slot_stride % 8 || c->head_stride % 8 ||
       c->slot_stride < c->head_dim || c->head_stride < c->head_dim)
     return SLS_ERR_INVALID_ARG;
