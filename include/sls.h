@@ -482,6 +482,7 @@ typedef struct sls_rope {
 #define SLS_F16 2             /* cache and query dtype of the attention calls */
 #define SLS_MAX_HEAD_DIM 128
 #define SLS_MAX_HEAD_GROUP 128 /* query heads per key head */
+#define SLS_MAX_PACKED_SEQUENCES 65536 /* sequences of a call with cu_seqlens */
 
 /*
  * Appends T new tokens to the cache and rotates their queries.  For every
@@ -497,7 +498,8 @@ typedef struct sls_rope {
  * past the table, is not appended (its query is still written).  Two sequences
  * must not append to the same slot.
  * Errors: INVALID_ARG (sizes, NULL pointers, strides or pointers that break
- * the 16-byte rule), UNSUPPORTED (dtype, head_dim, page_size, head ratio).
+ * the 16-byte rule), UNSUPPORTED (dtype, head_dim, page_size, head ratio, more
+ * than SLS_MAX_PACKED_SEQUENCES sequences with cu_seqlens).
  */
 int sls_qkv_append(const sls_rows_t* q, const sls_rows_t* k, const sls_rows_t* v, int64_t T,
                    int q_heads, const sls_kv_cache_t* cache, const int32_t* cu_seqlens,

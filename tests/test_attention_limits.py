@@ -16,3 +16,17 @@ def test_page_tables_of_more_tokens_than_32_bits_count(sls, page, most):  # noqa
         assert L.sls_attention_prefill(r, 0, 4, c, 256, 1, 1.0, r, None, 0, None) == status
         assert L.sls_qkv_append(r, r, r, 0, 4, c, 256, None, None, None, 1e-6, None, r,
                                 None) == status
+
+
+def test_packed_sequences_are_limited(sls):  # noqa: F811
+    """With offsets every token's or item's sequence is looked up among all of them; past the
+    limit a call is refused.  One token per sequence without offsets has no such limit."""
+    L, r = sls.lib(), rows()
+    for batch, status in ((65536, 0), (65537, 2), (1 << 30, 2)):
+        c = cache(sls, batch=batch)
+        assert L.sls_attention_prefill(r, 0, 4, c, 256, 1, 1.0, r, None, 0, None) == status
+        assert L.sls_qkv_append(r, r, r, 0, 4, c, 256, None, None, None, 1e-6, None, r,
+                                None) == status
+    # the limit is of offsets: here the count of tokens is what is wrong, not the batch
+    c = cache(sls, batch=65537)
+    assert L.sls_qkv_append(r, r, r, 0, 4, c, None, None, None, None, 1e-6, None, r, None) == 1
