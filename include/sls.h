@@ -470,7 +470,8 @@ typedef struct sls_rows {
  * turns by the angle p * inv_freq[i] and is scaled by `scale`:
  *   a' = scale (a cos t - b sin t),  b' = scale (b cos t + a sin t).
  * inv_freq: `pairs` floats, so any scaling for long contexts is a choice of
- * frequencies.  The angle is reduced from the exact product p * inv_freq[i].
+ * frequencies.  The angle is reduced from the exact product p * inv_freq[i], at
+ * any position while that is below 2^50.
  */
 typedef struct sls_rope {
   const float* inv_freq;

@@ -36,19 +36,31 @@ enum { QA_PAIRED, QA_INTERLEAVED, QA_ODD };  // halves of whole vectors (or no r
 // remainder (one fused multiply-add); Cody and Waite's reduction (W. J. Cody and
 // W. Waite, "Software Manual for the Elementary Functions", 1980) takes multiples
 // of 2 pi off it, 2 pi split into three float32 parts, each the rounding of what
-// the previous ones leave: with |p f| below 2^24 the first step is exact, and the
-// angle is right to a few 2^-24 at any position, where the rounded product alone
-// is off by up to 2^-24 |p f|.
-SLS_DEV float2 turn(float p, float f) {
-  const float x = __fmul_rn(p, f);
-  const float rest = __fmaf_rn(p, f, -x);
-  const float k = rintf(x * 0.15915494309189535f);
-  float r = __fmaf_rn(-k, 0x1.921fb6p+2f, x);
-  r = __fmaf_rn(-k, -0x1.777a5cp-23f, r);
-  r = __fmaf_rn(-k, -0x1.ee59dap-48f, r);
-  r += rest;
+// the previous ones leave: with |p| and |p f| below 2^24 the first step is exact,
+// and the angle is right to a few 2^-24, where the rounded product alone is off by
+// up to 2^-24 |p f|.  Past 2^24 the same is done in float64 with 2 pi in two parts,
+// which holds for |p f| up to 2^50.
+SLS_DEV float2 turn(int p, float f) {
+  const float q = (float)p;
+  const float x = __fmul_rn(q, f);
+  float r;
+  if (abs((int64_t)p) <= (1 << 24) && fabsf(x) < 0x1p24f) {
+    const float rest = __fmaf_rn(q, f, -x);
+    const float k = rintf(x * 0.15915494309189535f);
+    r = __fmaf_rn(-k, 0x1.921fb6p+2f, x);
+    r = __fmaf_rn(-k, -0x1.777a5cp-23f, r);
+    r = __fmaf_rn(-k, -0x1.ee59dap-48f, r);
+    r += rest;
+  } else {
+    const double y = __dmul_rn((double)p, (double)f);
+    const double rest = __fma_rn((double)p, (double)f, -y);
+    const double k = rint(y * 0.15915494309189535);
+    double z = __fma_rn(-k, 0x1.921fb54442d18p+2, y);
+    z = __fma_rn(-k, 0x1.1a62633145c07p-52, z);
+    r = (float)(z + rest);
+  }
   float s, c;
-  sincosf(fabsf(x) < 0x1p24f ? r : x, &s, &c);
+  sincosf(r, &s, &c);
   return make_float2(c, s);
 }
 
@@ -65,7 +77,7 @@ __global__ void __launch_bounds__(QA_T, 6)
 qkv_append_kernel(const __grid_constant__ AppendArgs a, int tokens, int heads_per_cta) {
   __shared__ float2 s_turn[QA_MAX_TOKENS][QA_MAX_PAIRS];  // (cos, sin) * scale
   __shared__ int64_t s_slot[QA_MAX_TOKENS];               // byte offset of the token's slot, or -1
-  __shared__ float s_pos[QA_MAX_TOKENS];
+  __shared__ int s_pos[QA_MAX_TOKENS];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int64_t t0 = (int64_t)blockIdx.x * tokens;
   const int nt = (int)min((int64_t)tokens, a.T - t0);
@@ -140,7 +152,7 @@ qkv_append_kernel(const __grid_constant__ AppendArgs a, int tokens, int heads_pe
         }
       }
       s_slot[i] = slot;
-      s_pos[i] = a.positions ? (float)a.positions[tt] : (float)idx;
+      s_pos[i] = a.positions ? a.positions[tt] : (int)idx;
     }
   }
   __syncthreads();
