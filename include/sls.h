@@ -531,7 +531,8 @@ int sls_attention_prefill(const sls_rows_t* q, int64_t T, int q_heads,
 
 /*
  * The single-token form: row s of q (B x q_heads rows) attends to all
- * kv_lens[s] tokens of sequence s; a sequence of length 0 gives zeros.  The
+ * kv_lens[s] tokens of sequence s; a sequence of length 0 gives zeros, and
+ * values that are not finite act as in sls_attention_prefill.  The
  * work of all sequences is cut into equal parts along the cached tokens, and
  * the parts of a row are joined in a fixed order.  workspace:
  * sls_attention_decode_workspace_size() bytes, holding nothing between calls.

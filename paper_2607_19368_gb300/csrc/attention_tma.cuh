@@ -10,9 +10,8 @@ namespace sls {
 
 // One lane of the warp, the same every time.  The copies and products that one lane
 // issues are written as predicated instructions of the whole warp, not as a branch of
-// that lane: their operands then stay in uniform registers, where a branch costs a
-// register move for each (prefill of 8192 tokens, the products' warp: 556 us with a
-// branch, 525 without).
+// that lane, with operands that are the same in all lanes (prefill of 8192 tokens, the
+// products' warp: 556 us with a branch, 525 without, in an early build).
 SLS_DEV uint32_t at_elect() {
   uint32_t r;
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n"

@@ -11,10 +11,10 @@
 // of its token, so that an element costs one multiplication, one fused
 // multiply-add and the product with the norm.
 //
-// 21345 tokens of 32 query, 8 key and 8 value heads of 128: 90.5 us, 5.8 TB/s, 85% of a
+// 21345 tokens of 32 query, 8 key and 8 value heads of 128: 90.2 us, 5.8 TB/s, 85% of a
 // plain copy's rate (a lane per vector with the turns read from shared memory for every
 // head took 252).  Two rows in flight and six CTAs of 128 threads per SM: four rows 92, eight CTAs 110 (their
-// registers spill), loads ahead of the rows at hand 99.  4 single tokens: 3.4 us, the
+// registers spill), loads ahead of the rows at hand 99.  4 single tokens: 3.5 us, the
 // chain of dependent loads (lengths, page, row).
 #include <algorithm>
 
@@ -305,8 +305,8 @@ int launch(const AppendArgs& a, cudaStream_t stream) {
   const bool narrow = a.c.head_dim <= 64;
   const int groups = QA_T / (narrow ? 4 : 8);
   // tokens of a CTA: as many as give every lane several heads to keep its factors for,
-  // fewer where the GPU would not fill (152 SMs of 4 CTAs each), down to one whose heads
-  // are shared out
+  // fewer where there would be less than 608 CTAs (four for each of 152 SMs, which hold six),
+  // down to one whose heads are shared out
   int tokens = QA_MAX_TOKENS;
   while (tokens > 1 && (a.T + tokens - 1) / tokens < 608) tokens /= 2;
   const int64_t tiles = (a.T + tokens - 1) / tokens;
