@@ -159,8 +159,8 @@ def _scale_of(a, code):
     """The least power of two s >= 2^-126 with a <= the largest code times s."""
     top, e = MANT[code]
     mant, exp = torch.frexp(a)
-    exp = torch.where(a > 0, exp - e + (mant > top).int(), -126).clamp(min=-126)
-    return torch.ldexp(torch.ones_like(a), exp)
+    exp = torch.where(a > 0, exp - e + (mant > top).int(), -126).clamp(min=-126).int()
+    return ((exp + 127) << 23).view(torch.float32)     # ldexp goes by pow, which may round
 
 
 def _to_code(x, code):
@@ -523,7 +523,8 @@ def _exact_power(a, code):
     """The least power of two with a <= the largest code times it."""
     mant, exp = torch.frexp(a / QMAX[code])             # a / 448 = 2^-7 is exact, its log2 is not
     exp = torch.where(mant > 0.5, exp, exp - 1)
-    return torch.where(a > 0, torch.ldexp(torch.ones_like(a), exp.clamp(min=-126)), 2.0 ** -126)
+    exp = torch.where(a > 0, exp, -126).clamp(min=-126).long()
+    return ((exp + 1023) << 52).view(torch.float64)
 
 
 def _exact_blocks(s, case, b, cache, scale, y, codes, scales):
