@@ -551,6 +551,137 @@ int sls_attention_decode(const sls_rows_t* q, int q_heads, const sls_kv_cache_t*
 int sls_attention_status(void* stream);
 
 /*
+ * ---------------------------------------------------------------------------
+ * The same cache made smaller: 8 bits an element, and fewer tokens.  (The paper
+ * has no counterpart: it shortens the prompt in front of the cache, these calls
+ * the cache behind it.)
+ *   sls_qkv_append_q8          sls_qkv_append into a cache of 8-bit codes
+ *   sls_attention_prefill_q8   sls_attention_prefill over it
+ *   sls_attention_decode_q8    sls_attention_decode over it
+ *   sls_attention_weights      adds the softmax weights that queries place on
+ *                              the cached tokens to a running sum
+ *   sls_cache_evict            keeps each sequence's heaviest tokens
+ *
+ * A cache of codes is an sls_kv_cache_t whose dtype is SLS_I8 (codes -127..127)
+ * or SLS_E4M3 (at most 448; no infinities), with a float32 scale for each block
+ * of `block` consecutive slots of a page and key head, for keys and for values:
+ * an element stands for code * scale.  head_dim is then a multiple of 16, and
+ * strides (in elements) are multiples of 16.  Lengths, page tables, page numbers
+ * outside the cache and slots that no length covers are as above.
+ * ---------------------------------------------------------------------------
+ */
+#define SLS_I8 3               /* 8-bit integers */
+#define SLS_E4M3 4             /* 4 bits of exponent, 3 of mantissa */
+
+typedef struct sls_kv_scales {
+  float* k;                  /* num_pages x (page_size / block) x kv_heads     */
+  float* v;                  /* the same layout and strides                    */
+  int block;                 /* 16, 32, 64 or 128, at most page_size           */
+  int64_t page_stride;       /* strides in floats, positive                    */
+  int64_t block_stride;
+  int64_t head_stride;
+} sls_kv_scales_t;
+
+/* A float for every slot and key head of a cache; a head's page_size floats are
+ * contiguous, strides (in floats) multiples of 4, the base 16-byte aligned. */
+typedef struct sls_kv_weights {
+  float* data;               /* num_pages x kv_heads x page_size               */
+  int64_t page_stride;
+  int64_t head_stride;
+} sls_kv_weights_t;
+
+/*
+ * sls_qkv_append whose keys (y, as there) and values go to a cache of codes.  q, k, v,
+ * q_out and the weights are of `dtype` (SLS_BF16 or SLS_F16).  For every block
+ * of slots and key head that takes new tokens, in float32:
+ *   a  = largest |y| of the new tokens' finite elements
+ *   s' = max(s, 2^e), 2^e the least power of two >= 2^-126 with a <= Q 2^e,
+ *        Q = 127 or 448; s the block's scale if it holds earlier tokens of the
+ *        sequence, else 0
+ *   codes round(y / s') (to nearest even), infinities as +-Q, NaN as NaN (E4M3)
+ *   or 0 (I8); where s' > s the earlier tokens' codes c become round(c s / s').
+ * So the scales that this call makes are powers of two.  Slots of the block past
+ * the sequence's end are left as they are.  Two sequences must not append to the
+ * same block.  Errors: as sls_qkv_append, and INVALID_ARG / UNSUPPORTED for
+ * scales (NULL, strides; block).
+ */
+int sls_qkv_append_q8(const sls_rows_t* q, const sls_rows_t* k, const sls_rows_t* v, int64_t T,
+                      int q_heads, const sls_kv_cache_t* cache, const sls_kv_scales_t* scales,
+                      int dtype, const int32_t* cu_seqlens, const int32_t* positions,
+                      const void* q_weight, const void* k_weight, float eps,
+                      const sls_rope_t* rope, const sls_rows_t* q_out, void* stream);
+
+/*
+ * sls_attention_prefill over a cache of codes; q and out are of `dtype`.  The
+ * codes of the sequences' pages are written out in `dtype` first (exactly where
+ * scales are powers of two and the value is in its range, else rounded once; float16 cut to
+ * +-65504), into the workspace: 4 bytes an element of as many pages as the page
+ * table, or the cache, has (the smaller), and that of sls_attention_prefill.
+ */
+size_t sls_attention_prefill_q8_workspace_size(int64_t T, int q_heads,
+                                               const sls_kv_cache_t* cache,
+                                               const sls_kv_scales_t* scales, int dtype);
+int sls_attention_prefill_q8(const sls_rows_t* q, int64_t T, int q_heads,
+                             const sls_kv_cache_t* cache, const sls_kv_scales_t* scales,
+                             int dtype, const int32_t* cu_seqlens, int causal, float scale,
+                             const sls_rows_t* out, void* workspace, size_t workspace_bytes,
+                             void* stream);
+
+/*
+ * sls_attention_decode over a cache of codes; q and out are of `dtype`.
+ */
+size_t sls_attention_decode_q8_workspace_size(int q_heads, const sls_kv_cache_t* cache,
+                                              const sls_kv_scales_t* scales, int dtype);
+int sls_attention_decode_q8(const sls_rows_t* q, int q_heads, const sls_kv_cache_t* cache,
+                            const sls_kv_scales_t* scales, int dtype, float scale,
+                            const sls_rows_t* out, void* workspace, size_t workspace_bytes,
+                            void* stream);
+
+/*
+ * Accumulated attention weights: for every sequence, key head h and cache index j
+ *   weights[j, h] += sum over the packed rows i and the query heads g of h of
+ *                    softmax_j(scale q_ig . k_jh)
+ * with the rows and the mask of sls_attention_prefill (cu_seqlens NULL: one token
+ * per sequence).  Reads the keys only; cache->v may be NULL.  scales: NULL for a
+ * 16-bit cache, whose dtype is `dtype`, the queries'.  Sums are float32, in a
+ * fixed order.  A page must belong to one sequence; weights of a page outside
+ * the cache are dropped.  A row whose scores are not finite leaves NaN in the
+ * sums of the tokens that it sees.
+ * Errors: as sls_attention_prefill, and INVALID_ARG for weights.
+ */
+size_t sls_attention_weights_workspace_size(int64_t T, int q_heads, const sls_kv_cache_t* cache,
+                                            const sls_kv_scales_t* scales, int dtype);
+int sls_attention_weights(const sls_rows_t* q, int64_t T, int q_heads,
+                          const sls_kv_cache_t* cache, const sls_kv_scales_t* scales, int dtype,
+                          const int32_t* cu_seqlens, int causal, float scale,
+                          const sls_kv_weights_t* weights, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/*
+ * Eviction.  Every sequence of more than `keep` tokens is cut to `keep`, for each
+ * key head on its own: the first `first` and the last `last` tokens stay, and of
+ * the others those of the largest weights (equal ones: the lowest index; NaN
+ * counts as less than any number).  What stays moves to indices 0 .. keep - 1 in its
+ * order: keys, values and weights.  Weights of the indices past them become 0,
+ * keys and values there are left as they are, kv_lens (that of `cache`, which is
+ * written) becomes keep.  In a cache of codes a block takes the largest of the scales
+ * that its tokens come from, s', and their codes become round(c s / s').
+ * kept: B x kv_heads x keep int32, the indices that stayed, ascending; of a
+ * shorter sequence, which is left alone, all of its own and then -1.
+ * Rotated keys keep their angles: give sls_qkv_append the positions of later
+ * tokens, which kv_lens no longer tells.  A page must belong to one sequence.  A
+ * page outside the cache reads as zeros (weights too) and is not written.
+ * scales: NULL for a 16-bit cache.  0 <= first, 0 <= last, first + last <= keep.
+ * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, as above.
+ */
+size_t sls_cache_evict_workspace_size(const sls_kv_cache_t* cache, const sls_kv_scales_t* scales,
+                                      int64_t keep);
+int sls_cache_evict(const sls_kv_cache_t* cache, const sls_kv_scales_t* scales,
+                    const sls_kv_weights_t* weights, int64_t keep, int64_t first, int64_t last,
+                    int32_t* kept, int32_t* kv_lens, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/*
  * Optional per-phase timing of sls_compress.  `events` is a host array of
  * 2 * SLS_NUM_PHASES cudaEvent_t handles (passed as void*) owned by the
  * caller; while set, every sls_compress call records events[2p] on its

@@ -10,7 +10,8 @@ The same names as the C entry points are exported:
 ``feature_map``, ``lanczos_topr``, ``simhash``, ``aggregate``, ``compress``,
 ``embed_gather``, ``compress_tokens``; the attention calls behind the pass
 (``qkv_append``, ``attention_prefill``, ``attention_decode``) are in
-``attention.py``.
+``attention.py``, those over a cache of 8-bit codes and eviction from a cache in
+``small_cache.py``.
 """
 from __future__ import annotations
 
@@ -599,6 +600,9 @@ def workspace_status(workspace: Workspace) -> int:
 
 from . import attention as _attention  # noqa: E402  (needs the names above)
 from .attention import *  # noqa: E402,F401,F403
+from . import small_cache as _small_cache  # noqa: E402
+from .small_cache import *  # noqa: E402,F401,F403
 
-EXPORTED.update(_attention.EXPORTED)
-__all__ += _attention.__all__
+for _part in (_attention, _small_cache):
+    EXPORTED.update(_part.EXPORTED)
+    __all__ += _part.__all__

@@ -121,12 +121,14 @@ def _ints(name: str, t: torch.Tensor, n: int, dev: int) -> int:
     return t.data_ptr()
 
 
-def _cache(cache_k, cache_v, page_table, kv_lens):
-    """(packed sls_kv_cache_t, shape, dtype, device index, batch, page table columns)"""
+def _cache(cache_k, cache_v, page_table, kv_lens, codes=_CODES):
+    """(packed sls_kv_cache_t, shape, dtype, device index, batch, page table columns); codes:
+    the element types that the call takes"""
     dt, shape, dev = cache_k.dtype, cache_k.shape, cache_k.get_device()
-    code = _CODES.get(dt)
+    code = codes.get(dt)
     if code is None:
-        raise TypeError(f"unsupported attention dtype {dt} (bfloat16 or float16)")
+        raise TypeError(f"unsupported attention dtype {dt} "
+                        f"({' or '.join(str(x)[6:] for x in codes)})")
     strides = cache_k.stride()
     if dev < 0 or len(shape) != 4 or cache_v.shape != shape or cache_v.dtype != dt \
             or cache_v.get_device() != dev or strides[3] != 1 or cache_v.stride() != strides:
