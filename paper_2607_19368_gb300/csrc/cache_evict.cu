@@ -1,10 +1,10 @@
 // Eviction: of every (sequence, key head) the first and last tokens and the heaviest others
 // stay, in order, and move to the front of the sequence's pages.
 //
-// Two launches.  The first selects: the weight that the last of the kept others has is found
-// digit by digit (counts of 2048, 2048 and 1024 digits of the weights as ordered integers), then
-// the tokens are gone through once in order, which gives every kept one its place; weights move
-// here.  The second moves keys and values.  A place is never behind its source, so a cluster of
+// Two launches.  The first selects: a cluster holds a sequence's weights in registers, finds
+// that of the last of the kept others digit by digit (counts of 2048, 2048 and 1024 digits of the
+// weights as ordered integers, summed through distributed shared memory), and counts what stays in
+// front of every token, which gives it its place; weights move here.  The second moves keys and values.  A place is never behind its source, so a cluster of
 // CTAs takes the places in waves, in order: what a wave reads lies at or behind its first place,
 // what earlier waves wrote lies in front of it, and the one barrier between a wave's reads and its
 // writes is all that moving in place needs.  Bound by the bytes of weights and moved rows.
@@ -18,8 +18,8 @@ namespace {
 
 constexpr int EV_T = 1024;    // selection
 constexpr int EV_BINS = 2048;
+constexpr int EV_V = 8;       // groups of four weights that a thread of the selection holds
 constexpr int EV_MOVE_T = 256;
-constexpr int EV_ROWS = 128;  // rows of a CTA's wave: whole blocks of codes
 constexpr int EV_CLUSTER = 8;
 
 // Weights as integers in their order: NaN first, the two zeros equal.
@@ -40,61 +40,69 @@ struct EvSeq {
   }
 };
 
-__global__ void __launch_bounds__(EV_T)
-cache_evict_select_kernel(const __grid_constant__ EvictArgs a, int32_t* lens_before) {
-  __shared__ unsigned s_bins[EV_BINS];
-  __shared__ unsigned s_warp[EV_T / 32][2];
-  __shared__ unsigned s_digit, s_above;
-  const CacheView& c = a.c;
-  const int seq = blockIdx.x / c.kv_heads, h = blockIdx.x - seq * c.kv_heads;
+SLS_DEV void ev_cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// What a CTA of the selection has in shared memory.
+struct EvShared {
+  unsigned bins[2][EV_BINS];
+  unsigned warp[EV_T / 32][2];
+  unsigned part[EV_V * EV_T / 32];  // kept for sure in the low half, equal ones in the high half
+  unsigned total;
+  unsigned digit, above;
+};
+
+// The digit of this pass at which the count from the top reaches `need`, from a thread's two
+// counts n0 (digit b = EV_BINS - 1 - 2 threadIdx.x) and n1 (b - 1).
+SLS_DEV void ev_digit(EvShared& s, unsigned n0, unsigned n1, unsigned need) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  at_go();
-  at_wait_ahead();
-  const int len = (int)cache_len(c, seq);
-  if (h == 0 && threadIdx.x == 0) lens_before[seq] = len;
-  int32_t* kept = a.kept + ((int64_t)seq * c.kv_heads + h) * a.keep;
-  if (len <= a.keep) {
-    for (int i = threadIdx.x; i < a.keep; i += EV_T) kept[i] = i < len ? i : -1;
-    return;
+  const int b = EV_BINS - 1 - 2 * threadIdx.x;
+  unsigned sum = n0 + n1;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const unsigned y = __shfl_up_sync(0xffffffffu, sum, d);
+    if (lane >= d) sum += y;
   }
-  const EvSeq e{a, seq, h};
+  if (lane == 31) s.warp[warp][0] = sum;
+  __syncthreads();
+  unsigned above = lane < warp ? s.warp[lane][0] : 0u;
+  above = __reduce_add_sync(0xffffffffu, above) + sum - n0 - n1;
+  if (above < need && need <= above + n0) s.digit = b, s.above = above;
+  else if (above + n0 < need && need <= above + n0 + n1) s.digit = b - 1, s.above = above + n0;
+  __syncthreads();
+}
+
+SLS_DEV int ev_shift(int pass) { return pass == 0 ? 21 : pass == 1 ? 10 : 0; }
+SLS_DEV uint32_t ev_digits(int pass) { return pass == 2 ? 1023u : 2047u; }
+
+// The selection by one CTA that reads the weights anew for every pass: any length.
+SLS_DEV void ev_select_long(const EvictArgs& a, const EvSeq& e, int len, int32_t* kept, EvShared& s) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int lo = a.first, hi = len - a.last;
   unsigned need = (unsigned)(a.keep - a.first - a.last);
-  // ---- the need-th largest of [lo, hi): its digits from the top, and how many equal it are kept
   uint32_t top = 0, mask = 0;
   for (int pass = 0; pass < 3 && need > 0; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-    const uint32_t digits = pass == 2 ? 1023u : 2047u;
-    for (int i = threadIdx.x; i < EV_BINS; i += EV_T) s_bins[i] = 0;
+    const int shift = ev_shift(pass);
+    const uint32_t digits = ev_digits(pass);
+    unsigned* bins = s.bins[0];
+    for (int i = threadIdx.x; i < EV_BINS; i += EV_T) bins[i] = 0;
     __syncthreads();
     for (int x = lo + threadIdx.x; x < hi; x += EV_T) {
       const float* w = e.weight(x);
       const uint32_t k = ev_key(w ? *w : 0.f);
-      if ((k & mask) == top) atomicAdd(&s_bins[(k >> shift) & digits], 1u);
+      if ((k & mask) == top) atomicAdd(&bins[(k >> shift) & digits], 1u);
     }
     __syncthreads();
-    // the digit at which the count from the top reaches `need`
-    const int b = EV_BINS - 1 - 2 * threadIdx.x;  // this thread's larger digit
-    const unsigned n0 = s_bins[b], n1 = s_bins[b - 1];
-    unsigned sum = n0 + n1;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const unsigned y = __shfl_up_sync(0xffffffffu, sum, d);
-      if (lane >= d) sum += y;
-    }
-    if (lane == 31) s_warp[warp][0] = sum;
-    __syncthreads();
-    unsigned above = sum - n0 - n1;
-    for (int w = 0; w < warp; ++w) above += s_warp[w][0];
-    if (above < need && need <= above + n0) s_digit = b, s_above = above;
-    else if (above + n0 < need && need <= above + n0 + n1) s_digit = b - 1, s_above = above + n0;
-    __syncthreads();
-    top |= s_digit << shift;
+    const int b = EV_BINS - 1 - 2 * threadIdx.x;
+    ev_digit(s, bins[b], bins[b - 1], need);
+    top |= s.digit << shift;
     mask |= digits << shift;
-    need -= s_above;
+    need -= s.above;
     __syncthreads();
   }
-  // ---- in order: larger ones and the first `need` equal ones stay
+  // in order: larger ones and the first `need` equal ones stay
   unsigned base_more = 0, base_same = 0;
   for (int x0 = 0; x0 < len; x0 += EV_T) {
     const int x = x0 + threadIdx.x;
@@ -108,18 +116,16 @@ cache_evict_select_kernel(const __grid_constant__ EvictArgs a, int32_t* lens_bef
       same = !more && mask != 0 && k == top;
     }
     const unsigned bm = __ballot_sync(0xffffffffu, more), bs = __ballot_sync(0xffffffffu, same);
-    if (lane == 0) s_warp[warp][0] = __popc(bm), s_warp[warp][1] = __popc(bs);
+    if (lane == 0) s.warp[warp][0] = __popc(bm), s.warp[warp][1] = __popc(bs);
     __syncthreads();  // the tile's weights are read, too
     const unsigned low = (1u << lane) - 1;
-    unsigned m = base_more + __popc(bm & low), s = base_same + __popc(bs & low);
-    unsigned all_m = 0, all_s = 0;
+    unsigned m = base_more + __popc(bm & low), q = base_same + __popc(bs & low);
     for (int v = 0; v < EV_T / 32; ++v) {
-      if (v < warp) m += s_warp[v][0], s += s_warp[v][1];
-      all_m += s_warp[v][0], all_s += s_warp[v][1];
+      if (v < warp) m += s.warp[v][0], q += s.warp[v][1];
+      base_more += s.warp[v][0], base_same += s.warp[v][1];
     }
-    base_more += all_m, base_same += all_s;
-    if (more || (same && s < need)) {
-      const unsigned to = m + min(s, need);
+    if (more || (same && q < need)) {
+      const unsigned to = m + min(q, need);
       kept[to] = x;
       if (to != (unsigned)x)
         if (float* p = e.weight(to)) *p = w;
@@ -130,28 +136,193 @@ cache_evict_select_kernel(const __grid_constant__ EvictArgs a, int32_t* lens_bef
     if (float* p = e.weight(x)) *p = 0.f;
 }
 
-SLS_DEV void ev_cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-
-// C: I8 or E4M3, or void for 16-bit elements
-template <typename C>
-__global__ void __launch_bounds__(EV_MOVE_T)
-cache_evict_move_kernel(const __grid_constant__ EvictArgs a, const int32_t* lens_before) {
-  constexpr bool CODES = !std::is_void<C>::value;
-  // vectors of 16 bytes of a thread: 128 rows of up to 256 (128) bytes
-  constexpr int V = EV_ROWS * SLS_MAX_HEAD_DIM * (CODES ? 1 : 2) / 16 / EV_MOVE_T;
-  __shared__ float s_was[EV_ROWS];
+__global__ void __launch_bounds__(EV_T)
+cache_evict_select_kernel(const __grid_constant__ EvictArgs a, int32_t* lens_before) {
+  __shared__ EvShared s;
   const CacheView& c = a.c;
   uint32_t rank, size;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(size));
   const int unit = blockIdx.x / size;
-  const int heads = 2 * c.kv_heads;
+  const int seq = unit / c.kv_heads, h = unit - seq * c.kv_heads;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (int i = threadIdx.x; i < 2 * EV_BINS; i += EV_T) s.bins[0][i] = 0;
+  at_go();
+  at_wait_ahead();
+  const int len = (int)cache_len(c, seq);
+  if (h == 0 && rank == 0 && threadIdx.x == 0) lens_before[seq] = len;
+  int32_t* kept = a.kept + ((int64_t)seq * c.kv_heads + h) * a.keep;
+  const EvSeq e{a, seq, h};
+  if (len <= a.keep) {
+    for (int i = rank * EV_T + threadIdx.x; i < a.keep; i += size * EV_T) kept[i] = i < len ? i : -1;
+    return;
+  }
+  if (len > (int64_t)size * EV_T * EV_V * 4) {
+    if (rank == 0) ev_select_long(a, e, len, kept, s);
+    return;
+  }
+  // this CTA's weights, four in a row for each thread at a time
+  const int groups = (len + 3) >> 2, per = (groups + size - 1) / size;
+  const int g0 = min(groups, (int)rank * per), mine = min(groups, g0 + per) - g0;
+  float w[EV_V][4];
+#pragma unroll
+  for (int v = 0; v < EV_V; ++v) {
+    const int g = v * EV_T + threadIdx.x;
+    float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (g < mine) {
+      const float* p = e.weight(4 * (int64_t)(g0 + g));
+      if (p) f = *reinterpret_cast<const float4*>(p);
+    }
+    w[v][0] = f.x, w[v][1] = f.y, w[v][2] = f.z, w[v][3] = f.w;
+  }
+  const int lo = a.first, hi = len - a.last;
+  unsigned need = (unsigned)(a.keep - a.first - a.last);
+  uint32_t top = 0, mask = 0;
+  __syncthreads();
+  for (int pass = 0; pass < 3 && need > 0; ++pass) {
+    const int shift = ev_shift(pass);
+    const uint32_t digits = ev_digits(pass);
+    unsigned* bins = s.bins[pass & 1];
+#pragma unroll
+    for (int v = 0; v < EV_V; ++v) {
+      if (v * EV_T >= mine) break;
+      const int x = 4 * (g0 + v * EV_T + (int)threadIdx.x);
+      if (v * EV_T + (int)threadIdx.x >= mine) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t k = ev_key(w[v][i]);
+        if (x + i >= lo && x + i < hi && (k & mask) == top)
+          atomicAdd(&bins[(k >> shift) & digits], 1u);
+      }
+    }
+    ev_cluster_sync();
+    // of all CTAs of the cluster
+    const int b = EV_BINS - 1 - 2 * threadIdx.x;
+    unsigned n[EV_CLUSTER][2];
+#pragma unroll
+    for (uint32_t r = 0; r < EV_CLUSTER; ++r) {
+      n[r][0] = n[r][1] = 0;
+      if (r >= size) continue;
+      uint32_t at;
+      asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(&bins[b - 1])), "r"(r));
+      asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];"
+                   : "=r"(n[r][1]), "=r"(n[r][0])
+                   : "r"(at)
+                   : "memory");
+    }
+    unsigned n0 = 0, n1 = 0;
+#pragma unroll
+    for (uint32_t r = 0; r < EV_CLUSTER; ++r) n0 += n[r][0], n1 += n[r][1];
+    // nobody reads the first pass's counts any more when the second pass's are complete
+    if (pass == 1)
+      for (int i = threadIdx.x; i < EV_BINS; i += EV_T) s.bins[0][i] = 0;
+    ev_digit(s, n0, n1, need);
+    top |= s.digit << shift;
+    mask |= digits << shift;
+    need -= s.above;
+    __syncthreads();
+  }
+  // ---- places: larger ones and the first `need` equal ones stay, in order
+  auto kind = [&](int x, float f) {  // 1: stays, 1 << 16: equal to the last one, 0: goes
+    const uint32_t k = ev_key(f);
+    if (x >= len) return 0u;
+    if (x < lo || x >= hi || (mask != 0 && k > top)) return 1u;
+    return mask != 0 && k == top ? 1u << 16 : 0u;
+  };
+  unsigned before[EV_V];
+#pragma unroll
+  for (int v = 0; v < EV_V; ++v) {
+    before[v] = 0;
+    if (v * EV_T >= mine) break;
+    const int g = v * EV_T + threadIdx.x, x = 4 * (g0 + g);
+    unsigned n = 0;
+    if (g < mine) n = kind(x, w[v][0]) + kind(x + 1, w[v][1]) + kind(x + 2, w[v][2]) + kind(x + 3, w[v][3]);
+    unsigned sum = n;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const unsigned y = __shfl_up_sync(0xffffffffu, sum, d);
+      if (lane >= d) sum += y;
+    }
+    if (lane == 31) s.part[v * (EV_T / 32) + warp] = sum;
+    before[v] = sum - n;
+  }
+  __syncthreads();
+  if (warp == 0) {
+    // counts before every warp's share of every v, in order; up to 2^15 of either kind a CTA
+    const int parts = (min(EV_V, (mine + EV_T - 1) / EV_T)) * (EV_T / 32);
+    unsigned base = 0;
+    for (int i = lane; i - lane < parts; i += 32) {
+      const unsigned n = i < parts ? s.part[i] : 0u;
+      unsigned sum = n;
+#pragma unroll
+      for (int d = 1; d < 32; d <<= 1) {
+        const unsigned y = __shfl_up_sync(0xffffffffu, sum, d);
+        if (lane >= d) sum += y;
+      }
+      if (i < parts) s.part[i] = base + sum - n;
+      base += __shfl_sync(0xffffffffu, sum, 31);
+    }
+    if (lane == 0) s.total = base;
+  }
+  ev_cluster_sync();  // all weights of the sequence are in registers, all totals known
+  unsigned more0 = 0, same0 = 0;
+  for (uint32_t r = 0; r < rank; ++r) {
+    uint32_t at;
+    unsigned x;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(&s.total)), "r"(r));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+    more0 += x & 0xffffu, same0 += x >> 16;
+  }
+#pragma unroll
+  for (int v = 0; v < EV_V; ++v) {
+    if (v * EV_T >= mine) break;
+    const int g = v * EV_T + threadIdx.x;
+    if (g >= mine) continue;
+    const unsigned base = before[v] + s.part[v * (EV_T / 32) + warp];
+    unsigned more = more0 + (base & 0xffffu), same = same0 + (base >> 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int x = 4 * (g0 + g) + i;
+      const unsigned k = kind(x, w[v][i]);
+      if (k == 1 || (k > 1 && same < need)) {
+        const unsigned to = more + min(same, need);
+        kept[to] = x;
+        if (to != (unsigned)x)
+          if (float* p = e.weight(to)) *p = w[v][i];
+      }
+      more += k & 1, same += k >> 16;
+    }
+  }
+  for (int x = a.keep + (int)(rank * EV_T + threadIdx.x); x < len; x += size * EV_T)
+    if (float* p = e.weight(x)) *p = 0.f;
+  ev_cluster_sync();  // no CTA leaves while another reads its shared memory
+}
+
+// C: I8 or E4M3, or void for 16-bit elements; BOTH: a cluster moves keys and values, which
+// share their places, else one of them.
+template <typename C, bool BOTH>
+struct EvMove {
+  static constexpr bool CODES = !std::is_void<C>::value;
+  static constexpr int ROWS = CODES || !BOTH ? 128 : 64;  // of a CTA's wave: whole blocks of codes
+  static constexpr int MATS = BOTH ? 2 : 1;
+  // vectors of 16 bytes of a thread for each of them
+  static constexpr int V = ROWS * SLS_MAX_HEAD_DIM * (CODES ? 1 : 2) / 16 / EV_MOVE_T;
+};
+
+template <typename C, bool BOTH>
+__global__ void __launch_bounds__(EV_MOVE_T, 3)
+cache_evict_move_kernel(const __grid_constant__ EvictArgs a, const int32_t* lens_before) {
+  using S = EvMove<C, BOTH>;
+  __shared__ int64_t s_from[S::ROWS], s_to[S::ROWS];  // byte offsets of rows, or -1
+  __shared__ float s_was[S::MATS][S::ROWS];
+  const CacheView& c = a.c;
+  uint32_t rank, size;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(size));
+  const int unit = blockIdx.x / size;
+  const int heads = BOTH ? c.kv_heads : 2 * c.kv_heads;
   const int seq = unit / heads, hk = unit - seq * heads;
-  const bool keys = hk < c.kv_heads;
-  const int h = keys ? hk : hk - c.kv_heads;
+  const int h = hk % c.kv_heads;
   at_go();
   at_wait_ahead();
   const int len = lens_before[seq];
@@ -159,66 +330,86 @@ cache_evict_move_kernel(const __grid_constant__ EvictArgs a, const int32_t* lens
   if (hk == 0 && rank == 0 && threadIdx.x == 0) a.lens[seq] = a.keep;
   const int32_t* kept = a.kept + ((int64_t)seq * c.kv_heads + h) * a.keep;
   const int32_t* table = c.table + seq * c.table_ld;
-  char* data = (keys ? c.k : c.v) + h * c.head_b;
-  float* scale = CODES ? (keys ? a.s.k : a.s.v) + h * a.s.head : nullptr;
-  const int vecs = c.head_dim * (CODES ? 1 : 2) / 16;
+  const bool values = !BOTH && hk >= c.kv_heads;
+  char* const mat[2] = {values ? c.v : c.k, c.v};
+  float* const scale[2] = {(values ? a.s.v : a.s.k) + h * a.s.head, a.s.v + h * a.s.head};
+  const int vecs = c.head_dim * (S::CODES ? 1 : 2) / 16;
   const int slots = (1 << c.page_shift) - 1;
-  auto page_of = [&](int x) {
-    const int64_t p = table[x >> c.page_shift];
-    return p >= 0 && p < c.num_pages ? p : (int64_t)-1;
-  };
-  for (int w0 = 0; w0 < a.keep; w0 += EV_ROWS * (int)size) {
-    const int j0 = w0 + (int)rank * EV_ROWS;
-    const int n = min(EV_ROWS, a.keep - j0);
-    uint4 x[V];
-    if constexpr (CODES) {
-      if (threadIdx.x < EV_ROWS) {
-        float f = 0.f;
-        if ((int)threadIdx.x < n) {
-          const int src = kept[j0 + threadIdx.x];
-          const int64_t p = page_of(src);
-          if (p >= 0) f = scale[p * a.s.page + ((src & slots) >> a.s.shift) * a.s.block];
-        }
-        s_was[threadIdx.x] = f;
-      }
-    }
+  for (int w0 = 0; w0 < a.keep; w0 += S::ROWS * (int)size) {
+    const int j0 = w0 + (int)rank * S::ROWS;
+    const int n = min(S::ROWS, a.keep - j0);
+    if ((int)threadIdx.x < n) {
+      const int to = j0 + threadIdx.x, from = kept[to];
+      const int64_t p = table[from >> c.page_shift], q = table[to >> c.page_shift];
+      const bool real = p >= 0 && p < c.num_pages;
+      s_from[threadIdx.x] = real ? p * c.page_b + (from & slots) * c.slot_b + h * c.head_b : -1;
+      s_to[threadIdx.x] = q >= 0 && q < c.num_pages
+                              ? q * c.page_b + (to & slots) * c.slot_b + h * c.head_b
+                              : -1;
+      if constexpr (S::CODES)
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
+        for (int m = 0; m < S::MATS; ++m)
+          s_was[m][threadIdx.x] =
+              real ? scale[m][p * a.s.page + ((from & slots) >> a.s.shift) * a.s.block] : 0.f;
+    }
+    __syncthreads();
+    uint4 x[S::MATS][S::V];
+#pragma unroll
+    for (int i = 0; i < S::V; ++i) {
       const int at = i * EV_MOVE_T + threadIdx.x, row = at / vecs;
-      x[i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int m = 0; m < S::MATS; ++m) x[m][i] = make_uint4(0, 0, 0, 0);
       if (row >= n) continue;
-      const int src = kept[j0 + row];
-      const int64_t p = page_of(src);
-      if (p >= 0)
-        x[i] = *reinterpret_cast<const uint4*>(data + p * c.page_b + (src & slots) * c.slot_b +
-                                               16 * (at - row * vecs));
+      const int64_t from = s_from[row];
+      if (from >= 0)
+#pragma unroll
+        for (int m = 0; m < S::MATS; ++m)
+          x[m][i] = *reinterpret_cast<const uint4*>(mat[m] + from + 16 * (at - row * vecs));
     }
     ev_cluster_sync();
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
+    for (int i = 0; i < S::V; ++i) {
       const int at = i * EV_MOVE_T + threadIdx.x, row = at / vecs;
       if (row >= n) continue;
-      const int64_t p = page_of(j0 + row);
-      if (p < 0) continue;
-      if constexpr (CODES) {
-        // the largest scale of the place's block
-        const int b0 = row >> a.s.shift << a.s.shift, b1 = min(n, b0 + (1 << a.s.shift));
-        float now = 0.f;
-        for (int k = b0; k < b1; ++k) now = fmaxf(now, s_was[k]);
-        const float was = s_was[row];
-        if (was != now) {
-          float y[16];
-          codes_float<C>(x[i], y);
-          x[i] = to_codes16<C>(y, now > 0.f ? was / now : 0.f);
+      const int64_t to = s_to[row];
+      if (to < 0) continue;
+#pragma unroll
+      for (int m = 0; m < S::MATS; ++m) {
+        if constexpr (S::CODES) {
+          // the largest scale of the place's block
+          const int b0 = row >> a.s.shift << a.s.shift, b1 = min(n, b0 + (1 << a.s.shift));
+          float now = 0.f;
+          for (int k = b0; k < b1; ++k) now = fmaxf(now, s_was[m][k]);
+          const float was = s_was[m][row];
+          if (was != now) {
+            float y[16];
+            codes_float<C>(x[m][i], y);
+            x[m][i] = to_codes16<C>(y, now > 0.f ? was / now : 0.f);
+          }
+          if (row == b0 && at == row * vecs) {
+            const int64_t q = table[(j0 + row) >> c.page_shift];
+            scale[m][q * a.s.page + (((j0 + row) & slots) >> a.s.shift) * a.s.block] = now;
+          }
         }
-        if (row == b0 && at == row * vecs)
-          scale[p * a.s.page + (((j0 + row) & slots) >> a.s.shift) * a.s.block] = now;
+        *reinterpret_cast<uint4*>(mat[m] + to + 16 * (at - row * vecs)) = x[m][i];
       }
-      *reinterpret_cast<uint4*>(data + p * c.page_b + ((j0 + row) & slots) * c.slot_b +
-                                16 * (at - row * vecs)) = x[i];
     }
-    if constexpr (CODES) __syncthreads();
+    __syncthreads();
   }
+}
+
+template <typename C>
+int launch_move(const EvictArgs& a, int sms, const int32_t* lens, cudaStream_t stream) {
+  const CacheView& c = a.c;
+  // keys and values by one cluster where there are clusters enough without
+  const int64_t units = (int64_t)c.B * c.kv_heads;
+  const bool both = units * EV_CLUSTER >= 2 * sms;
+  const int rows = both ? EvMove<C, true>::ROWS : EvMove<C, false>::ROWS;
+  int cluster = 1;  // no more CTAs than waves have rows for
+  while (cluster < EV_CLUSTER && cluster * rows < a.keep) cluster *= 2;
+  const dim3 grid((unsigned)(units * (both ? 1 : 2) * cluster));
+  return at_launch(both ? cache_evict_move_kernel<C, true> : cache_evict_move_kernel<C, false>,
+                   grid, EV_MOVE_T, 0, cluster, stream, a, lens);
 }
 
 }  // namespace
@@ -231,18 +422,23 @@ int launch_cache_evict(const EvictArgs& a, int code, void* workspace, cudaStream
   const CacheView& c = a.c;
   if (c.B == 0) return SLS_OK;
   if ((int64_t)c.B * c.kv_heads * 2 * EV_CLUSTER > 0x7fffffff) return SLS_ERR_UNSUPPORTED;
+  int dev = 0, sms = 0;
+  SLS_CUDA_TRY(cudaGetDevice(&dev));
+  SLS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   int32_t* lens = (int32_t*)workspace;
-  int st = at_launch(cache_evict_select_kernel, dim3((unsigned)(c.B * c.kv_heads)), EV_T, 0, 1,
+  // CTAs of a selection: as many as share out the GPU, no more than give every thread four weights
+  // of the longest table, and enough to hold it (past 8 x 32768 one CTA reads it anew each pass)
+  const int64_t room = (int64_t)c.max_pages << c.page_shift, units = (int64_t)c.B * c.kv_heads;
+  int size = 1;
+  while (size < EV_CLUSTER && ((units * size * 2 <= sms && size * EV_T * 4 < room) ||
+                               (int64_t)size * EV_T * EV_V * 4 < room))
+    size *= 2;
+  int st = at_launch(cache_evict_select_kernel, dim3((unsigned)(units * size)), EV_T, 0, size,
                      stream, a, lens);
   if (st != SLS_OK) return st;
-  // no more CTAs of a cluster than waves have rows for
-  int cluster = 1;
-  while (cluster < EV_CLUSTER && cluster * EV_ROWS < a.keep) cluster *= 2;
-  const dim3 grid((unsigned)(c.B * c.kv_heads * 2 * cluster));
-  auto kern = code == SLS_I8     ? cache_evict_move_kernel<I8>
-              : code == SLS_E4M3 ? cache_evict_move_kernel<E4M3>
-                                 : cache_evict_move_kernel<void>;
-  return at_launch(kern, grid, EV_MOVE_T, 0, cluster, stream, a, lens);
+  return code == SLS_I8     ? launch_move<I8>(a, sms, lens, stream)
+         : code == SLS_E4M3 ? launch_move<E4M3>(a, sms, lens, stream)
+                            : launch_move<void>(a, sms, lens, stream);
 }
 
 }  // namespace sls
