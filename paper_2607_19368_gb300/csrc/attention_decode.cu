@@ -432,68 +432,8 @@ attention_decode_cluster_kernel(const __grid_constant__ CUtensorMap tmK,
   }
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-  // rows rank, rank + size, ...: the warps of this CTA take the warps of the cluster in
-  // turn, in order, then their sums are joined in order
-  auto peer = [](const void* p, uint32_t cta) {
-    uint32_t x;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(x) : "r"(smem_u32(p)), "r"(cta));
-    return x;
-  };
-  auto ld = [](uint32_t x) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(x) : "memory");
-    return v;
-  };
-  auto ld4 = [](uint32_t x) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-                 : "r"(x)
-                 : "memory");
-    return v;
-  };
-  const int e0 = 4 * lane;
-  for (int rr = rank; rr < rows; rr += size) {
-    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (uint32_t p = 0; p < size; ++p) {
-      // warp `warp` of every CTA's W, CTA by CTA
-      const float pm = ld(peer(&s_m[warp][rr], p)), pl = ld(peer(&s_l[warp][rr], p));
-      const float4 v =
-          e0 < HD ? ld4(peer(out_s + rr * HD + e0, p)) : make_float4(0.f, 0.f, 0.f, 0.f);
-      const float mn = fmaxf(m, pm), base = mn == -INFINITY ? 0.f : mn;
-      const float f = at_exp2((m - base) * cs), g = at_exp2((pm - base) * cs);
-      l = l * f + pl * g;
-      o[0] = o[0] * f + v.x * g, o[1] = o[1] * f + v.y * g;
-      o[2] = o[2] * f + v.z * g, o[3] = o[3] * f + v.w * g;
-      m = mn;
-    }
-    if (lane == 0) s_join[warp][HD] = m, s_join[warp][HD + 1] = l;
-    if (e0 < HD) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s_join[warp][e0 + i] = o[i];
-    }
-    __syncthreads();
-    const int e = 2 * threadIdx.x;
-    if (e < c.head_dim) {
-      float top = -INFINITY;
-#pragma unroll
-      for (int x = 0; x < W; ++x) top = fmaxf(top, s_join[x][HD]);
-      const float base = top == -INFINITY ? 0.f : top;
-      float sum = 0.f, y = 0.f, z = 0.f;
-#pragma unroll
-      for (int x = 0; x < W; ++x) {
-        const float f = at_exp2((s_join[x][HD] - base) * cs);
-        sum += s_join[x][HD + 1] * f;
-        y += s_join[x][e] * f;
-        z += s_join[x][e + 1] * f;
-      }
-      const float inv = n > 0 ? 1.f / sum : 0.f;
-      *reinterpret_cast<uint32_t*>(a.out.data + seq * a.out.token_b +
-                                   (head0 + rr) * a.out.head_b + 2 * e) =
-          Half2<E>::narrow(y * inv, z * inv);
-    }
-    __syncthreads();
-  }
+  ad_cluster_join<E, HD, W>(a, seq, head0, rows, n, rank, size, cs, s_m[0], s_l[0], AD_ROWS, out_s,
+                            s_join);
   // no CTA leaves while another reads its shared memory
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
