@@ -288,7 +288,8 @@ attention_decode_kernel(const __grid_constant__ CUtensorMap tmK,
   at_wait_ahead();
   if (lane < S::STAGES) mbar_init(&full_bar[warp][lane], 1);
   mbar_fence_init();
-  const int R = ad_prefix<AD_T>(c, s_pre, p.prefix);
+  const auto steps = [&](int s) { return ad_steps(c, s); };
+  const int R = ad_prefix<AD_T>(c, s_pre, p.prefix, steps);
   const int64_t total = s_pre[AD_T];
   const int parts = ad_parts(total, p.groups);
   const int gw = blockIdx.x * S::WARPS + warp;
@@ -303,7 +304,7 @@ attention_decode_kernel(const __grid_constant__ CUtensorMap tmK,
 
   int seq;
   int64_t before;  // steps before seq
-  ad_find<AD_T>(c, s_pre, R, t0, seq, before);
+  ad_find<AD_T>(s_pre, R, t0, steps, seq, before);
 
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);

@@ -36,15 +36,15 @@ SLS_DEV int ad_parts(int64_t total, int groups) {
 }
 
 // Steps before every chunk of R sequences, for the CTA's T threads: s_pre[i] those before
-// chunk i, s_pre[T] all.  CTA 0 writes those before every sequence to `prefix`, if given.
-// Returns R.
-template <int T, int KEYS = AD_KEYS>
-SLS_DEV int ad_prefix(const CacheView& c, int64_t* s_pre, int64_t* prefix) {
+// chunk i, s_pre[T] all; steps(s): those of sequence s.  CTA 0 writes those before every sequence
+// to `prefix`, if given.  Returns R.
+template <int T, typename F>
+SLS_DEV int ad_prefix(const CacheView& c, int64_t* s_pre, int64_t* prefix, const F& steps) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int R = (c.B + T - 1) / T;
   int64_t mine = 0;
   const int s0 = min(c.B, (int)threadIdx.x * R), s1 = min(c.B, s0 + R);
-  for (int s = s0; s < s1; ++s) mine += ad_steps<KEYS>(c, s);
+  for (int s = s0; s < s1; ++s) mine += steps(s);
   int64_t pre = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -61,7 +61,7 @@ SLS_DEV int ad_prefix(const CacheView& c, int64_t* s_pre, int64_t* prefix) {
     int64_t at = pre - mine;
     for (int s = s0; s < s1; ++s) {
       prefix[s] = at;
-      at += ad_steps<KEYS>(c, s);
+      at += steps(s);
     }
     if (threadIdx.x == T - 1) prefix[c.B] = pre;
   }
@@ -70,8 +70,8 @@ SLS_DEV int ad_prefix(const CacheView& c, int64_t* s_pre, int64_t* prefix) {
 }
 
 // The sequence of step t0 (below the total), and the steps before it.
-template <int T, int KEYS = AD_KEYS>
-SLS_DEV void ad_find(const CacheView& c, const int64_t* s_pre, int R, int64_t t0, int& seq,
+template <int T, typename F>
+SLS_DEV void ad_find(const int64_t* s_pre, int R, int64_t t0, const F& steps, int& seq,
                      int64_t& before) {
   int lo = 0, hi = T - 1;  // the last chunk that starts at or before t0
   while (lo < hi) {
@@ -82,12 +82,17 @@ SLS_DEV void ad_find(const CacheView& c, const int64_t* s_pre, int R, int64_t t0
   seq = lo * R;
   before = s_pre[lo];
   for (;;) {
-    const int n = ad_steps<KEYS>(c, seq);
+    const int64_t n = steps(seq);
     if (t0 < before + n) break;
     before += n;
     ++seq;
   }
 }
+
+// Token of row j of an operand of sixteen, where a lane reads its fragments by whole 16 bytes:
+// tokens 2 c and 2 c + 1 are 2 c and (2 c ^ 4) + 1 of the cache, so that neither reads of keys (four
+// chunks of two rows) nor of values (two of four) meet a bank twice.
+SLS_DEV int ad_token(int j) { return j ^ (j & 1) << 2; }
 
 template <typename E>
 SLS_DEV void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {

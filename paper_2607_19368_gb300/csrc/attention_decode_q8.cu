@@ -45,9 +45,6 @@ struct Q8Shape {
   }
 };
 
-// Token of row j of sixteen.
-SLS_DEV int q8_token(int j) { return j ^ (j & 1) << 2; }
-
 SLS_DEV uint32_t q8_transpose(uint32_t x) {
   uint32_t y;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
@@ -210,7 +207,7 @@ struct Q8Rows {
   // steps [j0, j1) of a sequence of `len` tokens; cs: scale log2(e)
   SLS_DEV bool run(Q8Ring<HD, NH>& ring, int len, int j0, int j1, float cs) {
     const int lane = threadIdx.x & 31, r = lane >> 2, cq = lane & 3;
-    const int mine = q8_token(r);  // the token of this lane's rows r and (8 more) r + 8
+    const int mine = ad_token(r);  // the token of this lane's rows r and (8 more) r + 8
 #pragma unroll 1
     for (int j = j0; j < j1; ++j) {
       if (!ring.wait()) return false;
@@ -319,7 +316,7 @@ struct Q8Rows {
         uint32_t v[4][S::VB / 4];
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
-          const int key = 16 * mt + q8_token(2 * cq + (y & 1)) + 8 * (y >> 1);
+          const int key = 16 * mt + ad_token(2 * cq + (y & 1)) + 8 * (y >> 1);
           const unsigned char* p = stage + S::MAT_BYTES;
           if constexpr (S::VB == 16) {
             uint4 u = *reinterpret_cast<const uint4*>(p + S::at(key, r));
@@ -380,7 +377,8 @@ attention_decode_q8_kernel(const __grid_constant__ CUtensorMap tmK,
   at_wait_ahead();
   if (lane < S::STAGES) mbar_init(&full_bar[warp][lane], 1);
   mbar_fence_init();
-  const int R = ad_prefix<AD_T>(c, s_pre, p.prefix);
+  const auto steps = [&](int s) { return ad_steps(c, s); };
+  const int R = ad_prefix<AD_T>(c, s_pre, p.prefix, steps);
   const int64_t total = s_pre[AD_T];
   const int parts = ad_parts(total, p.groups);
   const int gw = blockIdx.x * S::WARPS + warp;
@@ -394,7 +392,7 @@ attention_decode_q8_kernel(const __grid_constant__ CUtensorMap tmK,
   const int head0 = kvh * group + row0;
   int seq;
   int64_t before;  // steps before seq
-  ad_find<AD_T>(c, s_pre, R, t0, seq, before);
+  ad_find<AD_T>(s_pre, R, t0, steps, seq, before);
 
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -523,22 +521,6 @@ attention_decode_q8_cluster_kernel(const __grid_constant__ CUtensorMap tmK,
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// K or V of the cache as (element, slot, head, page), boxes of a head's HD bytes and `slots` slots
-// of one head: a page number outside the cache reads as zeros.
-template <int HD>
-bool q8_cache_map(CUtensorMap* map, const CacheView& c, const void* base, int slots) {
-  const EncodeTiledFn fn = at_encode_fn();
-  if (!fn) return false;
-  const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)1 << c.page_shift,
-                              (cuuint64_t)c.kv_heads, (cuuint64_t)c.num_pages};
-  const cuuint64_t strides[3] = {(cuuint64_t)c.slot_b, (cuuint64_t)c.head_b, (cuuint64_t)c.page_b};
-  const cuuint32_t box[4] = {HD, (cuuint32_t)slots, 1, 1}, one[4] = {1, 1, 1, 1};
-  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), dims, strides, box, one,
-            CU_TENSOR_MAP_INTERLEAVE_NONE,
-            HD == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <typename E, typename C, int HD, int NH>
 int launch(const AttnArgs& a, const ScaleView& s, const AdHost& h, void* workspace,
            cudaStream_t stream) {
@@ -564,7 +546,7 @@ int launch(const AttnArgs& a, const ScaleView& s, const AdHost& h, void* workspa
   const CacheView& c = a.c;
   CUtensorMap k, v;
   const int slots = std::min(AD_KEYS, 1 << c.page_shift);
-  if (!q8_cache_map<HD>(&k, c, c.k, slots) || !q8_cache_map<HD>(&v, c, c.v, slots))
+  if (!at_code_map<HD>(&k, c, c.k, slots) || !at_code_map<HD>(&v, c, c.v, slots))
     return SLS_ERR_UNSUPPORTED;
   if (h.cluster > 0)
     return at_launch(cluster, dim3((unsigned)(c.B * h.vheads * h.cluster)), S::THREADS, S::SMEM,

@@ -91,4 +91,20 @@ inline bool at_cache_map(CUtensorMap* map, int dtype, const CacheView& c, const 
   return at_map(map, dtype, 4, base, dims, strides, box);
 }
 
+// K or V of a cache of codes as (element, slot, head, page), boxes of a head's HD bytes and `slots` slots
+// of one head: a page number outside the cache reads as zeros.
+template <int HD>
+bool at_code_map(CUtensorMap* map, const CacheView& c, const void* base, int slots) {
+  const EncodeTiledFn fn = at_encode_fn();
+  if (!fn) return false;
+  const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)1 << c.page_shift,
+                              (cuuint64_t)c.kv_heads, (cuuint64_t)c.num_pages};
+  const cuuint64_t strides[3] = {(cuuint64_t)c.slot_b, (cuuint64_t)c.head_b, (cuuint64_t)c.page_b};
+  const cuuint32_t box[4] = {HD, (cuuint32_t)slots, 1, 1}, one[4] = {1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), dims, strides, box, one,
+            CU_TENSOR_MAP_INTERLEAVE_NONE,
+            HD == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace sls

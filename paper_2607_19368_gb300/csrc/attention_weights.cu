@@ -9,8 +9,8 @@
 // 256 tokens; a small launch joins them; the second pass forms the scores again and sums columns
 // in registers, so that no sum is made by atomics: the same call gives the same bits.
 //
-// Where rows are few (a token for each sequence), the first pass stores its scores, 4 bytes a
-// row and token, and the last one only reads them: less than keys read again.
+// Where rows are few (a token for each sequence) the kernels of attention_weights_few.cu read keys
+// once instead.
 #include <algorithm>
 
 #include "attention_decode.cuh"
@@ -29,9 +29,7 @@ constexpr int AW_BLOCK = 16 * AW_TILES;
 struct AwPlan {
   float2* part;   // (token, query head, unit of the sequence): maximum and sum of its tokens
   float2* stat;   // (token, query head): maximum, one over the sum
-  float* scores;  // (token, query head, cache index), or NULL
   int units;      // of the longest sequence that the table holds
-  int64_t room;   // cache indices of a row of scores
 };
 
 template <typename E, typename KT>
@@ -54,7 +52,7 @@ SLS_DEV void aw_rows(const AttnArgs& a, int seq, int64_t& q0, int64_t& q1) {
 
 // SUM: the second pass
 template <typename E, typename KT, int HD, bool SUM>
-__global__ void __launch_bounds__(AW_T)
+__global__ void __launch_bounds__(AW_T, 2)
 attention_weights_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ ScaleView sc,
                          const __grid_constant__ WeightView wv, const __grid_constant__ AwPlan p) {
   using M = AwMma<E, KT>;
@@ -63,7 +61,8 @@ attention_weights_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
   extern __shared__ __align__(16) unsigned char smem[];
   uint4* s_q = reinterpret_cast<uint4*>(smem);                     // (tile, slice, lane)
   float* s_f = reinterpret_cast<float*>(s_q + AW_TILES * KS * 32);  // a row's factor
-  float2* s_ml = reinterpret_cast<float2*>(s_f + AW_BLOCK);        // (warp, row), or (row) of stat
+  int* s_see = reinterpret_cast<int*>(s_f + AW_BLOCK);              // tokens that a row sees
+  float2* s_ml = reinterpret_cast<float2*>(s_see + AW_BLOCK);      // (warp, row), or (row) of stat
   __shared__ int64_t s_pre[AW_T + 1];
   const CacheView& c = a.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -72,7 +71,8 @@ attention_weights_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
   const float cs = a.scale * 1.4426950408889634f;
 
   at_wait_ahead();
-  const int R = ad_prefix<AW_T, AW_KEYS>(c, s_pre, nullptr);
+  const auto count = [&](int s) { return ad_steps<AW_KEYS>(c, s); };
+  const int R = ad_prefix<AW_T>(c, s_pre, nullptr, count);
   const int64_t total = s_pre[AW_T] * c.kv_heads;
   const int64_t u0 = total * blockIdx.x / gridDim.x, u1 = total * (blockIdx.x + 1) / gridDim.x;
   int64_t staged = -1;  // the rows in shared memory: sequence times key heads plus head
@@ -80,7 +80,7 @@ attention_weights_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
     // units lie by sequence, key head and tokens
     int seq;
     int64_t before;
-    ad_find<AW_T, AW_KEYS>(c, s_pre, R, u / c.kv_heads, seq, before);
+    ad_find<AW_T>(s_pre, R, u / c.kv_heads, count, seq, before);
     const int units = ad_steps<AW_KEYS>(c, seq);
     const int64_t in = u - before * c.kv_heads;
     const int h = (int)(in / units), unit = (int)(in - (int64_t)h * units);
@@ -181,6 +181,8 @@ attention_weights_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
 #pragma unroll
           for (int k = 0; k < KS; ++k) s_q[(tile * KS + k) * 32 + lane] = f[k];
         }
+        for (int i = threadIdx.x; i < 16 * tiles; i += AW_T)
+          s_see[i] = i >= here ? 0 : a.causal ? len - n + (int)((b0 + i) / group) + 1 : len;
         if constexpr (SUM)
           for (int i = threadIdx.x; i < here; i += AW_T) {
             const int64_t tok = (b0 + i) / group;
@@ -211,10 +213,7 @@ attention_weights_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
           }
         }
         // tokens that each of the two rows sees
-        const int64_t row = b0 + 16 * tile + r;
-        const int t0 = (int)(row / group), t1 = (int)((row + 8) / group);
-        const int see0 = row >= rows ? 0 : a.causal ? len - n + t0 + 1 : len;
-        const int see1 = row + 8 >= rows ? 0 : a.causal ? len - n + t1 + 1 : len;
+        const int see0 = s_see[16 * tile + r], see1 = s_see[16 * tile + r + 8];
         bool hide[4][4] = {};
         if (!__all_sync(0xffffffffu, key0 + 32 <= min(see0, see1))) {
 #pragma unroll
@@ -240,18 +239,6 @@ attention_weights_kernel(const __grid_constant__ AttnArgs a, const __grid_consta
             l += __shfl_xor_sync(0xffffffffu, l, 1);
             l += __shfl_xor_sync(0xffffffffu, l, 2);
             if (cq == 0) s_ml[warp * AW_BLOCK + 16 * tile + r + 8 * x] = make_float2(m, l);
-          }
-          if (p.scores) {
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              if (row + 8 * x >= rows) continue;
-              const int t = x ? t1 : t0, g = (int)(row + 8 * x - (int64_t)t * group);
-              float* to = p.scores + ((q0 + t) * a.q_heads + h * group + g) * p.room + key0 + 2 * cq;
-#pragma unroll
-              for (int nb = 0; nb < 4; ++nb)
-                *reinterpret_cast<float2*>(to + 8 * nb) =
-                    make_float2(s[nb][2 * x], s[nb][2 * x + 1]);
-            }
           }
         } else {
           const float2 m0 = s_ml[16 * tile + r], m1 = s_ml[16 * tile + r + 8];
@@ -340,80 +327,25 @@ attention_weights_join_kernel(const __grid_constant__ AttnArgs a, const __grid_c
   if (lane == 0) p.stat[row] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.f / l);
 }
 
-// The last pass over stored scores: a thread for each token of a unit.
-__global__ void __launch_bounds__(AW_T)
-attention_weights_scores_kernel(const __grid_constant__ AttnArgs a,
-                                const __grid_constant__ WeightView wv,
-                                const __grid_constant__ AwPlan p) {
-  __shared__ int64_t s_pre[AW_T + 1];
-  const CacheView& c = a.c;
-  const int group = a.q_heads / c.kv_heads;
-  const float cs = a.scale * 1.4426950408889634f;
-  at_go();
-  at_wait_ahead();
-  const int R = ad_prefix<AW_T, AW_KEYS>(c, s_pre, nullptr);
-  const int64_t total = s_pre[AW_T] * c.kv_heads;
-  for (int64_t u = blockIdx.x; u < total; u += gridDim.x) {
-    int seq;
-    int64_t before;
-    ad_find<AW_T, AW_KEYS>(c, s_pre, R, u / c.kv_heads, seq, before);
-    const int units = ad_steps<AW_KEYS>(c, seq);
-    const int64_t in = u - before * c.kv_heads;
-    const int h = (int)(in / units), unit = (int)(in - (int64_t)h * units);
-    const int x = unit * AW_KEYS + threadIdx.x;
-    if (x >= cache_len(c, seq)) continue;
-    int64_t q0, q1;
-    aw_rows(a, seq, q0, q1);
-    float w = 0.f;
-    for (int64_t t = q0; t < q1; ++t)
-      for (int g = 0; g < group; ++g) {
-        const int64_t row = t * a.q_heads + h * group + g;
-        const float2 m = p.stat[row];
-        const float s = p.scores[row * p.room + x];
-        w += s == -INFINITY ? 0.f : at_exp2((s - m.x) * cs) * m.y;
-      }
-    const int64_t page = c.table[seq * c.table_ld + (x >> c.page_shift)];
-    if (page >= 0 && page < c.num_pages)
-      wv.data[page * wv.page + h * wv.head + (x & ((1 << c.page_shift) - 1))] += w;
-  }
+int aw_units(const CacheView& c) {
+  return (int)((((int64_t)c.max_pages << c.page_shift) + AW_KEYS - 1) / AW_KEYS);
 }
-
-struct AwHost {
-  int64_t room;
-  int units;
-  bool store;
-  size_t part_b, stat_b, score_b;
-};
-
-AwHost aw_host(const CacheView& c, int64_t T, int q_heads, int code) {
-  AwHost h;
-  const int64_t cap = (int64_t)c.max_pages << c.page_shift;
-  h.units = (int)((cap + AW_KEYS - 1) / AW_KEYS);
-  h.room = (int64_t)h.units * AW_KEYS;
-  // a score written and read, for the rows of a sequence on average, against its key read again
-  const int size = code == SLS_I8 || code == SLS_E4M3 ? 1 : 2;
-  h.store = 8 * T * (q_heads / c.kv_heads) <= (int64_t)c.B * c.head_dim * size;
-  h.part_b = sls_align256((size_t)T * q_heads * h.units * 8);
-  h.stat_b = sls_align256((size_t)T * q_heads * 8);
-  h.score_b = h.store ? sls_align256((size_t)T * q_heads * h.room * 4) : 0;
-  return h;
+size_t aw_part_bytes(const CacheView& c, int64_t T, int q_heads) {
+  return sls_align256((size_t)T * q_heads * aw_units(c) * 8);
 }
 
 template <typename E, typename KT, int HD>
-int launch(const AttnArgs& a, const ScaleView& s, const WeightView& w, const AwHost& h,
-           void* workspace, cudaStream_t stream) {
+int launch(const AttnArgs& a, const ScaleView& s, const WeightView& w, void* workspace, cudaStream_t stream) {
   int dev = 0, sms = 0;
   SLS_CUDA_TRY(cudaGetDevice(&dev));
   SLS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   AwPlan p;
+  p.units = aw_units(a.c);
   p.part = (float2*)workspace;
-  p.stat = (float2*)((char*)workspace + h.part_b);
-  p.scores = h.store ? (float*)((char*)workspace + h.part_b + h.stat_b) : nullptr;
-  p.units = h.units;
-  p.room = h.room;
-  const int64_t most = (int64_t)a.c.B * h.units * a.c.kv_heads;
+  p.stat = (float2*)((char*)workspace + aw_part_bytes(a.c, a.T, a.q_heads));
+  const int64_t most = (int64_t)a.c.B * p.units * a.c.kv_heads;
   const unsigned grid = (unsigned)std::min<int64_t>(most, 2 * sms);
-  constexpr size_t rows = (size_t)AW_TILES * (HD / 16) * 512 + AW_BLOCK * 4;
+  constexpr size_t rows = (size_t)AW_TILES * (HD / 16) * 512 + AW_BLOCK * 8;
   constexpr size_t smem1 = rows + AW_WARPS * AW_BLOCK * 8, smem2 = rows + AW_BLOCK * 8;
   auto first = attention_weights_kernel<E, KT, HD, false>;
   auto second = attention_weights_kernel<E, KT, HD, true>;
@@ -426,41 +358,39 @@ int launch(const AttnArgs& a, const ScaleView& s, const WeightView& w, const AwH
   st = at_launch(attention_weights_join_kernel, dim3((unsigned)((all + AW_WARPS - 1) / AW_WARPS)),
                  AW_T, 0, 1, stream, a, p);
   if (st != SLS_OK) return st;
-  if (h.store)
-    return at_launch(attention_weights_scores_kernel,
-                     dim3((unsigned)std::min<int64_t>(most, 8 * sms)), AW_T, 0, 1, stream, a, w, p);
   return at_launch(second, dim3(grid), AW_T, smem2, 1, stream, a, s, w, p);
 }
 
 template <typename E, typename KT>
-int launch(const AttnArgs& a, const ScaleView& s, const WeightView& w, const AwHost& h,
-           void* workspace, cudaStream_t stream) {
-  return a.c.head_dim > 64 ? launch<E, KT, 128>(a, s, w, h, workspace, stream)
-                           : launch<E, KT, 64>(a, s, w, h, workspace, stream);
+int launch(const AttnArgs& a, const ScaleView& s, const WeightView& w, void* workspace, cudaStream_t stream) {
+  return a.c.head_dim > 64 ? launch<E, KT, 128>(a, s, w, workspace, stream)
+                           : launch<E, KT, 64>(a, s, w, workspace, stream);
 }
 
 template <typename E>
-int launch(const AttnArgs& a, const ScaleView& s, const WeightView& w, int code, const AwHost& h,
-           void* workspace, cudaStream_t stream) {
-  return code == SLS_I8     ? launch<E, I8>(a, s, w, h, workspace, stream)
-         : code == SLS_E4M3 ? launch<E, E4M3>(a, s, w, h, workspace, stream)
-                            : launch<E, E>(a, s, w, h, workspace, stream);
+int launch(const AttnArgs& a, const ScaleView& s, const WeightView& w, int code, void* workspace, cudaStream_t stream) {
+  return code == SLS_I8     ? launch<E, I8>(a, s, w, workspace, stream)
+         : code == SLS_E4M3 ? launch<E, E4M3>(a, s, w, workspace, stream)
+                            : launch<E, E>(a, s, w, workspace, stream);
 }
 
 }  // namespace
 
 size_t attention_weights_workspace(const CacheView& c, int64_t T, int q_heads, int code) {
-  const AwHost h = aw_host(c, T, q_heads, code);
-  return h.part_b + h.stat_b + h.score_b;
+  if (c.B == 0 || T == 0 || c.max_pages == 0) return 0;
+  if (attention_weights_few(c, T, q_heads, code))
+    return attention_weights_few_workspace(c, T, q_heads);
+  return aw_part_bytes(c, T, q_heads) + sls_align256((size_t)T * q_heads * 8);
 }
 
 int launch_attention_weights(const AttnArgs& a, const ScaleView& s, const WeightView& w, int code,
                              int dtype, void* workspace, cudaStream_t stream) {
   if (a.c.B == 0 || a.T == 0 || a.c.max_pages == 0) return SLS_OK;
   if (a.T * a.q_heads > (int64_t)0x7fffffff * AW_WARPS) return SLS_ERR_UNSUPPORTED;
-  const AwHost h = aw_host(a.c, a.T, a.q_heads, code);
-  return dtype == SLS_BF16 ? launch<__nv_bfloat16>(a, s, w, code, h, workspace, stream)
-                           : launch<__half>(a, s, w, code, h, workspace, stream);
+  if (attention_weights_few(a.c, a.T, a.q_heads, code))
+    return launch_attention_weights_few(a, s, w, code, dtype, workspace, stream);
+  return dtype == SLS_BF16 ? launch<__nv_bfloat16>(a, s, w, code, workspace, stream)
+                           : launch<__half>(a, s, w, code, workspace, stream);
 }
 
 }  // namespace sls

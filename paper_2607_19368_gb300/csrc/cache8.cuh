@@ -129,6 +129,12 @@ size_t attention_weights_workspace(const CacheView& c, int64_t T, int q_heads, i
 int launch_attention_weights(const AttnArgs& a, const ScaleView& s, const WeightView& w, int code,
                              int dtype, void* workspace, cudaStream_t stream);
 
+// The path for few rows a sequence, and whether it is taken.
+bool attention_weights_few(const CacheView& c, int64_t T, int q_heads, int code);
+size_t attention_weights_few_workspace(const CacheView& c, int64_t T, int q_heads);
+int launch_attention_weights_few(const AttnArgs& a, const ScaleView& s, const WeightView& w,
+                                 int code, int dtype, void* workspace, cudaStream_t stream);
+
 struct EvictArgs {
   CacheView c;
   ScaleView s;
