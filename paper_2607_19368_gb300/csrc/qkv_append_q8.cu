@@ -21,6 +21,9 @@ namespace sls {
 namespace {
 
 constexpr int Q8_T = 256;
+// rows as they come; halves of whole vectors; pairs side by side; halves that split vectors
+enum { Q8_PLAIN, Q8_HALVES, Q8_SIDES, Q8_ODD };
+constexpr int Q8_KEY_CTAS = 608, Q8_VALUE_CTAS = 304;  // at least so many, heads permitting
 constexpr int Q8_FEW = 2;  // new tokens of a block up to which a job is one group's
 
 // Where a packed token goes.
@@ -45,178 +48,330 @@ SLS_DEV Q8Place q8_place(const AppendArgs& a, int s) {
   return Q8Place{s, b, max(b, e), x};
 }
 
-// A lane's sixteen elements of a row of keys or values: normalised and rotated.
-template <typename E, int L>
+// A lane's two vectors of eight elements of a row of keys or values: weighed and rotated, the
+// row's norm left to the factor that makes them codes.  Element e becomes A x_e + B x_e', with e'
+// its partner in the rotation, A = w_e cos and B = -+ w_e' sin: both from a table of the block's
+// tokens, four floats (A, A, B, B) for two elements, the lanes of a row side by side.  Where pairs
+// are halves of whole vectors a lane holds a vector and its partners', else two neighbours.
+template <typename E, int L, int MODE>
 struct Q8Lane {
+  static constexpr int PITCH = 8 * L + (L == 4 ? 4 : 0);  // float4 of a token; rows meet no bank twice
   const AppendArgs& a;
-  const float2* s_turn;  // (slot, element of a lane's pairs, lane): cos and sin times the scale
-  int l;
-  bool on;
+  const float4* s_tab;
+  int l, v0, v1;
+  bool on, turned;  // it has elements; (halves) they are rotated
   unsigned mates;
-  uint4 w[2], wp[2];     // weights of this lane's elements and of their partners
 
-  // Pairs lie so that the lanes of a row read neighbours: a lane's pairs are sixteen in a row, or
-  // eight where a pair is two elements side by side; a few float2 more a slot part the rows.
-  SLS_DEV static int width(const AppendArgs& a) { return a.interleaved ? 8 : 16; }
-  SLS_DEV static int lanes(const AppendArgs& a) {
-    return a.interleaved ? (a.pairs + 7) >> 3 : (a.pairs + 15) >> 4;
+  SLS_DEV Q8Lane(const AppendArgs& args, const float4* tab, int lane, int l_)
+      : a(args), s_tab(tab), l(l_), mates(((1u << L) - 1) << (lane & ~(L - 1))) {
+    const int half = MODE == Q8_HALVES ? a.pairs >> 3 : 0;
+    turned = l < half;
+    v0 = turned ? l : 2 * l;
+    v1 = turned ? l + half : 2 * l + 1;
+    on = v1 < a.c.head_dim >> 3;
   }
 
-  SLS_DEV Q8Lane(const AppendArgs& args, const float2* turns, int lane, int l_)
-      : a(args), s_turn(turns), l(l_), on(16 * l_ < args.c.head_dim),
-        mates(((1u << L) - 1) << (lane & ~(L - 1))) {
-    const E* kw = reinterpret_cast<const E*>(a.k_weight);
-#pragma unroll
-    for (int v = 0; v < 2; ++v) {
-      w[v] = wp[v] = make_uint4(0, 0, 0, 0);
-      if (!kw || !on) continue;
-      const int i0 = 16 * l + 8 * v;
-      w[v] = *reinterpret_cast<const uint4*>(kw + i0);
-      if (!a.interleaved && i0 < 2 * a.pairs) partner(kw, i0, wp[v]);
+  // Element e of token `slot` in the table: A, and B two floats on.
+  SLS_DEV float* entry(float4* tab, int slot, int e) const {
+    int lane = e >> 4, at = e & 15;
+    if (MODE == Q8_HALVES && e < 2 * a.pairs) {
+      const bool low = e < a.pairs;
+      lane = (low ? e : e - a.pairs) >> 3;
+      at = (low ? 0 : 8) + (e & 7);
     }
+    return reinterpret_cast<float*>(tab + slot * PITCH + (at >> 1) * L + lane) + (at & 1);
   }
-
-  // elements i0 .. i0 + 7 of the other half of the rotated part (zeros past it)
-  SLS_DEV void partner(const E* row, int i0, uint4& u) const {
-    const int pairs = a.pairs;
-    if ((pairs & 7) == 0) {
-      u = *reinterpret_cast<const uint4*>(row + (i0 < pairs ? i0 + pairs : i0 - pairs));
-      return;
+  // The table of n tokens from slot `lo` on, the first of them packed row `row` and cache index x.
+  SLS_DEV void enter(float4* tab, int lo, int n, int64_t row, int x) const {
+    const E* w = reinterpret_cast<const E*>(a.k_weight);
+    int width = 8;  // a thread keeps to one pair
+    while (width < a.pairs) width *= 2;
+    const int pr = threadIdx.x & (width - 1);
+    if (pr < a.pairs) {
+      const int e = MODE == Q8_SIDES ? 2 * pr : pr, o = MODE == Q8_SIDES ? e + 1 : pr + a.pairs;
+      const float we = (w ? (float)w[e] : 1.f) * a.rope_scale,
+                  wo = (w ? (float)w[o] : 1.f) * a.rope_scale, f = a.inv_freq[pr];
+      float* to_e = entry(tab, lo, e);
+      float* to_o = entry(tab, lo, o);
+#pragma unroll 1
+      for (int k = threadIdx.x / width; k < n; k += blockDim.x / width) {
+        const float2 cs = turn_fast(a.positions ? a.positions[row + k] : x + k, f);
+        to_e[4 * PITCH * k] = cs.x * we, to_e[4 * PITCH * k + 2] = -cs.y * wo;
+        to_o[4 * PITCH * k] = cs.x * wo, to_o[4 * PITCH * k + 2] = cs.y * we;
+      }
     }
-    uint32_t x[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int i = i0 + e;
-      x[e] = i < 2 * pairs ? reinterpret_cast<const uint16_t*>(row)[i < pairs ? i + pairs : i - pairs]
-                           : 0u;
+    // elements that are not rotated
+#pragma unroll 1
+    for (int e = 2 * a.pairs + (threadIdx.x & 15); e < a.c.head_dim; e += 16) {
+      const float we = w ? (float)w[e] : 1.f;
+#pragma unroll 1
+      for (int k = threadIdx.x >> 4; k < n; k += blockDim.x / 16) {
+        float* to = entry(tab, lo + k, e);
+        to[0] = we, to[2] = 0.f;
+      }
     }
-    u = make_uint4(x[0] | x[1] << 16, x[2] | x[3] << 16, x[4] | x[5] << 16, x[6] | x[7] << 16);
   }
 
   SLS_DEV void load(const char* p, uint4 (&u)[2]) const {
     u[0] = u[1] = make_uint4(0, 0, 0, 0);
     if (!on) return;
-    u[0] = *reinterpret_cast<const uint4*>(p + 32 * l);
-    u[1] = *reinterpret_cast<const uint4*>(p + 32 * l + 16);
+    u[0] = *reinterpret_cast<const uint4*>(p + 16 * v0);
+    u[1] = *reinterpret_cast<const uint4*>(p + 16 * v1);
   }
 
-  // u: the row at p, loaded; y: its elements; returns the largest finite size
-  SLS_DEV float row(const uint4 (&u)[2], const char* p, bool keys, int slot, float (&y)[16]) const {
-    const E* xs = reinterpret_cast<const E*>(p);
-    const int pairs = a.pairs;
-    uint4 up[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-    const bool turned = keys && 16 * l < 2 * pairs;
-    if (turned && !a.interleaved) {
-#pragma unroll
-      for (int v = 0; v < 2; ++v)
-        if (16 * l + 8 * v < 2 * pairs) partner(xs, 16 * l + 8 * v, up[v]);
-    }
-    float z[8];
+  // u: the row at p, loaded; y: its elements without the norm; most: the largest finite size.
+  // KEYS: else as it comes.
+  template <bool KEYS>
+  SLS_DEV float row(const uint4 (&u)[2], const char* p, int slot, float (&y)[16], float& most) const {
+    float norm = 1.f;
 #pragma unroll
     for (int v = 0; v < 2; ++v) {
+      float z[8];
       widen8<E>(u[v], z);
 #pragma unroll
       for (int e = 0; e < 8; ++e) y[8 * v + e] = z[e];
     }
-    float norm = 1.f;
-    const bool weighed = keys && a.k_weight != nullptr;
-    if (weighed) {
-      float s0 = 0.f, s1 = 0.f;
+    if constexpr (KEYS && MODE != Q8_PLAIN) {
+      if (a.k_weight) {
+        f32x2_t s = mul2(pk2(y[0], y[1]), pk2(y[0], y[1]));
 #pragma unroll
-      for (int e = 0; e < 16; e += 2) s0 = __fmaf_rn(y[e], y[e], s0), s1 = __fmaf_rn(y[e + 1], y[e + 1], s1);
-      s0 += s1;
+        for (int e = 2; e < 16; e += 2) s = fma2(pk2(y[e], y[e + 1]), pk2(y[e], y[e + 1]), s);
+        float s0, s1;
+        upk2(s, s0, s1);
+        s0 += s1;
 #pragma unroll
-      for (int o = L / 2; o > 0; o >>= 1) s0 += __shfl_xor_sync(mates, s0, o);
-      norm = rsqrtf(__fmaf_rn(s0, 1.f / (float)a.c.head_dim, a.eps));
-#pragma unroll
-      for (int v = 0; v < 2; ++v) {
-        widen8<E>(w[v], z);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[8 * v + e] *= norm * z[e];
+        for (int o = L / 2; o > 0; o >>= 1) s0 += __shfl_xor_sync(mates, s0, o);
+        norm = rsqrtf(__fmaf_rn(s0, 1.f / (float)a.c.head_dim, a.eps));
       }
-    }
-    if (turned) {
-      const int nl = lanes(a), stride = width(a) * nl + 4;
-      const float2* tt = s_turn + slot * stride;
-      if (a.interleaved) {
+      if (on) {
+        const float4* tab = s_tab + slot * PITCH + l;
+        const int pairs = a.pairs;
+        const E* xs = reinterpret_cast<const E*>(p);
 #pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-          if (8 * l + e / 2 >= pairs) continue;
-          const float2 cs = tt[(e / 2) * nl + l];
-          const float x0 = y[e], x1 = y[e + 1];
-          y[e] = x0 * cs.x - x1 * cs.y;
-          y[e + 1] = x1 * cs.x + x0 * cs.y;
-        }
-      } else {
-#pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          const int i0 = 16 * l + 8 * v;
-          if (i0 >= 2 * pairs) continue;
-          float zw[8];
-          widen8<E>(up[v], z);
-          widen8<E>(wp[v], zw);
-          if ((pairs & 7) == 0) {
-            const bool low = i0 < pairs;
-            const int p0 = low ? i0 : i0 - pairs;
-            const float2* t8 = tt + (p0 & 15) * nl + (p0 >> 4);
-            const float sign = low ? -1.f : 1.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const float2 cs = t8[e * nl];
-              const float x = weighed ? z[e] * (norm * zw[e]) : z[e];
-              y[8 * v + e] = y[8 * v + e] * cs.x + sign * (x * cs.y);
+        for (int e = 0; e < (MODE == Q8_HALVES ? 8 : 16); e += 2) {
+          const float4 f = tab[(e / 2) * L];
+          const f32x2_t x = pk2(y[e], y[e + 1]);
+          f32x2_t r = mul2(x, pk2(f.x, f.y));
+          if constexpr (MODE == Q8_HALVES) {
+            const float4 g = tab[(e / 2 + 4) * L];
+            const f32x2_t z = pk2(y[e + 8], y[e + 9]);
+            f32x2_t q = mul2(z, pk2(g.x, g.y));
+            if (turned) {
+              r = fma2(z, pk2(f.z, f.w), r);
+              q = fma2(x, pk2(g.z, g.w), q);
             }
+            upk2(q, y[e + 8], y[e + 9]);
+          } else if constexpr (MODE == Q8_SIDES) {
+            if (16 * l + e < 2 * pairs) r = fma2(pk2(y[e + 1], y[e]), pk2(f.z, f.w), r);
           } else {
+            // halves that split vectors: partners are read from the row again
+            float z[2];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int i = i0 + e;
-              if (i >= 2 * pairs) continue;
-              const bool low = i < pairs;
-              const int pr = low ? i : i - pairs;
-              const float2 cs = tt[(pr & 15) * nl + (pr >> 4)];
-              const float x = weighed ? z[e] * (norm * zw[e]) : z[e];
-              y[8 * v + e] = y[8 * v + e] * cs.x + (low ? -x : x) * cs.y;
+            for (int k = 0; k < 2; ++k) {
+              const int i = 16 * l + e + k, o = i < pairs ? i + pairs : i - pairs;
+              z[k] = i < 2 * pairs ? (float)xs[o] : 0.f;
             }
+            r = fma2(pk2(z[0], z[1]), pk2(f.z, f.w), r);
           }
+          upk2(r, y[e], y[e + 1]);
         }
       }
     }
-    float most = 0.f;
+    float m = fabsf(y[0]);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float x = fabsf(y[e]);
-      if (x <= 3.402823466e38f) most = fmaxf(most, x);
+    for (int e = 1; e < 16; ++e) m = fmaxf(m, fabsf(y[e]));
+    m *= norm;
+    if (!(m <= 3.402823466e38f)) {  // some element is not finite
+      m = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float x = fabsf(y[e] * norm);
+        if (x <= 3.402823466e38f) m = fmaxf(m, x);
+      }
     }
-    return most;
+    most = fmaxf(most, m);
+    return norm;
+  }
+
+  // This lane's codes of the row at d.
+  SLS_DEV void store(char* d, const uint4& c) const {
+    if (MODE == Q8_HALVES) {
+      *reinterpret_cast<uint2*>(d + 8 * v0) = make_uint2(c.x, c.y);
+      *reinterpret_cast<uint2*>(d + 8 * v1) = make_uint2(c.z, c.w);
+    } else {
+      *reinterpret_cast<uint4*>(d + 16 * l) = c;
+    }
+  }
+  SLS_DEV uint4 codes(const char* d) const {
+    if (MODE == Q8_HALVES) {
+      const uint2 x = *reinterpret_cast<const uint2*>(d + 8 * v0);
+      const uint2 y = *reinterpret_cast<const uint2*>(d + 8 * v1);
+      return make_uint4(x.x, x.y, y.x, y.y);
+    }
+    return *reinterpret_cast<const uint4*>(d + 16 * l);
   }
 };
 
-// E: input type; C: codes; L: lanes of a row (16 elements each); K: rows a lane holds
-template <typename E, typename C, int L, int K>
+// A block of a sequence, one of its two matrices.
+struct Q8Block {
+  int blk, lo, hi;       // its slots, the first new one, the one past the last
+  int j_first, j_end;    // heads
+  const char* rows;      // the packed row of slot 0, head 0
+  int64_t token_b, head_b;
+  char* codes;           // of slot 0, head 0
+  int64_t slot_b, code_head_b;
+  float* scales;         // of head 0
+  int64_t scale_head;
+  bool ints;             // codes are integers
+};
+
+SLS_DEV uint4 q8_codes(bool ints, const float (&y)[16], float by) {
+  return ints ? to_codes16<I8>(y, by) : to_codes16<E4M3>(y, by);
+}
+SLS_DEV float q8_scale(bool ints, float most) {
+  return ints ? code_scale<I8>(most) : code_scale<E4M3>(most);
+}
+// One over a scale: a power of two as a rule.
+SLS_DEV float q8_over(float s) {
+  const int bits = __float_as_int(s);
+  return (bits & 0x807fffff) == 0 && bits > 0 && bits < 0x7e800000 ? __int_as_float(0x7f000000 - bits)
+                                                                   : 1.f / s;
+}
+// Codes of earlier tokens in units of a larger scale.
+template <typename Lane>
+SLS_DEV void q8_again(const Lane& me, bool ints, char* d, float by) {
+  float z[16];
+  const uint4 u = me.codes(d);
+  if (ints) codes_float<I8>(u, z);
+  else codes_float<E4M3>(u, z);
+  me.store(d, q8_codes(ints, z, by));
+}
+
+// Few new tokens: a head is one group's of L lanes, all heads at once.
+template <bool KEYS, typename E, int L, int MODE>
+SLS_DEV void q8_few(const Q8Lane<E, L, MODE>& me, const Q8Block& b) {
+  constexpr int NG = Q8_T / L;
+#pragma unroll 1
+  for (int j = b.j_first + (int)threadIdx.x / L; j < b.j_end; j += NG) {
+    float y[16], most = 0.f, norm = 1.f;
+    uint4 u[2];
+    const char* const p = b.rows + j * b.head_b;
+#pragma unroll 1
+    for (int slot = b.lo; slot < b.hi; ++slot) {
+      me.load(p + slot * b.token_b, u);
+      norm = me.template row<KEYS>(u, p + slot * b.token_b, slot, y, most);
+    }
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(me.mates, most, o));
+    float* sp = b.scales + j * b.scale_head;
+    const float was = b.lo > 0 ? *sp : 0.f;
+    const float now = fmaxf(q8_scale(b.ints, most), was), by = q8_over(now);
+    char* d = b.codes + j * b.code_head_b;
+#pragma unroll 1
+    for (int slot = b.lo; slot < b.hi; ++slot) {
+      if (b.hi - b.lo > 1) {
+        me.load(p + slot * b.token_b, u);
+        norm = me.template row<KEYS>(u, p + slot * b.token_b, slot, y, most);
+      }
+      if (me.on) me.store(d + slot * b.slot_b, q8_codes(b.ints, y, norm * by));
+    }
+    if (me.on && now > was)
+#pragma unroll 1
+      for (int slot = 0; slot < b.lo; ++slot) q8_again(me, b.ints, d + slot * b.slot_b, was * by);
+    __syncwarp(me.mates);  // every lane has read the old scale
+    if (me.l == 0 && now != was) *sp = now;
+  }
+}
+
+// A block's tokens shared out over the groups, K rows for each, head after head (or several at
+// once where a block has fewer tokens than there are groups).
+template <bool KEYS, int K, typename E, int L, int MODE>
+SLS_DEV void q8_many(const Q8Lane<E, L, MODE>& me, const Q8Block& b, float (&s_most)[2][Q8_T / 32],
+                     int& parity) {
+  constexpr int NG = Q8_T / L;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = threadIdx.x / L;
+  const int per_job = min(b.blk, NG), together = NG / per_job;
+  const int first = grp & (per_job - 1);
+  const char* const mine = b.rows + first * b.token_b;
+  const int64_t next_row = per_job * b.token_b;
+  // the next head's rows are on their way while one is worked on
+  uint4 u[K][2];
+  auto fetch = [&](int j) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int slot = first + k * per_job;
+      if (j < b.j_end && slot >= b.lo && slot < b.hi) me.load(mine + k * next_row + j * b.head_b, u[k]);
+    }
+  };
+  int j = b.j_first + grp / per_job;
+  fetch(j);
+#pragma unroll 1
+  for (int j0 = b.j_first; j0 < b.j_end; j0 += together, j += together) {
+    const bool live = j < b.j_end;
+    float y[K][16], norm[K];
+    float most = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int slot = first + k * per_job;
+      // whole groups of L lanes take the branch or leave it
+      if (live && slot >= b.lo && slot < b.hi)
+        norm[k] = me.template row<KEYS>(u[k], mine + k * next_row + j * b.head_b, slot, y[k], most);
+    }
+    fetch(j + together);
+    // the rows of a warp are one head's: a block has at least as many slots as a warp rows.
+    // The old scale is read in front of the barrier, behind which it is written.
+    most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
+    const float was = live && b.lo > 0 ? b.scales[j * b.scale_head] : 0.f;
+    if (lane == 0) s_most[parity][warp] = most;
+    __syncthreads();
+    const int wj = per_job * L / 32, w0 = warp & ~(wj - 1);
+    most = s_most[parity][w0 + (lane & (wj - 1))];
+    most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
+    parity ^= 1;
+    if (!live) continue;
+    const float now = fmaxf(q8_scale(b.ints, most), was), by = q8_over(now);
+    char* d = b.codes + j * b.code_head_b;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int slot = first + k * per_job;
+      if (!me.on || slot >= b.hi) continue;
+      if (slot >= b.lo)
+        me.store(d + slot * b.slot_b, q8_codes(b.ints, y[k], norm[k] * by));
+      else if (now > was)
+        q8_again(me, b.ints, d + slot * b.slot_b, was * by);
+    }
+    if (first == 0 && me.l == 0 && now != was) b.scales[j * b.scale_head] = now;
+  }
+}
+
+// E: input type; L: lanes of a row (16 elements each); K: rows a lane holds, 0 where blocks take
+// few new tokens; MODE: of keys
+template <typename E, int L, int K, int MODE>
 __global__ void __launch_bounds__(Q8_T, K <= 2 ? 2 : 1)
 kv_append_q8_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ ScaleView sv,
-                    int tile, int jobs_per_cta) {
-  extern __shared__ float2 s_turn[];
+                    int tile, int key_ctas, int key_jobs, int value_jobs, bool ints) {
+  extern __shared__ float4 s_tab[];
   __shared__ float s_most[2][Q8_T / 32];
   __shared__ int s_ended[Q8_T / 32];
-  constexpr int NG = Q8_T / L;           // rows in flight
   const CacheView& c = a.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int grp = threadIdx.x / L, l = threadIdx.x % L;
   const int blk = 1 << sv.shift;
-  const int per_job = min(blk, NG);      // groups of a job (one head of keys or of values)
-  const int together = NG / per_job;     // jobs in flight
-  const int jobs = 2 * c.kv_heads;
-  const int j_first = blockIdx.y * jobs_per_cta, j_end = min(jobs, j_first + jobs_per_cta);
+  // the first CTAs of a tile take heads of keys, the others heads of values
+  const bool keys = (int)blockIdx.y < key_ctas;
+  const int j_first = keys ? blockIdx.y * key_jobs : (blockIdx.y - key_ctas) * value_jobs;
+  const int j_end = min(c.kv_heads, j_first + (keys ? key_jobs : value_jobs));
+  const RowsView& src = keys ? a.k : a.v;
+  char* const cache = keys ? c.k : c.v;
   const int64_t t_end = min(a.T, ((int64_t)blockIdx.x + 1) * tile);
   int64_t t = (int64_t)blockIdx.x * tile;
 
   at_go();
   at_wait_ahead();
-  const Q8Lane<E, L> me(a, s_turn, lane, l);
+  const Q8Lane<E, L, MODE> me(a, s_tab, lane, threadIdx.x % L);
   int seq = (int)t;
   if (a.cu) {
     int ended = 0;
+#pragma unroll 1
     for (int b = threadIdx.x; b < c.B; b += Q8_T) ended += a.cu[b + 1] <= t;
     ended = __reduce_add_sync(0xffffffffu, ended);
     if (lane == 0) s_ended[warp] = ended;
@@ -225,6 +380,7 @@ kv_append_q8_kernel(const __grid_constant__ AppendArgs a, const __grid_constant_
     for (int w = 0; w < Q8_T / 32; ++w) seq += s_ended[w];
   }
   int parity = 0;
+#pragma unroll 1
   for (; seq < c.B; ++seq) {
     const Q8Place at = q8_place(a, seq);
     if (a.cu ? (int64_t)a.cu[seq] >= t_end : seq >= t_end) break;
@@ -235,6 +391,7 @@ kv_append_q8_kernel(const __grid_constant__ AppendArgs a, const __grid_constant_
       row += blk - (idx & (blk - 1));
       idx = at.index0 + row - at.begin;
     }
+#pragma unroll 1
     while (row < min(at.end, t_end)) {
       const int64_t start = idx & ~(int64_t)(blk - 1);
       const int lo = (int)(idx - start);                             // first new slot
@@ -246,118 +403,30 @@ kv_append_q8_kernel(const __grid_constant__ AppendArgs a, const __grid_constant_
       if (page < 0 || page >= c.num_pages) continue;
       const int slot0 = (int)(start & ((1 << c.page_shift) - 1));
       const int64_t sc = page * sv.page + (slot0 >> sv.shift) * sv.block;
-      // the turns of the block's new tokens, for all heads of keys
-      __syncthreads();
-      if (j_first < c.kv_heads && a.pairs > 0) {
-        const int wd = me.width(a), nl = me.lanes(a), stride = wd * nl + 4;
-        for (int i = threadIdx.x; i < (hi - lo) * a.pairs; i += Q8_T) {
-          const int k = i / a.pairs, pr = i - k * a.pairs;
-          const int p = a.positions ? a.positions[row0 + lo + k] : (int)(start + lo + k);
-          const float2 cs = turn(p, a.inv_freq[pr]);
-          s_turn[(lo + k) * stride + (pr & (wd - 1)) * nl + pr / wd] =
-              make_float2(cs.x * a.rope_scale, cs.y * a.rope_scale);
-        }
-      }
-      __syncthreads();
-      auto source = [&](int j, int slot) {
-        const bool keys = j < c.kv_heads;
-        const RowsView& src = keys ? a.k : a.v;
-        return src.data + (row0 + slot) * src.token_b + (keys ? j : j - c.kv_heads) * src.head_b;
-      };
-      auto scale_at = [&](int j) {
-        return j < c.kv_heads ? sv.k + sc + j * sv.head : sv.v + sc + (j - c.kv_heads) * sv.head;
-      };
-      auto codes_at = [&](int j) {
-        return (j < c.kv_heads ? c.k + j * c.head_b : c.v + (j - c.kv_heads) * c.head_b) +
-               page * c.page_b + slot0 * c.slot_b + 16 * l;
-      };
-      auto again = [&](char* d, float by) {
-        float z[16];
-        codes_float<C>(*reinterpret_cast<const uint4*>(d), z);
-        *reinterpret_cast<uint4*>(d) = to_codes16<C>(z, by);
-      };
-      if (hi - lo <= Q8_FEW) {
-        // ---- few new tokens: a job is one group's, all jobs at once
-        for (int j = j_first + grp; j < j_end; j += NG) {
-          const bool keys = j < c.kv_heads;
-          float y[16], most = 0.f;
-          uint4 u[2];
-          for (int slot = lo; slot < hi; ++slot) {
-            me.load(source(j, slot), u);
-            most = fmaxf(most, me.row(u, source(j, slot), keys, slot, y));
-          }
-#pragma unroll
-          for (int o = L / 2; o > 0; o >>= 1)
-            most = fmaxf(most, __shfl_xor_sync(me.mates, most, o));
-          float* sp = scale_at(j);
-          const float was = lo > 0 ? *sp : 0.f;
-          const float now = fmaxf(code_scale<C>(most), was), by = 1.f / now;
-          char* d = codes_at(j);
-          for (int slot = lo; slot < hi; ++slot) {
-            if (hi - lo > 1) {
-              me.load(source(j, slot), u);
-              me.row(u, source(j, slot), keys, slot, y);
-            }
-            if (me.on) *reinterpret_cast<uint4*>(d + slot * c.slot_b) = to_codes16<C>(y, by);
-          }
-          if (me.on && now > was)
-            for (int slot = 0; slot < lo; ++slot) again(d + slot * c.slot_b, was * by);
-          __syncwarp(me.mates);  // every lane has read the old scale
-          if (l == 0 && now != was) *sp = now;
-        }
-        continue;
-      }
-      // the next job's rows are on their way while one is worked on
-      uint4 u[K][2];
-      auto fetch = [&](int j) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-          const int slot = grp % per_job + k * per_job;
-          if (j < j_end && slot >= lo && slot < hi) me.load(source(j, slot), u[k]);
-        }
-      };
-      fetch(j_first + grp / per_job);
-      for (int j0 = j_first; j0 < j_end; j0 += together) {
-        const int j = j0 + grp / per_job;
-        const bool live = j < j_end, keys = j < c.kv_heads;
-        float y[K][16];
-        float most = 0.f;
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-          const int slot = grp % per_job + k * per_job;
-          // whole groups of L lanes take the branch or leave it
-          if (live && slot >= lo && slot < hi)
-            most = fmaxf(most, me.row(u[k], source(j, slot), keys, slot, y[k]));
-        }
-        fetch(j + together);
-        // the rows of a warp are one head's: a block has at least as many slots as a warp rows.
-        // The old scale is read in front of the barrier, behind which it is written.
-        most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
-        const float was = live && lo > 0 ? *scale_at(j) : 0.f;
-        if (lane == 0) s_most[parity][warp] = most;
+      // the factors of the block's new tokens, for all heads of keys
+      if (MODE != Q8_PLAIN && keys) {
         __syncthreads();
-        const int wj = per_job * L / 32, w0 = warp / wj * wj;
-        for (int i = 0; i < wj; ++i) most = fmaxf(most, s_most[parity][w0 + i]);
-        parity ^= 1;
-        if (!live) continue;
-        const float now = fmaxf(code_scale<C>(most), was), by = 1.f / now;
-        char* d = codes_at(j);
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-          const int slot = grp % per_job + k * per_job;
-          if (!me.on || slot >= hi) continue;
-          if (slot >= lo) *reinterpret_cast<uint4*>(d + slot * c.slot_b) = to_codes16<C>(y[k], by);
-          else if (now > was) again(d + slot * c.slot_b, was * by);
-        }
-        if (grp % per_job == 0 && l == 0 && now != was) *scale_at(j) = now;
+        me.enter(s_tab, lo, hi - lo, row0 + lo, (int)(start + lo));
+        __syncthreads();
+      }
+      const Q8Block b{blk, lo, hi, j_first, j_end,
+                      src.data + row0 * src.token_b, src.token_b, src.head_b,
+                      cache + page * c.page_b + slot0 * c.slot_b, c.slot_b, c.head_b,
+                      (keys ? sv.k : sv.v) + sc, sv.head, ints};
+      if constexpr (K == 0) {
+        if (MODE != Q8_PLAIN && keys) q8_few<true>(me, b);
+        else q8_few<false>(me, b);
+      } else {
+        if (MODE != Q8_PLAIN && keys) q8_many<true, K>(me, b, s_most, parity);
+        else q8_many<false, K>(me, b, s_most, parity);
       }
     }
   }
 }
 
-template <typename E, typename C, int L>
-int launch(const AppendArgs& a, const ScaleView& s, cudaStream_t stream) {
-  const int blk = 1 << s.shift, jobs = 2 * a.c.kv_heads;
+template <typename E, int L, int MODE>
+int launch(const AppendArgs& a, const ScaleView& s, bool ints, cudaStream_t stream) {
+  const int blk = 1 << s.shift, jobs = a.c.kv_heads;
   // a block's tokens for a CTA, or as many as a sequence has new ones on average, and heads
   // shared out until there are some 1200 CTAs (eight for each of 152 SMs)
   int tile = blk;
@@ -366,26 +435,39 @@ int launch(const AppendArgs& a, const ScaleView& s, cudaStream_t stream) {
   // jobs that a CTA has in flight
   const int together = tile <= Q8_FEW ? Q8_T / L : std::max(1, Q8_T / L / blk);
   const int passes = (jobs + together - 1) / together;
-  const int share = (int)std::max<int64_t>(1, std::min<int64_t>((1216 + tiles - 1) / tiles, passes));
-  const int per = (passes + share - 1) / share * together;
-  const dim3 grid((unsigned)tiles, (unsigned)((jobs + per - 1) / per));
-  const int width = a.interleaved ? 8 : 16;
-  const size_t smem = a.pairs == 0 ? 0
-                      : (size_t)blk * ((a.pairs + width - 1) / width * width + 4) * sizeof(float2);
+  auto share = [&](int64_t ctas) {
+    const int n = (int)std::max<int64_t>(1, std::min<int64_t>((ctas + tiles - 1) / tiles, passes));
+    return (passes + n - 1) / n * together;
+  };
+  const int key_jobs = share(Q8_KEY_CTAS), value_jobs = share(Q8_VALUE_CTAS);
+  const int key_ctas = (jobs + key_jobs - 1) / key_jobs;
+  const dim3 grid((unsigned)tiles, (unsigned)(key_ctas + (jobs + value_jobs - 1) / value_jobs));
+  const size_t smem = MODE != Q8_PLAIN ? (size_t)blk * Q8Lane<E, L, MODE>::PITCH * sizeof(float4) : 0;
+  auto go = [&](auto kern) {
+    if (smem > 48 * 1024)
+      SLS_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                        (int)smem));
+    return at_launch(kern, grid, Q8_T, smem, 1, stream, a, s, tile, key_ctas, key_jobs, value_jobs,
+                     ints);
+  };
+  if (tile <= Q8_FEW) return go(kv_append_q8_kernel<E, L, 0, MODE>);
   const int rows = blk * L / Q8_T;
-  auto kern = rows <= 1 ? kv_append_q8_kernel<E, C, L, 1>
-              : rows == 2 ? kv_append_q8_kernel<E, C, L, 2> : kv_append_q8_kernel<E, C, L, L / 2>;
-  if (smem > 48 * 1024)
-    SLS_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                      (int)smem));
-  return at_launch(kern, grid, Q8_T, smem, 1, stream, a, s, tile, per);
+  if (rows <= 1) return go(kv_append_q8_kernel<E, L, 1, MODE>);
+  return rows == 2 ? go(kv_append_q8_kernel<E, L, 2, MODE>) : go(kv_append_q8_kernel<E, L, L / 2, MODE>);
+}
+
+template <typename E, int L>
+int launch(const AppendArgs& a, const ScaleView& s, bool ints, cudaStream_t stream) {
+  if (a.pairs == 0 && !a.k_weight) return launch<E, L, Q8_PLAIN>(a, s, ints, stream);
+  if (a.interleaved) return launch<E, L, Q8_SIDES>(a, s, ints, stream);
+  return (a.pairs & 7) == 0 ? launch<E, L, Q8_HALVES>(a, s, ints, stream)
+                            : launch<E, L, Q8_ODD>(a, s, ints, stream);
 }
 
 template <typename E>
 int launch(const AppendArgs& a, const ScaleView& s, int code, cudaStream_t stream) {
-  if (code == SLS_I8)
-    return a.c.head_dim > 64 ? launch<E, I8, 8>(a, s, stream) : launch<E, I8, 4>(a, s, stream);
-  return a.c.head_dim > 64 ? launch<E, E4M3, 8>(a, s, stream) : launch<E, E4M3, 4>(a, s, stream);
+  return a.c.head_dim > 64 ? launch<E, 8>(a, s, code == SLS_I8, stream)
+                           : launch<E, 4>(a, s, code == SLS_I8, stream);
 }
 
 }  // namespace
