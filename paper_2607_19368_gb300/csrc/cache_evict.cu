@@ -1,7 +1,7 @@
 // Eviction: of every (sequence, key head) the first and last tokens and the heaviest others
 // stay, in order, and move to the front of the sequence's pages.
 //
-// Two launches.  The first selects: a cluster holds a sequence's weights in registers, finds
+// Two launches.  The first selects: a cluster holds a sequence's weights in shared memory, finds
 // that of the last of the kept others digit by digit (counts of 2048, 2048 and 1024 digits of the
 // weights as ordered integers, summed through distributed shared memory), and counts what stays in
 // front of every token, which gives it its place; weights move here.  The second moves keys and values.  A place is never behind its source, so a cluster of
@@ -16,9 +16,10 @@ namespace sls {
 
 namespace {
 
-constexpr int EV_T = 1024;    // selection
+constexpr int EV_T = 512;     // selection
+constexpr int EV_PER = 4;     // digits that a thread counts up: EV_BINS / EV_T
 constexpr int EV_BINS = 2048;
-constexpr int EV_V = 8;       // groups of four weights that a thread of the selection holds
+constexpr int EV_ROOM = 12288;  // groups of four weights that a CTA of the selection holds at most
 constexpr int EV_MOVE_T = 256;
 constexpr int EV_CLUSTER = 8;
 
@@ -46,20 +47,22 @@ SLS_DEV void ev_cluster_sync() {
 }
 
 // What a CTA of the selection has in shared memory.
-struct EvShared {
+struct __align__(16) EvShared {
   unsigned bins[2][EV_BINS];
   unsigned warp[EV_T / 32][2];
-  unsigned part[EV_V * EV_T / 32];  // kept for sure in the low half, equal ones in the high half
-  unsigned total;
-  unsigned digit, above;
+  unsigned total[EV_CLUSTER];  // of the cluster's CTAs: staying ones, equal ones
+  unsigned digit, above, count;  // a pass's digit, how many are above it and have it
 };
 
-// The digit of this pass at which the count from the top reaches `need`, from a thread's two
-// counts n0 (digit b = EV_BINS - 1 - 2 threadIdx.x) and n1 (b - 1).
-SLS_DEV void ev_digit(EvShared& s, unsigned n0, unsigned n1, unsigned need) {
+// The digit of this pass at which the count from the top reaches `need`, from a thread's counts:
+// n[i] of digit ev_first() + i.
+SLS_DEV int ev_first() { return EV_BINS - EV_PER - EV_PER * (int)threadIdx.x; }
+SLS_DEV void ev_digit(EvShared& s, const unsigned (&n)[EV_PER], unsigned need) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int b = EV_BINS - 1 - 2 * threadIdx.x;
-  unsigned sum = n0 + n1;
+  unsigned own = 0;
+#pragma unroll
+  for (int i = 0; i < EV_PER; ++i) own += n[i];
+  unsigned sum = own;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
     const unsigned y = __shfl_up_sync(0xffffffffu, sum, d);
@@ -68,9 +71,13 @@ SLS_DEV void ev_digit(EvShared& s, unsigned n0, unsigned n1, unsigned need) {
   if (lane == 31) s.warp[warp][0] = sum;
   __syncthreads();
   unsigned above = lane < warp ? s.warp[lane][0] : 0u;
-  above = __reduce_add_sync(0xffffffffu, above) + sum - n0 - n1;
-  if (above < need && need <= above + n0) s.digit = b, s.above = above;
-  else if (above + n0 < need && need <= above + n0 + n1) s.digit = b - 1, s.above = above + n0;
+  above = __reduce_add_sync(0xffffffffu, above) + sum - own;
+#pragma unroll
+  for (int i = EV_PER - 1; i >= 0; --i) {
+    if (above < need && need <= above + n[i])
+      s.digit = ev_first() + i, s.above = above, s.count = n[i];
+    above += n[i];
+  }
   __syncthreads();
 }
 
@@ -89,18 +96,23 @@ SLS_DEV void ev_select_long(const EvictArgs& a, const EvSeq& e, int len, int32_t
     unsigned* bins = s.bins[0];
     for (int i = threadIdx.x; i < EV_BINS; i += EV_T) bins[i] = 0;
     __syncthreads();
-    for (int x = lo + threadIdx.x; x < hi; x += EV_T) {
-      const float* w = e.weight(x);
+    for (int x0 = lo; x0 < hi; x0 += EV_T) {
+      const int x = x0 + threadIdx.x;
+      const float* w = x < hi ? e.weight(x) : nullptr;
       const uint32_t k = ev_key(w ? *w : 0.f);
-      if ((k & mask) == top) atomicAdd(&bins[(k >> shift) & digits], 1u);
+      if (x < hi && (k & mask) == top) atomicAdd(&bins[(k >> shift) & digits], 1u);
     }
     __syncthreads();
-    const int b = EV_BINS - 1 - 2 * threadIdx.x;
-    ev_digit(s, bins[b], bins[b - 1], need);
+    unsigned n[EV_PER];
+#pragma unroll
+    for (int i = 0; i < EV_PER; ++i) n[i] = bins[ev_first() + i];
+    ev_digit(s, n, need);
     top |= s.digit << shift;
     mask |= digits << shift;
     need -= s.above;
+    const bool all = need == s.count;  // all that share these digits stay
     __syncthreads();
+    if (all) break;
   }
   // in order: larger ones and the first `need` equal ones stay
   unsigned base_more = 0, base_same = 0;
@@ -112,8 +124,8 @@ SLS_DEV void ev_select_long(const EvictArgs& a, const EvSeq& e, int len, int32_t
       const float* p = e.weight(x);
       w = p ? *p : 0.f;
       const uint32_t k = ev_key(w);
-      more = x < lo || x >= hi || (mask != 0 && k > top);
-      same = !more && mask != 0 && k == top;
+      more = x < lo || x >= hi || (k & mask) > top;
+      same = !more && mask != 0 && (k & mask) == top;
     }
     const unsigned bm = __ballot_sync(0xffffffffu, more), bs = __ballot_sync(0xffffffffu, same);
     if (lane == 0) s.warp[warp][0] = __popc(bm), s.warp[warp][1] = __popc(bs);
@@ -136,8 +148,9 @@ SLS_DEV void ev_select_long(const EvictArgs& a, const EvSeq& e, int len, int32_t
     if (float* p = e.weight(x)) *p = 0.f;
 }
 
-__global__ void __launch_bounds__(EV_T)
-cache_evict_select_kernel(const __grid_constant__ EvictArgs a, int32_t* lens_before) {
+__global__ void __launch_bounds__(EV_T, 2)
+cache_evict_select_kernel(const __grid_constant__ EvictArgs a, int room4, int32_t* lens_before) {
+  extern __shared__ float4 s_w[];  // room4 of them
   __shared__ EvShared s;
   const CacheView& c = a.c;
   uint32_t rank, size;
@@ -157,145 +170,132 @@ cache_evict_select_kernel(const __grid_constant__ EvictArgs a, int32_t* lens_bef
     for (int i = rank * EV_T + threadIdx.x; i < a.keep; i += size * EV_T) kept[i] = i < len ? i : -1;
     return;
   }
-  if (len > (int64_t)size * EV_T * EV_V * 4) {
+  // this CTA's weights, four in a row at a time, to shared memory: loops over them stay short, and
+  // nearly all of the time of a call this small goes into fetching its instructions
+  const int groups = (len + 3) >> 2, per = (groups + size - 1) / size;
+  if (per > room4) {
     if (rank == 0) ev_select_long(a, e, len, kept, s);
     return;
   }
-  // this CTA's weights, four in a row for each thread at a time
-  const int groups = (len + 3) >> 2, per = (groups + size - 1) / size;
   const int g0 = min(groups, (int)rank * per), mine = min(groups, g0 + per) - g0;
-  float w[EV_V][4];
-#pragma unroll
-  for (int v = 0; v < EV_V; ++v) {
-    const int g = v * EV_T + threadIdx.x;
-    float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (g < mine) {
-      const float* p = e.weight(4 * (int64_t)(g0 + g));
-      if (p) f = *reinterpret_cast<const float4*>(p);
-    }
-    w[v][0] = f.x, w[v][1] = f.y, w[v][2] = f.z, w[v][3] = f.w;
+#pragma unroll 4
+  for (int g = threadIdx.x; g < mine; g += EV_T) {
+    const float* p = e.weight(4 * (int64_t)(g0 + g));
+    s_w[g] = p ? *reinterpret_cast<const float4*>(p) : make_float4(0.f, 0.f, 0.f, 0.f);
   }
   const int lo = a.first, hi = len - a.last;
   unsigned need = (unsigned)(a.keep - a.first - a.last);
   uint32_t top = 0, mask = 0;
   __syncthreads();
+#pragma unroll 1
   for (int pass = 0; pass < 3 && need > 0; ++pass) {
     const int shift = ev_shift(pass);
     const uint32_t digits = ev_digits(pass);
     unsigned* bins = s.bins[pass & 1];
-#pragma unroll
-    for (int v = 0; v < EV_V; ++v) {
-      if (v * EV_T >= mine) break;
-      const int x = 4 * (g0 + v * EV_T + (int)threadIdx.x);
-      if (v * EV_T + (int)threadIdx.x >= mine) continue;
+#pragma unroll 1
+    for (int g = threadIdx.x; g < mine; g += EV_T) {
+      const float4 f = s_w[g];
+      const float w[4] = {f.x, f.y, f.z, f.w};
+      const int x = 4 * (g0 + g);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t k = ev_key(w[v][i]);
+        const uint32_t k = ev_key(w[i]);
         if (x + i >= lo && x + i < hi && (k & mask) == top)
           atomicAdd(&bins[(k >> shift) & digits], 1u);
       }
     }
     ev_cluster_sync();
     // of all CTAs of the cluster
-    const int b = EV_BINS - 1 - 2 * threadIdx.x;
-    unsigned n[EV_CLUSTER][2];
-#pragma unroll
-    for (uint32_t r = 0; r < EV_CLUSTER; ++r) {
-      n[r][0] = n[r][1] = 0;
-      if (r >= size) continue;
+    unsigned n[EV_PER] = {};
+#pragma unroll 4
+    for (uint32_t r = 0; r < size; ++r) {
       uint32_t at;
-      asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(&bins[b - 1])), "r"(r));
-      asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];"
-                   : "=r"(n[r][1]), "=r"(n[r][0])
+      unsigned x[EV_PER];
+      asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(&bins[ev_first()])), "r"(r));
+      asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3])
                    : "r"(at)
                    : "memory");
-    }
-    unsigned n0 = 0, n1 = 0;
 #pragma unroll
-    for (uint32_t r = 0; r < EV_CLUSTER; ++r) n0 += n[r][0], n1 += n[r][1];
+      for (int i = 0; i < EV_PER; ++i) n[i] += x[i];
+    }
     // nobody reads the first pass's counts any more when the second pass's are complete
     if (pass == 1)
       for (int i = threadIdx.x; i < EV_BINS; i += EV_T) s.bins[0][i] = 0;
-    ev_digit(s, n0, n1, need);
+    ev_digit(s, n, need);
     top |= s.digit << shift;
     mask |= digits << shift;
     need -= s.above;
+    if (need == s.count) break;  // all that share these digits stay
     __syncthreads();
   }
-  // ---- places: larger ones and the first `need` equal ones stay, in order
-  auto kind = [&](int x, float f) {  // 1: stays, 1 << 16: equal to the last one, 0: goes
+  // ---- places: larger ones and the first `need` equal ones stay, in order.  A thread has groups
+  // in a row; counts hold what stays in their low half and what is equal in their high half (at most
+  // 49152 a CTA).
+  auto kind = [&](int x, float f) {
     const uint32_t k = ev_key(f);
     if (x >= len) return 0u;
-    if (x < lo || x >= hi || (mask != 0 && k > top)) return 1u;
-    return mask != 0 && k == top ? 1u << 16 : 0u;
+    if (x < lo || x >= hi || (k & mask) > top) return 1u;
+    return mask != 0 && (k & mask) == top ? 1u << 16 : 0u;
   };
-  unsigned before[EV_V];
-#pragma unroll
-  for (int v = 0; v < EV_V; ++v) {
-    before[v] = 0;
-    if (v * EV_T >= mine) break;
-    const int g = v * EV_T + threadIdx.x, x = 4 * (g0 + g);
-    unsigned n = 0;
-    if (g < mine) n = kind(x, w[v][0]) + kind(x + 1, w[v][1]) + kind(x + 2, w[v][2]) + kind(x + 3, w[v][3]);
-    unsigned sum = n;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const unsigned y = __shfl_up_sync(0xffffffffu, sum, d);
-      if (lane >= d) sum += y;
-    }
-    if (lane == 31) s.part[v * (EV_T / 32) + warp] = sum;
-    before[v] = sum - n;
+  const int q = (mine + EV_T - 1) / EV_T, first = min(mine, (int)threadIdx.x * q),
+            last = min(mine, first + q);
+  unsigned own = 0;
+#pragma unroll 1
+  for (int g = first; g < last; ++g) {
+    const float4 f = s_w[g];
+    const int x = 4 * (g0 + g);
+    own += kind(x, f.x) + kind(x + 1, f.y) + kind(x + 2, f.z) + kind(x + 3, f.w);
   }
+  unsigned sum = own;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const unsigned y = __shfl_up_sync(0xffffffffu, sum, d);
+    if (lane >= d) sum += y;
+  }
+  if (lane == 31) s.warp[warp][1] = sum;
   __syncthreads();
-  if (warp == 0) {
-    // counts before every warp's share of every v, in order; up to 2^15 of either kind a CTA
-    const int parts = (min(EV_V, (mine + EV_T - 1) / EV_T)) * (EV_T / 32);
-    unsigned base = 0;
-    for (int i = lane; i - lane < parts; i += 32) {
-      const unsigned n = i < parts ? s.part[i] : 0u;
-      unsigned sum = n;
-#pragma unroll
-      for (int d = 1; d < 32; d <<= 1) {
-        const unsigned y = __shfl_up_sync(0xffffffffu, sum, d);
-        if (lane >= d) sum += y;
-      }
-      if (i < parts) s.part[i] = base + sum - n;
-      base += __shfl_sync(0xffffffffu, sum, 31);
-    }
-    if (lane == 0) s.total = base;
-  }
-  ev_cluster_sync();  // all weights of the sequence are in registers, all totals known
-  unsigned more0 = 0, same0 = 0;
-  for (uint32_t r = 0; r < rank; ++r) {
+  const unsigned each = lane < EV_T / 32 ? s.warp[lane][1] : 0u;
+  const unsigned total = __reduce_add_sync(0xffffffffu, each);
+  unsigned base = __reduce_add_sync(0xffffffffu, lane < warp ? each : 0u) + sum - own;
+  if (warp == 0 && lane < size) {
     uint32_t at;
-    unsigned x;
-    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(&s.total)), "r"(r));
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
-    more0 += x & 0xffffu, same0 += x >> 16;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(&s.total[rank])), "r"(lane));
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(total) : "memory");
   }
-#pragma unroll
-  for (int v = 0; v < EV_V; ++v) {
-    if (v * EV_T >= mine) break;
-    const int g = v * EV_T + threadIdx.x;
-    if (g >= mine) continue;
-    const unsigned base = before[v] + s.part[v * (EV_T / 32) + warp];
-    unsigned more = more0 + (base & 0xffffu), same = same0 + (base >> 16);
+  // all weights of the sequence are in shared memory, all totals known; nobody touches another
+  // CTA's shared memory after this
+  ev_cluster_sync();
+  unsigned more = base & 0xffffu, same = base >> 16;
+  for (uint32_t r = 0; r < rank; ++r) more += s.total[r] & 0xffffu, same += s.total[r] >> 16;
+#pragma unroll 1
+  for (int g = first; g < last; ++g) {
+    const float4 f = s_w[g];
+    const float w[4] = {f.x, f.y, f.z, f.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int x = 4 * (g0 + g) + i;
-      const unsigned k = kind(x, w[v][i]);
+      const unsigned k = kind(x, w[i]);
       if (k == 1 || (k > 1 && same < need)) {
         const unsigned to = more + min(same, need);
         kept[to] = x;
         if (to != (unsigned)x)
-          if (float* p = e.weight(to)) *p = w[v][i];
+          if (float* p = e.weight(to)) *p = w[i];
       }
       more += k & 1, same += k >> 16;
     }
   }
-  for (int x = a.keep + (int)(rank * EV_T + threadIdx.x); x < len; x += size * EV_T)
+  // four slots at a time from the first multiple of four on
+  const int z0 = (a.keep + 3) & ~3;
+  for (int x = a.keep + threadIdx.x; x < min(z0, len) && rank == 0; x += EV_T)
     if (float* p = e.weight(x)) *p = 0.f;
-  ev_cluster_sync();  // no CTA leaves while another reads its shared memory
+#pragma unroll 1
+  for (int x = z0 + 4 * (int)(rank * EV_T + threadIdx.x); x < len; x += 4 * size * EV_T)
+    if (float* p = e.weight(x)) {
+      if (x + 4 <= len) *reinterpret_cast<float4*>(p) = make_float4(0.f, 0.f, 0.f, 0.f);
+      else
+        for (int i = 0; x + i < len; ++i) p[i] = 0.f;
+    }
 }
 
 // C: I8 or E4M3, or void for 16-bit elements; BOTH: a cluster moves keys and values, which
@@ -310,11 +310,11 @@ struct EvMove {
 };
 
 template <typename C, bool BOTH>
-__global__ void __launch_bounds__(EV_MOVE_T, 3)
+__global__ void __launch_bounds__(EV_MOVE_T, 4)
 cache_evict_move_kernel(const __grid_constant__ EvictArgs a, const int32_t* lens_before) {
   using S = EvMove<C, BOTH>;
   __shared__ int64_t s_from[S::ROWS], s_to[S::ROWS];  // byte offsets of rows, or -1
-  __shared__ float s_was[S::MATS][S::ROWS];
+  __shared__ float s_was[S::MATS][S::ROWS], s_by[S::MATS][S::ROWS];  // codes: old scale, old / new
   const CacheView& c = a.c;
   uint32_t rank, size;
   asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -366,7 +366,30 @@ cache_evict_move_kernel(const __grid_constant__ EvictArgs a, const int32_t* lens
         for (int m = 0; m < S::MATS; ++m)
           x[m][i] = *reinterpret_cast<const uint4*>(mat[m] + from + 16 * (at - row * vecs));
     }
+    float now[S::MATS];  // codes: of thread `row`'s block, the largest scale that its rows come from
+    if constexpr (S::CODES) {
+      const int row = threadIdx.x;
+      if (row < n) {
+        const int b0 = row >> a.s.shift << a.s.shift, b1 = min(n, b0 + (1 << a.s.shift));
+#pragma unroll
+        for (int m = 0; m < S::MATS; ++m) {
+          now[m] = 0.f;
+          for (int k = b0; k < b1; ++k) now[m] = fmaxf(now[m], s_was[m][k]);
+          const float was = s_was[m][row];
+          s_by[m][row] = was == now[m] ? 1.f : now[m] > 0.f ? was / now[m] : 0.f;
+        }
+      }
+    }
     ev_cluster_sync();
+    if constexpr (S::CODES) {
+      const int row = threadIdx.x;
+      if (row < n && (row & ((1 << a.s.shift) - 1)) == 0 && s_to[row] >= 0) {
+        const int64_t q = table[(j0 + row) >> c.page_shift];
+#pragma unroll
+        for (int m = 0; m < S::MATS; ++m)
+          scale[m][q * a.s.page + (((j0 + row) & slots) >> a.s.shift) * a.s.block] = now[m];
+      }
+    }
 #pragma unroll
     for (int i = 0; i < S::V; ++i) {
       const int at = i * EV_MOVE_T + threadIdx.x, row = at / vecs;
@@ -376,19 +399,11 @@ cache_evict_move_kernel(const __grid_constant__ EvictArgs a, const int32_t* lens
 #pragma unroll
       for (int m = 0; m < S::MATS; ++m) {
         if constexpr (S::CODES) {
-          // the largest scale of the place's block
-          const int b0 = row >> a.s.shift << a.s.shift, b1 = min(n, b0 + (1 << a.s.shift));
-          float now = 0.f;
-          for (int k = b0; k < b1; ++k) now = fmaxf(now, s_was[m][k]);
-          const float was = s_was[m][row];
-          if (was != now) {
+          const float by = s_by[m][row];
+          if (by != 1.f) {
             float y[16];
             codes_float<C>(x[m][i], y);
-            x[m][i] = to_codes16<C>(y, now > 0.f ? was / now : 0.f);
-          }
-          if (row == b0 && at == row * vecs) {
-            const int64_t q = table[(j0 + row) >> c.page_shift];
-            scale[m][q * a.s.page + (((j0 + row) & slots) >> a.s.shift) * a.s.block] = now;
+            x[m][i] = to_codes16<C>(y, by);
           }
         }
         *reinterpret_cast<uint4*>(mat[m] + to + 16 * (at - row * vecs)) = x[m][i];
@@ -427,14 +442,18 @@ int launch_cache_evict(const EvictArgs& a, int code, void* workspace, cudaStream
   SLS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   int32_t* lens = (int32_t*)workspace;
   // CTAs of a selection: as many as share out the GPU, no more than give every thread four weights
-  // of the longest table, and enough to hold it (past 8 x 32768 one CTA reads it anew each pass)
+  // of the longest table, and enough to hold it (past 8 x 49152 tokens one CTA reads it anew each
+  // pass)
   const int64_t room = (int64_t)c.max_pages << c.page_shift, units = (int64_t)c.B * c.kv_heads;
   int size = 1;
-  while (size < EV_CLUSTER && ((units * size * 2 <= sms && size * EV_T * 4 < room) ||
-                               (int64_t)size * EV_T * EV_V * 4 < room))
+  while (size < EV_CLUSTER && ((units * size <= sms && size * EV_T * 4 < room) ||
+                               (int64_t)size * EV_ROOM * 4 < room))
     size *= 2;
-  int st = at_launch(cache_evict_select_kernel, dim3((unsigned)(units * size)), EV_T, 0, size,
-                     stream, a, lens);
+  const int room4 = (int)std::min<int64_t>(EV_ROOM, ((room + 3) / 4 + size - 1) / size);
+  SLS_CUDA_TRY(cudaFuncSetAttribute(cache_evict_select_kernel,
+                                    cudaFuncAttributeMaxDynamicSharedMemorySize, EV_ROOM * 16));
+  int st = at_launch(cache_evict_select_kernel, dim3((unsigned)(units * size)), EV_T,
+                     (size_t)room4 * 16, size, stream, a, room4, lens);
   if (st != SLS_OK) return st;
   return code == SLS_I8     ? launch_move<I8>(a, sms, lens, stream)
          : code == SLS_E4M3 ? launch_move<E4M3>(a, sms, lens, stream)

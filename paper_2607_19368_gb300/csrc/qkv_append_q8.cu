@@ -23,7 +23,7 @@ namespace {
 constexpr int Q8_T = 256;
 // rows as they come; halves of whole vectors; pairs side by side; halves that split vectors
 enum { Q8_PLAIN, Q8_HALVES, Q8_SIDES, Q8_ODD };
-constexpr int Q8_KEY_CTAS = 608, Q8_VALUE_CTAS = 304;  // at least so many, heads permitting
+constexpr int Q8_KEY_CTAS = 304, Q8_VALUE_CTAS = 304;  // at least so many, heads permitting
 constexpr int Q8_FEW = 2;  // new tokens of a block up to which a job is one group's
 
 // Where a packed token goes.
