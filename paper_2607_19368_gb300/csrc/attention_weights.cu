@@ -3,299 +3,376 @@
 //   w_j += sum_i exp(s_ij - m_i) / l_i,   m_i = max_j s_ij,  l_i = sum_j exp(s_ij - m_i).
 //
 // A column can be summed only when the rows' m and l are known, so there are two passes over
-// the scores.  A CTA owns 256 cached tokens of a (sequence, key head), 32 a warp, whose keys
-// stay in registers as mma.sync operands (codes become float16 once) while rows pass by,
-// sixteen at a time from shared memory.  The first pass leaves a row's maximum and sum over the
-// 256 tokens; a small launch joins them; the second pass forms the scores again and sums columns
-// in registers, so that no sum is made by atomics: the same call gives the same bits.
+// the scores, both on the tensor cores in 128 x 128 tiles.  The first has rows as the lanes of
+// tensor memory, so that a thread finds the maximum and sum of a row's 64 tokens by itself; a
+// small launch joins the pieces of rows.  The second has tokens as lanes: a thread adds up a
+// token's column, with the rows' maxima and sums read from shared memory by all at once.  No sum is
+// made by atomics: the same call gives the same bits.
+//
+// Bound by exponentials (two a score) and, for few rows, by the products of padded tiles; the keys'
+// bytes are below either from some ten rows on.  A CTA goes through phases in step (keys to shared
+// memory, codes to float16 on the way; products; scores), with the next keys on their way in
+// registers; two CTAs an SM fill each other's gaps.  32 rows (tokens) of 7 heads over 32768
+// tokens of 4 key heads, e4m3: 86 us with mma.sync, whose products took the time, see the table
+// of cases for now.
 //
 // Where rows are few (a token for each sequence) the kernels of attention_weights_few.cu read keys
 // once instead.
 #include <algorithm>
 
 #include "attention_decode.cuh"
+#include "attention_umma.cuh"
 #include "cache8.cuh"
 
 namespace sls {
 
 namespace {
 
-constexpr int AW_WARPS = 8;
-constexpr int AW_T = 32 * AW_WARPS;
-constexpr int AW_KEYS = 32 * AW_WARPS;  // tokens of a CTA's unit
-constexpr int AW_TILES = 16;            // row tiles in shared memory at a time
-constexpr int AW_BLOCK = 16 * AW_TILES;
+constexpr int AW_T = 256;
+constexpr int AW_TILE = 128;  // rows or tokens
+constexpr int AW_JOIN_WARPS = 8;
 
 struct AwPlan {
-  float2* part;   // (token, query head, unit of the sequence): maximum and sum of its tokens
-  float2* stat;   // (token, query head): maximum, one over the sum
-  int units;      // of the longest sequence that the table holds
+  int ctas;         // of the first pass: most parts
+  int64_t* prefix;  // B + 1: first-pass steps before every sequence
+  float2* ml;       // (part, first or last piece, row of a tile): maximum and sum
+  float2* stat;     // (token, query head): maximum; sum, then one over it
 };
 
-template <typename E, typename KT>
-using AwMma = typename std::conditional<std::is_same<E, KT>::value, E, __half>::type;
-
-// first of the four elements of slice k that a lane's quarter cq of a row holds
-template <bool CODES>
-SLS_DEV int aw_element(int k, int cq) {
-  return CODES ? 64 * (k >> 2) + 16 * cq + 4 * (k & 3) : 32 * (k >> 1) + 8 * cq + 4 * (k & 1);
-}
+// KT: element of keys (E, or codes)
+template <typename E, typename KT, int HD>
+struct AwShape {
+  static constexpr bool CODES = !std::is_same<E, KT>::value;
+  using M = typename std::conditional<CODES, __half, E>::type;  // of the products
+  static constexpr int HALF_BYTES = AW_TILE * 128;
+  static constexpr int TILE_BYTES = HD / 64 * HALF_BYTES;
+  static constexpr int KEY_LANES = HD / (CODES ? 16 : 8);       // threads of a key's row
+  static constexpr int KEY_LOADS = AW_TILE * KEY_LANES / AW_T;  // 16-byte loads of a thread
+  static constexpr int ROW_LANES = HD / 8;
+  static constexpr int ROW_LOADS = AW_TILE * ROW_LANES / AW_T;
+  static constexpr uint32_t FMT = std::is_same<M, __nv_bfloat16>::value ? 1u : 0u;
+  static constexpr uint32_t IDESC = (1u << 4) | (FMT << 7) | (FMT << 10) |
+                                    ((uint32_t)(AW_TILE >> 4) << 24) |
+                                    ((uint32_t)(AW_TILE >> 3) << 17);
+  // Byte of 16-byte chunk ch of a row of a tile.
+  SLS_DEV static int at(int row, int ch) {
+    return (ch >> 3) * HALF_BYTES + row * 128 + (((ch & 7) ^ (row & 7)) << 4);
+  }
+};
 
 // The packed rows of a sequence.
-SLS_DEV void aw_rows(const AttnArgs& a, int seq, int64_t& q0, int64_t& q1) {
-  if (a.cu) {
-    seq_rows(a.cu, seq, a.T, q0, q1);
-  } else {
-    q0 = seq, q1 = seq + 1;
+SLS_DEV void aw_tokens(const AttnArgs& a, int seq, int64_t& q0, int64_t& q1) {
+  if (a.cu) seq_rows(a.cu, seq, a.T, q0, q1);
+  else q0 = seq, q1 = seq + 1;
+}
+
+SLS_DEV int64_t aw_row_tiles(const AttnArgs& a, int seq) {
+  int64_t q0, q1;
+  aw_tokens(a, seq, q0, q1);
+  return ((q1 - q0) * (a.q_heads / a.c.kv_heads) + AW_TILE - 1) / AW_TILE;
+}
+
+// A key head of a sequence.
+struct AwHead {
+  int seq, h, len, n, group;
+  int64_t q0, rows;
+  SLS_DEV AwHead(const AttnArgs& a, int s, int head) : seq(s), h(head) {
+    len = (int)cache_len(a.c, s);
+    int64_t q1;
+    aw_tokens(a, s, q0, q1);
+    n = (int)(q1 - q0);
+    group = a.q_heads / a.c.kv_heads;
+    rows = (int64_t)n * group;
+  }
+  // tokens that row `row` sees
+  SLS_DEV int see(const AttnArgs& a, int64_t row) const {
+    return row >= rows ? 0 : a.causal ? max(0, len - n + (int)(row / group) + 1) : len;
+  }
+  // most tokens that a row of a tile sees
+  SLS_DEV int most(const AttnArgs& a, int64_t tile) const {
+    return see(a, min(rows, (tile + 1) * AW_TILE) - 1);
+  }
+  SLS_DEV int64_t packed(const AttnArgs& a, int64_t row) const {  // its (token, query head)
+    const int64_t tok = row / group;
+    return (q0 + tok) * a.q_heads + h * group + (row - tok * group);
+  }
+};
+
+// 128 keys from token key0 on: to registers, and from there to a tile.
+template <typename E, typename KT, int HD>
+struct AwKeys {
+  using S = AwShape<E, KT, HD>;
+  uint4 raw[S::KEY_LOADS];
+  float scale;  // of key threadIdx.x
+
+  SLS_DEV void load(const AttnArgs& a, const ScaleView& sc, const AwHead& w, int key0) {
+    const CacheView& c = a.c;
+    const int ch = threadIdx.x % S::KEY_LANES, slots = (1 << c.page_shift) - 1;
+    const int32_t* table = c.table + w.seq * c.table_ld;
+#pragma unroll
+    for (int i = 0; i < S::KEY_LOADS; ++i) {
+      const int x = key0 + i * (AW_T / S::KEY_LANES) + threadIdx.x / S::KEY_LANES;
+      raw[i] = make_uint4(0, 0, 0, 0);
+      if (x >= w.len || ch * (S::CODES ? 16 : 8) >= c.head_dim) continue;
+      const int64_t page = table[x >> c.page_shift];
+      if (page >= 0 && page < c.num_pages)
+        raw[i] = *reinterpret_cast<const uint4*>(c.k + page * c.page_b + (x & slots) * c.slot_b +
+                                                 w.h * c.head_b + 16 * ch);
+    }
+    if constexpr (S::CODES) {
+      scale = 0.f;
+      const int x = key0 + threadIdx.x;
+      if (threadIdx.x < AW_TILE && x < w.len) {
+        const int64_t page = table[x >> c.page_shift];
+        if (page >= 0 && page < c.num_pages)
+          scale = sc.k[page * sc.page + ((x & slots) >> sc.shift) * sc.block + w.h * sc.head];
+      }
+    }
+  }
+
+  SLS_DEV void store(unsigned char* tile, float* scales) const {
+    const int ch = threadIdx.x % S::KEY_LANES;
+#pragma unroll
+    for (int i = 0; i < S::KEY_LOADS; ++i) {
+      const int row = i * (AW_T / S::KEY_LANES) + threadIdx.x / S::KEY_LANES;
+      if constexpr (S::CODES) {
+        uint4 y, z;
+        codes_half<KT>(raw[i].x, y.x, y.y);
+        codes_half<KT>(raw[i].y, y.z, y.w);
+        codes_half<KT>(raw[i].z, z.x, z.y);
+        codes_half<KT>(raw[i].w, z.z, z.w);
+        *reinterpret_cast<uint4*>(tile + S::at(row, 2 * ch)) = y;
+        *reinterpret_cast<uint4*>(tile + S::at(row, 2 * ch + 1)) = z;
+      } else {
+        *reinterpret_cast<uint4*>(tile + S::at(row, ch)) = raw[i];
+      }
+    }
+    if constexpr (S::CODES)
+      if (threadIdx.x < AW_TILE) scales[threadIdx.x] = scale;
+  }
+};
+
+// A tile of rows to shared memory; factors (codes with bfloat16 queries: a row's power of two, as in
+// the decode kernel) to `factor`, `stride` floats apart.
+template <typename E, typename KT, int HD>
+SLS_DEV void aw_stage_rows(const AttnArgs& a, const AwHead& w, int64_t tile, unsigned char* out,
+                           float* factor, int stride) {
+  using S = AwShape<E, KT, HD>;
+  const int ch = threadIdx.x % S::ROW_LANES;
+#pragma unroll
+  for (int i = 0; i < S::ROW_LOADS; ++i) {
+    const int r = i * (AW_T / S::ROW_LANES) + threadIdx.x / S::ROW_LANES;
+    const int64_t row = tile * AW_TILE + r;
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (row < w.rows && 8 * ch < a.c.head_dim) {
+      const int64_t tok = row / w.group;
+      u = *reinterpret_cast<const uint4*>(a.q.data + (w.q0 + tok) * a.q.token_b +
+                                          (w.h * w.group + (row - tok * w.group)) * a.q.head_b + 16 * ch);
+    }
+    float back = 1.f;
+    if constexpr (!std::is_same<E, typename S::M>::value) {
+      float x[8], top = 0.f;
+      widen8<E>(u, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
+#pragma unroll
+      for (int d = 1; d < S::ROW_LANES; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+      // the largest element to [2^14, 2^15)
+      const int e = max(__float_as_int(top) >> 23, 16);
+      const float by = __int_as_float((127 + 14 + 127 - e) << 23);
+      back = __int_as_float((e - 14) << 23);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] *= by;
+      u = narrow8<__half>(x);
+    }
+    *reinterpret_cast<uint4*>(out + S::at(r, ch)) = u;
+    if (ch == 0) factor[r * stride] = back;
   }
 }
 
-// SUM: the second pass
-template <typename E, typename KT, int HD, bool SUM>
+// D = A B^T of two tiles, to tensor memory columns d on; commits to `bar`.
+template <typename E, typename KT, int HD>
+SLS_DEV void aw_products(uint32_t lead, uint32_t d, const unsigned char* a, const unsigned char* b,
+                         uint64_t* bar) {
+  using S = AwShape<E, KT, HD>;
+  const uint32_t ad = ap_desc(smem_u32(a), 16), bd = ap_desc(smem_u32(b), 16);
+#pragma unroll
+  for (int k = 0; k < HD / 16; ++k) {
+    const uint32_t off = ((k >> 2) * S::HALF_BYTES + (k & 3) * 32) >> 4;
+    ap_mma_ss(lead, d, ad + off, bd + off, S::IDESC, k > 0);
+  }
+  ap_commit(lead, bar);
+}
+
+// Writes to shared memory are seen by the tensor cores after this and a barrier.
+SLS_DEV void aw_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+template <int COLUMNS>
+SLS_DEV uint32_t aw_alloc(uint32_t* holder) {
+  if (threadIdx.x < 32) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
+                     smem_u32(holder)),
+                 "r"(COLUMNS)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  ap_fence_before();
+  __syncthreads();
+  ap_fence_after();
+  return *holder;
+}
+template <int COLUMNS>
+SLS_DEV void aw_free(uint32_t tmem) {
+  ap_fence_before();
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    ap_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(COLUMNS)
+                 : "memory");
+  }
+}
+
+// ---- first pass: maxima and sums of rows -------------------------------------------------
+template <typename E, typename KT, int HD>
 __global__ void __launch_bounds__(AW_T, 2)
-attention_weights_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ ScaleView sc,
-                         const __grid_constant__ WeightView wv, const __grid_constant__ AwPlan p) {
-  using M = AwMma<E, KT>;
-  constexpr bool CODES = !std::is_same<E, KT>::value;
-  constexpr int KS = HD / 16;
-  extern __shared__ __align__(16) unsigned char smem[];
-  uint4* s_q = reinterpret_cast<uint4*>(smem);                     // (tile, slice, lane)
-  float* s_f = reinterpret_cast<float*>(s_q + AW_TILES * KS * 32);  // a row's factor
-  int* s_see = reinterpret_cast<int*>(s_f + AW_BLOCK);              // tokens that a row sees
-  float2* s_ml = reinterpret_cast<float2*>(s_see + AW_BLOCK);      // (warp, row), or (row) of stat
+attention_weights_rows_kernel(const __grid_constant__ AttnArgs a,
+                              const __grid_constant__ ScaleView sc, const __grid_constant__ AwPlan p,
+                              int* status) {
+  using S = AwShape<E, KT, HD>;
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
   __shared__ int64_t s_pre[AW_T + 1];
+  __shared__ float s_factor[AW_TILE];
+  __shared__ __align__(16) float s_scale[AW_TILE];
+  __shared__ float2 s_ml[AW_TILE];
+  __shared__ uint64_t bar;
+  __shared__ uint32_t holder;
   const CacheView& c = a.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int r = lane >> 2, cq = lane & 3;
-  const int group = a.q_heads / c.kv_heads;
   const float cs = a.scale * 1.4426950408889634f;
+  unsigned char* rows_s = reinterpret_cast<unsigned char*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  unsigned char* keys_s = rows_s + S::TILE_BYTES;
 
   at_wait_ahead();
-  const auto count = [&](int s) { return ad_steps<AW_KEYS>(c, s); };
-  const int R = ad_prefix<AW_T>(c, s_pre, nullptr, count);
-  const int64_t total = s_pre[AW_T] * c.kv_heads;
-  const int64_t u0 = total * blockIdx.x / gridDim.x, u1 = total * (blockIdx.x + 1) / gridDim.x;
-  int64_t staged = -1;  // the rows in shared memory: sequence times key heads plus head
-  for (int64_t u = u0; u < u1; ++u) {
-    // units lie by sequence, key head and tokens
-    int seq;
-    int64_t before;
-    ad_find<AW_T>(s_pre, R, u / c.kv_heads, count, seq, before);
-    const int units = ad_steps<AW_KEYS>(c, seq);
-    const int64_t in = u - before * c.kv_heads;
-    const int h = (int)(in / units), unit = (int)(in - (int64_t)h * units);
-    const int len = (int)cache_len(c, seq);
-    int64_t q0, q1;
-    aw_rows(a, seq, q0, q1);
-    const int n = (int)(q1 - q0);
-    const int64_t rows = (int64_t)n * group;
-    if (rows == 0) continue;
+  if (threadIdx.x == 0) mbar_init(&bar, 1);
+  mbar_fence_init();
+  const auto steps = [&](int s) {
+    return (int64_t)ad_steps<AW_TILE>(c, s) * aw_row_tiles(a, s) * c.kv_heads;
+  };
+  const int R = ad_prefix<AW_T>(c, s_pre, p.prefix, steps);
+  const int64_t total = s_pre[AW_T];
+  const int parts = (int)min((int64_t)p.ctas, total);
+  if ((int)blockIdx.x >= parts) return;
+  const int64_t t0 = total * blockIdx.x / parts, t1 = total * (blockIdx.x + 1) / parts;
+  const uint32_t tmem = aw_alloc<AW_TILE>(&holder);
+  const uint32_t lead = at_elect();
+  int seq;
+  int64_t before;  // steps before seq
+  ad_find<AW_T>(s_pre, R, t0, steps, seq, before);
+  // this thread's row of a tile, and its columns
+  const int r = 32 * (warp & 3) + lane, col0 = 64 * (warp >> 2);
+  const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + col0;
+  unsigned phase = 0;
+  bool ok = true;
 
-    // ---- this warp's keys ----
-    const int key0 = unit * AW_KEYS + warp * 32;
-    uint32_t kf[4][KS][2];
-    float ks[4];
-#pragma unroll
-    for (int nb = 0; nb < 4; ++nb) {
-      const int x = key0 + 8 * nb + r;
-      int64_t page = -1;
-      const int slot = x & ((1 << c.page_shift) - 1);
-      if (x < len) page = c.table[seq * c.table_ld + (x >> c.page_shift)];
-      const bool real = page >= 0 && page < c.num_pages;
-      const char* k = c.k + (real ? page : 0) * c.page_b + slot * c.slot_b + h * c.head_b;
-      ks[nb] = 1.f;
-      if constexpr (CODES) {
-        ks[nb] = real ? sc.k[page * sc.page + (slot >> sc.shift) * sc.block + h * sc.head] : 0.f;
-#pragma unroll
-        for (int i = 0; i < KS / 4; ++i) {
-          uint4 w = make_uint4(0, 0, 0, 0);
-          if (real && 64 * i + 16 * cq < c.head_dim)
-            w = *reinterpret_cast<const uint4*>(k + 64 * i + 16 * cq);
-          codes_half<KT>(w.x, kf[nb][4 * i][0], kf[nb][4 * i][1]);
-          codes_half<KT>(w.y, kf[nb][4 * i + 1][0], kf[nb][4 * i + 1][1]);
-          codes_half<KT>(w.z, kf[nb][4 * i + 2][0], kf[nb][4 * i + 2][1]);
-          codes_half<KT>(w.w, kf[nb][4 * i + 3][0], kf[nb][4 * i + 3][1]);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < KS / 2; ++i) {
-          uint4 w = make_uint4(0, 0, 0, 0);
-          if (real && 32 * i + 8 * cq < c.head_dim)
-            w = *reinterpret_cast<const uint4*>(k + 64 * i + 16 * cq);
-          kf[nb][2 * i][0] = w.x, kf[nb][2 * i][1] = w.y;
-          kf[nb][2 * i + 1][0] = w.z, kf[nb][2 * i + 1][1] = w.w;
-        }
-      }
-      // the scale of the tokens of this lane's columns: eight tokens share a block
-      if constexpr (CODES) ks[nb] = __shfl_sync(0xffffffffu, ks[nb], 0);
+  int64_t t = t0;
+  while (t < t1 && ok) {
+    // ---- a piece: key tiles [j0, j1) of a tile of rows ----
+    const int64_t all = steps(seq);
+    if (t - before >= all) {
+      before += all;
+      ++seq;
+      continue;
     }
-    float col[4][2];
-#pragma unroll
-    for (int nb = 0; nb < 4; ++nb) col[nb][0] = col[nb][1] = 0.f;
-
-    for (int64_t b0 = 0; b0 < rows; b0 += AW_BLOCK) {
-      const int here = (int)min((int64_t)AW_BLOCK, rows - b0);
-      const int tiles = (here + 15) / 16;
-      // ---- rows to shared memory, in the order of the products' operands ----
-      const bool again = staged == (int64_t)seq * c.kv_heads + h && rows <= AW_BLOCK;
-      if (!again) {
-        __syncthreads();
-        for (int tile = warp; tile < tiles; tile += AW_WARPS) {
-          uint4 f[KS];
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const int64_t row = b0 + 16 * tile + r + 8 * x;
-            const int64_t tok = row / group;
-            const int g = (int)(row - tok * group);
-            const char* qp = a.q.data + (q0 + tok) * a.q.token_b + (h * group + g) * a.q.head_b;
-            uint2 raw[KS];
-            float top = 0.f;
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {
-              const int e = aw_element<CODES>(k, cq);
-              raw[k] = row < rows && e < c.head_dim ? *reinterpret_cast<const uint2*>(qp + 2 * e)
-                                                    : make_uint2(0u, 0u);
-              const float2 y = Half2<E>::widen(raw[k].x), z = Half2<E>::widen(raw[k].y);
-              top = fmaxf(fmaxf(fmaxf(top, fabsf(y.x)), fmaxf(fabsf(y.y), fabsf(z.x))), fabsf(z.y));
-            }
-            if constexpr (!std::is_same<E, M>::value) {
-              // bfloat16 to float16: the largest element of a row to [2^14, 2^15)
-              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-              const int e = max(__float_as_int(top) >> 23, 16);
-              const float by = __int_as_float((127 + 14 + 127 - e) << 23);
-              if (cq == 0) s_f[16 * tile + r + 8 * x] = __int_as_float((e - 14) << 23);
-#pragma unroll
-              for (int k = 0; k < KS; ++k) {
-                const float2 y = Half2<E>::widen(raw[k].x), z = Half2<E>::widen(raw[k].y);
-                raw[k].x = Half2<__half>::narrow(y.x * by, y.y * by);
-                raw[k].y = Half2<__half>::narrow(z.x * by, z.y * by);
-              }
-            }
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {
-              if (x == 0) f[k].x = raw[k].x, f[k].z = raw[k].y;
-              else f[k].y = raw[k].x, f[k].w = raw[k].y;
-            }
-          }
-#pragma unroll
-          for (int k = 0; k < KS; ++k) s_q[(tile * KS + k) * 32 + lane] = f[k];
-        }
-        for (int i = threadIdx.x; i < 16 * tiles; i += AW_T)
-          s_see[i] = i >= here ? 0 : a.causal ? len - n + (int)((b0 + i) / group) + 1 : len;
-        if constexpr (SUM)
-          for (int i = threadIdx.x; i < here; i += AW_T) {
-            const int64_t tok = (b0 + i) / group;
-            s_ml[i] = p.stat[(q0 + tok) * a.q_heads + h * group + (int)(b0 + i - tok * group)];
-          }
-        __syncthreads();
+    const int n = ad_steps<AW_TILE>(c, seq);
+    const int64_t item = (t - before) / n, tiles = aw_row_tiles(a, seq);
+    const int j0 = (int)(t - before - item * n), j1 = (int)min((int64_t)n, j0 + t1 - t);
+    const AwHead w(a, seq, (int)(item / tiles));
+    const int64_t tile = item - w.h * tiles, row = tile * AW_TILE + r;
+    aw_stage_rows<E, KT, HD>(a, w, tile, rows_s, s_factor, 1);
+    const int see = w.see(a, row);
+    const int last = min(j1, (w.most(a, tile) + AW_TILE - 1) / AW_TILE);
+    float m = -INFINITY, l = 0.f;
+    AwKeys<E, KT, HD> keys;
+    if (j0 < last) keys.load(a, sc, w, j0 * AW_TILE);
+    __syncthreads();
+    const float factor = s_factor[r], f = factor * cs;
+#pragma unroll 1
+    for (int j = j0; j < last; ++j) {
+      keys.store(keys_s, s_scale);
+      aw_fence();
+      __syncthreads();
+      if (warp == 0) {
+        ap_fence_after();
+        aw_products<E, KT, HD>(lead, tmem, rows_s, keys_s, &bar);
       }
-      staged = (int64_t)seq * c.kv_heads + h;
-
-      for (int tile = 0; tile < tiles && key0 < len; ++tile) {
-        float s[4][4];
+      if (j + 1 < last) keys.load(a, sc, w, (j + 1) * AW_TILE);
+      ok = mbar_wait(&bar, phase);
+      phase ^= 1;
+      ap_fence_after();
+      const int lim = see - j * AW_TILE - col0;  // of the 64 columns, those that the row sees
 #pragma unroll
-        for (int nb = 0; nb < 4; ++nb) s[nb][0] = s[nb][1] = s[nb][2] = s[nb][3] = 0.f;
+      for (int half = 0; half < 2; ++half) {
+        float v[32];
+        ap_ld32(from + 32 * half, v);
+        ap_wait_ld<32>(v);
+        if constexpr (S::CODES) {
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          const uint4 f = s_q[(tile * KS + k) * 32 + lane];
-          const uint32_t q[4] = {f.x, f.y, f.z, f.w};
-#pragma unroll
-          for (int nb = 0; nb < 4; ++nb) mma16816<M>(s[nb], q, kf[nb][k][0], kf[nb][k][1]);
-        }
-        if constexpr (CODES) {
-          const float f0 = std::is_same<E, M>::value ? 1.f : s_f[16 * tile + r];
-          const float f1 = std::is_same<E, M>::value ? 1.f : s_f[16 * tile + r + 8];
-#pragma unroll
-          for (int nb = 0; nb < 4; ++nb) {
-            s[nb][0] *= ks[nb] * f0, s[nb][1] *= ks[nb] * f0;
-            s[nb][2] *= ks[nb] * f1, s[nb][3] *= ks[nb] * f1;
+          for (int i = 0; i < 32; i += 4) {
+            const float4 k = *reinterpret_cast<const float4*>(&s_scale[col0 + 32 * half + i]);
+            v[i] *= k.x, v[i + 1] *= k.y, v[i + 2] *= k.z, v[i + 3] *= k.w;
           }
         }
-        // tokens that each of the two rows sees
-        const int see0 = s_see[16 * tile + r], see1 = s_see[16 * tile + r + 8];
-        bool hide[4][4] = {};
-        if (!__all_sync(0xffffffffu, key0 + 32 <= min(see0, see1))) {
+        if (__any_sync(0xffffffffu, lim < 32 * half + 32)) {
 #pragma unroll
-          for (int nb = 0; nb < 4; ++nb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              hide[nb][i] = key0 + 8 * nb + 2 * cq + (i & 1) >= (i < 2 ? see0 : see1);
-              if (hide[nb][i]) s[nb][i] = -INFINITY;
-            }
+          for (int i = 0; i < 32; ++i)
+            if (32 * half + i >= lim) v[i] = -INFINITY;
         }
-        if constexpr (!SUM) {
+        float top = v[0];
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            float m = -INFINITY, l = 0.f;
+        for (int i = 1; i < 32; ++i) top = fmaxf(top, v[i]);
+        top = fmaxf(m, top);
+        const float base = top == -INFINITY ? 0.f : top;
+        float sum[4] = {l * at_exp2((m - base) * f), 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int nb = 0; nb < 4; ++nb) m = fmaxf(fmaxf(m, s[nb][2 * x]), s[nb][2 * x + 1]);
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 1));
-            m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 2));
-            const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll
-            for (int nb = 0; nb < 4; ++nb)
-              l += at_exp2((s[nb][2 * x] - base) * cs) + at_exp2((s[nb][2 * x + 1] - base) * cs);
-            l += __shfl_xor_sync(0xffffffffu, l, 1);
-            l += __shfl_xor_sync(0xffffffffu, l, 2);
-            if (cq == 0) s_ml[warp * AW_BLOCK + 16 * tile + r + 8 * x] = make_float2(m, l);
-          }
-        } else {
-          const float2 m0 = s_ml[16 * tile + r], m1 = s_ml[16 * tile + r + 8];
-#pragma unroll
-          for (int nb = 0; nb < 4; ++nb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float2 m = i < 2 ? m0 : m1;
-              const float w = at_exp2((s[nb][i] - m.x) * cs) * m.y;
-              col[nb][i & 1] += hide[nb][i] ? 0.f : w;
-            }
-        }
+        for (int i = 0; i < 32; ++i) sum[i & 3] += at_exp2((v[i] - base) * f);
+        l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        m = top;
       }
-      if constexpr (!SUM) {
-        __syncthreads();
-        const int live = min(AW_WARPS, (len - unit * AW_KEYS + 31) / 32);
-        for (int i = threadIdx.x; i < here; i += AW_T) {
-          float m = -INFINITY, l = 0.f;
-          for (int w = 0; w < live; ++w) m = fmaxf(m, s_ml[w * AW_BLOCK + i].x);
-          const float base = m == -INFINITY ? 0.f : m;
-          for (int w = 0; w < live; ++w) {
-            const float2 x = s_ml[w * AW_BLOCK + i];
-            l += x.y * at_exp2((x.x - base) * cs);
-          }
-          const int64_t tok = (b0 + i) / group;
-          const int g = (int)(b0 + i - tok * group);
-          p.part[((q0 + tok) * a.q_heads + h * group + g) * p.units + unit] = make_float2(m, l);
-        }
-        __syncthreads();
-      }
+      ap_fence_before();
+      // scores are read and the keys' tile is free
+      ok = __syncthreads_and(ok);
+      if (!ok) break;
     }
-    if constexpr (SUM) {
-#pragma unroll
-      for (int nb = 0; nb < 4; ++nb)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          float w = col[nb][i];
-#pragma unroll
-          for (int o = 4; o < 32; o <<= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
-          const int x = key0 + 8 * nb + 2 * cq + i;
-          if (r != 0 || x >= len) continue;
-          const int64_t page = c.table[seq * c.table_ld + (x >> c.page_shift)];
-          if (page >= 0 && page < c.num_pages)
-            wv.data[page * wv.page + h * wv.head + (x & ((1 << c.page_shift) - 1))] += w;
-        }
+    if (!ok) {
+      if (threadIdx.x == 0) atomicExch(status, SLS_ERR_TIMEOUT);
+      break;
     }
+    if (warp >= 4) s_ml[r] = make_float2(m, l);
+    __syncthreads();
+    if (warp < 4 && row < w.rows) {
+      const float2 o = s_ml[r];
+      const float top = fmaxf(m, o.x), base = top == -INFINITY ? 0.f : top;
+      l = l * at_exp2((m - base) * f) + o.y * at_exp2((o.x - base) * f);
+      const float2 y = make_float2(top * factor, l);
+      if (j0 == 0 && j1 == n) p.stat[w.packed(a, row)] = y;
+      // the part's first piece goes to slot 0, a later one (its last) to slot 1
+      else p.ml[(int64_t)(2 * blockIdx.x + (t > t0)) * AW_TILE + r] = y;
+    }
+    __syncthreads();
+    t += j1 - j0;
   }
+  aw_free<AW_TILE>(tmem);
 }
 
-// A warp for each row: the sequence's units in order.
-__global__ void __launch_bounds__(AW_T)
+// A warp for each row: its pieces in order.
+__global__ void __launch_bounds__(32 * AW_JOIN_WARPS)
 attention_weights_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ AwPlan p) {
   const CacheView& c = a.c;
   const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * AW_WARPS + (threadIdx.x >> 5);
-  if (row >= a.T * a.q_heads) return;
-  const int64_t t = row / a.q_heads;
+  const int64_t id = (int64_t)blockIdx.x * AW_JOIN_WARPS + (threadIdx.x >> 5);
+  if (id >= a.T * a.q_heads) return;
+  const int64_t t = id / a.q_heads;
   const float cs = a.scale * 1.4426950408889634f;
   at_go();
   at_wait_ahead();
@@ -306,72 +383,248 @@ attention_weights_join_kernel(const __grid_constant__ AttnArgs a, const __grid_c
     seq = __reduce_add_sync(0xffffffffu, ended);
     if (seq >= c.B || t < a.cu[seq]) return;
   }
-  const int units = ad_steps<AW_KEYS>(c, seq);
-  const float2* part = p.part + row * p.units;
+  const int hq = (int)(id - t * a.q_heads);
+  const AwHead w(a, seq, hq / (a.q_heads / c.kv_heads));
+  const int n = ad_steps<AW_TILE>(c, seq);
   float m = -INFINITY, l = 0.f;
-  for (int u = lane; u < units; u += 32) {
-    const float2 x = part[u];
-    const float top = fmaxf(m, x.x), base = top == -INFINITY ? 0.f : top;
-    l = l * at_exp2((m - base) * cs) + x.y * at_exp2((x.x - base) * cs);
-    m = top;
-  }
+  if (n > 0) {
+    const int64_t row = (t - w.q0) * w.group + (hq - w.h * w.group), tile = row / AW_TILE;
+    const int64_t total = p.prefix[c.B];
+    const int parts = (int)min((int64_t)p.ctas, total);
+    const int64_t s0 = p.prefix[seq] + (w.h * aw_row_tiles(a, seq) + tile) * n, s1 = s0 + n;
+    // the part of step x is the last whose start total * g / parts is at most x
+    const int g0 = (int)(((s0 + 1) * parts - 1) / total), g1 = (int)((s1 * parts - 1) / total);
+    if (g0 == g1) {
+      const float2 y = p.stat[id];
+      m = y.x, l = y.y;
+    } else {
+      for (int g = g0 + lane; g <= g1; g += 32) {
+        // the item's first piece is its part's last unless the part starts with it
+        const int late = g == g0 && total * g / parts < s0;
+        const float2 y = p.ml[(int64_t)(2 * g + late) * AW_TILE + (row - tile * AW_TILE)];
+        const float top = fmaxf(m, y.x), base = top == -INFINITY ? 0.f : top;
+        l = l * at_exp2((m - base) * cs) + y.y * at_exp2((y.x - base) * cs);
+        m = top;
+      }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float m2 = __shfl_xor_sync(0xffffffffu, m, o), l2 = __shfl_xor_sync(0xffffffffu, l, o);
-    const float top = fmaxf(m, m2), base = top == -INFINITY ? 0.f : top;
-    // the same order of the two addends in both lanes
-    const float x = l * at_exp2((m - base) * cs), y = l2 * at_exp2((m2 - base) * cs);
-    l = (lane & o) ? y + x : x + y;
-    m = top;
+      for (int o = 16; o > 0; o >>= 1) {
+        const float m2 = __shfl_xor_sync(0xffffffffu, m, o), l2 = __shfl_xor_sync(0xffffffffu, l, o);
+        const float top = fmaxf(m, m2), base = top == -INFINITY ? 0.f : top;
+        // the same order of the two addends in both lanes
+        const float x = l * at_exp2((m - base) * cs), y = l2 * at_exp2((m2 - base) * cs);
+        l = (lane & o) ? y + x : x + y;
+        m = top;
+      }
+    }
   }
-  if (lane == 0) p.stat[row] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.f / l);
+  __syncwarp();
+  if (lane == 0) p.stat[id] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.f / l);
 }
 
-int aw_units(const CacheView& c) {
-  return (int)((((int64_t)c.max_pages << c.page_shift) + AW_KEYS - 1) / AW_KEYS);
-}
-size_t aw_part_bytes(const CacheView& c, int64_t T, int q_heads) {
-  return sls_align256((size_t)T * q_heads * aw_units(c) * 8);
-}
-
+// ---- second pass: sums of columns ----------------------------------------------------------
 template <typename E, typename KT, int HD>
-int launch(const AttnArgs& a, const ScaleView& s, const WeightView& w, void* workspace, cudaStream_t stream) {
+__global__ void __launch_bounds__(AW_T, 2)
+attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ ScaleView sc,
+                             const __grid_constant__ WeightView wv, const __grid_constant__ AwPlan p,
+                             int* status) {
+  using S = AwShape<E, KT, HD>;
+  extern __shared__ __align__(1024) unsigned char smem_raw[];
+  __shared__ int64_t s_pre[AW_T + 1];
+  __shared__ float4 s_row[2 * AW_TILE];  // factor, maximum, one over the sum, tokens seen (an integer)
+  __shared__ float s_scale[AW_TILE], s_sum[AW_TILE];
+  __shared__ uint64_t bar[2];
+  __shared__ uint32_t holder;
+  const CacheView& c = a.c;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const float cs = a.scale * 1.4426950408889634f;
+  unsigned char* rows_s = reinterpret_cast<unsigned char*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  unsigned char* keys_s = rows_s + 2 * S::TILE_BYTES;
+
+  at_wait_ahead();
+  if (threadIdx.x < 2) mbar_init(&bar[threadIdx.x], 1);
+  mbar_fence_init();
+  // sequences without rows have nothing to add
+  const auto steps = [&](int s) {
+    return aw_row_tiles(a, s) == 0 ? (int64_t)0 : (int64_t)ad_steps<AW_TILE>(c, s) * c.kv_heads;
+  };
+  const int R = ad_prefix<AW_T>(c, s_pre, nullptr, steps);
+  const int64_t total = s_pre[AW_T];
+  const int64_t t0 = total * blockIdx.x / gridDim.x, t1 = total * (blockIdx.x + 1) / gridDim.x;
+  if (t0 >= t1) return;
+  const uint32_t tmem = aw_alloc<2 * AW_TILE>(&holder);
+  const uint32_t lead = at_elect();
+  int seq;
+  int64_t before;
+  ad_find<AW_T>(s_pre, R, t0, steps, seq, before);
+  // this thread's token of a tile, and its rows
+  const int r = 32 * (warp & 3) + lane, col0 = 64 * (warp >> 2);
+  const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + col0;
+  unsigned phase[2] = {0, 0};
+  bool ok = true;
+  int64_t staged = -1;  // the pair of row tiles in shared memory, where a head has no more
+
+#pragma unroll 1
+  for (int64_t t = t0; t < t1 && ok; ++t) {
+    while (t - before >= steps(seq)) {
+      before += steps(seq);
+      ++seq;
+    }
+    const int n = ad_steps<AW_TILE>(c, seq);
+    const AwHead w(a, seq, (int)((t - before) / n));
+    const int key0 = (int)(t - before - (int64_t)w.h * n) * AW_TILE, x = key0 + r;
+    const int64_t tiles = (w.rows + AW_TILE - 1) / AW_TILE;
+    AwKeys<E, KT, HD> keys;
+    keys.load(a, sc, w, key0);
+    float col = 0.f;
+    keys.store(keys_s, s_scale);
+#pragma unroll 1
+    for (int64_t b = 0; b < tiles; b += 2) {
+      const int here = (int)min((int64_t)2, tiles - b);
+      if (staged != (int64_t)seq * c.kv_heads + w.h || tiles > 2) {
+        for (int i = 0; i < here; ++i)
+          aw_stage_rows<E, KT, HD>(a, w, b + i, rows_s + i * S::TILE_BYTES, &s_row[i * AW_TILE].x, 4);
+        const int64_t row = b * AW_TILE + threadIdx.x;
+        float2 y = make_float2(0.f, 0.f);
+        if (row < w.rows) y = p.stat[w.packed(a, row)];
+        s_row[threadIdx.x].y = y.x, s_row[threadIdx.x].z = y.y;
+        s_row[threadIdx.x].w = __int_as_float(w.see(a, row));
+        staged = (int64_t)seq * c.kv_heads + w.h;
+      }
+      aw_fence();
+      __syncthreads();
+      // a tile whose last row sees none of these tokens adds nothing
+      bool live[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) live[i] = i < here && w.most(a, b + i) > key0;
+      if (warp == 0) {
+        ap_fence_after();
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (live[i])
+            aw_products<E, KT, HD>(lead, tmem + i * AW_TILE, keys_s, rows_s + i * S::TILE_BYTES, &bar[i]);
+      }
+      const float scale = S::CODES ? s_scale[r] : 1.f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (!live[i]) continue;
+        ok &= mbar_wait(&bar[i], phase[i]);
+        phase[i] ^= 1;
+        ap_fence_after();
+        const float4* rows = s_row + i * AW_TILE + col0;
+        // rows in order see ever more: the first of the 64 sees all of these tokens, or not
+        const bool whole = b * AW_TILE + i * AW_TILE + col0 + 63 < w.rows &&
+                           __float_as_int(rows[0].w) >= key0 + AW_TILE;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          float v[32];
+          ap_ld32(from + i * AW_TILE + 32 * half, v);
+          ap_wait_ld<32>(v);
+          if (whole) {
+#pragma unroll
+            for (int k = 0; k < 32; ++k) {
+              const float4 f = rows[32 * half + k];
+              const float d = S::CODES ? __fmaf_rn(v[k] * scale, f.x, -f.y) : v[k] - f.y;
+              col = __fmaf_rn(at_exp2(d * cs), f.z, col);
+            }
+          } else {
+#pragma unroll
+            for (int k = 0; k < 32; ++k) {
+              const float4 f = rows[32 * half + k];
+              const float d = S::CODES ? __fmaf_rn(v[k] * scale, f.x, -f.y) : v[k] - f.y;
+              const float e = at_exp2(d * cs) * f.z;
+              col += x < __float_as_int(f.w) ? e : 0.f;
+            }
+          }
+        }
+      }
+      ap_fence_before();
+      // scores are read, tiles are free
+      ok = __syncthreads_and(ok);
+      if (!ok) break;
+    }
+    if (!ok) {
+      if (threadIdx.x == 0) atomicExch(status, SLS_ERR_TIMEOUT);
+      break;
+    }
+    if (warp >= 4) s_sum[r] = col;
+    __syncthreads();
+    if (warp < 4 && x < w.len) {
+      const int64_t page = c.table[seq * c.table_ld + (x >> c.page_shift)];
+      if (page >= 0 && page < c.num_pages)
+        wv.data[page * wv.page + w.h * wv.head + (x & ((1 << c.page_shift) - 1))] += col + s_sum[r];
+    }
+  }
+  aw_free<2 * AW_TILE>(tmem);
+}
+
+struct AwHost {
+  int ctas;
+  size_t prefix_b, ml_b, stat_b;
+};
+
+int aw_host(const CacheView& c, int64_t T, int q_heads, AwHost* h) {
   int dev = 0, sms = 0;
   SLS_CUDA_TRY(cudaGetDevice(&dev));
   SLS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  h->ctas = 2 * sms;
+  h->prefix_b = sls_align256(((size_t)c.B + 1) * 8);
+  h->ml_b = sls_align256((size_t)h->ctas * 2 * AW_TILE * 8);
+  h->stat_b = sls_align256((size_t)T * q_heads * 8);
+  return SLS_OK;
+}
+
+template <typename E, typename KT, int HD>
+int launch(const AttnArgs& a, const ScaleView& s, const WeightView& w, const AwHost& h,
+           void* workspace, cudaStream_t stream) {
+  using S = AwShape<E, KT, HD>;
+  static bool set[64] = {};  // per device
+  static int* words[64] = {};
+  int dev = 0;
+  SLS_CUDA_TRY(cudaGetDevice(&dev));
+  constexpr size_t smem1 = 2 * S::TILE_BYTES + 1024, smem2 = 3 * S::TILE_BYTES + 1024;
+  auto first = attention_weights_rows_kernel<E, KT, HD>;
+  auto second = attention_weights_sum_kernel<E, KT, HD>;
+  if (dev >= 64 || !set[dev]) {
+    SLS_CUDA_TRY(cudaFuncSetAttribute(first, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem1));
+    SLS_CUDA_TRY(
+        cudaFuncSetAttribute(second, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem2));
+  }
+  int* word = dev < 64 ? words[dev] : nullptr;
+  if (!word) {
+    const int st = decode_status_word(&word);
+    if (st != SLS_OK) return st;
+  }
+  if (dev < 64) words[dev] = word, set[dev] = true;
   AwPlan p;
-  p.units = aw_units(a.c);
-  p.part = (float2*)workspace;
-  p.stat = (float2*)((char*)workspace + aw_part_bytes(a.c, a.T, a.q_heads));
-  const int64_t most = (int64_t)a.c.B * p.units * a.c.kv_heads;
-  const unsigned grid = (unsigned)std::min<int64_t>(most, 2 * sms);
-  constexpr size_t rows = (size_t)AW_TILES * (HD / 16) * 512 + AW_BLOCK * 8;
-  constexpr size_t smem1 = rows + AW_WARPS * AW_BLOCK * 8, smem2 = rows + AW_BLOCK * 8;
-  auto first = attention_weights_kernel<E, KT, HD, false>;
-  auto second = attention_weights_kernel<E, KT, HD, true>;
-  SLS_CUDA_TRY(cudaFuncSetAttribute(first, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem1));
-  SLS_CUDA_TRY(
-      cudaFuncSetAttribute(second, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem2));
-  int st = at_launch(first, dim3(grid), AW_T, smem1, 1, stream, a, s, w, p);
+  char* at = (char*)workspace;
+  p.ctas = h.ctas;
+  p.prefix = (int64_t*)at;
+  p.ml = (float2*)(at += h.prefix_b);
+  p.stat = (float2*)(at + h.ml_b);
+  int st = at_launch(first, dim3((unsigned)h.ctas), AW_T, smem1, 1, stream, a, s, p, word);
   if (st != SLS_OK) return st;
   const int64_t all = a.T * a.q_heads;
-  st = at_launch(attention_weights_join_kernel, dim3((unsigned)((all + AW_WARPS - 1) / AW_WARPS)),
-                 AW_T, 0, 1, stream, a, p);
+  st = at_launch(attention_weights_join_kernel,
+                 dim3((unsigned)((all + AW_JOIN_WARPS - 1) / AW_JOIN_WARPS)), 32 * AW_JOIN_WARPS, 0, 1,
+                 stream, a, p);
   if (st != SLS_OK) return st;
-  return at_launch(second, dim3(grid), AW_T, smem2, 1, stream, a, s, w, p);
+  return at_launch(second, dim3((unsigned)h.ctas), AW_T, smem2, 1, stream, a, s, w, p, word);
 }
 
 template <typename E, typename KT>
-int launch(const AttnArgs& a, const ScaleView& s, const WeightView& w, void* workspace, cudaStream_t stream) {
-  return a.c.head_dim > 64 ? launch<E, KT, 128>(a, s, w, workspace, stream)
-                           : launch<E, KT, 64>(a, s, w, workspace, stream);
+int launch(const AttnArgs& a, const ScaleView& s, const WeightView& w, const AwHost& h,
+           void* workspace, cudaStream_t stream) {
+  return a.c.head_dim > 64 ? launch<E, KT, 128>(a, s, w, h, workspace, stream)
+                           : launch<E, KT, 64>(a, s, w, h, workspace, stream);
 }
 
 template <typename E>
-int launch(const AttnArgs& a, const ScaleView& s, const WeightView& w, int code, void* workspace, cudaStream_t stream) {
-  return code == SLS_I8     ? launch<E, I8>(a, s, w, workspace, stream)
-         : code == SLS_E4M3 ? launch<E, E4M3>(a, s, w, workspace, stream)
-                            : launch<E, E>(a, s, w, workspace, stream);
+int launch(const AttnArgs& a, const ScaleView& s, const WeightView& w, int code, const AwHost& h,
+           void* workspace, cudaStream_t stream) {
+  return code == SLS_I8     ? launch<E, I8>(a, s, w, h, workspace, stream)
+         : code == SLS_E4M3 ? launch<E, E4M3>(a, s, w, h, workspace, stream)
+                            : launch<E, E>(a, s, w, h, workspace, stream);
 }
 
 }  // namespace
@@ -380,17 +633,21 @@ size_t attention_weights_workspace(const CacheView& c, int64_t T, int q_heads, i
   if (c.B == 0 || T == 0 || c.max_pages == 0) return 0;
   if (attention_weights_few(c, T, q_heads, code))
     return attention_weights_few_workspace(c, T, q_heads);
-  return aw_part_bytes(c, T, q_heads) + sls_align256((size_t)T * q_heads * 8);
+  AwHost h;
+  return aw_host(c, T, q_heads, &h) == SLS_OK ? h.prefix_b + h.ml_b + h.stat_b : 0;
 }
 
 int launch_attention_weights(const AttnArgs& a, const ScaleView& s, const WeightView& w, int code,
                              int dtype, void* workspace, cudaStream_t stream) {
   if (a.c.B == 0 || a.T == 0 || a.c.max_pages == 0) return SLS_OK;
-  if (a.T * a.q_heads > (int64_t)0x7fffffff * AW_WARPS) return SLS_ERR_UNSUPPORTED;
+  if (a.T * a.q_heads > (int64_t)0x7fffffff * AW_JOIN_WARPS) return SLS_ERR_UNSUPPORTED;
   if (attention_weights_few(a.c, a.T, a.q_heads, code))
     return launch_attention_weights_few(a, s, w, code, dtype, workspace, stream);
-  return dtype == SLS_BF16 ? launch<__nv_bfloat16>(a, s, w, code, workspace, stream)
-                           : launch<__half>(a, s, w, code, workspace, stream);
+  AwHost h;
+  const int st = aw_host(a.c, a.T, a.q_heads, &h);
+  if (st != SLS_OK) return st;
+  return dtype == SLS_BF16 ? launch<__nv_bfloat16>(a, s, w, code, h, workspace, stream)
+                           : launch<__half>(a, s, w, code, h, workspace, stream);
 }
 
 }  // namespace sls
