@@ -138,12 +138,6 @@ SLS_DEV void ap_st16(uint32_t addr, const uint32_t* u) {
 }
 SLS_DEV void ap_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-SLS_DEV float ap_max3(float a, float b, float c) {
-  float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-  return d;
-}
-
 // Bounded wait of a whole warp; false when the time is up or another role gave up.
 SLS_DEV bool ap_wait(uint64_t* bar, unsigned parity, volatile int* abort_flag) {
   bool ok = mbar_try_wait(bar, parity);

@@ -9,6 +9,9 @@
 // token's column, with the rows' maxima and sums read from shared memory by all at once.  No sum is
 // made by atomics: the same call gives the same bits.
 //
+// The exponent of a weight is formed by one multiply-add, score times scale less the row's maximum and
+// the logarithm of its sum: rounded by 2^-24 of the score, as the score itself is.
+//
 // Bound by exponentials (two a score) and, for few rows, by the products of padded tiles; the keys'
 // bytes are below either from some ten rows on.  A CTA goes through phases in step (keys to shared
 // memory, codes to float16 on the way; products; scores), with the next keys on their way in
@@ -33,10 +36,11 @@ constexpr int AW_TILE = 128;  // rows or tokens
 constexpr int AW_JOIN_WARPS = 8;
 
 struct AwPlan {
+  int group;        // query heads of a key head
   int ctas;         // of the first pass: most parts
   int64_t* prefix;  // B + 1: first-pass steps before every sequence
   float2* ml;       // (part, first or last piece, row of a tile): maximum and sum
-  float2* stat;     // (token, query head): maximum; sum, then one over it
+  float2* stat;     // (token, query head): maximum, sum; then what makes the weight of a score
 };
 
 // KT: element of keys (E, or codes)
@@ -66,35 +70,59 @@ SLS_DEV void aw_tokens(const AttnArgs& a, int seq, int64_t& q0, int64_t& q1) {
   else q0 = seq, q1 = seq + 1;
 }
 
-SLS_DEV int64_t aw_row_tiles(const AttnArgs& a, int seq) {
+SLS_DEV int64_t aw_row_tiles(const AttnArgs& a, int group, int seq) {
   int64_t q0, q1;
   aw_tokens(a, seq, q0, q1);
-  return ((q1 - q0) * (a.q_heads / a.c.kv_heads) + AW_TILE - 1) / AW_TILE;
+  return ((q1 - q0) * group + AW_TILE - 1) >> 7;
+}
+
+// x / y, in 32 bits where that is enough: a division in 64 takes some hundred instructions, which
+// is what a tile's scores take
+SLS_DEV int64_t aw_div(int64_t x, int y) {
+  return (uint64_t)x >> 32 ? x / y : (int64_t)((unsigned)x / (unsigned)y);
 }
 
 // A key head of a sequence.
 struct AwHead {
   int seq, h, len, n, group;
   int64_t q0, rows;
-  SLS_DEV AwHead(const AttnArgs& a, int s, int head) : seq(s), h(head) {
+  SLS_DEV AwHead(const AttnArgs& a, int g, int s, int head) : seq(s), h(head), group(g) {
     len = (int)cache_len(a.c, s);
     int64_t q1;
     aw_tokens(a, s, q0, q1);
     n = (int)(q1 - q0);
-    group = a.q_heads / a.c.kv_heads;
     rows = (int64_t)n * group;
   }
-  // tokens that row `row` sees
-  SLS_DEV int see(const AttnArgs& a, int64_t row) const {
-    return row >= rows ? 0 : a.causal ? max(0, len - n + (int)(row / group) + 1) : len;
+};
+
+// A tile of its rows.
+struct AwRows {
+  int count;     // rows of the tile
+  int tok, rem;  // the first row's token, and which of its query heads
+  int mul;       // x / group = x * mul >> 16 for x < 256
+  SLS_DEV AwRows(const AwHead& w, int64_t tile) {
+    const int64_t base = tile * AW_TILE;
+    count = (int)max((int64_t)0, min((int64_t)AW_TILE, w.rows - base));
+    tok = (int)aw_div(base, w.group);
+    rem = (int)(base - (int64_t)tok * w.group);
+    mul = (65536 + w.group - 1) / w.group;
   }
-  // most tokens that a row of a tile sees
-  SLS_DEV int most(const AttnArgs& a, int64_t tile) const {
-    return see(a, min(rows, (tile + 1) * AW_TILE) - 1);
+  // token and query head of row r of the tile
+  SLS_DEV int token(int r, const AwHead& w, int& g) const {
+    const int d = ((rem + r) * mul) >> 16;
+    g = rem + r - d * w.group;
+    return tok + d;
   }
-  SLS_DEV int64_t packed(const AttnArgs& a, int64_t row) const {  // its (token, query head)
-    const int64_t tok = row / group;
-    return (q0 + tok) * a.q_heads + h * group + (row - tok * group);
+  // tokens of the cache that it sees
+  SLS_DEV int see(const AttnArgs& a, const AwHead& w, int r) const {
+    int g;
+    return r >= count ? 0 : a.causal ? max(0, w.len - w.n + token(r, w, g) + 1) : w.len;
+  }
+  // its (token, query head) among all
+  SLS_DEV int64_t packed(const AttnArgs& a, const AwHead& w, int r) const {
+    int g;
+    const int t = token(r, w, g);
+    return (w.q0 + t) * a.q_heads + w.h * w.group + g;
   }
 };
 
@@ -153,21 +181,21 @@ struct AwKeys {
 };
 
 // A tile of rows to shared memory; factors (codes with bfloat16 queries: a row's power of two, as in
-// the decode kernel) to `factor`, `stride` floats apart.
+// the decode kernel) to `factor`.
 template <typename E, typename KT, int HD>
-SLS_DEV void aw_stage_rows(const AttnArgs& a, const AwHead& w, int64_t tile, unsigned char* out,
-                           float* factor, int stride) {
+SLS_DEV void aw_stage_rows(const AttnArgs& a, const AwHead& w, const AwRows& rows,
+                           unsigned char* out, float* factor) {
   using S = AwShape<E, KT, HD>;
   const int ch = threadIdx.x % S::ROW_LANES;
 #pragma unroll
   for (int i = 0; i < S::ROW_LOADS; ++i) {
     const int r = i * (AW_T / S::ROW_LANES) + threadIdx.x / S::ROW_LANES;
-    const int64_t row = tile * AW_TILE + r;
     uint4 u = make_uint4(0, 0, 0, 0);
-    if (row < w.rows && 8 * ch < a.c.head_dim) {
-      const int64_t tok = row / w.group;
+    if (r < rows.count && 8 * ch < a.c.head_dim) {
+      int g;
+      const int tok = rows.token(r, w, g);
       u = *reinterpret_cast<const uint4*>(a.q.data + (w.q0 + tok) * a.q.token_b +
-                                          (w.h * w.group + (row - tok * w.group)) * a.q.head_b + 16 * ch);
+                                          (w.h * w.group + g) * a.q.head_b + 16 * ch);
     }
     float back = 1.f;
     if constexpr (!std::is_same<E, typename S::M>::value) {
@@ -186,7 +214,7 @@ SLS_DEV void aw_stage_rows(const AttnArgs& a, const AwHead& w, int64_t tile, uns
       u = narrow8<__half>(x);
     }
     *reinterpret_cast<uint4*>(out + S::at(r, ch)) = u;
-    if (ch == 0) factor[r * stride] = back;
+    if (ch == 0) factor[r] = back;
   }
 }
 
@@ -242,9 +270,10 @@ attention_weights_rows_kernel(const __grid_constant__ AttnArgs a,
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   __shared__ int64_t s_pre[AW_T + 1];
   __shared__ float s_factor[AW_TILE];
-  __shared__ __align__(16) float s_scale[AW_TILE];
+  // of four tiles: a thread may fetch two ahead of one that still reads
+  __shared__ __align__(16) float s_scale[4][AW_TILE];
   __shared__ float2 s_ml[AW_TILE];
-  __shared__ uint64_t bar;
+  __shared__ uint64_t bar[2];
   __shared__ uint32_t holder;
   const CacheView& c = a.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -254,17 +283,17 @@ attention_weights_rows_kernel(const __grid_constant__ AttnArgs a,
   unsigned char* keys_s = rows_s + S::TILE_BYTES;
 
   at_wait_ahead();
-  if (threadIdx.x == 0) mbar_init(&bar, 1);
+  if (threadIdx.x < 2) mbar_init(&bar[threadIdx.x], 1);
   mbar_fence_init();
   const auto steps = [&](int s) {
-    return (int64_t)ad_steps<AW_TILE>(c, s) * aw_row_tiles(a, s) * c.kv_heads;
+    return (int64_t)ad_steps<AW_TILE>(c, s) * aw_row_tiles(a, p.group, s) * c.kv_heads;
   };
   const int R = ad_prefix<AW_T>(c, s_pre, p.prefix, steps);
   const int64_t total = s_pre[AW_T];
   const int parts = (int)min((int64_t)p.ctas, total);
   if ((int)blockIdx.x >= parts) return;
   const int64_t t0 = total * blockIdx.x / parts, t1 = total * (blockIdx.x + 1) / parts;
-  const uint32_t tmem = aw_alloc<AW_TILE>(&holder);
+  const uint32_t tmem = aw_alloc<2 * AW_TILE>(&holder);
   const uint32_t lead = at_elect();
   int seq;
   int64_t before;  // steps before seq
@@ -272,7 +301,7 @@ attention_weights_rows_kernel(const __grid_constant__ AttnArgs a,
   // this thread's row of a tile, and its columns
   const int r = 32 * (warp & 3) + lane, col0 = 64 * (warp >> 2);
   const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + col0;
-  unsigned phase = 0;
+  unsigned turn = 0;  // tiles of keys so far: they take turns at memory, columns and barriers
   bool ok = true;
 
   int64_t t = t0;
@@ -285,41 +314,53 @@ attention_weights_rows_kernel(const __grid_constant__ AttnArgs a,
       continue;
     }
     const int n = ad_steps<AW_TILE>(c, seq);
-    const int64_t item = (t - before) / n, tiles = aw_row_tiles(a, seq);
+    const int64_t item = aw_div(t - before, n), tiles = aw_row_tiles(a, p.group, seq);
     const int j0 = (int)(t - before - item * n), j1 = (int)min((int64_t)n, j0 + t1 - t);
-    const AwHead w(a, seq, (int)(item / tiles));
-    const int64_t tile = item - w.h * tiles, row = tile * AW_TILE + r;
-    aw_stage_rows<E, KT, HD>(a, w, tile, rows_s, s_factor, 1);
-    const int see = w.see(a, row);
-    const int last = min(j1, (w.most(a, tile) + AW_TILE - 1) / AW_TILE);
+    const int h = (int)(tiles >> 31 ? item / tiles : aw_div(item, (int)tiles));
+    const AwHead w(a, p.group, seq, h);
+    const AwRows rows(w, item - h * tiles);
+    aw_stage_rows<E, KT, HD>(a, w, rows, rows_s, s_factor);
+    const int see = rows.see(a, w, r);
+    // tokens that the last row sees, and so any
+    const int last = min(j1, (rows.see(a, w, rows.count - 1) + AW_TILE - 1) / AW_TILE);
     float m = -INFINITY, l = 0.f;
     AwKeys<E, KT, HD> keys;
-    if (j0 < last) keys.load(a, sc, w, j0 * AW_TILE);
-    __syncthreads();
-    const float factor = s_factor[r], f = factor * cs;
-#pragma unroll 1
-    for (int j = j0; j < last; ++j) {
-      keys.store(keys_s, s_scale);
+    // products of the next tile run while the scores of one are worked on
+    auto next = [&](int j, unsigned k) {
+      keys.store(keys_s + (k & 1) * S::TILE_BYTES, s_scale[k & 3]);
       aw_fence();
-      __syncthreads();
+      __syncthreads();  // and the scores that were in these columns are read
       if (warp == 0) {
         ap_fence_after();
-        aw_products<E, KT, HD>(lead, tmem, rows_s, keys_s, &bar);
+        aw_products<E, KT, HD>(lead, tmem + (k & 1) * AW_TILE, rows_s, keys_s + (k & 1) * S::TILE_BYTES,
+                               &bar[k & 1]);
       }
       if (j + 1 < last) keys.load(a, sc, w, (j + 1) * AW_TILE);
-      ok = mbar_wait(&bar, phase);
-      phase ^= 1;
+    };
+    if (j0 < last) {
+      keys.load(a, sc, w, j0 * AW_TILE);
+      next(j0, turn);
+    } else {
+      __syncthreads();
+    }
+    const float factor = s_factor[r], f = factor * cs;
+#pragma unroll 1
+    for (int j = j0; j < last; ++j, ++turn) {
+      if (j + 1 < last) next(j + 1, turn + 1);
+      if (ok) ok = mbar_wait(&bar[turn & 1], (turn >> 1) & 1);
       ap_fence_after();
+      const uint32_t at = from + (turn & 1) * AW_TILE;
+      const float* scales = s_scale[turn & 3] + col0;
       const int lim = see - j * AW_TILE - col0;  // of the 64 columns, those that the row sees
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
+#pragma unroll 1
+      for (int half = 0; half < 2 && 32 * (warp & 3) < rows.count; ++half) {
         float v[32];
-        ap_ld32(from + 32 * half, v);
+        ap_ld32(at + 32 * half, v);
         ap_wait_ld<32>(v);
         if constexpr (S::CODES) {
 #pragma unroll
           for (int i = 0; i < 32; i += 4) {
-            const float4 k = *reinterpret_cast<const float4*>(&s_scale[col0 + 32 * half + i]);
+            const float4 k = *reinterpret_cast<const float4*>(scales + 32 * half + i);
             v[i] *= k.x, v[i + 1] *= k.y, v[i + 2] *= k.z, v[i + 3] *= k.w;
           }
         }
@@ -328,41 +369,39 @@ attention_weights_rows_kernel(const __grid_constant__ AttnArgs a,
           for (int i = 0; i < 32; ++i)
             if (32 * half + i >= lim) v[i] = -INFINITY;
         }
-        float top = v[0];
+        float top = ap_max3(v[0], v[1], v[2]);
 #pragma unroll
-        for (int i = 1; i < 32; ++i) top = fmaxf(top, v[i]);
-        top = fmaxf(m, top);
-        const float base = top == -INFINITY ? 0.f : top;
-        float sum[4] = {l * at_exp2((m - base) * f), 0.f, 0.f, 0.f};
+        for (int i = 3; i < 31; i += 2) top = ap_max3(top, v[i], v[i + 1]);
+        top = ap_max3(top, v[31], m);
+        const float base = top == -INFINITY ? 0.f : top, off = -base * f;
+        float sum[4] = {l * at_exp2(__fmaf_rn(m, f, off)), 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < 32; ++i) sum[i & 3] += at_exp2((v[i] - base) * f);
+        for (int i = 0; i < 32; ++i) sum[i & 3] += at_exp2(__fmaf_rn(v[i], f, off));
         l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
         m = top;
       }
       ap_fence_before();
-      // scores are read and the keys' tile is free
-      ok = __syncthreads_and(ok);
-      if (!ok) break;
     }
+    ok = __syncthreads_and(ok);
     if (!ok) {
       if (threadIdx.x == 0) atomicExch(status, SLS_ERR_TIMEOUT);
       break;
     }
     if (warp >= 4) s_ml[r] = make_float2(m, l);
     __syncthreads();
-    if (warp < 4 && row < w.rows) {
+    if (warp < 4 && r < rows.count) {
       const float2 o = s_ml[r];
       const float top = fmaxf(m, o.x), base = top == -INFINITY ? 0.f : top;
       l = l * at_exp2((m - base) * f) + o.y * at_exp2((o.x - base) * f);
       const float2 y = make_float2(top * factor, l);
-      if (j0 == 0 && j1 == n) p.stat[w.packed(a, row)] = y;
+      if (j0 == 0 && j1 == n) p.stat[rows.packed(a, w, r)] = y;
       // the part's first piece goes to slot 0, a later one (its last) to slot 1
       else p.ml[(int64_t)(2 * blockIdx.x + (t > t0)) * AW_TILE + r] = y;
     }
     __syncthreads();
     t += j1 - j0;
   }
-  aw_free<AW_TILE>(tmem);
+  aw_free<2 * AW_TILE>(tmem);
 }
 
 // A warp for each row: its pieces in order.
@@ -384,14 +423,14 @@ attention_weights_join_kernel(const __grid_constant__ AttnArgs a, const __grid_c
     if (seq >= c.B || t < a.cu[seq]) return;
   }
   const int hq = (int)(id - t * a.q_heads);
-  const AwHead w(a, seq, hq / (a.q_heads / c.kv_heads));
+  const AwHead w(a, p.group, seq, hq / p.group);
   const int n = ad_steps<AW_TILE>(c, seq);
   float m = -INFINITY, l = 0.f;
   if (n > 0) {
-    const int64_t row = (t - w.q0) * w.group + (hq - w.h * w.group), tile = row / AW_TILE;
+    const int64_t row = (t - w.q0) * w.group + (hq - w.h * w.group), tile = row >> 7;
     const int64_t total = p.prefix[c.B];
     const int parts = (int)min((int64_t)p.ctas, total);
-    const int64_t s0 = p.prefix[seq] + (w.h * aw_row_tiles(a, seq) + tile) * n, s1 = s0 + n;
+    const int64_t s0 = p.prefix[seq] + (w.h * aw_row_tiles(a, p.group, seq) + tile) * n, s1 = s0 + n;
     // the part of step x is the last whose start total * g / parts is at most x
     const int g0 = (int)(((s0 + 1) * parts - 1) / total), g1 = (int)((s1 * parts - 1) / total);
     if (g0 == g1) {
@@ -418,7 +457,8 @@ attention_weights_join_kernel(const __grid_constant__ AttnArgs a, const __grid_c
     }
   }
   __syncwarp();
-  if (lane == 0) p.stat[id] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.f / l);
+  // 2^(score cs + this) is the weight
+  if (lane == 0) p.stat[id].x = l == 0.f ? -INFINITY : -m * cs - log2f(l);
 }
 
 // ---- second pass: sums of columns ----------------------------------------------------------
@@ -430,7 +470,9 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
   using S = AwShape<E, KT, HD>;
   extern __shared__ __align__(1024) unsigned char smem_raw[];
   __shared__ int64_t s_pre[AW_T + 1];
-  __shared__ float4 s_row[2 * AW_TILE];  // factor, maximum, one over the sum, tokens seen (an integer)
+  __shared__ float s_factor[2 * AW_TILE];
+  __shared__ __align__(16) float2 s_row[2 * AW_TILE];  // factor and summand of a row's exponents
+  __shared__ __align__(16) int s_see[2 * AW_TILE];     // tokens that it sees
   __shared__ float s_scale[AW_TILE], s_sum[AW_TILE];
   __shared__ uint64_t bar[2];
   __shared__ uint32_t holder;
@@ -446,7 +488,7 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
   mbar_fence_init();
   // sequences without rows have nothing to add
   const auto steps = [&](int s) {
-    return aw_row_tiles(a, s) == 0 ? (int64_t)0 : (int64_t)ad_steps<AW_TILE>(c, s) * c.kv_heads;
+    return aw_row_tiles(a, p.group, s) == 0 ? (int64_t)0 : (int64_t)ad_steps<AW_TILE>(c, s) * c.kv_heads;
   };
   const int R = ad_prefix<AW_T>(c, s_pre, nullptr, steps);
   const int64_t total = s_pre[AW_T];
@@ -461,99 +503,154 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
   const int r = 32 * (warp & 3) + lane, col0 = 64 * (warp >> 2);
   const uint32_t from = tmem + ((uint32_t)(warp & 3) << 21) + col0;
   unsigned phase[2] = {0, 0};
-  bool ok = true;
-  int64_t staged = -1;  // the pair of row tiles in shared memory, where a head has no more
-
-#pragma unroll 1
-  for (int64_t t = t0; t < t1 && ok; ++t) {
+  bool ok = true, live[2];
+  AwKeys<E, KT, HD> keys;
+  int key0;
+  auto unit = [&](int64_t t) {  // a unit's keys to registers
     while (t - before >= steps(seq)) {
       before += steps(seq);
       ++seq;
     }
-    const int n = ad_steps<AW_TILE>(c, seq);
-    const AwHead w(a, seq, (int)((t - before) / n));
-    const int key0 = (int)(t - before - (int64_t)w.h * n) * AW_TILE, x = key0 + r;
-    const int64_t tiles = (w.rows + AW_TILE - 1) / AW_TILE;
-    AwKeys<E, KT, HD> keys;
+    const int n = ad_steps<AW_TILE>(c, seq), h = (int)aw_div(t - before, n);
+    key0 = (int)(t - before - (int64_t)h * n) * AW_TILE;
+    const AwHead w(a, p.group, seq, h);
     keys.load(a, sc, w, key0);
-    float col = 0.f;
-    keys.store(keys_s, s_scale);
+    return w;
+  };
+  // two tiles of rows (or one) to shared memory
+  auto stage = [&](const AwHead& w, const AwRows& r0, const AwRows& r1) {
+    aw_stage_rows<E, KT, HD>(a, w, r0, rows_s, s_factor);
+    if (r1.count > 0) aw_stage_rows<E, KT, HD>(a, w, r1, rows_s + S::TILE_BYTES, s_factor + AW_TILE);
+    const int k = threadIdx.x & (AW_TILE - 1);
+    const AwRows& mine = threadIdx.x < AW_TILE ? r0 : r1;
+    float add = -INFINITY;
+    if (k < mine.count) add = p.stat[mine.packed(a, w, k)].x;
+    __syncthreads();
+    s_row[threadIdx.x] = make_float2(s_factor[threadIdx.x] * cs, add);
+    s_see[threadIdx.x] = mine.see(a, w, k);
+  };
+  // products of a tile; one whose last row sees none of the tokens adds nothing
+  auto issue = [&](int i, const AwHead& w, const AwRows& rows, int start) {
+    live[i] = rows.count > 0 && rows.see(a, w, rows.count - 1) > start;
+    if (live[i] && warp == 0) {
+      ap_fence_after();
+      aw_products<E, KT, HD>(lead, tmem + i * AW_TILE, keys_s, rows_s + i * S::TILE_BYTES, &bar[i]);
+    }
+  };
+  auto wait = [&](int i) {
+    if (!live[i]) return;
+    if (ok) ok = mbar_wait(&bar[i], phase[i]);
+    phase[i] ^= 1;
+    ap_fence_after();
+  };
+  float col[4];
+  auto add = [&](int i, int count, int start, float scale) {
+    const int row0 = i * AW_TILE + col0, x = start + r;
+    // rows in order see ever more: the first of the 64 sees all of these tokens, or not
+    const bool whole = col0 + 63 < count && s_see[row0] >= start + AW_TILE;
 #pragma unroll 1
-    for (int64_t b = 0; b < tiles; b += 2) {
-      const int here = (int)min((int64_t)2, tiles - b);
-      if (staged != (int64_t)seq * c.kv_heads + w.h || tiles > 2) {
-        for (int i = 0; i < here; ++i)
-          aw_stage_rows<E, KT, HD>(a, w, b + i, rows_s + i * S::TILE_BYTES, &s_row[i * AW_TILE].x, 4);
-        const int64_t row = b * AW_TILE + threadIdx.x;
-        float2 y = make_float2(0.f, 0.f);
-        if (row < w.rows) y = p.stat[w.packed(a, row)];
-        s_row[threadIdx.x].y = y.x, s_row[threadIdx.x].z = y.y;
-        s_row[threadIdx.x].w = __int_as_float(w.see(a, row));
-        staged = (int64_t)seq * c.kv_heads + w.h;
-      }
-      aw_fence();
-      __syncthreads();
-      // a tile whose last row sees none of these tokens adds nothing
-      bool live[2];
+    for (int half = 0; half < 64 && col0 + half < count; half += 32) {
+      float v[32];
+      ap_ld32(from + i * AW_TILE + half, v);
+      ap_wait_ld<32>(v);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) live[i] = i < here && w.most(a, b + i) > key0;
-      if (warp == 0) {
-        ap_fence_after();
+      for (int k = 0; k < 32; k += 4) {
+        const float4 f = *reinterpret_cast<const float4*>(&s_row[row0 + half + k]);
+        const float4 g = *reinterpret_cast<const float4*>(&s_row[row0 + half + k + 2]);
+        if constexpr (S::CODES) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-          if (live[i])
-            aw_products<E, KT, HD>(lead, tmem + i * AW_TILE, keys_s, rows_s + i * S::TILE_BYTES, &bar[i]);
-      }
-      const float scale = S::CODES ? s_scale[r] : 1.f;
+          for (int j = 0; j < 4; ++j) v[k + j] *= scale;
+        }
+        const float e[4] = {at_exp2(__fmaf_rn(v[k], f.x, f.y)), at_exp2(__fmaf_rn(v[k + 1], f.z, f.w)),
+                            at_exp2(__fmaf_rn(v[k + 2], g.x, g.y)),
+                            at_exp2(__fmaf_rn(v[k + 3], g.z, g.w))};
+        if (whole) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (!live[i]) continue;
-        ok &= mbar_wait(&bar[i], phase[i]);
-        phase[i] ^= 1;
-        ap_fence_after();
-        const float4* rows = s_row + i * AW_TILE + col0;
-        // rows in order see ever more: the first of the 64 sees all of these tokens, or not
-        const bool whole = b * AW_TILE + i * AW_TILE + col0 + 63 < w.rows &&
-                           __float_as_int(rows[0].w) >= key0 + AW_TILE;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          float v[32];
-          ap_ld32(from + i * AW_TILE + 32 * half, v);
-          ap_wait_ld<32>(v);
-          if (whole) {
-#pragma unroll
-            for (int k = 0; k < 32; ++k) {
-              const float4 f = rows[32 * half + k];
-              const float d = S::CODES ? __fmaf_rn(v[k] * scale, f.x, -f.y) : v[k] - f.y;
-              col = __fmaf_rn(at_exp2(d * cs), f.z, col);
-            }
-          } else {
-#pragma unroll
-            for (int k = 0; k < 32; ++k) {
-              const float4 f = rows[32 * half + k];
-              const float d = S::CODES ? __fmaf_rn(v[k] * scale, f.x, -f.y) : v[k] - f.y;
-              const float e = at_exp2(d * cs) * f.z;
-              col += x < __float_as_int(f.w) ? e : 0.f;
-            }
-          }
+          for (int j = 0; j < 4; ++j) col[j] += e[j];
+        } else {
+          const int4 see = *reinterpret_cast<const int4*>(&s_see[row0 + half + k]);
+          col[0] += x < see.x ? e[0] : 0.f, col[1] += x < see.y ? e[1] : 0.f;
+          col[2] += x < see.z ? e[2] : 0.f, col[3] += x < see.w ? e[3] : 0.f;
         }
       }
-      ap_fence_before();
-      // scores are read, tiles are free
-      ok = __syncthreads_and(ok);
-      if (!ok) break;
     }
+    ap_fence_before();
+  };
+
+  // The first two tiles of rows of a head stay in shared memory from unit to unit, and the products
+  // of a unit's first tile run while the scores of the last unit's second are worked on.
+  AwHead next = unit(t0);
+  bool begin = true;
+  float scale = 1.f;
+#pragma unroll 1
+  for (int64_t t = t0; t < t1; ++t) {
+    const AwHead w = next;
+    const int start = key0, x = start + r;
+    const int64_t tiles = (w.rows + AW_TILE - 1) >> 7;
+    const AwRows r0(w, 0), r1(w, 1);
+    if (begin) {
+      stage(w, r0, r1);
+      keys.store(keys_s, s_scale);
+      aw_fence();
+      __syncthreads();
+      issue(0, w, r0, start);
+      issue(1, w, r1, start);
+      if constexpr (S::CODES) scale = s_scale[r];
+    }
+    const float mine = scale;
+    // the token's weight so far, and the next unit's keys
+    float* to = nullptr;
+    float was = 0.f;
+    if (warp < 4 && x < w.len) {
+      const int64_t page = c.table[w.seq * c.table_ld + (x >> c.page_shift)];
+      if (page >= 0 && page < c.num_pages) {
+        to = wv.data + page * wv.page + w.h * wv.head + (x & ((1 << c.page_shift) - 1));
+        was = *to;
+      }
+    }
+    if (t + 1 < t1) next = unit(t + 1);
+    const bool same = t + 1 < t1 && next.seq == w.seq && next.h == w.h && tiles <= 2;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) col[j] = 0.f;
+    wait(0);
+    if (live[0]) add(0, r0.count, start, mine);
+    wait(1);
+    const bool second = live[1];
+    if (same) {
+      // the unit's products are done: its keys' place is free; at the barrier so are the first
+      // tile's columns
+      keys.store(keys_s, s_scale);
+      aw_fence();
+      __syncthreads();
+      issue(0, w, r0, key0);
+      if constexpr (S::CODES) scale = s_scale[r];
+    }
+    if (second) add(1, r1.count, start, mine);
+#pragma unroll 1
+    for (int64_t b = 2; b < tiles; b += 2) {
+      const AwRows a0(w, b), a1(w, b + 1);
+      __syncthreads();
+      stage(w, a0, a1);
+      aw_fence();
+      __syncthreads();
+      issue(0, w, a0, start);
+      issue(1, w, a1, start);
+      wait(0);
+      if (live[0]) add(0, a0.count, start, mine);
+      wait(1);
+      if (live[1]) add(1, a1.count, start, mine);
+    }
+    const float sum = (col[0] + col[1]) + (col[2] + col[3]);
+    if (warp >= 4) s_sum[r] = sum;
+    // and the second tile's columns are read
+    ok = __syncthreads_and(ok);
     if (!ok) {
       if (threadIdx.x == 0) atomicExch(status, SLS_ERR_TIMEOUT);
       break;
     }
-    if (warp >= 4) s_sum[r] = col;
-    __syncthreads();
-    if (warp < 4 && x < w.len) {
-      const int64_t page = c.table[seq * c.table_ld + (x >> c.page_shift)];
-      if (page >= 0 && page < c.num_pages)
-        wv.data[page * wv.page + w.h * wv.head + (x & ((1 << c.page_shift) - 1))] += col + s_sum[r];
-    }
+    if (same) issue(1, w, r1, key0);
+    begin = !same;
+    if (to) *to = was + (sum + s_sum[r]);
   }
   aw_free<2 * AW_TILE>(tmem);
 }
@@ -582,7 +679,7 @@ int launch(const AttnArgs& a, const ScaleView& s, const WeightView& w, const AwH
   static int* words[64] = {};
   int dev = 0;
   SLS_CUDA_TRY(cudaGetDevice(&dev));
-  constexpr size_t smem1 = 2 * S::TILE_BYTES + 1024, smem2 = 3 * S::TILE_BYTES + 1024;
+  constexpr size_t smem1 = 3 * S::TILE_BYTES + 1024, smem2 = 3 * S::TILE_BYTES + 1024;
   auto first = attention_weights_rows_kernel<E, KT, HD>;
   auto second = attention_weights_sum_kernel<E, KT, HD>;
   if (dev >= 64 || !set[dev]) {
@@ -598,6 +695,7 @@ int launch(const AttnArgs& a, const ScaleView& s, const WeightView& w, const AwH
   if (dev < 64) words[dev] = word, set[dev] = true;
   AwPlan p;
   char* at = (char*)workspace;
+  p.group = a.q_heads / a.c.kv_heads;
   p.ctas = h.ctas;
   p.prefix = (int64_t*)at;
   p.ml = (float2*)(at += h.prefix_b);
