@@ -672,14 +672,11 @@ int sls_attention_weights(const sls_rows_t* q, int64_t T, int q_heads,
  * tokens, which kv_lens no longer tells.  A page must belong to one sequence.  A
  * page outside the cache reads as zeros (weights too) and is not written.
  * scales: NULL for a 16-bit cache.  0 <= first, 0 <= last, first + last <= keep.
- * Errors: INVALID_ARG, UNSUPPORTED, WORKSPACE, as above.
+ * Errors: INVALID_ARG, UNSUPPORTED, as above.
  */
-size_t sls_cache_evict_workspace_size(const sls_kv_cache_t* cache, const sls_kv_scales_t* scales,
-                                      int64_t keep);
 int sls_cache_evict(const sls_kv_cache_t* cache, const sls_kv_scales_t* scales,
                     const sls_kv_weights_t* weights, int64_t keep, int64_t first, int64_t last,
-                    int32_t* kept, int32_t* kv_lens, void* workspace, size_t workspace_bytes,
-                    void* stream);
+                    int32_t* kept, int32_t* kv_lens, void* stream);
 
 /*
  * Optional per-phase timing of sls_compress.  `events` is a host array of

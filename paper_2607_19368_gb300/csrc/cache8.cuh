@@ -105,7 +105,7 @@ SLS_DEV uint4 to_codes16(const float (&x)[16], float by) {
 }
 
 // ---- launchers (code: SLS_I8 or SLS_E4M3; dtype: SLS_BF16 or SLS_F16) --------------
-int launch_kv_append_q8(const AppendArgs& a, const ScaleView& s, int code, int dtype,
+int launch_qkv_append_q8(const AppendArgs& a, const ScaleView& s, int code, int dtype,
                         cudaStream_t stream);
 
 // Codes of the sequences' pages written out in 16 bits: `out` is the same cache, its own
@@ -143,7 +143,6 @@ struct EvictArgs {
   int32_t* kept;
   int32_t* lens;  // as c.kv_lens, to be written
 };
-size_t cache_evict_workspace(const CacheView& c, int64_t keep);
-int launch_cache_evict(const EvictArgs& a, int code, void* workspace, cudaStream_t stream);
+int launch_cache_evict(const EvictArgs& a, int code, cudaStream_t stream);
 
 }  // namespace sls

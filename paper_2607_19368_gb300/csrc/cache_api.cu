@@ -94,12 +94,7 @@ int sls_qkv_append_q8(const sls_rows_t* q, const sls_rows_t* k, const sls_rows_t
   a.q_weight = q_weight;
   a.k_weight = k_weight;
   a.eps = eps;
-  // the queries by the 16-bit append, without keys and values
-  AppendArgs only_q = a;
-  only_q.c.kv_heads = 0;
-  st = launch_qkv_append(only_q, dtype, (cudaStream_t)stream);
-  if (st != SLS_OK) return st;
-  return launch_kv_append_q8(a, s, cache->dtype, dtype, (cudaStream_t)stream);
+  return launch_qkv_append_q8(a, s, cache->dtype, dtype, (cudaStream_t)stream);
 }
 
 size_t sls_attention_prefill_q8_workspace_size(int64_t T, int q_heads,
@@ -208,18 +203,9 @@ int sls_attention_weights(const sls_rows_t* q, int64_t T, int q_heads,
   return launch_attention_weights(a, s, w, cache->dtype, dtype, workspace, (cudaStream_t)stream);
 }
 
-size_t sls_cache_evict_workspace_size(const sls_kv_cache_t* cache, const sls_kv_scales_t* scales,
-                                      int64_t keep) {
-  CacheView c;
-  ScaleView s;
-  if (!cache || any_cache(cache, scales, cache->kv_heads, false, &c, &s) != SLS_OK) return 0;
-  return cache_evict_workspace(c, keep);
-}
-
 int sls_cache_evict(const sls_kv_cache_t* cache, const sls_kv_scales_t* scales,
                     const sls_kv_weights_t* weights, int64_t keep, int64_t first, int64_t last,
-                    int32_t* kept, int32_t* kv_lens, void* workspace, size_t workspace_bytes,
-                    void* stream) {
+                    int32_t* kept, int32_t* kv_lens, void* stream) {
   EvictArgs a{};
   if (!cache) return SLS_ERR_INVALID_ARG;
   int st = any_cache(cache, scales, cache->kv_heads, false, &a.c, &a.s);
@@ -234,9 +220,7 @@ int sls_cache_evict(const sls_kv_cache_t* cache, const sls_kv_scales_t* scales,
   a.last = (int)last;
   a.kept = kept;
   a.lens = kv_lens;
-  const size_t need = cache_evict_workspace(a.c, keep);
-  if (need > 0 && (!aligned16(workspace) || workspace_bytes < need)) return SLS_ERR_WORKSPACE;
-  return launch_cache_evict(a, cache->dtype, workspace, (cudaStream_t)stream);
+  return launch_cache_evict(a, cache->dtype, (cudaStream_t)stream);
 }
 
 }  // extern "C"

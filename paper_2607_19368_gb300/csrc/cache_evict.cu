@@ -149,7 +149,7 @@ SLS_DEV void ev_select_long(const EvictArgs& a, const EvSeq& e, int len, int32_t
 }
 
 __global__ void __launch_bounds__(EV_T, 2)
-cache_evict_select_kernel(const __grid_constant__ EvictArgs a, int room4, int32_t* lens_before) {
+cache_evict_select_kernel(const __grid_constant__ EvictArgs a, int room4) {
   extern __shared__ float4 s_w[];  // room4 of them
   __shared__ EvShared s;
   const CacheView& c = a.c;
@@ -163,7 +163,6 @@ cache_evict_select_kernel(const __grid_constant__ EvictArgs a, int room4, int32_
   at_go();
   at_wait_ahead();
   const int len = (int)cache_len(c, seq);
-  if (h == 0 && rank == 0 && threadIdx.x == 0) lens_before[seq] = len;
   int32_t* kept = a.kept + ((int64_t)seq * c.kv_heads + h) * a.keep;
   const EvSeq e{a, seq, h};
   if (len <= a.keep) {
@@ -311,7 +310,7 @@ struct EvMove {
 
 template <typename C, bool BOTH>
 __global__ void __launch_bounds__(EV_MOVE_T, 4)
-cache_evict_move_kernel(const __grid_constant__ EvictArgs a, const int32_t* lens_before) {
+cache_evict_move_kernel(const __grid_constant__ EvictArgs a) {
   using S = EvMove<C, BOTH>;
   __shared__ int64_t s_from[S::ROWS], s_to[S::ROWS];  // byte offsets of rows, or -1
   __shared__ float s_was[S::MATS][S::ROWS], s_by[S::MATS][S::ROWS];  // codes: old scale, old / new
@@ -325,10 +324,11 @@ cache_evict_move_kernel(const __grid_constant__ EvictArgs a, const int32_t* lens
   const int h = hk % c.kv_heads;
   at_go();
   at_wait_ahead();
-  const int len = lens_before[seq];
-  if (len <= a.keep) return;  // the whole cluster
-  if (hk == 0 && rank == 0 && threadIdx.x == 0) a.lens[seq] = a.keep;
+  // the one reader of a length here cuts it
+  if (hk == 0 && rank == 0 && threadIdx.x == 0 && cache_len(c, seq) > a.keep) a.lens[seq] = a.keep;
   const int32_t* kept = a.kept + ((int64_t)seq * c.kv_heads + h) * a.keep;
+  // kept indices rise: where the last one is in its place all are, and -1 ends a shorter sequence
+  if (a.keep == 0 || kept[a.keep - 1] < a.keep) return;  // the whole cluster
   const int32_t* table = c.table + seq * c.table_ld;
   const bool values = !BOTH && hk >= c.kv_heads;
   char* const mat[2] = {values ? c.v : c.k, c.v};
@@ -414,7 +414,7 @@ cache_evict_move_kernel(const __grid_constant__ EvictArgs a, const int32_t* lens
 }
 
 template <typename C>
-int launch_move(const EvictArgs& a, int sms, const int32_t* lens, cudaStream_t stream) {
+int launch_move(const EvictArgs& a, int sms, cudaStream_t stream) {
   const CacheView& c = a.c;
   // keys and values by one cluster where there are clusters enough without
   const int64_t units = (int64_t)c.B * c.kv_heads;
@@ -424,23 +424,25 @@ int launch_move(const EvictArgs& a, int sms, const int32_t* lens, cudaStream_t s
   while (cluster < EV_CLUSTER && cluster * rows < a.keep) cluster *= 2;
   const dim3 grid((unsigned)(units * (both ? 1 : 2) * cluster));
   return at_launch(both ? cache_evict_move_kernel<C, true> : cache_evict_move_kernel<C, false>,
-                   grid, EV_MOVE_T, 0, cluster, stream, a, lens);
+                   grid, EV_MOVE_T, 0, cluster, stream, a);
 }
 
 }  // namespace
 
-size_t cache_evict_workspace(const CacheView& c, int64_t) {
-  return sls_align256((size_t)c.B * 4);
-}
-
-int launch_cache_evict(const EvictArgs& a, int code, void* workspace, cudaStream_t stream) {
+int launch_cache_evict(const EvictArgs& a, int code, cudaStream_t stream) {
   const CacheView& c = a.c;
   if (c.B == 0) return SLS_OK;
   if ((int64_t)c.B * c.kv_heads * 2 * EV_CLUSTER > 0x7fffffff) return SLS_ERR_UNSUPPORTED;
-  int dev = 0, sms = 0;
+  static int sm_count[64] = {};  // per device
+  int dev = 0;
   SLS_CUDA_TRY(cudaGetDevice(&dev));
-  SLS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-  int32_t* lens = (int32_t*)workspace;
+  int sms = dev < 64 ? sm_count[dev] : 0;
+  if (sms == 0) {
+    SLS_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    SLS_CUDA_TRY(cudaFuncSetAttribute(cache_evict_select_kernel,
+                                      cudaFuncAttributeMaxDynamicSharedMemorySize, EV_ROOM * 16));
+    if (dev < 64) sm_count[dev] = sms;
+  }
   // CTAs of a selection: as many as share out the GPU, no more than give every thread four weights
   // of the longest table, and enough to hold it (past 8 x 49152 tokens one CTA reads it anew each
   // pass)
@@ -450,14 +452,12 @@ int launch_cache_evict(const EvictArgs& a, int code, void* workspace, cudaStream
                                (int64_t)size * EV_ROOM * 4 < room))
     size *= 2;
   const int room4 = (int)std::min<int64_t>(EV_ROOM, ((room + 3) / 4 + size - 1) / size);
-  SLS_CUDA_TRY(cudaFuncSetAttribute(cache_evict_select_kernel,
-                                    cudaFuncAttributeMaxDynamicSharedMemorySize, EV_ROOM * 16));
   int st = at_launch(cache_evict_select_kernel, dim3((unsigned)(units * size)), EV_T,
-                     (size_t)room4 * 16, size, stream, a, room4, lens);
+                     (size_t)room4 * 16, size, stream, a, room4);
   if (st != SLS_OK) return st;
-  return code == SLS_I8     ? launch_move<I8>(a, sms, lens, stream)
-         : code == SLS_E4M3 ? launch_move<E4M3>(a, sms, lens, stream)
-                            : launch_move<void>(a, sms, lens, stream);
+  return code == SLS_I8     ? launch_move<I8>(a, sms, stream)
+         : code == SLS_E4M3 ? launch_move<E4M3>(a, sms, stream)
+                            : launch_move<void>(a, sms, stream);
 }
 
 }  // namespace sls

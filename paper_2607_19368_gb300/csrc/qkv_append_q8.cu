@@ -10,7 +10,8 @@
 // eight lanes a row; rows stay in registers between the maximum over the block and the codes,
 // so that inputs are read once.  Warps of one head exchange maxima through shared memory.
 //
-// The queries go through the 16-bit append's kernel, with no key heads.
+// The queries go through the 16-bit append's kernel, with no key heads; those of few tokens are
+// turned by CTAs of this launch.
 #include <algorithm>
 
 #include "attention_turn.cuh"
@@ -58,12 +59,13 @@ struct Q8Lane {
   static constexpr int PITCH = 8 * L + (L == 4 ? 4 : 0);  // float4 of a token; rows meet no bank twice
   const AppendArgs& a;
   const float4* s_tab;
+  const E* w;       // keys' (or queries') weights, or NULL
   int l, v0, v1;
   bool on, turned;  // it has elements; (halves) they are rotated
   unsigned mates;
 
-  SLS_DEV Q8Lane(const AppendArgs& args, const float4* tab, int lane, int l_)
-      : a(args), s_tab(tab), l(l_), mates(((1u << L) - 1) << (lane & ~(L - 1))) {
+  SLS_DEV Q8Lane(const AppendArgs& args, const float4* tab, const void* weight, int lane, int l_)
+      : a(args), s_tab(tab), w(reinterpret_cast<const E*>(weight)), l(l_), mates(((1u << L) - 1) << (lane & ~(L - 1))) {
     const int half = MODE == Q8_HALVES ? a.pairs >> 3 : 0;
     turned = l < half;
     v0 = turned ? l : 2 * l;
@@ -82,8 +84,9 @@ struct Q8Lane {
     return reinterpret_cast<float*>(tab + slot * PITCH + (at >> 1) * L + lane) + (at & 1);
   }
   // The table of n tokens from slot `lo` on, the first of them packed row `row` and cache index x.
+  // FAST: by the hardware's sine and cosine, for what becomes codes.
+  template <bool FAST>
   SLS_DEV void enter(float4* tab, int lo, int n, int64_t row, int x) const {
-    const E* w = reinterpret_cast<const E*>(a.k_weight);
     int width = 8;  // a thread keeps to one pair
     while (width < a.pairs) width *= 2;
     const int pr = threadIdx.x & (width - 1);
@@ -95,7 +98,8 @@ struct Q8Lane {
       float* to_o = entry(tab, lo, o);
 #pragma unroll 1
       for (int k = threadIdx.x / width; k < n; k += blockDim.x / width) {
-        const float2 cs = turn_fast(a.positions ? a.positions[row + k] : x + k, f);
+        const int p = a.positions ? a.positions[row + k] : x + k;
+        const float2 cs = FAST ? turn_fast(p, f) : turn(p, f);
         to_e[4 * PITCH * k] = cs.x * we, to_e[4 * PITCH * k + 2] = -cs.y * wo;
         to_o[4 * PITCH * k] = cs.x * wo, to_o[4 * PITCH * k + 2] = cs.y * we;
       }
@@ -132,7 +136,7 @@ struct Q8Lane {
       for (int e = 0; e < 8; ++e) y[8 * v + e] = z[e];
     }
     if constexpr (KEYS && MODE != Q8_PLAIN) {
-      if (a.k_weight) {
+      if (w) {
         f32x2_t s = mul2(pk2(y[0], y[1]), pk2(y[0], y[1]));
 #pragma unroll
         for (int e = 2; e < 16; e += 2) s = fma2(pk2(y[e], y[e + 1]), pk2(y[e], y[e + 1]), s);
@@ -344,19 +348,60 @@ SLS_DEV void q8_many(const Q8Lane<E, L, MODE>& me, const Q8Block& b, float (&s_m
   }
 }
 
+// The queries of packed rows [t, t_end), from the sequence of row t on: a group of lanes for each
+// head, a token at a time.
+template <int MODE, typename E, int L>
+SLS_DEV void q8_queries(const Q8Lane<E, L, MODE>& me, float4* tab, int64_t t, int64_t t_end, int seq) {
+  const AppendArgs& a = me.a;
+  const CacheView& c = a.c;
+#pragma unroll 1
+  for (int64_t row = t; row < t_end; ++row) {
+    // the cache index, which turns where no positions are given: -1 outside every sequence
+    while (a.cu && seq < c.B && a.cu[seq + 1] <= row) ++seq;
+    if (!a.cu) seq = (int)row;
+    int64_t x = -1;
+    if (seq < c.B) x = a.cu ? (int64_t)c.kv_lens[seq] - a.cu[seq + 1] + row : (int64_t)c.kv_lens[seq] - 1;
+    if (a.cu && seq < c.B && row < a.cu[seq]) x = -1;
+    if (MODE != Q8_PLAIN) {
+      __syncthreads();
+      me.template enter<false>(tab, 0, 1, row, (int)x);
+      __syncthreads();
+    }
+#pragma unroll 1
+    for (int h = (int)threadIdx.x / L; h < a.q_heads; h += Q8_T / L) {
+      const char* p = a.q.data + row * a.q.token_b + h * a.q.head_b;
+      uint4 u[2];
+      float y[16], most = 0.f;
+      me.load(p, u);
+      const float norm = me.template row<true>(u, p, 0, y, most);
+      if (MODE == Q8_ODD) __syncwarp(me.mates);  // partners are read before a row is written in place
+      if (!me.on) continue;
+      char* d = a.out.data + row * a.out.token_b + h * a.out.head_b;
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        float z[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) z[e] = y[8 * v + e] * norm;
+        *reinterpret_cast<uint4*>(d + 16 * (v ? me.v1 : me.v0)) = narrow8<E>(z);
+      }
+    }
+  }
+}
+
 // E: input type; L: lanes of a row (16 elements each); K: rows a lane holds, 0 where blocks take
 // few new tokens; MODE: of keys
 template <typename E, int L, int K, int MODE>
 __global__ void __launch_bounds__(Q8_T, K <= 2 ? 2 : 1)
 kv_append_q8_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ ScaleView sv,
-                    int tile, int key_ctas, int key_jobs, int value_jobs, bool ints) {
+                    int tile, int key_ctas, int key_jobs, int value_jobs, int query_cta, bool ints) {
   extern __shared__ float4 s_tab[];
   __shared__ float s_most[2][Q8_T / 32];
   __shared__ int s_ended[Q8_T / 32];
   const CacheView& c = a.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int blk = 1 << sv.shift;
-  // the first CTAs of a tile take heads of keys, the others heads of values
+  // the first CTAs of a tile take heads of keys, the next heads of values, the last (few tokens)
+  // all queries
   const bool keys = (int)blockIdx.y < key_ctas;
   const int j_first = keys ? blockIdx.y * key_jobs : (blockIdx.y - key_ctas) * value_jobs;
   const int j_end = min(c.kv_heads, j_first + (keys ? key_jobs : value_jobs));
@@ -367,7 +412,7 @@ kv_append_q8_kernel(const __grid_constant__ AppendArgs a, const __grid_constant_
 
   at_go();
   at_wait_ahead();
-  const Q8Lane<E, L, MODE> me(a, s_tab, lane, threadIdx.x % L);
+  const Q8Lane<E, L, MODE> me(a, s_tab, a.k_weight, lane, threadIdx.x % L);
   int seq = (int)t;
   if (a.cu) {
     int ended = 0;
@@ -378,6 +423,12 @@ kv_append_q8_kernel(const __grid_constant__ AppendArgs a, const __grid_constant_
     __syncthreads();
     seq = 0;
     for (int w = 0; w < Q8_T / 32; ++w) seq += s_ended[w];
+  }
+  if constexpr (K == 0) {
+    if ((int)blockIdx.y == query_cta) {
+      q8_queries<MODE>(Q8Lane<E, L, MODE>(a, s_tab, a.q_weight, lane, threadIdx.x % L), s_tab, t, t_end, seq);
+      return;
+    }
   }
   int parity = 0;
 #pragma unroll 1
@@ -406,7 +457,7 @@ kv_append_q8_kernel(const __grid_constant__ AppendArgs a, const __grid_constant_
       // the factors of the block's new tokens, for all heads of keys
       if (MODE != Q8_PLAIN && keys) {
         __syncthreads();
-        me.enter(s_tab, lo, hi - lo, row0 + lo, (int)(start + lo));
+        me.template enter<true>(s_tab, lo, hi - lo, row0 + lo, (int)(start + lo));
         __syncthreads();
       }
       const Q8Block b{blk, lo, hi, j_first, j_end,
@@ -424,16 +475,22 @@ kv_append_q8_kernel(const __grid_constant__ AppendArgs a, const __grid_constant_
   }
 }
 
+// Packed tokens of a CTA: a block's, or as many as a sequence has new ones on average.
+int q8_tile(const AppendArgs& a, int blk) {
+  int tile = blk;
+  while (tile > 1 && a.T < (int64_t)tile * a.c.B) tile /= 2;
+  return tile;
+}
+
 template <typename E, int L, int MODE>
 int launch(const AppendArgs& a, const ScaleView& s, bool ints, cudaStream_t stream) {
   const int blk = 1 << s.shift, jobs = a.c.kv_heads;
-  // a block's tokens for a CTA, or as many as a sequence has new ones on average, and heads
-  // shared out until there are some 1200 CTAs (eight for each of 152 SMs)
-  int tile = blk;
-  while (tile > 1 && a.T < (int64_t)tile * a.c.B) tile /= 2;
+  // heads are shared out until there are some 1200 CTAs (eight for each of 152 SMs)
+  const int tile = q8_tile(a, blk);
+  const bool few = tile <= Q8_FEW;
   const int64_t tiles = (a.T + tile - 1) / tile;
   // jobs that a CTA has in flight
-  const int together = tile <= Q8_FEW ? Q8_T / L : std::max(1, Q8_T / L / blk);
+  const int together = few ? Q8_T / L : std::max(1, Q8_T / L / blk);
   const int passes = (jobs + together - 1) / together;
   auto share = [&](int64_t ctas) {
     const int n = (int)std::max<int64_t>(1, std::min<int64_t>((ctas + tiles - 1) / tiles, passes));
@@ -441,16 +498,17 @@ int launch(const AppendArgs& a, const ScaleView& s, bool ints, cudaStream_t stre
   };
   const int key_jobs = share(Q8_KEY_CTAS), value_jobs = share(Q8_VALUE_CTAS);
   const int key_ctas = (jobs + key_jobs - 1) / key_jobs;
-  const dim3 grid((unsigned)tiles, (unsigned)(key_ctas + (jobs + value_jobs - 1) / value_jobs));
+  const int query_cta = key_ctas + (jobs + value_jobs - 1) / value_jobs;
+  const dim3 grid((unsigned)tiles, (unsigned)(query_cta + few));
   const size_t smem = MODE != Q8_PLAIN ? (size_t)blk * Q8Lane<E, L, MODE>::PITCH * sizeof(float4) : 0;
   auto go = [&](auto kern) {
     if (smem > 48 * 1024)
       SLS_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                         (int)smem));
     return at_launch(kern, grid, Q8_T, smem, 1, stream, a, s, tile, key_ctas, key_jobs, value_jobs,
-                     ints);
+                     query_cta, ints);
   };
-  if (tile <= Q8_FEW) return go(kv_append_q8_kernel<E, L, 0, MODE>);
+  if (few) return go(kv_append_q8_kernel<E, L, 0, MODE>);
   const int rows = blk * L / Q8_T;
   if (rows <= 1) return go(kv_append_q8_kernel<E, L, 1, MODE>);
   return rows == 2 ? go(kv_append_q8_kernel<E, L, 2, MODE>) : go(kv_append_q8_kernel<E, L, L / 2, MODE>);
@@ -458,7 +516,8 @@ int launch(const AppendArgs& a, const ScaleView& s, bool ints, cudaStream_t stre
 
 template <typename E, int L>
 int launch(const AppendArgs& a, const ScaleView& s, bool ints, cudaStream_t stream) {
-  if (a.pairs == 0 && !a.k_weight) return launch<E, L, Q8_PLAIN>(a, s, ints, stream);
+  const bool few = q8_tile(a, 1 << s.shift) <= Q8_FEW;
+  if (a.pairs == 0 && !a.k_weight && !(few && a.q_weight)) return launch<E, L, Q8_PLAIN>(a, s, ints, stream);
   if (a.interleaved) return launch<E, L, Q8_SIDES>(a, s, ints, stream);
   return (a.pairs & 7) == 0 ? launch<E, L, Q8_HALVES>(a, s, ints, stream)
                             : launch<E, L, Q8_ODD>(a, s, ints, stream);
@@ -472,9 +531,17 @@ int launch(const AppendArgs& a, const ScaleView& s, int code, cudaStream_t strea
 
 }  // namespace
 
-int launch_kv_append_q8(const AppendArgs& a, const ScaleView& s, int code, int dtype,
+int launch_qkv_append_q8(const AppendArgs& a, const ScaleView& s, int code, int dtype,
                         cudaStream_t stream) {
   if (a.T == 0) return SLS_OK;
+  if (q8_tile(a, 1 << s.shift) > Q8_FEW) {
+    // the queries by the 16-bit append, without keys and values: their angles are formed once for
+    // all heads there, and a launch more is nothing beside them
+    AppendArgs only_q = a;
+    only_q.c.kv_heads = 0;
+    const int st = launch_qkv_append(only_q, dtype, stream);
+    if (st != SLS_OK) return st;
+  }
   return dtype == SLS_BF16 ? launch<__nv_bfloat16>(a, s, code, stream)
                            : launch<__half>(a, s, code, stream);
 }

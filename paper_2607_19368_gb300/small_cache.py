@@ -47,8 +47,7 @@ EXPORTED = {
     "sls_attention_weights_workspace_size": (_sz, [_i64, _i32, _vp, _vp, _i32]),
     "sls_attention_weights": (_i32, [_vp, _i64, _i32, _vp, _vp, _i32, _vp, _i32, _f32, _vp, _vp,
                                      _sz, _vp]),
-    "sls_cache_evict_workspace_size": (_sz, [_vp, _vp, _i64]),
-    "sls_cache_evict": (_i32, [_vp, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp, _sz, _vp]),
+    "sls_cache_evict": (_i32, [_vp, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp]),
 }
 
 _CODES8 = {torch.int8: SLS_I8, torch.float8_e4m3fn: SLS_E4M3}
@@ -118,9 +117,7 @@ def _bytes(fn, dev, code, block, rest, cache) -> int:
             return int(lib.sls_attention_decode_q8_workspace_size(rest[0], c, s, rest[1]))
         if fn == "prefill":
             return int(lib.sls_attention_prefill_q8_workspace_size(rest[0], rest[1], c, s, rest[2]))
-        if fn == "weights":
-            return int(lib.sls_attention_weights_workspace_size(rest[0], rest[1], c, s, rest[2]))
-        return int(lib.sls_cache_evict_workspace_size(c, s, rest[0]))
+        return int(lib.sls_attention_weights_workspace_size(rest[0], rest[1], c, s, rest[2]))
 
 
 def qkv_append_q8(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_k: torch.Tensor,
@@ -142,7 +139,7 @@ def qkv_append_q8(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_k: to
     s, _ = _scales(k_scale, v_scale, n, ps, H, dev)
     shape = q.shape
     if out is None:
-        out = torch.empty_like(q)
+        out = q.new_empty(shape)
     elif out.shape != shape:
         raise ValueError("out: the shape of q")
     T = shape[0]
@@ -255,8 +252,7 @@ def attention_weights(q: torch.Tensor, cache_k: torch.Tensor, page_table: torch.
 def cache_evict(cache_k: torch.Tensor, cache_v: torch.Tensor, page_table: torch.Tensor,
                 kv_lens: torch.Tensor, weights: torch.Tensor, keep: int, first: int = 0,
                 last: int = 0, k_scale: Optional[torch.Tensor] = None,
-                v_scale: Optional[torch.Tensor] = None,
-                workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+                v_scale: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Cuts every sequence of more than `keep` tokens to `keep`: for each key head its first
     `first` and last `last` tokens and the others of the largest weights stay (equal ones: the
     lowest index) and move to the front in their order: keys, values, weights and, for codes,
@@ -264,20 +260,15 @@ def cache_evict(cache_k: torch.Tensor, cache_v: torch.Tensor, page_table: torch.
     stayed (B x kv_heads x keep int32, ascending, -1 past a shorter sequence's end).  Give
     later calls of ``qkv_append`` their positions: lengths no longer tell them."""
     eight = k_scale is not None
-    c, (n, ps, H, hd), dt, dev, B, cols = _cache(cache_k, cache_v, page_table, kv_lens,
-                                                 _CODES8 if eight else _at._CODES)
+    c, (n, ps, H, _), _, dev, B, _ = _cache(cache_k, cache_v, page_table, kv_lens,
+                                            _CODES8 if eight else _at._CODES)
     if eight != (v_scale is not None):
         raise ValueError("k_scale, v_scale: both or none")
-    s, block = _scales(k_scale, v_scale, n, ps, H, dev) if eight else (None, 0)
+    s = _scales(k_scale, v_scale, n, ps, H, dev)[0] if eight else None
     w = _weights(weights, n, ps, H, dev)
     if keep < 0 or first < 0 or last < 0 or first + last > keep:
         raise ValueError("keep: at least first + last, none of them negative")
     kept = kv_lens.new_empty((B, H, keep))
-    nbytes = _bytes("evict", dev, _ANY[dt], block, (keep,), (H, hd, ps, n, B, cols))
-    wp = 0
-    if nbytes:
-        workspace = _scratch(nbytes, workspace, kept, dev)
-        wp, nbytes = workspace.data_ptr(), workspace.numel()
     _call("sls_cache_evict", dev, c, s, w, keep, first, last, kept.data_ptr(),
-          kv_lens.data_ptr(), wp, nbytes)
+          kv_lens.data_ptr())
     return kept

@@ -51,6 +51,9 @@ APPEND = [
     ([200], [264], 8, 8, 48, 1024, 128, 0, False, True, True),       # no rotation
     ([300, 500], [4000, 501], 40, 8, 128, 128, 128, 64, True, False, True),
     ([700, 1, 64], [700, 129, 64], 2, 1, 128, 128, 64, 40, False, True, True),
+    ([1, 2, 0], [50, 7, 9], 10, 2, 80, 16, 16, 9, False, True, True),   # few tokens, odd halves
+    ([1, 1, 3], [50, 7, 20], 40, 8, 128, 32, 16, 0, False, True, False),  # a norm alone
+    ([2, 1], [2, 128], 3, 3, 32, 128, 128, 5, True, False, False),
 ]
 
 
@@ -87,6 +90,7 @@ def test_append(sls, case, code, dtype):
     K = S.append(b, "k", ky, ke)
     V = S.append(b, "v", v.double(), torch.zeros_like(ke[:, :1]).expand(-1, Hkv, -1))
     old_codes = {x: b[x].clone() for x in "kv"}
+    twin = dict(b, **{x: b[x].clone() for x in ("k", "v", "k_scale", "v_scale")})
     got = sls.qkv_append_q8(q, k, v, *cache(b), cu_seqlens=b["cu"], positions=pos, q_weight=qw,
                             k_weight=kw, eps=1e-5, rope=rope)
     S.check(got, qo, qe + R.U[dtype] * qo.abs() + R.TINY[dtype], "q")
@@ -102,6 +106,11 @@ def test_append(sls, case, code, dtype):
         # what no sequence covers is left as it was
         raw = b[x].view(torch.uint8)[hole]
         assert torch.equal(raw, old_codes[x].view(torch.uint8)[hole]), x
+    # in place
+    again = sls.qkv_append_q8(q, k, v, *cache(twin), cu_seqlens=b["cu"], positions=pos, q_weight=qw,
+                              k_weight=kw, eps=1e-5, rope=rope, out=q)
+    assert again is q and torch.equal(q, got)
+    assert all(torch.equal(twin[x].view(torch.uint8), b[x].view(torch.uint8)) for x in "kv")
 
 
 @pytest.mark.parametrize("code", CODES)
