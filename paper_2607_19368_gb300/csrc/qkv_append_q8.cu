@@ -6,9 +6,10 @@
 //
 // A CTA takes blocks whose first new token lies among its `tile` packed tokens, one after the
 // other, and all or a share of their heads: cosines and sines are formed once for all heads.
-// A lane holds sixteen elements of a token's head (its code is one 16-byte store), four or
-// eight lanes a row; rows stay in registers between the maximum over the block and the codes,
-// so that inputs are read once.  Warps of one head exchange maxima through shared memory.
+// A lane holds sixteen elements of a token's head, four or eight lanes a row.  A warp has a head of
+// a block to itself and goes over its rows twice, the second time from the caches: rows kept in
+// registers between the maximum and the codes need all of a CTA's warps for one head, and a barrier
+// for each.
 //
 // The queries go through the 16-bit append's kernel, with no key heads; those of few tokens are
 // turned by CTAs of this launch.
@@ -24,7 +25,7 @@ namespace {
 constexpr int Q8_T = 256;
 // rows as they come; halves of whole vectors; pairs side by side; halves that split vectors
 enum { Q8_PLAIN, Q8_HALVES, Q8_SIDES, Q8_ODD };
-constexpr int Q8_KEY_CTAS = 304, Q8_VALUE_CTAS = 304;  // at least so many, heads permitting
+constexpr int Q8_WARPS = 1216, Q8_CTAS = 912;  // at least so many, heads permitting: for 152 SMs
 constexpr int Q8_FEW = 2;  // new tokens of a block up to which a job is one group's
 
 // Where a packed token goes.
@@ -251,6 +252,14 @@ SLS_DEV void q8_again(const Lane& me, bool ints, char* d, float by) {
   me.store(d, q8_codes(ints, z, by));
 }
 
+// The larger sizes of two pairs of elements; a NaN is as if it were not there.
+template <typename E>
+SLS_DEV uint32_t q8_larger(uint32_t a, uint32_t b) {
+  using H = typename std::conditional<std::is_same<E, __half>::value, __half2, __nv_bfloat162>::type;
+  const H m = __hmax2(*reinterpret_cast<const H*>(&a), __habs2(*reinterpret_cast<const H*>(&b)));
+  return *reinterpret_cast<const uint32_t*>(&m);
+}
+
 // Few new tokens: a head is one group's of L lanes, all heads at once.
 template <bool KEYS, typename E, int L, int MODE>
 SLS_DEV void q8_few(const Q8Lane<E, L, MODE>& me, const Q8Block& b) {
@@ -287,65 +296,97 @@ SLS_DEV void q8_few(const Q8Lane<E, L, MODE>& me, const Q8Block& b) {
   }
 }
 
-// A block's tokens shared out over the groups, K rows for each, head after head (or several at
-// once where a block has fewer tokens than there are groups).
-template <bool KEYS, int K, typename E, int L, int MODE>
-SLS_DEV void q8_many(const Q8Lane<E, L, MODE>& me, const Q8Block& b, float (&s_most)[2][Q8_T / 32],
-                     int& parity) {
-  constexpr int NG = Q8_T / L;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, grp = threadIdx.x / L;
-  const int per_job = min(b.blk, NG), together = NG / per_job;
-  const int first = grp & (per_job - 1);
-  const char* const mine = b.rows + first * b.token_b;
-  const int64_t next_row = per_job * b.token_b;
-  // the next head's rows are on their way while one is worked on
-  uint4 u[K][2];
-  auto fetch = [&](int j) {
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int slot = first + k * per_job;
-      if (j < b.j_end && slot >= b.lo && slot < b.hi) me.load(mine + k * next_row + j * b.head_b, u[k]);
-    }
-  };
-  int j = b.j_first + grp / per_job;
-  fetch(j);
+// A head is `share` warps', each with a run of every 32 / L tokens, which go over their rows twice:
+// for the maximum, and (from the caches) for the codes.  Alone (share 1) a warp waits for no other.
+template <bool KEYS, typename E, int L, int MODE>
+SLS_DEV void q8_many(const Q8Lane<E, L, MODE>& me, const Q8Block& b, int j, bool live, int share,
+                     float (&s_most)[2][Q8_T / 32], int& parity) {
+  constexpr int AT = 32 / L;  // rows of a warp at a time
+  constexpr int AHEAD = 2;    // loaded before the first is worked on
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int step = AT * share, slot0 = (warp & (share - 1)) * AT + lane / L;
+  const char* const p = b.rows + j * b.head_b;
+  float most = 0.f;
+  if (live) {
+    uint32_t top[4] = {0u, 0u, 0u, 0u};  // (as they come) pairs of sizes
 #pragma unroll 1
-  for (int j0 = b.j_first; j0 < b.j_end; j0 += together, j += together) {
-    const bool live = j < b.j_end;
-    float y[K][16], norm[K];
-    float most = 0.f;
+    for (int s = slot0; s - lane / L < b.hi; s += AHEAD * step) {
+      uint4 u[AHEAD][2];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int slot = first + k * per_job;
-      // whole groups of L lanes take the branch or leave it
-      if (live && slot >= b.lo && slot < b.hi)
-        norm[k] = me.template row<KEYS>(u[k], mine + k * next_row + j * b.head_b, slot, y[k], most);
+      for (int k = 0; k < AHEAD; ++k) {
+        const int slot = s + k * step;
+        u[k][0] = u[k][1] = make_uint4(0, 0, 0, 0);
+        if (slot >= b.lo && slot < b.hi) me.load(p + slot * b.token_b, u[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        const int slot = s + k * step;
+        if constexpr (KEYS && MODE != Q8_PLAIN) {
+          float y[16];
+          if (slot >= b.lo && slot < b.hi) me.template row<KEYS>(u[k], p + slot * b.token_b, slot, y, most);
+        } else {
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            top[0] = q8_larger<E>(top[0], u[k][v].x), top[1] = q8_larger<E>(top[1], u[k][v].y);
+            top[2] = q8_larger<E>(top[2], u[k][v].z), top[3] = q8_larger<E>(top[3], u[k][v].w);
+          }
+        }
+      }
     }
-    fetch(j + together);
-    // the rows of a warp are one head's: a block has at least as many slots as a warp rows.
-    // The old scale is read in front of the barrier, behind which it is written.
-    most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
-    const float was = live && b.lo > 0 ? b.scales[j * b.scale_head] : 0.f;
+    if constexpr (!(KEYS && MODE != Q8_PLAIN)) {
+      const float2 f = Half2<E>::widen(q8_larger<E>(q8_larger<E>(top[0], top[1]), q8_larger<E>(top[2], top[3])));
+      most = fmaxf(f.x, f.y);
+      if (__any_sync(0xffffffffu, most > 3.402823466e38f)) {  // an infinity among them: look again
+        most = 0.f;
+#pragma unroll 1
+        for (int slot = slot0; slot < b.hi; slot += step) {
+          uint4 u[2];
+          float y[16];
+          if (slot < b.lo) continue;
+          me.load(p + slot * b.token_b, u);
+          me.template row<KEYS>(u, p + slot * b.token_b, slot, y, most);
+        }
+      }
+    }
+  }
+  most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
+  float* const sp = b.scales + j * b.scale_head;
+  const float was = live && b.lo > 0 ? *sp : 0.f;
+  if (share > 1) {
+    // the old scale is read in front of the barrier, behind which it is written
     if (lane == 0) s_most[parity][warp] = most;
     __syncthreads();
-    const int wj = per_job * L / 32, w0 = warp & ~(wj - 1);
-    most = s_most[parity][w0 + (lane & (wj - 1))];
-    most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most)));
+    const float each = s_most[parity][(warp & ~(share - 1)) + (lane & (share - 1))];
+    most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(each)));
     parity ^= 1;
-    if (!live) continue;
-    const float now = fmaxf(q8_scale(b.ints, most), was), by = q8_over(now);
-    char* d = b.codes + j * b.code_head_b;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int slot = first + k * per_job;
-      if (!me.on || slot >= b.hi) continue;
-      if (slot >= b.lo)
-        me.store(d + slot * b.slot_b, q8_codes(b.ints, y[k], norm[k] * by));
-      else if (now > was)
-        q8_again(me, b.ints, d + slot * b.slot_b, was * by);
-    }
-    if (first == 0 && me.l == 0 && now != was) b.scales[j * b.scale_head] = now;
+  } else {
+    __syncwarp();
   }
+  if (!live) return;
+  const float now = fmaxf(q8_scale(b.ints, most), was), by = q8_over(now);
+  char* const d = b.codes + j * b.code_head_b;
+#pragma unroll 1
+  for (int s = slot0; s - lane / L < b.hi; s += 2 * step) {
+    uint4 u[2][2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int slot = s + k * step;
+      if (slot >= b.lo && slot < b.hi) me.load(p + slot * b.token_b, u[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int slot = s + k * step;
+      if (slot >= b.hi) continue;
+      if (slot >= b.lo) {
+        float y[16], again = 0.f;
+        const float norm = me.template row<KEYS>(u[k], p + slot * b.token_b, slot, y, again);
+        if (me.on) me.store(d + slot * b.slot_b, q8_codes(b.ints, y, norm * by));
+      } else if (me.on && now > was) {
+        q8_again(me, b.ints, d + slot * b.slot_b, was * by);
+      }
+    }
+  }
+  if (slot0 == 0 && me.l == 0 && now != was) *sp = now;
 }
 
 // The queries of packed rows [t, t_end), from the sequence of row t on: a group of lanes for each
@@ -388,25 +429,20 @@ SLS_DEV void q8_queries(const Q8Lane<E, L, MODE>& me, float4* tab, int64_t t, in
   }
 }
 
-// E: input type; L: lanes of a row (16 elements each); K: rows a lane holds, 0 where blocks take
-// few new tokens; MODE: of keys
-template <typename E, int L, int K, int MODE>
-__global__ void __launch_bounds__(Q8_T, K <= 2 ? 2 : 1)
+// E: input type; L: lanes of a row (16 elements each); FEW: blocks take few new tokens; MODE: of
+// keys.  Jobs are the heads of keys, then those of values.
+template <typename E, int L, bool FEW, int MODE>
+__global__ void __launch_bounds__(Q8_T, 2)
 kv_append_q8_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ ScaleView sv,
-                    int tile, int key_ctas, int key_jobs, int value_jobs, int query_cta, bool ints) {
+                    int tile, int jobs_per_cta, int share, int query_cta, bool ints) {
   extern __shared__ float4 s_tab[];
   __shared__ float s_most[2][Q8_T / 32];
   __shared__ int s_ended[Q8_T / 32];
   const CacheView& c = a.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int blk = 1 << sv.shift;
-  // the first CTAs of a tile take heads of keys, the next heads of values, the last (few tokens)
-  // all queries
-  const bool keys = (int)blockIdx.y < key_ctas;
-  const int j_first = keys ? blockIdx.y * key_jobs : (blockIdx.y - key_ctas) * value_jobs;
-  const int j_end = min(c.kv_heads, j_first + (keys ? key_jobs : value_jobs));
-  const RowsView& src = keys ? a.k : a.v;
-  char* const cache = keys ? c.k : c.v;
+  const int j_first = blockIdx.y * jobs_per_cta;
+  const int j_end = min(2 * c.kv_heads, j_first + jobs_per_cta);
   const int64_t t_end = min(a.T, ((int64_t)blockIdx.x + 1) * tile);
   int64_t t = (int64_t)blockIdx.x * tile;
 
@@ -424,7 +460,7 @@ kv_append_q8_kernel(const __grid_constant__ AppendArgs a, const __grid_constant_
     seq = 0;
     for (int w = 0; w < Q8_T / 32; ++w) seq += s_ended[w];
   }
-  if constexpr (K == 0) {
+  if constexpr (FEW) {  // the last CTA of a tile has all queries
     if ((int)blockIdx.y == query_cta) {
       q8_queries<MODE>(Q8Lane<E, L, MODE>(a, s_tab, a.q_weight, lane, threadIdx.x % L), s_tab, t, t_end, seq);
       return;
@@ -455,21 +491,30 @@ kv_append_q8_kernel(const __grid_constant__ AppendArgs a, const __grid_constant_
       const int slot0 = (int)(start & ((1 << c.page_shift) - 1));
       const int64_t sc = page * sv.page + (slot0 >> sv.shift) * sv.block;
       // the factors of the block's new tokens, for all heads of keys
-      if (MODE != Q8_PLAIN && keys) {
+      if (MODE != Q8_PLAIN && j_first < c.kv_heads) {
         __syncthreads();
         me.template enter<true>(s_tab, lo, hi - lo, row0 + lo, (int)(start + lo));
         __syncthreads();
       }
-      const Q8Block b{blk, lo, hi, j_first, j_end,
-                      src.data + row0 * src.token_b, src.token_b, src.head_b,
-                      cache + page * c.page_b + slot0 * c.slot_b, c.slot_b, c.head_b,
-                      (keys ? sv.k : sv.v) + sc, sv.head, ints};
-      if constexpr (K == 0) {
-        if (MODE != Q8_PLAIN && keys) q8_few<true>(me, b);
-        else q8_few<false>(me, b);
+      const int64_t at_codes = page * c.page_b + slot0 * c.slot_b;
+      const Q8Block k{blk, lo, hi, j_first, min(j_end, c.kv_heads),
+                      a.k.data + row0 * a.k.token_b, a.k.token_b, a.k.head_b,
+                      c.k + at_codes, c.slot_b, c.head_b, sv.k + sc, sv.head, ints};
+      const Q8Block v{blk, lo, hi, max(0, j_first - c.kv_heads), j_end - c.kv_heads,
+                      a.v.data + row0 * a.v.token_b, a.v.token_b, a.v.head_b,
+                      c.v + at_codes, c.slot_b, c.head_b, sv.v + sc, sv.head, ints};
+      if constexpr (FEW) {
+        q8_few<true>(me, k);
+        q8_few<false>(me, v);
       } else {
-        if (MODE != Q8_PLAIN && keys) q8_many<true, K>(me, b, s_most, parity);
-        else q8_many<false, K>(me, b, s_most, parity);
+        const int together = Q8_T / 32 / share;
+#pragma unroll 1
+        for (int j0 = j_first; j0 < j_end; j0 += together) {
+          const int j = j0 + warp / share;
+          const bool live = j < j_end;
+          if (j < c.kv_heads) q8_many<true>(me, k, live ? j : 0, live, share, s_most, parity);
+          else q8_many<false>(me, v, live ? j - c.kv_heads : 0, live, share, s_most, parity);
+        }
       }
     }
   }
@@ -484,34 +529,28 @@ int q8_tile(const AppendArgs& a, int blk) {
 
 template <typename E, int L, int MODE>
 int launch(const AppendArgs& a, const ScaleView& s, bool ints, cudaStream_t stream) {
-  const int blk = 1 << s.shift, jobs = a.c.kv_heads;
-  // heads are shared out until there are some 1200 CTAs (eight for each of 152 SMs)
+  const int blk = 1 << s.shift, jobs = 2 * a.c.kv_heads;
   const int tile = q8_tile(a, blk);
   const bool few = tile <= Q8_FEW;
   const int64_t tiles = (a.T + tile - 1) / tile;
-  // jobs that a CTA has in flight
-  const int together = few ? Q8_T / L : std::max(1, Q8_T / L / blk);
+  // a warp for a head, or several where that leaves the GPU with less than eight warps an SM
+  int share = 1;
+  while (share < 8 && share * 32 / L < blk && tiles * jobs * share < Q8_WARPS) share *= 2;
+  // jobs that a CTA has in flight, and has in all: every one, shared out where tiles are few
+  const int together = few ? Q8_T / L : Q8_T / 32 / share;
   const int passes = (jobs + together - 1) / together;
-  auto share = [&](int64_t ctas) {
-    const int n = (int)std::max<int64_t>(1, std::min<int64_t>((ctas + tiles - 1) / tiles, passes));
-    return (passes + n - 1) / n * together;
-  };
-  const int key_jobs = share(Q8_KEY_CTAS), value_jobs = share(Q8_VALUE_CTAS);
-  const int key_ctas = (jobs + key_jobs - 1) / key_jobs;
-  const int query_cta = key_ctas + (jobs + value_jobs - 1) / value_jobs;
+  const int ctas = few ? 2 : (int)std::max<int64_t>(1, std::min<int64_t>((Q8_CTAS + tiles - 1) / tiles, passes));
+  const int per = (jobs + ctas - 1) / ctas;
+  const int query_cta = (jobs + per - 1) / per;
   const dim3 grid((unsigned)tiles, (unsigned)(query_cta + few));
   const size_t smem = MODE != Q8_PLAIN ? (size_t)blk * Q8Lane<E, L, MODE>::PITCH * sizeof(float4) : 0;
   auto go = [&](auto kern) {
     if (smem > 48 * 1024)
       SLS_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                         (int)smem));
-    return at_launch(kern, grid, Q8_T, smem, 1, stream, a, s, tile, key_ctas, key_jobs, value_jobs,
-                     query_cta, ints);
+    return at_launch(kern, grid, Q8_T, smem, 1, stream, a, s, tile, per, share, query_cta, ints);
   };
-  if (few) return go(kv_append_q8_kernel<E, L, 0, MODE>);
-  const int rows = blk * L / Q8_T;
-  if (rows <= 1) return go(kv_append_q8_kernel<E, L, 1, MODE>);
-  return rows == 2 ? go(kv_append_q8_kernel<E, L, 2, MODE>) : go(kv_append_q8_kernel<E, L, L / 2, MODE>);
+  return few ? go(kv_append_q8_kernel<E, L, true, MODE>) : go(kv_append_q8_kernel<E, L, false, MODE>);
 }
 
 template <typename E, int L>
