@@ -127,7 +127,8 @@ def weights(b, before, causal=True, scale=None):
     """(sums, bound) in float64: `before` plus every seen token's softmax weights.  Bound: a
     weight is off by its score's error (products exact, hd float32 sums, 2^-23 of them each)
     twice (itself and the sum), 2^-17 for exponential, sum and division; one rounding a row
-    of the running sums."""
+    of the running sums; float32 exponentials below 2^-126, the least normal number, are 0, so
+    that each of the rows may miss up to that."""
     q, page = b["q"].double(), b["page"]
     T, Hq, hd = q.shape
     Hkv = b["k"].shape[2]
@@ -157,7 +158,7 @@ def weights(b, before, causal=True, scale=None):
                     err += (P * (2 * d + 2.0 ** -17)).sum(0)
                 w = torch.zeros_like(out[0, 0, 0]) + add
                 out[pg[ok], c, st[ok]] += w[ok]
-                bound[pg[ok], c, st[ok]] = (err + 2.0 ** -23 * (n * G + 1) * out[pg.clamp(0, out.shape[0] - 1), c, st].abs())[ok]
+                bound[pg[ok], c, st[ok]] = (err + n * G * 2.0 ** -126 + 2.0 ** -23 * (n * G + 1) * out[pg.clamp(0, out.shape[0] - 1), c, st].abs())[ok]
         t0 += n
     return out, bound
 
