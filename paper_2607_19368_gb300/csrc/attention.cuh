@@ -126,6 +126,9 @@ struct AppendArgs {
   int pairs;
   int interleaved;
   float rope_scale;
+  // the launch ahead waited for what is ahead of it before it let this one start, and neither
+  // touches what the other writes: this one need not wait for its end before its own
+  bool beside;
 };
 int launch_qkv_append(const AppendArgs& a, int dtype, cudaStream_t stream);
 

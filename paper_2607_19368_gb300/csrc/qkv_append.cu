@@ -92,7 +92,7 @@ qkv_append_kernel(const __grid_constant__ AppendArgs a, int tokens, int heads_pe
     }
   };
   at_go();
-  at_wait_ahead();
+  if (!a.beside) at_wait_ahead();
   const char* q_src = a.q.data + t * a.q.token_b;
   load(q_src, a.q.head_b, sq.first, tok < nt ? sq.end : 0);  // while the tokens are looked up
 
@@ -258,13 +258,16 @@ qkv_append_kernel(const __grid_constant__ AppendArgs a, int tokens, int heads_pe
   };
   turned(q_src, a.q.head_b, a.out.data + t * a.out.token_b, a.out.head_b, sq,
          reinterpret_cast<const E*>(a.q_weight), true);
-  if (slot < 0) return;
-  turned(a.k.data + t * a.k.token_b, a.k.head_b, c.k + slot, c.head_b, sk,
-         reinterpret_cast<const E*>(a.k_weight), false);
-  for (int h0 = sv.first; h0 < sv.end; h0 += stride) {
-    load(a.v.data + t * a.v.token_b, a.v.head_b, h0, sv.end);
-    store(c.v + slot, c.head_b, h0, sv.end);
+  if (slot >= 0) {
+    turned(a.k.data + t * a.k.token_b, a.k.head_b, c.k + slot, c.head_b, sk,
+           reinterpret_cast<const E*>(a.k_weight), false);
+    for (int h0 = sv.first; h0 < sv.end; h0 += stride) {
+      load(a.v.data + t * a.v.token_b, a.v.head_b, h0, sv.end);
+      store(c.v + slot, c.head_b, h0, sv.end);
+    }
   }
+  // what follows waits for this launch, and so for the one beside it
+  if (a.beside) at_wait_ahead();
 }
 
 template <typename E>

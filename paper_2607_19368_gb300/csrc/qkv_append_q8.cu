@@ -11,8 +11,9 @@
 // registers between the maximum and the codes need all of a CTA's warps for one head, and a barrier
 // for each.
 //
-// The queries go through the 16-bit append's kernel, with no key heads; those of few tokens are
-// turned by CTAs of this launch.
+// The queries go through the 16-bit append's kernel, with no key heads, which starts while the last
+// CTAs here run (21345 tokens: 131 us one after the other); those of few tokens are turned by CTAs of
+// this launch.
 #include <algorithm>
 
 #include "attention_turn.cuh"
@@ -446,8 +447,8 @@ kv_append_q8_kernel(const __grid_constant__ AppendArgs a, const __grid_constant_
   const int64_t t_end = min(a.T, ((int64_t)blockIdx.x + 1) * tile);
   int64_t t = (int64_t)blockIdx.x * tile;
 
-  at_go();
   at_wait_ahead();
+  at_go();
   const Q8Lane<E, L, MODE> me(a, s_tab, a.k_weight, lane, threadIdx.x % L);
   int seq = (int)t;
   if (a.cu) {
@@ -573,16 +574,15 @@ int launch(const AppendArgs& a, const ScaleView& s, int code, cudaStream_t strea
 int launch_qkv_append_q8(const AppendArgs& a, const ScaleView& s, int code, int dtype,
                         cudaStream_t stream) {
   if (a.T == 0) return SLS_OK;
-  if (q8_tile(a, 1 << s.shift) > Q8_FEW) {
-    // the queries by the 16-bit append, without keys and values: their angles are formed once for
-    // all heads there, and a launch more is nothing beside them
-    AppendArgs only_q = a;
-    only_q.c.kv_heads = 0;
-    const int st = launch_qkv_append(only_q, dtype, stream);
-    if (st != SLS_OK) return st;
-  }
-  return dtype == SLS_BF16 ? launch<__nv_bfloat16>(a, s, code, stream)
-                           : launch<__half>(a, s, code, stream);
+  const int st = dtype == SLS_BF16 ? launch<__nv_bfloat16>(a, s, code, stream)
+                                   : launch<__half>(a, s, code, stream);
+  if (st != SLS_OK || q8_tile(a, 1 << s.shift) <= Q8_FEW) return st;
+  // The queries by the 16-bit append, without keys and values, in the gaps of the launch above:
+  // angles are formed once for all heads there.
+  AppendArgs only_q = a;
+  only_q.c.kv_heads = 0;
+  only_q.beside = true;
+  return launch_qkv_append(only_q, dtype, stream);
 }
 
 }  // namespace sls
