@@ -126,35 +126,43 @@ struct AwRows {
   }
 };
 
-// 128 keys from token key0 on: to registers, and from there to a tile.
+// 128 keys from token key0 on: their pages, then the keys, to registers, and from there to a tile.
+// Page numbers are fetched a tile ahead, so that keys are one latency away.
 template <typename E, typename KT, int HD>
 struct AwKeys {
   using S = AwShape<E, KT, HD>;
   uint4 raw[S::KEY_LOADS];
-  float scale;  // of key threadIdx.x
+  int page[S::KEY_LOADS], own;  // of the keys to load next (-1: none), and that of key threadIdx.x
+  float scale;                  // of key threadIdx.x
 
+  SLS_DEV void pages(const AttnArgs& a, const AwHead& w, int key0) {
+    const CacheView& c = a.c;
+    const int32_t* table = c.table + w.seq * c.table_ld;
+    const bool on = threadIdx.x % S::KEY_LANES * (S::CODES ? 16 : 8) < c.head_dim;
+#pragma unroll
+    for (int i = 0; i < S::KEY_LOADS; ++i) {
+      const int x = key0 + i * (AW_T / S::KEY_LANES) + threadIdx.x / S::KEY_LANES;
+      page[i] = on && x < w.len ? table[x >> c.page_shift] : -1;
+    }
+    const int x = key0 + threadIdx.x;
+    own = S::CODES && threadIdx.x < AW_TILE && x < w.len ? table[x >> c.page_shift] : -1;
+  }
   SLS_DEV void load(const AttnArgs& a, const ScaleView& sc, const AwHead& w, int key0) {
     const CacheView& c = a.c;
-    const int ch = threadIdx.x % S::KEY_LANES, slots = (1 << c.page_shift) - 1;
-    const int32_t* table = c.table + w.seq * c.table_ld;
+    const int slots = (1 << c.page_shift) - 1;
+    const char* base = c.k + w.h * c.head_b + 16 * (threadIdx.x % S::KEY_LANES);
 #pragma unroll
     for (int i = 0; i < S::KEY_LOADS; ++i) {
       const int x = key0 + i * (AW_T / S::KEY_LANES) + threadIdx.x / S::KEY_LANES;
       raw[i] = make_uint4(0, 0, 0, 0);
-      if (x >= w.len || ch * (S::CODES ? 16 : 8) >= c.head_dim) continue;
-      const int64_t page = table[x >> c.page_shift];
-      if (page >= 0 && page < c.num_pages)
-        raw[i] = *reinterpret_cast<const uint4*>(c.k + page * c.page_b + (x & slots) * c.slot_b +
-                                                 w.h * c.head_b + 16 * ch);
+      if (page[i] >= 0 && page[i] < c.num_pages)
+        raw[i] = *reinterpret_cast<const uint4*>(base + page[i] * c.page_b + (x & slots) * c.slot_b);
     }
     if constexpr (S::CODES) {
       scale = 0.f;
       const int x = key0 + threadIdx.x;
-      if (threadIdx.x < AW_TILE && x < w.len) {
-        const int64_t page = table[x >> c.page_shift];
-        if (page >= 0 && page < c.num_pages)
-          scale = sc.k[page * sc.page + ((x & slots) >> sc.shift) * sc.block + w.h * sc.head];
-      }
+      if (own >= 0 && own < c.num_pages)
+        scale = sc.k[own * sc.page + ((x & slots) >> sc.shift) * sc.block + w.h * sc.head];
     }
   }
 
@@ -187,16 +195,22 @@ SLS_DEV void aw_stage_rows(const AttnArgs& a, const AwHead& w, const AwRows& row
                            unsigned char* out, float* factor) {
   using S = AwShape<E, KT, HD>;
   const int ch = threadIdx.x % S::ROW_LANES;
+  uint4 all[S::ROW_LOADS];
 #pragma unroll
   for (int i = 0; i < S::ROW_LOADS; ++i) {
     const int r = i * (AW_T / S::ROW_LANES) + threadIdx.x / S::ROW_LANES;
-    uint4 u = make_uint4(0, 0, 0, 0);
+    all[i] = make_uint4(0, 0, 0, 0);
     if (r < rows.count && 8 * ch < a.c.head_dim) {
       int g;
       const int tok = rows.token(r, w, g);
-      u = *reinterpret_cast<const uint4*>(a.q.data + (w.q0 + tok) * a.q.token_b +
-                                          (w.h * w.group + g) * a.q.head_b + 16 * ch);
+      all[i] = *reinterpret_cast<const uint4*>(a.q.data + (w.q0 + tok) * a.q.token_b +
+                                               (w.h * w.group + g) * a.q.head_b + 16 * ch);
     }
+  }
+#pragma unroll
+  for (int i = 0; i < S::ROW_LOADS; ++i) {
+    const int r = i * (AW_T / S::ROW_LANES) + threadIdx.x / S::ROW_LANES;
+    uint4 u = all[i];
     float back = 1.f;
     if constexpr (!std::is_same<E, typename S::M>::value) {
       float x[8], top = 0.f;
@@ -319,12 +333,13 @@ attention_weights_rows_kernel(const __grid_constant__ AttnArgs a,
     const int h = (int)(tiles >> 31 ? item / tiles : aw_div(item, (int)tiles));
     const AwHead w(a, p.group, seq, h);
     const AwRows rows(w, item - h * tiles);
+    AwKeys<E, KT, HD> keys;
+    keys.pages(a, w, j0 * AW_TILE);
     aw_stage_rows<E, KT, HD>(a, w, rows, rows_s, s_factor);
     const int see = rows.see(a, w, r);
     // tokens that the last row sees, and so any
     const int last = min(j1, (rows.see(a, w, rows.count - 1) + AW_TILE - 1) / AW_TILE);
     float m = -INFINITY, l = 0.f;
-    AwKeys<E, KT, HD> keys;
     // products of the next tile run while the scores of one are worked on
     auto next = [&](int j, unsigned k) {
       keys.store(keys_s + (k & 1) * S::TILE_BYTES, s_scale[k & 3]);
@@ -336,9 +351,11 @@ attention_weights_rows_kernel(const __grid_constant__ AttnArgs a,
                                &bar[k & 1]);
       }
       if (j + 1 < last) keys.load(a, sc, w, (j + 1) * AW_TILE);
+      if (j + 2 < last) keys.pages(a, w, (j + 2) * AW_TILE);
     };
     if (j0 < last) {
       keys.load(a, sc, w, j0 * AW_TILE);
+      keys.pages(a, w, (j0 + 1) * AW_TILE);
       next(j0, turn);
     } else {
       __syncthreads();
@@ -505,17 +522,25 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
   unsigned phase[2] = {0, 0};
   bool ok = true, live[2];
   AwKeys<E, KT, HD> keys;
-  int key0;
-  auto unit = [&](int64_t t) {  // a unit's keys to registers
-    while (t - before >= steps(seq)) {
-      before += steps(seq);
-      ++seq;
+  // the unit after the next: its head, first token and pages, a unit ahead of its keys
+  int n = ad_steps<AW_TILE>(c, seq), plan0;
+  AwHead ahead(a, p.group, seq, (int)aw_div(t0 - before, n));
+  int tile = (int)(t0 - before - (int64_t)ahead.h * n);
+  auto plan = [&] {
+    plan0 = tile * AW_TILE;
+    keys.pages(a, ahead, plan0);
+  };
+  auto advance = [&] {
+    if (++tile == n) {
+      tile = 0;
+      if (++ahead.h == c.kv_heads) {
+        do ++seq;
+        while (steps(seq) == 0);
+        n = ad_steps<AW_TILE>(c, seq);
+        ahead = AwHead(a, p.group, seq, 0);
+      }
     }
-    const int n = ad_steps<AW_TILE>(c, seq), h = (int)aw_div(t - before, n);
-    key0 = (int)(t - before - (int64_t)h * n) * AW_TILE;
-    const AwHead w(a, p.group, seq, h);
-    keys.load(a, sc, w, key0);
-    return w;
+    plan();
   };
   // two tiles of rows (or one) to shared memory
   auto stage = [&](const AwHead& w, const AwRows& r0, const AwRows& r1) {
@@ -579,7 +604,12 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
 
   // The first two tiles of rows of a head stay in shared memory from unit to unit, and the products
   // of a unit's first tile run while the scores of the last unit's second are worked on.
-  AwHead next = unit(t0);
+  plan();
+  AwHead next = ahead;
+  int key0 = plan0;
+  keys.load(a, sc, next, key0);
+  if (t0 + 1 < t1) advance();
+  AwRows r0(next, 0), r1(next, 1);
   bool begin = true;
   float scale = 1.f;
 #pragma unroll 1
@@ -587,8 +617,8 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
     const AwHead w = next;
     const int start = key0, x = start + r;
     const int64_t tiles = (w.rows + AW_TILE - 1) >> 7;
-    const AwRows r0(w, 0), r1(w, 1);
     if (begin) {
+      r0 = AwRows(w, 0), r1 = AwRows(w, 1);
       stage(w, r0, r1);
       keys.store(keys_s, s_scale);
       aw_fence();
@@ -608,7 +638,12 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
         was = *to;
       }
     }
-    if (t + 1 < t1) next = unit(t + 1);
+    if (t + 1 < t1) {
+      next = ahead;
+      key0 = plan0;
+      keys.load(a, sc, next, key0);
+      if (t + 2 < t1) advance();
+    }
     const bool same = t + 1 < t1 && next.seq == w.seq && next.h == w.h && tiles <= 2;
 #pragma unroll
     for (int j = 0; j < 4; ++j) col[j] = 0.f;
