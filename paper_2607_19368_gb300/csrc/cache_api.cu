@@ -211,7 +211,7 @@ int sls_cache_evict(const sls_kv_cache_t* cache, const sls_kv_scales_t* scales,
   int st = any_cache(cache, scales, cache->kv_heads, false, &a.c, &a.s);
   if (st != SLS_OK) return st;
   if ((st = weight_view(weights, a.c, &a.w)) != SLS_OK) return st;
-  if (keep < 0 || first < 0 || last < 0 || keep > 0x7fffffff || first + last > keep)
+  if (keep < 0 || first < 0 || last < 0 || keep > 0x7fffffff || first > keep || last > keep - first)
     return SLS_ERR_INVALID_ARG;
   if (cache->batch > 0 && (kv_lens != cache->kv_lens || (keep > 0 && !kept)))
     return SLS_ERR_INVALID_ARG;

@@ -157,6 +157,8 @@ def test_options_that_are_refused(sls):
     assert evict(keep=-1) == 1 and evict(first=-1) == 1 and evict(last=-1) == 1
     assert evict(first=4, last=5) == 1 and evict(kept=None) == 1 and evict(lens=None) == 1
     assert evict(lens=512) == 1 and evict(keep=1 << 40) == 1
+    # sums past 64 bits
+    assert evict(first=(1 << 63) - 1, last=1) == 1 and evict(first=1, last=(1 << 63) - 1) == 1
     # more sequences than a packed call looks through
     many = cache(batch=65537)
     got = calls(L, many, s, evict=False)
