@@ -583,7 +583,8 @@ typedef struct sls_kv_scales {
 } sls_kv_scales_t;
 
 /* A float for every slot and key head of a cache; a head's page_size floats are
- * contiguous, strides (in floats) multiples of 4, the base 16-byte aligned. */
+ * contiguous, strides (in floats) multiples of 4 and at least page_size, the base 16-byte
+ * aligned. */
 typedef struct sls_kv_weights {
   float* data;               /* num_pages x kv_heads x page_size               */
   int64_t page_stride;
@@ -645,8 +646,8 @@ int sls_attention_decode_q8(const sls_rows_t* q, int q_heads, const sls_kv_cache
  * per sequence).  Reads the keys only; cache->v may be NULL.  scales: NULL for a
  * 16-bit cache, whose dtype is `dtype`, the queries'.  Sums are float32, in a
  * fixed order.  A page must belong to one sequence; weights of a page outside
- * the cache are dropped.  A row whose scores are not finite leaves NaN in the
- * sums of the tokens that it sees.
+ * the cache are dropped.  A row with a score that is NaN or +infinity leaves NaN in
+ * the sums of the tokens that it sees; a score of -infinity is a weight of 0.
  * Errors: as sls_attention_prefill, and INVALID_ARG for weights.
  */
 size_t sls_attention_weights_workspace_size(int64_t T, int q_heads, const sls_kv_cache_t* cache,

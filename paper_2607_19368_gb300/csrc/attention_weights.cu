@@ -441,6 +441,7 @@ attention_weights_join_kernel(const __grid_constant__ AttnArgs a, const __grid_c
   }
   const int hq = (int)(id - t * a.q_heads);
   const AwHead w(a, p.group, seq, hq / p.group);
+  if (t >= w.q0 + w.n) return;  // offsets that do not ascend
   const int n = ad_steps<AW_TILE>(c, seq);
   float m = -INFINITY, l = 0.f;
   if (n > 0) {

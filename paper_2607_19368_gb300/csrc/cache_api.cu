@@ -51,6 +51,8 @@ int weight_view(const sls_kv_weights_t* w, const CacheView& c, WeightView* v) {
   if (w->page_stride < 0 || w->page_stride % 4 || w->head_stride % 4 ||
       w->head_stride < (1 << c.page_shift))
     return SLS_ERR_INVALID_ARG;
+  // every page has weights of its own
+  if (c.num_pages > 1 && w->page_stride < (1 << c.page_shift)) return SLS_ERR_INVALID_ARG;
   v->data = w->data;
   v->page = w->page_stride;
   v->head = w->head_stride;

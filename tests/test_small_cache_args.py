@@ -147,7 +147,8 @@ def test_options_that_are_refused(sls):
     assert L.sls_attention_weights(r, 3, 4, wide, None, 1, 256, 1, 1.0, weights(), None, 0,
                                    None) == 2
     for bad in (None, weights(data=0), weights(data=8), weights(page_stride=-4),
-                weights(page_stride=62), weights(head_stride=30), weights(head_stride=28)):
+                weights(page_stride=62), weights(page_stride=0), weights(head_stride=30),
+                weights(head_stride=28)):
         assert L.sls_attention_weights(r, 3, 4, c, s, 1, 256, 1, 1.0, bad, None, 0, None) == 1
         assert L.sls_cache_evict(c, s, bad, 8, 1, 2, 256, 256, None) == 1
 
