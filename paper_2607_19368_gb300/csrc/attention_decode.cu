@@ -295,7 +295,7 @@ attention_decode_kernel(const __grid_constant__ CUtensorMap tmK,
   const int gw = blockIdx.x * S::WARPS + warp;
   const int g = gw / p.vheads, vh = gw - g * p.vheads;
   if (g >= parts) return;
-  const int64_t t0 = total * g / parts, t1 = total * (g + 1) / parts;
+  const int64_t t0 = ad_div(total * g, parts), t1 = ad_div(total * (g + 1), parts);
   const int group = a.q_heads / c.kv_heads;
   const int blocks = (group + AD_ROWS - 1) / AD_ROWS;
   const int kvh = vh / blocks, row0 = (vh - kvh * blocks) * AD_ROWS;

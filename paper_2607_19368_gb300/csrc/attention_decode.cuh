@@ -69,6 +69,12 @@ SLS_DEV int ad_prefix(const CacheView& c, int64_t* s_pre, int64_t* prefix, const
   return R;
 }
 
+// x / y, neither negative, in 32 bits where that is enough: a division in 64 takes some hundred
+// instructions, which a small call fetches for the first time as a rule.
+SLS_DEV int64_t ad_div(int64_t x, int64_t y) {
+  return (uint64_t)(x | y) >> 32 ? x / y : (int64_t)((unsigned)x / (unsigned)y);
+}
+
 // The sequence of step t0 (below the total), and the steps before it.
 template <int T, typename F>
 SLS_DEV void ad_find(const int64_t* s_pre, int R, int64_t t0, const F& steps, int& seq,
@@ -200,7 +206,7 @@ attention_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant_
   const int64_t row =
       WARPS == 1 ? (int64_t)blockIdx.x * AD_JOIN_WARPS + (threadIdx.x >> 5) : blockIdx.x;
   if (row >= (int64_t)c.B * a.q_heads) return;
-  const int seq = (int)(row / a.q_heads), h = (int)(row - (int64_t)seq * a.q_heads);
+  const int seq = (int)ad_div(row, a.q_heads), h = (int)(row - (int64_t)seq * a.q_heads);
   const int group = a.q_heads / c.kv_heads, blocks = (group + AD_ROWS - 1) / AD_ROWS;
   const int kvh = h / group, in = h - kvh * group;
   const int vh = kvh * blocks + in / AD_ROWS, rr = in % AD_ROWS;
@@ -217,7 +223,7 @@ attention_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant_
   const int parts = ad_parts(total, p.groups);
   const float cs = a.scale * 1.4426950408889634f;
   // the part of step t is the last whose start total * g / parts is at most t
-  const int g0 = (int)(((b0 + 1) * parts - 1) / total), g1 = (int)((b1 * parts - 1) / total);
+  const int g0 = (int)ad_div((b0 + 1) * parts - 1, total), g1 = (int)ad_div(b1 * parts - 1, total);
   if (g0 == g1) return;
   float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
   const int n = g1 - g0 + 1;
@@ -227,7 +233,7 @@ attention_join_kernel(const __grid_constant__ AttnArgs a, const __grid_constant_
   for (int x = x0; x < x1; ++x) {
     const int g = g0 + x;
     // the sequence's first piece is its part's last unless the part starts with it
-    const int late = x == 0 && total * g / parts < b0;
+    const int late = x == 0 && ad_div(total * g, parts) < b0;
     const int64_t slot = ((int64_t)(2 * g + late) * p.vheads + vh) * AD_ROWS + rr;
     const float2 ml = p.ml[slot];
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);

@@ -76,12 +76,6 @@ SLS_DEV int64_t aw_row_tiles(const AttnArgs& a, int group, int seq) {
   return ((q1 - q0) * group + AW_TILE - 1) >> 7;
 }
 
-// x / y, in 32 bits where that is enough: a division in 64 takes some hundred instructions, which
-// is what a tile's scores take
-SLS_DEV int64_t aw_div(int64_t x, int y) {
-  return (uint64_t)x >> 32 ? x / y : (int64_t)((unsigned)x / (unsigned)y);
-}
-
 // A key head of a sequence.
 struct AwHead {
   int seq, h, len, n, group;
@@ -103,7 +97,7 @@ struct AwRows {
   SLS_DEV AwRows(const AwHead& w, int64_t tile) {
     const int64_t base = tile * AW_TILE;
     count = (int)max((int64_t)0, min((int64_t)AW_TILE, w.rows - base));
-    tok = (int)aw_div(base, w.group);
+    tok = (int)ad_div(base, w.group);
     rem = (int)(base - (int64_t)tok * w.group);
     mul = (65536 + w.group - 1) / w.group;
   }
@@ -306,7 +300,7 @@ attention_weights_rows_kernel(const __grid_constant__ AttnArgs a,
   const int64_t total = s_pre[AW_T];
   const int parts = (int)min((int64_t)p.ctas, total);
   if ((int)blockIdx.x >= parts) return;
-  const int64_t t0 = total * blockIdx.x / parts, t1 = total * (blockIdx.x + 1) / parts;
+  const int64_t t0 = ad_div(total * blockIdx.x, parts), t1 = ad_div(total * (blockIdx.x + 1), parts);
   const uint32_t tmem = aw_alloc<2 * AW_TILE>(&holder);
   const uint32_t lead = at_elect();
   int seq;
@@ -328,9 +322,9 @@ attention_weights_rows_kernel(const __grid_constant__ AttnArgs a,
       continue;
     }
     const int n = ad_steps<AW_TILE>(c, seq);
-    const int64_t item = aw_div(t - before, n), tiles = aw_row_tiles(a, p.group, seq);
+    const int64_t item = ad_div(t - before, n), tiles = aw_row_tiles(a, p.group, seq);
     const int j0 = (int)(t - before - item * n), j1 = (int)min((int64_t)n, j0 + t1 - t);
-    const int h = (int)(tiles >> 31 ? item / tiles : aw_div(item, (int)tiles));
+    const int h = (int)ad_div(item, tiles);
     const AwHead w(a, p.group, seq, h);
     const AwRows rows(w, item - h * tiles);
     AwKeys<E, KT, HD> keys;
@@ -428,7 +422,7 @@ attention_weights_join_kernel(const __grid_constant__ AttnArgs a, const __grid_c
   const int lane = threadIdx.x & 31;
   const int64_t id = (int64_t)blockIdx.x * AW_JOIN_WARPS + (threadIdx.x >> 5);
   if (id >= a.T * a.q_heads) return;
-  const int64_t t = id / a.q_heads;
+  const int64_t t = ad_div(id, a.q_heads);
   const float cs = a.scale * 1.4426950408889634f;
   at_go();
   at_wait_ahead();
@@ -450,14 +444,14 @@ attention_weights_join_kernel(const __grid_constant__ AttnArgs a, const __grid_c
     const int parts = (int)min((int64_t)p.ctas, total);
     const int64_t s0 = p.prefix[seq] + (w.h * aw_row_tiles(a, p.group, seq) + tile) * n, s1 = s0 + n;
     // the part of step x is the last whose start total * g / parts is at most x
-    const int g0 = (int)(((s0 + 1) * parts - 1) / total), g1 = (int)((s1 * parts - 1) / total);
+    const int g0 = (int)ad_div((s0 + 1) * parts - 1, total), g1 = (int)ad_div(s1 * parts - 1, total);
     if (g0 == g1) {
       const float2 y = p.stat[id];
       m = y.x, l = y.y;
     } else {
       for (int g = g0 + lane; g <= g1; g += 32) {
         // the item's first piece is its part's last unless the part starts with it
-        const int late = g == g0 && total * g / parts < s0;
+        const int late = g == g0 && ad_div(total * g, parts) < s0;
         const float2 y = p.ml[(int64_t)(2 * g + late) * AW_TILE + (row - tile * AW_TILE)];
         const float top = fmaxf(m, y.x), base = top == -INFINITY ? 0.f : top;
         l = l * at_exp2((m - base) * cs) + y.y * at_exp2((y.x - base) * cs);
@@ -491,7 +485,8 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
   __shared__ float s_factor[2 * AW_TILE];
   __shared__ __align__(16) float2 s_row[2 * AW_TILE];  // factor and summand of a row's exponents
   __shared__ __align__(16) int s_see[2 * AW_TILE];     // tokens that it sees
-  __shared__ float s_scale[AW_TILE], s_sum[AW_TILE];
+  // of two units: a thread may still read its token's when another fetches the next unit's
+  __shared__ float s_scale[2][AW_TILE], s_sum[AW_TILE];
   __shared__ uint64_t bar[2];
   __shared__ uint32_t holder;
   const CacheView& c = a.c;
@@ -510,7 +505,7 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
   };
   const int R = ad_prefix<AW_T>(c, s_pre, nullptr, steps);
   const int64_t total = s_pre[AW_T];
-  const int64_t t0 = total * blockIdx.x / gridDim.x, t1 = total * (blockIdx.x + 1) / gridDim.x;
+  const int64_t t0 = ad_div(total * blockIdx.x, gridDim.x), t1 = ad_div(total * (blockIdx.x + 1), gridDim.x);
   if (t0 >= t1) return;
   const uint32_t tmem = aw_alloc<2 * AW_TILE>(&holder);
   const uint32_t lead = at_elect();
@@ -525,7 +520,7 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
   AwKeys<E, KT, HD> keys;
   // the unit after the next: its head, first token and pages, a unit ahead of its keys
   int n = ad_steps<AW_TILE>(c, seq), plan0;
-  AwHead ahead(a, p.group, seq, (int)aw_div(t0 - before, n));
+  AwHead ahead(a, p.group, seq, (int)ad_div(t0 - before, n));
   int tile = (int)(t0 - before - (int64_t)ahead.h * n);
   auto plan = [&] {
     plan0 = tile * AW_TILE;
@@ -621,12 +616,12 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
     if (begin) {
       r0 = AwRows(w, 0), r1 = AwRows(w, 1);
       stage(w, r0, r1);
-      keys.store(keys_s, s_scale);
+      keys.store(keys_s, s_scale[t & 1]);
       aw_fence();
       __syncthreads();
       issue(0, w, r0, start);
       issue(1, w, r1, start);
-      if constexpr (S::CODES) scale = s_scale[r];
+      if constexpr (S::CODES) scale = s_scale[t & 1][r];
     }
     const float mine = scale;
     // the token's weight so far, and the next unit's keys
@@ -655,11 +650,11 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
     if (same) {
       // the unit's products are done: its keys' place is free; at the barrier so are the first
       // tile's columns
-      keys.store(keys_s, s_scale);
+      keys.store(keys_s, s_scale[(t + 1) & 1]);
       aw_fence();
       __syncthreads();
       issue(0, w, r0, key0);
-      if constexpr (S::CODES) scale = s_scale[r];
+      if constexpr (S::CODES) scale = s_scale[(t + 1) & 1][r];
     }
     if (second) add(1, r1.count, start, mine);
 #pragma unroll 1

@@ -89,7 +89,7 @@ attention_scores_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
   const int gw = blockIdx.x * S::WARPS + warp;
   const int g = gw / c.kv_heads, kvh = gw - g * c.kv_heads;
   if (g >= parts) return;
-  const int64_t t0 = total * g / parts, t1 = total * (g + 1) / parts;
+  const int64_t t0 = ad_div(total * g, parts), t1 = ad_div(total * (g + 1), parts);
   int seq;
   int64_t before;  // steps before seq
   ad_find<AD_T>(s_pre, R, t0, steps, seq, before);
@@ -103,7 +103,7 @@ attention_scores_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
   // ---- copies ahead: the step to issue next, as in the decode kernels
   int is = seq, ilen = (int)cache_len(c, seq), isteps = ad_steps(c, seq);
   int64_t ileft = steps(seq) - (t0 - before);  // steps of this sequence, all passes, to issue
-  int ij = (int)((t0 - before) % isteps);
+  int ij = (int)(t0 - before - ad_div(t0 - before, isteps) * isteps);
   int64_t left = t1 - t0;
   int batch0 = -1, page = -1;
   unsigned issued = 0, used = 0;
@@ -171,7 +171,7 @@ attention_scores_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
       ++seq;
       continue;
     }
-    const int pass = (int)((t - before) / n);
+    const int pass = (int)ad_div(t - before, n);
     const int j0 = (int)((t - before) - (int64_t)pass * n);
     const int j1 = (int)min((int64_t)n, j0 + t1 - t);
     int64_t q0, q1;
@@ -348,11 +348,11 @@ attention_scores_sum_kernel(const __grid_constant__ AttnArgs a,
     const int here = (int)min((int64_t)AF_SUM_T, rows - b0);
     __syncthreads();
     for (int i = warp; i < here; i += AF_SUM_T / 32) {
-      const int64_t row = b0 + i, tok = row / group;
+      const int64_t row = b0 + i, tok = ad_div(row, group);
       const int64_t pass = row / AF_ROWS;
       const int64_t s0 = first + pass * n, s1 = s0 + n;  // steps of the row's pass
       // the part of step t is the last whose start total * g / parts is at most t
-      const int g0 = (int)(((s0 + 1) * parts - 1) / total), g1 = (int)((s1 * parts - 1) / total);
+      const int g0 = (int)ad_div((s0 + 1) * parts - 1, total), g1 = (int)ad_div(s1 * parts - 1, total);
       float m = -INFINITY, l = 0.f;
       if (g0 == g1) {
         const float2 y = p.stat[(q0 + tok) * a.q_heads + h * group + (row - tok * group)];
@@ -360,7 +360,7 @@ attention_scores_sum_kernel(const __grid_constant__ AttnArgs a,
       } else {
         for (int g = g0 + lane; g <= g1; g += 32) {
           // the pass's first piece is its part's last unless the part starts with it
-          const int late = g == g0 && total * g / parts < s0;
+          const int late = g == g0 && ad_div(total * g, parts) < s0;
           const float2 y =
               p.ml[((int64_t)(2 * g + late) * c.kv_heads + h) * AF_ROWS + (row - pass * AF_ROWS)];
           const float top = fmaxf(m, y.x), base = top == -INFINITY ? 0.f : top;
@@ -383,7 +383,7 @@ attention_scores_sum_kernel(const __grid_constant__ AttnArgs a,
     if (x < len) {
       const float* sp = p.scores + (q0 * a.q_heads + h * group) * p.room + x;
       for (int i = 0; i < here; ++i) {
-        const int64_t tok = (b0 + i) / group;
+        const int64_t tok = ad_div(b0 + i, group);
         const float4 f =
             *reinterpret_cast<const float4*>(sp + (tok * a.q_heads + (b0 + i - tok * group)) * p.room);
         const float s[4] = {f.x, f.y, f.z, f.w};
