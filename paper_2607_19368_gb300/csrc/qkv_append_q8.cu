@@ -431,9 +431,11 @@ SLS_DEV void q8_queries(const Q8Lane<E, L, MODE>& me, float4* tab, int64_t t, in
 }
 
 // E: input type; L: lanes of a row (16 elements each); FEW: blocks take few new tokens; MODE: of
-// keys.  Jobs are the heads of keys, then those of values.
+// keys.  Jobs are the heads of keys, then those of values.  Rows as they come leave registers for
+// three CTAs an SM (10717 tokens of 5 heads of 64, the call 21.8 us with two, 20.6 with three); keys
+// that are turned spill there (21345 tokens of 8 heads 119.5 us with two, 144 with three).
 template <typename E, int L, bool FEW, int MODE>
-__global__ void __launch_bounds__(Q8_T, 2)
+__global__ void __launch_bounds__(Q8_T, MODE == Q8_PLAIN && !FEW ? 3 : 2)
 kv_append_q8_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ ScaleView sv,
                     int tile, int jobs_per_cta, int share, int query_cta, bool ints) {
   extern __shared__ float4 s_tab[];
