@@ -16,12 +16,16 @@ namespace {
 
 constexpr int CE_T = 256;
 
+// Two products rounded; float16 cut to +-65504, NaN kept.
 template <typename E>
-SLS_DEV E ce_narrow(float x) {
-  if constexpr (std::is_same<E, __half>::value)
-    return __float2half_rn(x > 65504.f ? 65504.f : x < -65504.f ? -65504.f : x);
-  else
-    return __float2bfloat16_rn(x);
+SLS_DEV uint32_t ce_narrow(float x, float y) {
+  const uint32_t u = Half2<E>::narrow(x, y);
+  if constexpr (std::is_same<E, __half>::value) {
+    const __half2 most = __half2half2(__ushort_as_half(0x7bff)), h = *reinterpret_cast<const __half2*>(&u);
+    const __half2 cut = __hmax2_nan(__hmin2_nan(h, most), __hneg2(most));
+    return *reinterpret_cast<const uint32_t*>(&cut);
+  }
+  return u;
 }
 
 // grid: (sequence and page of its table, 2 x key heads)
@@ -42,22 +46,23 @@ cache_expand_kernel(const __grid_constant__ CacheView c, const __grid_constant__
   const int64_t to = compact ? (int64_t)seq * c.max_pages + col : page;
   if (compact && blockIdx.y == 0 && threadIdx.x == 0) table[to] = real ? (int)to : -1;
   if (!real) return;
-  const int vecs = c.head_dim >> 4;  // of 16 codes
+  const unsigned vecs = c.head_dim >> 4;  // of 16 codes
   const char* src = (keys ? c.k : c.v) + page * c.page_b + h * c.head_b;
   const float* sc = (keys ? s.k : s.v) + page * s.page + h * s.head;
   E* dst = reinterpret_cast<E*>(pool + (keys ? 0 : pool_b)) +
            (((to * c.kv_heads + h) << c.page_shift) * c.head_dim);
-  for (int i = threadIdx.x; i < used * vecs; i += CE_T) {
+#pragma unroll 1
+  for (unsigned i = threadIdx.x; i < used * vecs; i += CE_T) {
     const int slot = i / vecs, v = i - slot * vecs;
     float x[16];
     codes_float<C>(*reinterpret_cast<const uint4*>(src + slot * c.slot_b + 16 * v), x);
     const float f = sc[(slot >> s.shift) * s.block];
-    __align__(16) E y[16];
+    uint32_t y[8];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) y[e] = ce_narrow<E>(x[e] * f);
+    for (int e = 0; e < 8; ++e) y[e] = ce_narrow<E>(x[2 * e] * f, x[2 * e + 1] * f);
     uint4* d = reinterpret_cast<uint4*>(dst + (int64_t)slot * c.head_dim + 16 * v);
-    d[0] = reinterpret_cast<const uint4*>(y)[0];
-    d[1] = reinterpret_cast<const uint4*>(y)[1];
+    d[0] = make_uint4(y[0], y[1], y[2], y[3]);
+    d[1] = make_uint4(y[4], y[5], y[6], y[7]);
   }
 }
 
