@@ -18,6 +18,7 @@ namespace {
 
 constexpr int AF_SUM_T = 256;
 constexpr int AF_UNIT = 4 * AF_SUM_T;  // tokens of a CTA of the second launch
+constexpr int AF_AHEAD = 4;            // rows whose scores it fetches first
 
 // SIZE: bytes of an element of keys
 template <int HD, int SIZE>
@@ -342,7 +343,25 @@ attention_scores_sum_kernel(const __grid_constant__ AttnArgs a,
   const int64_t total = p.prefix[c.B], first = p.prefix[seq];
   const int parts = ad_parts(total, p.groups);
   const int n = ad_steps(c, seq);
-  const int64_t page = x < len ? c.table[seq * c.table_ld + (x >> c.page_shift)] : -1;
+  // the first rows' scores and the tokens' weights so far are fetched while the pieces are joined
+  const float* sp = p.scores + (q0 * a.q_heads + h * group) * p.room + x;
+  auto scores = [&](int64_t row) {
+    const int64_t tok = ad_div(row, group);
+    return *reinterpret_cast<const float4*>(sp + (tok * a.q_heads + (row - tok * group)) * p.room);
+  };
+  float4 ahead[AF_AHEAD];
+#pragma unroll
+  for (int i = 0; i < AF_AHEAD; ++i)
+    if (x < len && i < rows) ahead[i] = scores(i);
+  float4 was = make_float4(0.f, 0.f, 0.f, 0.f);
+  float* to = nullptr;  // four slots of one page
+  if (x < len && rows > 0) {
+    const int64_t page = c.table[seq * c.table_ld + (x >> c.page_shift)];
+    if (page >= 0 && page < c.num_pages) {
+      to = wv.data + page * wv.page + h * wv.head + (x & ((1 << c.page_shift) - 1));
+      was = *reinterpret_cast<const float4*>(to);
+    }
+  }
   float w[4] = {0.f, 0.f, 0.f, 0.f};
   for (int64_t b0 = 0; b0 < rows; b0 += AF_SUM_T) {
     const int here = (int)min((int64_t)AF_SUM_T, rows - b0);
@@ -380,32 +399,30 @@ attention_scores_sum_kernel(const __grid_constant__ AttnArgs a,
       if (lane == 0) s_stat[i] = make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.f / l);
     }
     __syncthreads();
-    if (x < len) {
-      const float* sp = p.scores + (q0 * a.q_heads + h * group) * p.room + x;
-      for (int i = 0; i < here; ++i) {
-        const int64_t tok = ad_div(b0 + i, group);
-        const float4 f =
-            *reinterpret_cast<const float4*>(sp + (tok * a.q_heads + (b0 + i - tok * group)) * p.room);
-        const float s[4] = {f.x, f.y, f.z, f.w};
-        const float2 y = s_stat[i];
+    auto add = [&](const float4& f, int i) {
+      const float s[4] = {f.x, f.y, f.z, f.w};
+      const float2 y = s_stat[i];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          w[k] += s[k] == -INFINITY ? 0.f : at_exp2((s[k] - y.x) * cs) * y.y;
-      }
+      for (int k = 0; k < 4; ++k)
+        w[k] += s[k] == -INFINITY ? 0.f : at_exp2((s[k] - y.x) * cs) * y.y;
+    };
+    if (x < len) {
+      if (b0 == 0)
+#pragma unroll
+        for (int i = 0; i < AF_AHEAD; ++i)
+          if (i < here) add(ahead[i], i);
+      for (int i = b0 == 0 ? AF_AHEAD : 0; i < here; ++i) add(scores(b0 + i), i);
     }
   }
-  if (rows == 0 || page < 0 || page >= c.num_pages) return;
-  // four slots of one page; those past the end are left as they are
-  float* to = wv.data + page * wv.page + h * wv.head + (x & ((1 << c.page_shift) - 1));
-  if (x + 4 <= len) {
-    float4 f = *reinterpret_cast<float4*>(to);
-    f.x += w[0], f.y += w[1], f.z += w[2], f.w += w[3];
-    *reinterpret_cast<float4*>(to) = f;
-  } else {
+  if (!to) return;
+  // those past the end are left as they are
+  if (x + 4 <= len)
+    *reinterpret_cast<float4*>(to) =
+        make_float4(was.x + w[0], was.y + w[1], was.z + w[2], was.w + w[3]);
+  else
 #pragma unroll
     for (int k = 0; k < 4; ++k)
       if (x + k < len) to[k] += w[k];
-  }
 }
 
 struct AfHost {
