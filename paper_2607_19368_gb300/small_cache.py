@@ -147,20 +147,17 @@ def qkv_append_q8(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cache_k: to
         raise ValueError("k and v: one row per token of q and key head")
     rq, ro = _rows("q", q, dt, 0, hd, dev), _rows("out", out, dt, 0, hd, dev)
     rk, rv = _rows("k", k, dt, H, hd, dev), _rows("v", v, dt, H, hd, dev)
-    if cu_seqlens is not None:
-        cu_seqlens = _ints("cu_seqlens", cu_seqlens, B + 1, dev)
-    elif T != B:
+    if cu_seqlens is None and T != B:
         raise ValueError("without cu_seqlens q has one token per sequence")
-    if positions is not None:
-        positions = _ints("positions", positions, T, dev)
-    if q_weight is not None:
-        q_weight = _weight("q_weight", q_weight, dt, hd, dev)
-    if k_weight is not None:
-        k_weight = _weight("k_weight", k_weight, dt, hd, dev)
+    # tensors keep their names: one that a caller makes for this call lives until it is enqueued
+    cu = None if cu_seqlens is None else _ints("cu_seqlens", cu_seqlens, B + 1, dev)
+    pos = None if positions is None else _ints("positions", positions, T, dev)
+    wq = None if q_weight is None else _weight("q_weight", q_weight, dt, hd, dev)
+    wk = None if k_weight is None else _weight("k_weight", k_weight, dt, hd, dev)
     if rope is not None and rope.inv_freq.get_device() != dev:
         raise ValueError("rope: frequencies on the cache's device")
-    _call("sls_qkv_append_q8", dev, rq, rk, rv, T, shape[1], c, s, dtype, cu_seqlens, positions,
-          q_weight, k_weight, eps, None if rope is None else rope._c, ro)
+    _call("sls_qkv_append_q8", dev, rq, rk, rv, T, shape[1], c, s, dtype, cu, pos, wq, wk, eps,
+          None if rope is None else rope._c, ro)
     return out
 
 
@@ -235,16 +232,16 @@ def attention_weights(q: torch.Tensor, cache_k: torch.Tensor, page_table: torch.
     w = _weights(weights, n, ps, H, dev)
     rq = _rows("q", q, q.dtype, 0, hd, dev)
     T, Hq, _ = q.shape
-    if cu_seqlens is not None:
-        cu_seqlens = _ints("cu_seqlens", cu_seqlens, B + 1, dev)
-    elif T != B:
+    if cu_seqlens is None and T != B:
         raise ValueError("without cu_seqlens q has one token per sequence")
+    # not by the tensor's own name: one made for this call must outlive the workspace's allocation
+    cu = None if cu_seqlens is None else _ints("cu_seqlens", cu_seqlens, B + 1, dev)
     nbytes = _bytes("weights", dev, _ANY[dt], block, (T, Hq, dtype), (H, hd, ps, n, B, cols))
     wp = 0
     if nbytes:
         workspace = _scratch(nbytes, workspace, q, dev)
         wp, nbytes = workspace.data_ptr(), workspace.numel()
-    _call("sls_attention_weights", dev, rq, T, Hq, c, s, dtype, cu_seqlens, causal,
+    _call("sls_attention_weights", dev, rq, T, Hq, c, s, dtype, cu, causal,
           hd ** -0.5 if scale is None else float(scale), w, wp, nbytes)
     return weights
 

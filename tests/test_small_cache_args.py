@@ -1,6 +1,7 @@
 """Refusals of the calls that make the cache smaller, without a GPU."""
 import ctypes
 import math
+import weakref
 
 import pytest
 import torch
@@ -200,3 +201,47 @@ def test_binding_refuses_what_it_cannot_pass(sls):
         sls.cache_evict(k, k, t, n, w, 4)
     with pytest.raises(TypeError):
         sls.attention_decode(q, k, k, t, n)                            # the 16-bit call
+
+
+def test_arguments_live_until_the_call(sls, monkeypatch):
+    """Tensors that a caller makes for one call are not freed before its workspace is allocated,
+    which could take their memory, nor before its launches."""
+    from paper_2607_19368_gb300 import small_cache as C
+    refs, alive = [], []
+
+    def temp(*shape, dtype=torch.int32):
+        t = torch.zeros(*shape, dtype=dtype)
+        refs.append(weakref.ref(t))
+        return t
+
+    def look(*a, **kw):
+        alive.append([r() is not None for r in refs])
+        return torch.empty(16, dtype=torch.uint8)
+
+    k = torch.zeros(4, 32, 2, 64, dtype=torch.int8)
+    monkeypatch.setattr(C, "_cache", lambda *a: (b"", k.shape, k.dtype, 0, 2, 2))
+    for name in ("_rows", "_ints", "_weight", "_weights"):
+        monkeypatch.setattr(C, name, lambda *a: 256)
+    monkeypatch.setattr(C, "_scales", lambda *a: (b"", 16))
+    monkeypatch.setattr(C, "_bytes", lambda *a: 16)
+    monkeypatch.setattr(C, "_attention_rows", lambda q, out, *a: (b"", b"", q, 1.0))
+    monkeypatch.setattr(C, "_scratch", look)
+    monkeypatch.setattr(C, "_call", look)
+    f32, bf16 = torch.float32, torch.bfloat16
+    q = torch.zeros(2, 4, 64, dtype=bf16)
+    C.attention_weights(temp(2, 4, 64, dtype=bf16), k, temp(2, 2), temp(2),
+                        temp(4, 2, 32, dtype=f32), temp(3), k_scale=temp(4, 2, 2, dtype=f32))
+    assert alive == [[True] * 6] * 2
+    refs.clear(), alive.clear()
+    C.attention_prefill_q8(temp(2, 4, 64, dtype=bf16), k, k, temp(4, 2, 2, dtype=f32),
+                           temp(4, 2, 2, dtype=f32), temp(2, 2), temp(2), temp(3), out=q)
+    assert alive == [[True] * 6] * 2
+    refs.clear(), alive.clear()
+    C.attention_decode_q8(temp(2, 4, 64, dtype=bf16), k, k, temp(4, 2, 2, dtype=f32),
+                          temp(4, 2, 2, dtype=f32), temp(2, 2), temp(2), out=q)
+    assert alive == [[True] * 5] * 2
+    refs.clear(), alive.clear()
+    C.qkv_append_q8(q, temp(2, 2, 64, dtype=bf16), temp(2, 2, 64, dtype=bf16), k, k,
+                    temp(4, 2, 2, dtype=f32), temp(4, 2, 2, dtype=f32), temp(2, 2), temp(2),
+                    temp(3), temp(2), temp(64, dtype=bf16), temp(64, dtype=bf16))
+    assert alive == [[True] * 10]
