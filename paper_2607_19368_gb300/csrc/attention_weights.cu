@@ -9,8 +9,10 @@
 // token's column, with the rows' maxima and sums read from shared memory by all at once.  No sum is
 // made by atomics: the same call gives the same bits.
 //
-// The exponent of a weight is formed by one multiply-add, score times scale less the row's maximum and
-// the logarithm of its sum: rounded by 2^-24 of the score, as the score itself is.
+// An exponent is one multiply-add of the score, with the row's maximum times the scale, rounded, as
+// the summand; what that rounding is off by, the same for all of a row, is taken out of its
+// sum and of the factor of its weights (left in, it is 2^-24 of the maximum's exponent: 1.4e-6 of the
+// weights instead of 2e-7 where scores reach 30).
 //
 // Bound by exponentials (two a score) and, for few rows, by the products of padded tiles; the keys'
 // bytes are below either from some ten rows on.  A CTA goes through phases in step (keys to shared
@@ -268,6 +270,12 @@ SLS_DEV void aw_free(uint32_t tmem) {
   }
 }
 
+// A sum of 2^(v f + off), off the rounded -m f, as that of 2^((v - m) f): the rounding's remainder x is
+// exact by one multiply-add and far below 1, 2^-x to first order.
+SLS_DEV float aw_exact(float sum, float m, float f, float off) {
+  return __fmaf_rn(sum, -0.69314718f * __fmaf_rn(m, f, off), sum);
+}
+
 // ---- first pass: maxima and sums of rows -------------------------------------------------
 template <typename E, typename KT, int HD>
 __global__ void __launch_bounds__(AW_T, 2)
@@ -385,10 +393,11 @@ attention_weights_rows_kernel(const __grid_constant__ AttnArgs a,
         for (int i = 3; i < 31; i += 2) top = ap_max3(top, v[i], v[i + 1]);
         top = ap_max3(top, v[31], m);
         const float base = top == -INFINITY ? 0.f : top, off = -base * f;
-        float sum[4] = {l * at_exp2(__fmaf_rn(m, f, off)), 0.f, 0.f, 0.f};
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 32; ++i) sum[i & 3] += at_exp2(__fmaf_rn(v[i], f, off));
-        l = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        const float here = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        l = __fmaf_rn(l, at_exp2((m - base) * f), aw_exact(here, base, f, off));
         m = top;
       }
       ap_fence_before();
@@ -469,8 +478,12 @@ attention_weights_join_kernel(const __grid_constant__ AttnArgs a, const __grid_c
     }
   }
   __syncwarp();
-  // 2^(score cs + this) is the weight
-  if (lane == 0) p.stat[id].x = l == 0.f ? -INFINITY : -m * cs - log2f(l);
+  // y 2^(score cs + x) is the weight
+  if (lane == 0) {
+    const float x = -m * cs;
+    p.stat[id] = l == 0.f ? make_float2(-INFINITY, 0.f)
+                          : make_float2(x, aw_exact(1.f / l, m, cs, x));
+  }
 }
 
 // ---- second pass: sums of columns ----------------------------------------------------------
@@ -484,6 +497,7 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
   __shared__ int64_t s_pre[AW_T + 1];
   __shared__ float s_factor[2 * AW_TILE];
   __shared__ __align__(16) float2 s_row[2 * AW_TILE];  // factor and summand of a row's exponents
+  __shared__ __align__(16) float s_inv[2 * AW_TILE];   // factor of its weights
   __shared__ __align__(16) int s_see[2 * AW_TILE];     // tokens that it sees
   // of two units: a thread may still read its token's when another fetches the next unit's
   __shared__ float s_scale[2][AW_TILE], s_sum[AW_TILE];
@@ -544,10 +558,11 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
     if (r1.count > 0) aw_stage_rows<E, KT, HD>(a, w, r1, rows_s + S::TILE_BYTES, s_factor + AW_TILE);
     const int k = threadIdx.x & (AW_TILE - 1);
     const AwRows& mine = threadIdx.x < AW_TILE ? r0 : r1;
-    float add = -INFINITY;
-    if (k < mine.count) add = p.stat[mine.packed(a, w, k)].x;
+    float2 stat = make_float2(-INFINITY, 0.f);
+    if (k < mine.count) stat = p.stat[mine.packed(a, w, k)];
     __syncthreads();
-    s_row[threadIdx.x] = make_float2(s_factor[threadIdx.x] * cs, add);
+    s_row[threadIdx.x] = make_float2(s_factor[threadIdx.x] * cs, stat.x);
+    s_inv[threadIdx.x] = stat.y;
     s_see[threadIdx.x] = mine.see(a, w, k);
   };
   // products of a tile; one whose last row sees none of the tokens adds nothing
@@ -582,16 +597,20 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
 #pragma unroll
           for (int j = 0; j < 4; ++j) v[k + j] *= scale;
         }
+        const float4 y = *reinterpret_cast<const float4*>(&s_inv[row0 + half + k]);
+        const float by[4] = {y.x, y.y, y.z, y.w};
         const float e[4] = {at_exp2(__fmaf_rn(v[k], f.x, f.y)), at_exp2(__fmaf_rn(v[k + 1], f.z, f.w)),
                             at_exp2(__fmaf_rn(v[k + 2], g.x, g.y)),
                             at_exp2(__fmaf_rn(v[k + 3], g.z, g.w))};
         if (whole) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) col[j] += e[j];
+          for (int j = 0; j < 4; ++j) col[j] = __fmaf_rn(e[j], by[j], col[j]);
         } else {
           const int4 see = *reinterpret_cast<const int4*>(&s_see[row0 + half + k]);
-          col[0] += x < see.x ? e[0] : 0.f, col[1] += x < see.y ? e[1] : 0.f;
-          col[2] += x < see.z ? e[2] : 0.f, col[3] += x < see.w ? e[3] : 0.f;
+          const int s[4] = {see.x, see.y, see.z, see.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (x < s[j]) col[j] = __fmaf_rn(e[j], by[j], col[j]);
         }
       }
     }

@@ -322,6 +322,33 @@ def test_weights(sls, case, code, dtype):
     assert torch.equal(first, w)
 
 
+@pytest.mark.parametrize("rows", [1, 16])
+def test_weights_of_scores_far_from_zero(sls, rows):
+    """Scores of 423 that differ by 0 or 3.33 and are exact (one element of a query and a code
+    each): what is left are the exponents' roundings, which go by the distance from the maximum and
+    not by the score.  In units of 2^-24: an exponent of at most 4.8 is off by 2 for the rounded
+    factor and 1 for its own rounding, all of that times 4.8 log(2), and its power by 4: 14, for the
+    weight and for the sum; sums of earlier tokens are taken to a larger maximum in at most three
+    places, 14 each; their additions and products are at most 16, a weight's own and its column's 16:
+    102."""
+    m, page, block, scale = 300, 64, 32, 1.6661376953125
+    k = torch.zeros(5, page, 1, 64, dtype=torch.int8, device="cuda")
+    idx = torch.arange(5 * page, device="cuda").view(5, page)
+    k[:, :, 0, 0] = torch.where((idx < 128) | (idx % 3 == 0), 126, 127).to(torch.int8)
+    ones = torch.ones(5, page // block, 1, device="cuda")
+    table = torch.arange(5, dtype=torch.int32, device="cuda")[None]
+    lens = torch.tensor([m], dtype=torch.int32, device="cuda")
+    q = torch.zeros(rows, 1, 64, dtype=torch.bfloat16, device="cuda")
+    q[:, 0, 0] = 2
+    w = torch.zeros(5, 1, page, device="cuda")
+    sls.attention_weights(q, k, table, lens, w, torch.tensor([0, rows], dtype=torch.int32, device="cuda"),
+                          k_scale=ones, causal=False, scale=scale)
+    s = 2 * k[:, :, 0, 0].double().flatten()[:m] * scale
+    want = rows * torch.softmax(s, 0)
+    error = ((w.flatten()[:m].double() - want).abs() / want).max().item()
+    assert error <= 102 * 2 ** -24, error * 2 ** 24
+
+
 # ---------------------------------------------------------------------------
 # eviction
 # ---------------------------------------------------------------------------
