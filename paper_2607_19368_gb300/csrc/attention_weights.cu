@@ -18,8 +18,10 @@
 // bytes are below either from some ten rows on.  A CTA goes through phases in step (keys to shared
 // memory, codes to float16 on the way; products; scores), with the next keys on their way in
 // registers; two CTAs an SM fill each other's gaps.  32 rows (tokens) of 7 heads over 32768
-// tokens of 4 key heads, e4m3: 86 us with mma.sync, whose products took the time, see the table
-// of cases for now.
+// tokens of 4 key heads, e4m3: 58.3 us, 24.0 the first pass and 34.5 the second (86 us with mma.sync,
+// whose products took the time); 58.7 million exponentials are 12 us at 16 a cycle and SM.  A CTA has
+// 7 tiles of a row tile, then 3.4 units of two: in a trace 9000 to 15000 of its 36000 and 46000
+// cycles go until the first scores (lengths, pages, rows), a tile's scores take 1700 to 2400.
 //
 // Where rows are few (a token for each sequence) the kernels of attention_weights_few.cu read keys
 // once instead.
@@ -777,9 +779,9 @@ int launch(const AttnArgs& a, const ScaleView& s, const WeightView& w, int code,
 
 }  // namespace
 
-size_t attention_weights_workspace(const CacheView& c, int64_t T, int q_heads, int code) {
+size_t attention_weights_workspace(const CacheView& c, int64_t T, int q_heads) {
   if (c.B == 0 || T == 0 || c.max_pages == 0) return 0;
-  if (attention_weights_few(c, T, q_heads, code))
+  if (attention_weights_few(c, T, q_heads))
     return attention_weights_few_workspace(c, T, q_heads);
   AwHost h;
   return aw_host(c, T, q_heads, &h) == SLS_OK ? h.prefix_b + h.ml_b + h.stat_b : 0;
@@ -789,7 +791,7 @@ int launch_attention_weights(const AttnArgs& a, const ScaleView& s, const Weight
                              int dtype, void* workspace, cudaStream_t stream) {
   if (a.c.B == 0 || a.T == 0 || a.c.max_pages == 0) return SLS_OK;
   if (a.T * a.q_heads > (int64_t)0x7fffffff * AW_JOIN_WARPS) return SLS_ERR_UNSUPPORTED;
-  if (attention_weights_few(a.c, a.T, a.q_heads, code))
+  if (attention_weights_few(a.c, a.T, a.q_heads))
     return launch_attention_weights_few(a, s, w, code, dtype, workspace, stream);
   AwHost h;
   const int st = aw_host(a.c, a.T, a.q_heads, &h);

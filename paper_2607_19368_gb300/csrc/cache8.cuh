@@ -124,13 +124,13 @@ size_t attention_decode_q8_workspace(const CacheView& c, int q_heads);
 int launch_attention_decode_q8(const AttnArgs& a, const ScaleView& s, int code, int dtype,
                                void* workspace, cudaStream_t stream);
 
+size_t attention_weights_workspace(const CacheView& c, int64_t T, int q_heads);
 // code: SLS_I8, SLS_E4M3, or dtype for a 16-bit cache
-size_t attention_weights_workspace(const CacheView& c, int64_t T, int q_heads, int code);
 int launch_attention_weights(const AttnArgs& a, const ScaleView& s, const WeightView& w, int code,
                              int dtype, void* workspace, cudaStream_t stream);
 
 // The path for few rows a sequence, and whether it is taken.
-bool attention_weights_few(const CacheView& c, int64_t T, int q_heads, int code);
+bool attention_weights_few(const CacheView& c, int64_t T, int q_heads);
 size_t attention_weights_few_workspace(const CacheView& c, int64_t T, int q_heads);
 int launch_attention_weights_few(const AttnArgs& a, const ScaleView& s, const WeightView& w,
                                  int code, int dtype, void* workspace, cudaStream_t stream);

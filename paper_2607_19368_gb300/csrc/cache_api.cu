@@ -176,7 +176,7 @@ size_t sls_attention_weights_workspace_size(int64_t T, int q_heads, const sls_kv
   if (T < 0 || T > kMaxTokens || !dtype_ok(dtype) ||
       any_cache(cache, scales, q_heads, true, &c, &s) != SLS_OK)
     return 0;
-  return attention_weights_workspace(c, T, q_heads, cache->dtype);
+  return attention_weights_workspace(c, T, q_heads);
 }
 
 int sls_attention_weights(const sls_rows_t* q, int64_t T, int q_heads,
@@ -200,7 +200,7 @@ int sls_attention_weights(const sls_rows_t* q, int64_t T, int q_heads,
   a.cu = cu_seqlens;
   a.causal = causal != 0;
   a.scale = scale;
-  const size_t need = attention_weights_workspace(a.c, T, q_heads, cache->dtype);
+  const size_t need = attention_weights_workspace(a.c, T, q_heads);
   if (need > 0 && (!aligned16(workspace) || workspace_bytes < need)) return SLS_ERR_WORKSPACE;
   return launch_attention_weights(a, s, w, cache->dtype, dtype, workspace, (cudaStream_t)stream);
 }

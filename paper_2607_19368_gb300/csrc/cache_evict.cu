@@ -7,7 +7,12 @@
 // front of every token, which gives it its place; weights move here.  The second moves keys and values.  A place is never behind its source, so a cluster of
 // CTAs takes the places in waves, in order: what a wave reads lies at or behind its first place,
 // what earlier waves wrote lies in front of it, and the one barrier between a wave's reads and its
-// writes is all that moving in place needs.  Bound by the bytes of weights and moved rows.
+// writes is all that moving in place needs.
+//
+// Bound by the bytes of weights and moved rows in the limit, here by latency: a selection is a
+// chain of a dozen barriers over a cluster, a wave one of dependent loads (index, page, row) and a
+// barrier.  One prompt of 32768 tokens to 2048, 4 heads of 128, bfloat16: 20 us; 24 of up to 8192 to
+// 1024, 8 heads, e4m3: 38 us, of it 22 and 24 under a profiler for the two launches, which overlap.
 #include <algorithm>
 
 #include "cache8.cuh"
@@ -416,7 +421,8 @@ cache_evict_move_kernel(const __grid_constant__ EvictArgs a) {
 template <typename C>
 int launch_move(const EvictArgs& a, int sms, cudaStream_t stream) {
   const CacheView& c = a.c;
-  // keys and values by one cluster where there are clusters enough without
+  // keys and values by one cluster where there are clusters enough without (sequences to 8192, 8 heads
+  // of 128 in e4m3, to 1024: 4 of them 17.8 us so, 17.5 apart; 6 21.4 and 23.3; 12 29.8 and 32.0)
   const int64_t units = (int64_t)c.B * c.kv_heads;
   const bool both = units * EV_CLUSTER >= 2 * sms;
   const int rows = both ? EvMove<C, true>::ROWS : EvMove<C, false>::ROWS;

@@ -14,6 +14,11 @@
 // The queries go through the 16-bit append's kernel, with no key heads, which starts while the last
 // CTAs here run (21345 tokens: 131 us one after the other); those of few tokens are turned by CTAs of
 // this launch.
+//
+// Bound by memory in the limit; keys and values are held up by latency and instructions instead (16
+// warps an SM, 42% of issue slots, 19% of DRAM's rate in a profile of them alone), which the queries'
+// launch makes up for in part.  21345 tokens of 32 + 8 heads of 128, e4m3: 118.8 us, 4.1 TB/s; 10717
+// tokens of 25 + 5 heads of 64, int8: 20.2 us, 2.7 TB/s; 4 single tokens 4.2 us, latency.
 #include <algorithm>
 
 #include "attention_turn.cuh"
@@ -27,7 +32,10 @@ constexpr int Q8_T = 256;
 // rows as they come; halves of whole vectors; pairs side by side; halves that split vectors
 enum { Q8_PLAIN, Q8_HALVES, Q8_SIDES, Q8_ODD };
 constexpr int Q8_WARPS = 1216, Q8_CTAS = 912;  // at least so many, heads permitting: for 152 SMs
-constexpr int Q8_FEW = 2;  // new tokens of a block up to which a job is one group's
+// New tokens of a block up to which a head is one group's (64 sequences of 2 / 3 / 4 / 6 / 8 tokens,
+// 4 heads of 128: 5.5 / 7.9 / 8.6 / 9.3 / 14.1 us so, 6.6 / 9.1 / 9.3 / 7.5 / 10.1 by warps; the number
+// is rounded down to a power of two).
+constexpr int Q8_FEW = 2;
 
 // Where a packed token goes.
 struct Q8Place {

@@ -322,7 +322,7 @@ def test_weights(sls, case, code, dtype):
     assert torch.equal(first, w)
 
 
-@pytest.mark.parametrize("rows", [1, 16])
+@pytest.mark.parametrize("rows", [1, 16, 40])
 def test_weights_of_scores_far_from_zero(sls, rows):
     """Scores of 423 that differ by 0 or 3.33 and are exact (one element of a query and a code
     each): what is left are the exponents' roundings, which go by the distance from the maximum and
