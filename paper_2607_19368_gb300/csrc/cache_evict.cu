@@ -171,7 +171,8 @@ cache_evict_select_kernel(const __grid_constant__ EvictArgs a, int room4) {
   int32_t* kept = a.kept + ((int64_t)seq * c.kv_heads + h) * a.keep;
   const EvSeq e{a, seq, h};
   if (len <= a.keep) {
-    for (int i = rank * EV_T + threadIdx.x; i < a.keep; i += size * EV_T) kept[i] = i < len ? i : -1;
+    for (int64_t i = rank * EV_T + threadIdx.x; i < a.keep; i += size * EV_T)
+      kept[i] = i < len ? (int)i : -1;
     return;
   }
   // this CTA's weights, four in a row at a time, to shared memory: loops over them stay short, and
@@ -290,11 +291,11 @@ cache_evict_select_kernel(const __grid_constant__ EvictArgs a, int room4) {
     }
   }
   // four slots at a time from the first multiple of four on
-  const int z0 = (a.keep + 3) & ~3;
-  for (int x = a.keep + threadIdx.x; x < min(z0, len) && rank == 0; x += EV_T)
+  const int64_t z0 = ((int64_t)a.keep + 3) & ~(int64_t)3;
+  for (int x = a.keep + threadIdx.x; x < min(z0, (int64_t)len) && rank == 0; x += EV_T)
     if (float* p = e.weight(x)) *p = 0.f;
 #pragma unroll 1
-  for (int x = z0 + 4 * (int)(rank * EV_T + threadIdx.x); x < len; x += 4 * size * EV_T)
+  for (int64_t x = z0 + 4 * (int64_t)(rank * EV_T + threadIdx.x); x < len; x += 4 * size * EV_T)
     if (float* p = e.weight(x)) {
       if (x + 4 <= len) *reinterpret_cast<float4*>(p) = make_float4(0.f, 0.f, 0.f, 0.f);
       else

@@ -328,3 +328,18 @@ def test_weights_of_many_rows(sls, dtype):
         sls.attention_weights(b["q"], b["k"], b["table"], b["kv_lens"], w, cu_seqlens=b["cu"],
                               scale=scale)
         S.check(w, want, bound, f"scale {scale}")
+
+
+def test_eviction_that_keeps_as_many_as_there_can_be(sls):
+    """kept has 2^31 - 1 places for a sequence of 40 tokens: every other one is -1, and nothing
+    outside is written."""
+    k = torch.zeros(3, 16, 1, 16, dtype=torch.bfloat16, device="cuda")
+    table = torch.arange(3, dtype=torch.int32, device="cuda").view(1, 3)
+    lens = torch.tensor([40], dtype=torch.int32, device="cuda")
+    w = torch.rand(3, 1, 16, device="cuda")
+    before = w.clone()
+    kept = sls.cache_evict(k, k.clone(), table, lens, w, 2 ** 31 - 1)
+    assert kept.shape == (1, 1, 2 ** 31 - 1)
+    assert kept[0, 0, :40].tolist() == list(range(40))
+    assert kept[0, 0, 40:].min().item() == -1 and kept[0, 0, 40:].max().item() == -1
+    assert lens.tolist() == [40] and torch.equal(w, before)
