@@ -134,9 +134,10 @@ struct Q8Lane {
   }
 
   // u: the row at p, loaded; y: its elements without the norm; most: the largest finite size.
-  // KEYS: else as it comes.
+  // KEYS: else as it comes.  known: the norm, where it is (and `most` is not wanted).
   template <bool KEYS>
-  SLS_DEV float row(const uint4 (&u)[2], const char* p, int slot, float (&y)[16], float& most) const {
+  SLS_DEV float row(const uint4 (&u)[2], const char* p, int slot, float (&y)[16], float& most,
+                    const float* known = nullptr) const {
     float norm = 1.f;
 #pragma unroll
     for (int v = 0; v < 2; ++v) {
@@ -146,7 +147,9 @@ struct Q8Lane {
       for (int e = 0; e < 8; ++e) y[8 * v + e] = z[e];
     }
     if constexpr (KEYS && MODE != Q8_PLAIN) {
-      if (w) {
+      if (known) {
+        norm = *known;
+      } else if (w) {
         f32x2_t s = mul2(pk2(y[0], y[1]), pk2(y[0], y[1]));
 #pragma unroll
         for (int e = 2; e < 16; e += 2) s = fma2(pk2(y[e], y[e + 1]), pk2(y[e], y[e + 1]), s);
@@ -309,7 +312,7 @@ SLS_DEV void q8_few(const Q8Lane<E, L, MODE>& me, const Q8Block& b) {
 // for the maximum, and (from the caches) for the codes.  Alone (share 1) a warp waits for no other.
 template <bool KEYS, typename E, int L, int MODE>
 SLS_DEV void q8_many(const Q8Lane<E, L, MODE>& me, const Q8Block& b, int j, bool live, int share,
-                     float (&s_most)[2][Q8_T / 32], int& parity) {
+                     float (&s_most)[2][Q8_T / 32], int& parity, float* norms) {
   constexpr int AT = 32 / L;  // rows of a warp at a time
   constexpr int AHEAD = 2;    // loaded before the first is worked on
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -332,7 +335,10 @@ SLS_DEV void q8_many(const Q8Lane<E, L, MODE>& me, const Q8Block& b, int j, bool
         const int slot = s + k * step;
         if constexpr (KEYS && MODE != Q8_PLAIN) {
           float y[16];
-          if (slot >= b.lo && slot < b.hi) me.template row<KEYS>(u[k], p + slot * b.token_b, slot, y, most);
+          if (slot >= b.lo && slot < b.hi) {
+            const float norm = me.template row<KEYS>(u[k], p + slot * b.token_b, slot, y, most);
+            if (me.l == 0) norms[slot] = norm;
+          }
         } else {
 #pragma unroll
           for (int v = 0; v < 2; ++v) {
@@ -388,7 +394,7 @@ SLS_DEV void q8_many(const Q8Lane<E, L, MODE>& me, const Q8Block& b, int j, bool
       if (slot >= b.hi) continue;
       if (slot >= b.lo) {
         float y[16], again = 0.f;
-        const float norm = me.template row<KEYS>(u[k], p + slot * b.token_b, slot, y, again);
+        const float norm = me.template row<KEYS>(u[k], p + slot * b.token_b, slot, y, again, norms + slot);
         if (me.on) me.store(d + slot * b.slot_b, q8_codes(b.ints, y, norm * by));
       } else if (me.on && now > was) {
         q8_again(me, b.ints, d + slot * b.slot_b, was * by);
@@ -396,6 +402,7 @@ SLS_DEV void q8_many(const Q8Lane<E, L, MODE>& me, const Q8Block& b, int j, bool
     }
   }
   if (slot0 == 0 && me.l == 0 && now != was) *sp = now;
+  __syncwarp();  // the norms are read
 }
 
 // The queries of packed rows [t, t_end), from the sequence of row t on: a group of lanes for each
@@ -448,6 +455,7 @@ kv_append_q8_kernel(const __grid_constant__ AppendArgs a, const __grid_constant_
                     int tile, int jobs_per_cta, int share, int query_cta, bool ints) {
   extern __shared__ float4 s_tab[];
   __shared__ float s_most[2][Q8_T / 32];
+  __shared__ float s_norm[FEW || MODE == Q8_PLAIN ? 1 : Q8_T / 32][128];  // of a warp's rows
   __shared__ int s_ended[Q8_T / 32];
   const CacheView& c = a.c;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -523,8 +531,9 @@ kv_append_q8_kernel(const __grid_constant__ AppendArgs a, const __grid_constant_
         for (int j0 = j_first; j0 < j_end; j0 += together) {
           const int j = j0 + warp / share;
           const bool live = j < j_end;
-          if (j < c.kv_heads) q8_many<true>(me, k, live ? j : 0, live, share, s_most, parity);
-          else q8_many<false>(me, v, live ? j - c.kv_heads : 0, live, share, s_most, parity);
+          float* const norms = s_norm[MODE == Q8_PLAIN ? 0 : warp];
+          if (j < c.kv_heads) q8_many<true>(me, k, live ? j : 0, live, share, s_most, parity, norms);
+          else q8_many<false>(me, v, live ? j - c.kv_heads : 0, live, share, s_most, parity, norms);
         }
       }
     }
