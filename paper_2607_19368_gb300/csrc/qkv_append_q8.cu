@@ -250,6 +250,17 @@ SLS_DEV uint4 q8_codes(bool ints, const float (&y)[16], float by) {
 SLS_DEV float q8_scale(bool ints, float most) {
   return ints ? code_scale<I8>(most) : code_scale<E4M3>(most);
 }
+// Codes of a row that lacks its norm, by = 1 / scale.  One product has both factors, except where they
+// leave float32's range together (norm 1 / sqrt(eps) of a row of zeros, by 2^126 of a block of them).
+SLS_DEV uint4 q8_row_codes(bool ints, float (&y)[16], float norm, float by) {
+  float f = norm * by;
+  if (f > 3.402823466e38f) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) y[e] *= norm;
+    f = by;
+  }
+  return q8_codes(ints, y, f);
+}
 // One over a scale: a power of two as a rule.
 SLS_DEV float q8_over(float s) {
   const int bits = __float_as_int(s);
@@ -300,7 +311,7 @@ SLS_DEV void q8_few(const Q8Lane<E, L, MODE>& me, const Q8Block& b) {
         me.load(p + slot * b.token_b, u);
         norm = me.template row<KEYS>(u, p + slot * b.token_b, slot, y, most);
       }
-      if (me.on) me.store(d + slot * b.slot_b, q8_codes(b.ints, y, norm * by));
+      if (me.on) me.store(d + slot * b.slot_b, q8_row_codes(b.ints, y, norm, by));
     }
     if (me.on && now > was)
 #pragma unroll 1
@@ -397,7 +408,7 @@ SLS_DEV void q8_many(const Q8Lane<E, L, MODE>& me, const Q8Block& b, int j, bool
       if (slot >= b.lo) {
         float y[16], again = 0.f;
         const float norm = me.template row<KEYS>(u[k], p + slot * b.token_b, slot, y, again, norms + slot);
-        if (me.on) me.store(d + slot * b.slot_b, q8_codes(b.ints, y, norm * by));
+        if (me.on) me.store(d + slot * b.slot_b, q8_row_codes(b.ints, y, norm, by));
       } else if (me.on && now > was) {
         q8_again(me, b.ints, d + slot * b.slot_b, was * by);
       }
