@@ -7,8 +7,8 @@
 // 103.8 us, 5.8 TB/s; one of 2061 tokens 8.0 us, latency.  A warp owns a (sequence, key head) at a time, its parts
 // and pieces as in the 16-bit kernel, and multiplies float16 (every code is one exactly) by
 // mma.sync.  What the 8 bits change:
-//  * The scale of a block of tokens multiplies finished scores, and weights instead of values
-//    (in units of the largest value scale so far, so that they stay in float16's range).
+//  * The scale of a block of tokens multiplies finished scores, and weights instead of values.  Weights
+//    are then in units of their own for each head, to stay in float16's range: see q8_unit.
 //  * bfloat16 queries become float16 times a power of two for each row, which scores take back:
 //    exact down to 2^-31 of the row's largest element, and to 2^-39 of it below.
 //  * Keys and values are the 16-row operands, query heads the 8 columns (S^T = K Q^T, O^T = V^T
@@ -29,6 +29,26 @@ namespace sls {
 namespace {
 
 constexpr float Q8_SHIFT = 15.f;  // log2 of a factor of all weights, see the 16-bit kernel
+
+// 1 over a power of two from 2^-126 to 2^126.
+SLS_DEV float q8_inverse(float x) { return __int_as_float(0x7f000000 - __float_as_int(x)); }
+// The least power of two from 2^-126 to 2^126 that is at least x.
+SLS_DEV float q8_power(float x) {
+  const int bits = __float_as_int(x), e = (bits >> 23) + ((bits & 0x7fffff) != 0);
+  return __int_as_float(min(max(e, 1), 253) << 23);
+}
+// The unit of a head's weights (times values' scales) from this step on, a power of two.  None of
+// them may be larger; a much larger unit costs their float16 bits, and all of them past 2^39.  So it
+// goes by what a step needs, most = its largest weight times scale, and not by its scales alone: tokens
+// that the head does not look at may have any (2^40 times the others' made its results zeros).  For a
+// common spread of scales, up to 16, it takes the step's largest scale all the same, and rises seldom.
+// was: the unit before, shrink: what the earlier weights are multiplied by now.  The unit stays
+// within 2^126 of the step's scales, so that no scale in units overflows.
+SLS_DEV float q8_unit(float was, float shrink, float scale, float most) {
+  float u = fmaxf(was * shrink, fminf(was, scale));
+  if (scale > u) u = scale <= 16.f * u ? scale : fmaxf(fmaxf(u, most), scale * 0x1p-126f);
+  return q8_power(u);
+}
 
 // NH: blocks of eight query heads a key head
 template <int HD, int NH>
@@ -146,9 +166,9 @@ struct Q8Ring {
   }
 };
 
-// The rows of a piece: queries as operands (lane / 4: the head), unnormalised outputs in units of
-// sv (VB elements of heads 2 (lane % 4) and the next), those heads' maxima in use and this lane's
-// part of their sums of weights.
+// The rows of a piece: queries as operands (lane / 4: the head), unnormalised outputs (VB elements of
+// heads 2 (lane % 4) and the next), those heads' maxima in use, this lane's part of their sums of
+// weights, and 1 over the units that outputs are in.
 template <typename E, typename C, int HD, int NH>
 struct Q8Rows {
   using S = Q8Shape<HD, NH>;
@@ -156,8 +176,7 @@ struct Q8Rows {
   static constexpr int MT = HD / 16;  // 16-row tiles of outputs
   uint32_t q[NH][KS][2];
   float o[NH][MT][4];
-  float mx[NH][2], l[NH][2], qf[NH][2];
-  float sv;
+  float mx[NH][2], l[NH][2], qf[NH][2], per[NH][2];
 
   SLS_DEV void start(const AttnArgs& a, int seq, int head0, int rows) {
     const int lane = threadIdx.x & 31, r = lane >> 2, cq = lane & 3;
@@ -199,11 +218,11 @@ struct Q8Rows {
         qf[x][j] = __shfl_sync(0xffffffffu, back, 4 * (2 * cq + j));
         mx[x][j] = -INFINITY;
         l[x][j] = 0.f;
+        per[x][j] = 0x1p126f;
       }
 #pragma unroll
       for (int b = 0; b < MT; ++b) o[x][b][0] = o[x][b][1] = o[x][b][2] = o[x][b][3] = 0.f;
     }
-    sv = 0.f;
   }
 
   // steps [j0, j1) of a sequence of `len` tokens; cs: scale log2(e)
@@ -259,6 +278,7 @@ struct Q8Rows {
       }
       float top[NH][2];
       bool up = false;
+      const float vmax = fmaxf(fabsf(f4.z), fabsf(f4.w));
 #pragma unroll
       for (int x = 0; x < NH; ++x)
 #pragma unroll
@@ -267,20 +287,31 @@ struct Q8Rows {
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
           top[x][i] = fmaxf(m, mx[x][i]);
-          up |= top[x][i] > mx[x][i];
+          up |= top[x][i] > mx[x][i] || vmax * per[x][i] > 1.f;
         }
-      const float nsv = fmaxf(sv, fmaxf(f4.z, f4.w));
-      if (__any_sync(0xffffffffu, up) || nsv > sv) {
-        const float g = nsv > sv ? sv / nsv : 1.f;
+      if (__any_sync(0xffffffffu, up)) {
 #pragma unroll
         for (int x = 0; x < NH; ++x) {
           float f[2];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
+            // the halves' largest weights
+            float most[2];
+            const float base = top[x][i] == -INFINITY ? 0.f : top[x][i];
+#pragma unroll
+            for (int mt = 0; mt < 2; ++mt) {
+              float m = fmaxf(s[x][mt][i], s[x][mt][2 + i]);
+#pragma unroll
+              for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+              most[mt] = at_exp2((m - base) * cs);
+            }
             f[i] = top[x][i] > mx[x][i] ? at_exp2((mx[x][i] - top[x][i]) * cs) : 1.f;
             mx[x][i] = top[x][i];
             l[x][i] *= f[i];
-            f[i] *= g;
+            const float was = q8_inverse(per[x][i]);
+            per[x][i] = q8_inverse(
+                q8_unit(was, f[i], vmax, fmaxf(most[0] * fabsf(f4.z), most[1] * fabsf(f4.w))));
+            f[i] = f[i] * was * per[x][i];
           }
 #pragma unroll
           for (int b = 0; b < MT; ++b) {
@@ -288,10 +319,7 @@ struct Q8Rows {
             o[x][b][2] *= f[0], o[x][b][3] *= f[1];
           }
         }
-        sv = nsv;
       }
-      const float unit = sv > 0.f ? 1.f / sv : 0.f;
-      const float vs[2] = {f4.z * unit, f4.w * unit};
       uint32_t w[NH][2][2];
 #pragma unroll
       for (int x = 0; x < NH; ++x) {
@@ -301,12 +329,13 @@ struct Q8Rows {
         float sum[2] = {0.f, 0.f};
 #pragma unroll
         for (int mt = 0; mt < 2; ++mt) {
+          const float vs[2] = {(mt ? f4.w : f4.z) * per[x][0], (mt ? f4.w : f4.z) * per[x][1]};
           float e[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             e[i] = at_exp2(__fmaf_rn(s[x][mt][i] - base[i & 1], cs, Q8_SHIFT));
             sum[i & 1] += e[i];
-            e[i] *= vs[mt];
+            e[i] *= vs[i & 1];
           }
           w[x][mt][0] = q8_transpose(Half2<__half>::narrow(e[0], e[1]));
           w[x][mt][1] = q8_transpose(Half2<__half>::narrow(e[2], e[3]));
@@ -428,14 +457,14 @@ attention_decode_q8_kernel(const __grid_constant__ CUtensorMap tmK,
         if (rr >= rows) continue;
         if (!whole && lane < 4) p.ml[slot + rr] = make_float2(w.mx[x][i], w.l[x][i]);
         if (e0 >= c.head_dim) continue;
-        const float f = whole ? w.sv / w.l[x][i] : w.sv;
+        const float unit = q8_inverse(w.per[x][i]), f = whole ? 1.f / w.l[x][i] : 1.f;
         char* out = a.out.data + seq * a.out.token_b + (head0 + rr) * a.out.head_b + 2 * e0;
         float* piece = p.o + (slot + rr) * p.hd_pad + e0;
 #pragma unroll
         for (int b = 0; b < S::VB; b += 8) {
           float y[8];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) y[k] = w.out(x, i, b + k) * f;
+          for (int k = 0; k < 8; ++k) y[k] = w.out(x, i, b + k) * f * unit;
           if (whole) {
             *reinterpret_cast<uint4*>(out + 2 * b) = narrow8<E>(y);
           } else {
@@ -508,11 +537,12 @@ attention_decode_q8_cluster_kernel(const __grid_constant__ CUtensorMap tmK,
         s_l[warp][rr] = ok ? w.l[x][i] : 0.f;
       }
       if (rr >= rows) continue;
+      const float unit = q8_inverse(w.per[x][i]);
 #pragma unroll
       for (int b = 0; b < S::VB; b += 4)
         *reinterpret_cast<float4*>(out_s + rr * HD + S::VB * (lane >> 2) + b) =
-            make_float4(w.out(x, i, b) * w.sv, w.out(x, i, b + 1) * w.sv,
-                        w.out(x, i, b + 2) * w.sv, w.out(x, i, b + 3) * w.sv);
+            make_float4(w.out(x, i, b) * unit, w.out(x, i, b + 1) * unit,
+                        w.out(x, i, b + 2) * unit, w.out(x, i, b + 3) * unit);
     }
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");

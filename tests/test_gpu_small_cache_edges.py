@@ -1,10 +1,11 @@
-"""The calls that make the cache smaller at the edges of their numbers: keys of zeros behind a norm."""
+"""The calls that make the cache smaller at the edges of their numbers: keys of zeros behind a norm,
+scales below zero, values that are far apart in size."""
 import pytest
 import torch
 
 from tests import attention_ref as R
 from tests import small_cache_ref as S
-from tests.test_gpu_small_cache import CODES, cache
+from tests.test_gpu_small_cache import CODES, batch, cache
 
 pytestmark = pytest.mark.gpu
 
@@ -101,3 +102,86 @@ def test_append_of_the_smallest_keys_behind_a_norm(sls, n, code):
     qkv[:, H:2 * H] = qkv[:, H:2 * H].sign() * 2.0 ** -128
     appended(sls, b, qkv.bfloat16(), H, torch.ones(hd, device="cuda").bfloat16(), None, None, False,
              1e-6)
+
+
+# ---------------------------------------------------------------------------
+# scales of either sign
+# ---------------------------------------------------------------------------
+
+def turned_over(b, seed):
+    """The same values with the codes and scales of some blocks negated: all of sequence 0's, half of
+    the others'."""
+    out = dict(b)
+    g = torch.Generator("cpu").manual_seed(seed)
+    for x in "kv":
+        sc = b[x + "_scale"]
+        over = torch.rand(sc.shape, generator=g).to(sc.device) < 0.5
+        over[b["table"][0][b["table"][0] < sc.shape[0]].long()] = True
+        rows = over.repeat_interleave(b["block"], 1)[..., None]
+        c = b[x].view(torch.uint8)
+        neg = (-b[x]).view(torch.uint8) if b[x].dtype == torch.int8 else c ^ 0x80
+        out[x] = torch.where(rows, neg, c).view(b[x].dtype)
+        out[x + "_scale"] = torch.where(over, -sc, sc)
+    return out
+
+
+@pytest.mark.parametrize("code", CODES)
+def test_scales_below_zero_attended(sls, code):
+    new, m, page, block = [3, 20, 1], [70, 200, 900], 32, 16
+    b = batch(new, m, 8, 2, 64, page, block, torch.bfloat16, code, seed=41)
+    t = turned_over(b, 1)
+    want, bound = R.attention(S.plain(b))
+    S.check(sls.attention_prefill_q8(b["q"], *cache(t), b["cu"]), want, bound, "prefill")
+    w = torch.zeros(b["k"].shape[0], 2, page, device="cuda")
+    sums, err = S.weights(S.plain(b), w)
+    sls.attention_weights(b["q"], t["k"], b["table"], b["kv_lens"], w, cu_seqlens=b["cu"],
+                          k_scale=t["k_scale"])
+    S.check(w, sums, err, "weights")
+    for many in (1, 40):       # clusters, and parts with pieces
+        last = b["q"][b["cu"][1:].long() - 1].repeat(many, 1, 1)
+        big = {k: t[k].repeat(many, 1) if k == "table" else t[k].repeat(many) for k in ("table", "kv_lens")}
+        ref = dict(S.plain(b), q=last[:3], new=[1] * 3)
+        want, bound = R.attention(ref, causal=False)
+        got = sls.attention_decode_q8(last, t["k"], t["v"], t["k_scale"], t["v_scale"], big["table"],
+                                      big["kv_lens"])
+        S.check(got, want.repeat(many, 1, 1), bound.repeat(many, 1, 1), "decode")
+
+
+# ---------------------------------------------------------------------------
+# values far apart
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("B", [2, 64])                  # clusters, and parts with pieces
+@pytest.mark.parametrize("where", [0, 1, 18, 37])       # block of sixteen among 37.5
+def test_decode_of_large_values_that_one_head_sees(sls, where, B, code):
+    """A block of values 2^40 times the others', which one query head of a key head looks at and the
+    other (its weights there 2^-60 and less) does not: the other's result keeps its bits."""
+    H, hd, m, page = 8, 64, 600, 16
+    b = batch([1] * B, [m] * B, 2 * H, H, hd, page, 16, torch.bfloat16, code, seed=where)
+    g = torch.Generator("cuda").manual_seed(9)
+    u = torch.randn(B, H, hd, generator=g, device="cuda").sign()
+    b["q"] = torch.stack([2 * u, -2 * u], 2).view(B, 2 * H, hd).bfloat16()
+    used = min(16, m - 16 * where)
+    for s in range(B):
+        pg = int(b["table"][s, where])
+        b["k"].view(torch.uint8)[pg, :used] = (96 * u[s]).to(code).view(torch.uint8)
+        b["k_scale"][pg, 0] = 2.0 ** -5
+        b["v_scale"][pg, 0] *= 2.0 ** 40
+    want, bound = R.attention(S.plain(b), causal=False)
+    # R.attention counts a float16 weight's 11 bits, not its least step (its 16-bit weights of bfloat16
+    # have none): a weight times its value's scale, in units U of its head, is off by half of 2^-24; times
+    # code and unit, over a sum of at least 2^15 (the largest weight is 2^15): 2^-40 U |code| a token.  U
+    # is at most 16 times the scales that the head needs, rounded up to a power of two: 32 of the largest
+    # scale, that of the block left out where the head's weights there, below 2^-60, need less than 1 / 16
+    # of it.  (An element that is 0 where the head looks shows this: what is left of 600 tokens of 2^-30.)
+    tiny = torch.zeros_like(bound)
+    for s in range(B):
+        pages = b["table"][s, :-(-m // page)].long()
+        sc = b["v_scale"][pages, 0].double()                                   # blocks x key heads
+        codes = torch.nan_to_num(S.values(b, "v")[pages], nan=0.0) / sc[:, None, :, None]
+        total = codes.abs().sum((0, 1))                                       # key heads x elements
+        other = torch.cat([sc[:where], sc[where + 1:]]).amax(0)
+        unit = 32 * torch.stack([sc.amax(0), other], 1)                       # key heads x query heads
+        tiny[s] = (2.0 ** -40 * unit[:, :, None] * total[:, None]).view(2 * H, hd)
+    S.check(sls.attention_decode_q8(b["q"], *cache(b)), want, bound + tiny, "decode")
