@@ -630,8 +630,8 @@ int sls_attention_prefill_q8(const sls_rows_t* q, int64_t T, int q_heads,
 
 /*
  * sls_attention_decode over a cache of codes; q and out are of `dtype`.  Scales of values may be
- * at most 2^126 in size.  A weight times its value's scale is held in float16: 11 bits of it, and half of
- * 2^-24 of a unit that is at most 32 times the largest one of its query head, or 32 times the largest scale.
+ * at most 2^126 in size.  Weights times values' scales are held in float16: to 11 bits, or to 2^-40 of a
+ * unit that is less than 32 times the largest of them of the query head.
  */
 size_t sls_attention_decode_q8_workspace_size(int q_heads, const sls_kv_cache_t* cache,
                                               const sls_kv_scales_t* scales, int dtype);

@@ -40,13 +40,13 @@ SLS_DEV float q8_power(float x) {
 // The unit of a head's weights (times values' scales) from this step on, a power of two.  None of
 // them may be larger; a much larger unit costs their float16 bits, and all of them past 2^39.  So it
 // goes by what a step needs, most = its largest weight times scale, and not by its scales alone: tokens
-// that the head does not look at may have any (2^40 times the others' made its results zeros).  For a
-// common spread of scales, up to 16, it takes the step's largest scale all the same, and rises seldom.
-// was: the unit before, shrink: what the earlier weights are multiplied by now.  The unit stays
-// within 2^126 of the step's scales, so that no scale in units overflows.
+// that the head does not look at may have any (2^40 times the others' made its results zeros).  Within
+// 16 of that it takes the step's largest scale all the same, and rises seldom: a unit is less than 32
+// times what is needed.  was: the unit before, shrink: what the earlier weights are multiplied by now.
+// The unit stays within 2^126 of the step's scales, so that no scale in units overflows.
 SLS_DEV float q8_unit(float was, float shrink, float scale, float most) {
-  float u = fmaxf(was * shrink, fminf(was, scale));
-  if (scale > u) u = scale <= 16.f * u ? scale : fmaxf(fmaxf(u, most), scale * 0x1p-126f);
+  float u = fmaxf(was * shrink, fminf(was, most));
+  if (scale > u) u = scale <= 16.f * most ? scale : fmaxf(fmaxf(u, most), scale * 0x1p-126f);
   return q8_power(u);
 }
 
