@@ -596,11 +596,11 @@ typedef struct sls_kv_weights {
  * q_out and the weights are of `dtype` (SLS_BF16 or SLS_F16).  For every block
  * of slots and key head that takes new tokens, in float32:
  *   a  = largest |y| of the new tokens' finite elements
- *   s' = max(s, 2^e), 2^e the least power of two >= 2^-126 with a <= Q 2^e,
+ *   s' = max(|s|, 2^e), 2^e the least power of two >= 2^-126 with a <= Q 2^e,
  *        Q = 127 or 448; s the block's scale if it holds earlier tokens of the
  *        sequence, else 0
  *   codes round(y / s') (to nearest even), infinities as +-Q, NaN as NaN (E4M3)
- *   or 0 (I8); where s' > s the earlier tokens' codes c become round(c s / s').
+ *   or 0 (I8); where s' is not s the earlier tokens' codes c become round(c s / s').
  * So the scales that this call makes are powers of two.  Slots of the block past
  * the sequence's end are left as they are.  Two sequences must not append to the
  * same block.  Errors: as sls_qkv_append, and INVALID_ARG / UNSUPPORTED for

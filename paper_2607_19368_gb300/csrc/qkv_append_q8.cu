@@ -1,8 +1,8 @@
 // New keys (normalised, rotated) and values as 8-bit codes: a power-of-two scale for each block
 // of a page's slots and key head,
-//   s' = max(s, 2^e), 2^e the least with max|y| <= Q 2^e,   c = round(y / s'),
-// s the scale of a block that holds earlier tokens, whose codes c become round(c s / s') when
-// it grows.
+//   s' = max(|s|, 2^e), 2^e the least with max|y| <= Q 2^e,   c = round(y / s'),
+// s the scale of a block that holds earlier tokens, whose codes c become round(c s / s') where that
+// is not s.
 //
 // A CTA takes blocks whose first new token lies among its `tile` packed tokens, one after the
 // other, and all or a share of their heads: cosines and sines are formed once for all heads.
@@ -303,7 +303,7 @@ SLS_DEV void q8_few(const Q8Lane<E, L, MODE>& me, const Q8Block& b) {
     for (int o = L / 2; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(me.mates, most, o));
     float* sp = b.scales + j * b.scale_head;
     const float was = b.lo > 0 ? *sp : 0.f;
-    const float now = fmaxf(q8_scale(b.ints, most), was), by = q8_over(now);
+    const float now = fmaxf(q8_scale(b.ints, most), fabsf(was)), by = q8_over(now);
     char* d = b.codes + j * b.code_head_b;
 #pragma unroll 1
     for (int slot = b.lo; slot < b.hi; ++slot) {
@@ -313,7 +313,7 @@ SLS_DEV void q8_few(const Q8Lane<E, L, MODE>& me, const Q8Block& b) {
       }
       if (me.on) me.store(d + slot * b.slot_b, q8_row_codes(b.ints, y, norm, by));
     }
-    if (me.on && now > was)
+    if (me.on && now != was)
 #pragma unroll 1
       for (int slot = 0; slot < b.lo; ++slot) q8_again(me, b.ints, d + slot * b.slot_b, was * by);
     __syncwarp(me.mates);  // every lane has read the old scale
@@ -391,7 +391,7 @@ SLS_DEV void q8_many(const Q8Lane<E, L, MODE>& me, const Q8Block& b, int j, bool
     __syncwarp();
   }
   if (!live) return;
-  const float now = fmaxf(q8_scale(b.ints, most), was), by = q8_over(now);
+  const float now = fmaxf(q8_scale(b.ints, most), fabsf(was)), by = q8_over(now);
   char* const d = b.codes + j * b.code_head_b;
 #pragma unroll 1
   for (int s = slot0; s - lane / L < b.hi; s += 2 * step) {
@@ -409,7 +409,7 @@ SLS_DEV void q8_many(const Q8Lane<E, L, MODE>& me, const Q8Block& b, int j, bool
         float y[16], again = 0.f;
         const float norm = me.template row<KEYS>(u[k], p + slot * b.token_b, slot, y, again, norms + slot);
         if (me.on) me.store(d + slot * b.slot_b, q8_row_codes(b.ints, y, norm, by));
-      } else if (me.on && now > was) {
+      } else if (me.on && now != was) {
         q8_again(me, b.ints, d + slot * b.slot_b, was * by);
       }
     }

@@ -147,6 +147,25 @@ def test_scales_below_zero_attended(sls, code):
         S.check(got, want.repeat(many, 1, 1), bound.repeat(many, 1, 1), "decode")
 
 
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("size", [0.01, 100.0])
+@pytest.mark.parametrize("n", [1, 12])
+def test_scales_below_zero_appended_to(sls, n, size, code):
+    """A block that holds earlier tokens takes the size of its scale, and their codes its sign."""
+    new, m, H, hd, page, block = [n] * 3, [n + 5, n + 27, n + 44], 4, 64, 32, 16
+    b = only_earlier(new, m, H, hd, page, block, torch.bfloat16, code, seed=43)
+    t = turned_over(b, 2)
+    g = torch.Generator("cuda").manual_seed(5)
+    x = (size * torch.randn(sum(new), 3 * H, hd, generator=g, device="cuda")).bfloat16()
+    for c in (b, t):
+        sls.qkv_append_q8(x[:, :H], x[:, H:2 * H], x[:, 2 * H:], *cache(c), cu_seqlens=b["cu"])
+    for i in "kv":
+        assert torch.equal(S.values(t, i).nan_to_num(7.0), S.values(b, i).nan_to_num(7.0)), i
+        for s, length in enumerate(m):
+            at = b["table"][s, (length - 1) // page].long(), (length - 1) % page // block
+            assert torch.equal(t[i + "_scale"][at], b[i + "_scale"][at])
+
+
 # ---------------------------------------------------------------------------
 # values far apart
 # ---------------------------------------------------------------------------
