@@ -565,9 +565,10 @@ int sls_attention_status(void* stream);
  * A cache of codes is an sls_kv_cache_t whose dtype is SLS_I8 (codes -127..127)
  * or SLS_E4M3 (at most 448; no infinities), with a float32 scale for each block
  * of `block` consecutive slots of a page and key head, for keys and for values:
- * an element stands for code * scale.  head_dim is then a multiple of 16, and
- * strides (in elements) are multiples of 16.  Lengths, page tables, page numbers
- * outside the cache and slots that no length covers are as above.
+ * an element stands for code * scale.  The calls take scales of either sign.
+ * head_dim is then a multiple of 16, and strides (in elements) are multiples of 16.
+ * Lengths, page tables, page numbers outside the cache and slots that no length
+ * covers are as above.
  * ---------------------------------------------------------------------------
  */
 #define SLS_I8 3               /* 8-bit integers */
@@ -667,8 +668,8 @@ int sls_attention_weights(const sls_rows_t* q, int64_t T, int q_heads,
  * counts as less than any number).  What stays moves to indices 0 .. keep - 1 in its
  * order: keys, values and weights.  Weights of the indices past them become 0,
  * keys and values there are left as they are, kv_lens (that of `cache`, which is
- * written) becomes keep.  In a cache of codes a block takes the largest of the scales
- * that its tokens come from, s', and their codes become round(c s / s').
+ * written) becomes keep.  In a cache of codes a block takes the size of the largest of the
+ * scales that its tokens come from, s', and their codes become round(c s / s').
  * kept: B x kv_heads x keep int32, the indices that stayed, ascending; of a
  * shorter sequence, which is left alone, all of its own and then -1.
  * Rotated keys keep their angles: give sls_qkv_append the positions of later

@@ -372,7 +372,7 @@ cache_evict_move_kernel(const __grid_constant__ EvictArgs a) {
         for (int m = 0; m < S::MATS; ++m)
           x[m][i] = *reinterpret_cast<const uint4*>(mat[m] + from + 16 * (at - row * vecs));
     }
-    float now[S::MATS];  // codes: of thread `row`'s block, the largest scale that its rows come from
+    float now[S::MATS];  // codes: of thread `row`'s block, the size of the largest scale that its rows come from
     if constexpr (S::CODES) {
       const int row = threadIdx.x;
       if (row < n) {
@@ -380,7 +380,7 @@ cache_evict_move_kernel(const __grid_constant__ EvictArgs a) {
 #pragma unroll
         for (int m = 0; m < S::MATS; ++m) {
           now[m] = 0.f;
-          for (int k = b0; k < b1; ++k) now[m] = fmaxf(now[m], s_was[m][k]);
+          for (int k = b0; k < b1; ++k) now[m] = fmaxf(now[m], fabsf(s_was[m][k]));
           const float was = s_was[m][row];
           s_by[m][row] = was == now[m] ? 1.f : now[m] > 0.f ? was / now[m] : 0.f;
         }

@@ -166,6 +166,25 @@ def test_scales_below_zero_appended_to(sls, n, size, code):
             assert torch.equal(t[i + "_scale"][at], b[i + "_scale"][at])
 
 
+@pytest.mark.parametrize("code", CODES)
+def test_scales_below_zero_evicted(sls, code):
+    m, page, block, keep = [300, 20, 90], 32, 16, 41
+    b = batch([1] * 3, m, 2, 2, 64, page, block, torch.bfloat16, code, seed=44)
+    t = turned_over(b, 3)
+    t["kv_lens"] = b["kv_lens"].clone()
+    w = torch.rand(b["k"].shape[0], 2, page, device="cuda")
+    got = []
+    for c in (b, t):
+        got.append(sls.cache_evict(c["k"], c["v"], c["table"], c["kv_lens"], w.clone(), keep, first=3,
+                                   last=9, k_scale=c["k_scale"], v_scale=c["v_scale"]))
+    assert torch.equal(*got)
+    for i in "kv":
+        a, z = S.values(b, i), S.values(t, i)
+        for s, length in enumerate(m):
+            n = min(length, keep)
+            assert torch.equal(R.gather(a, b["table"][s], n, page), R.gather(z, b["table"][s], n, page))
+
+
 # ---------------------------------------------------------------------------
 # values far apart
 # ---------------------------------------------------------------------------
