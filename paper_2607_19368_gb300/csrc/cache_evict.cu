@@ -192,6 +192,9 @@ cache_evict_select_kernel(const __grid_constant__ EvictArgs a, int room4) {
   unsigned need = (unsigned)(a.keep - a.first - a.last);
   uint32_t top = 0, mask = 0;
   __syncthreads();
+  // Another CTA's shared memory may be written once that CTA runs: a digit's barrier says so, and where
+  // the first and last tokens are all that stays this one.
+  if (need == 0) ev_cluster_sync();
 #pragma unroll 1
   for (int pass = 0; pass < 3 && need > 0; ++pass) {
     const int shift = ev_shift(pass);

@@ -223,3 +223,40 @@ def test_decode_of_large_values_that_one_head_sees(sls, where, B, code):
         unit = 32 * torch.stack([sc.amax(0), other], 1)                       # key heads x query heads
         tiny[s] = (2.0 ** -40 * unit[:, :, None] * total[:, None]).view(2 * H, hd)
     S.check(sls.attention_decode_q8(b["q"], *cache(b)), want, bound + tiny, "decode")
+
+
+# ---------------------------------------------------------------------------
+# eviction that leaves no choice
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("lengths", [[3000], [20000, 70, 9000], [131072], [400000]])
+@pytest.mark.parametrize("first,last", [(4, 60), (0, 2049), (33, 0), (0, 0)])
+def test_evict_to_the_first_and_last(sls, lengths, first, last):
+    """No weight decides: sinks and a recent window stay, or nothing, by clusters of every size (two
+    to eight CTAs for three sequences and for one) and past what they hold."""
+    page, Hkv, hd, keep = 128, 2, 16, first + last
+    B, per = len(lengths), [-(-m // page) for m in lengths]
+    g = torch.Generator("cuda").manual_seed(sum(lengths))
+    table = torch.zeros(B, max(per), dtype=torch.int32, device="cuda")
+    order = torch.randperm(sum(per), generator=g, device="cuda").int()
+    for s in range(B):
+        table[s, :per[s]] = order[sum(per[:s]):sum(per[:s + 1])]
+    n = sum(per)
+    k = torch.randint(-99, 99, (n, page, Hkv, hd), generator=g, device="cuda").half()
+    v = torch.randint(-99, 99, (n, page, Hkv, hd), generator=g, device="cuda").half()
+    w = torch.rand(n, Hkv, page, generator=g, device="cuda") + 1
+    old = [t.clone() for t in (k, v, w.transpose(1, 2)[..., None])]
+    lens = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    kept = sls.cache_evict(k, v, table, lens, w, keep, first=first, last=last)
+    assert lens.tolist() == [min(m, keep) for m in lengths]
+    for s, m in enumerate(lengths):
+        i = torch.arange(m, device="cuda")
+        stay = i if m <= keep else torch.cat([i[:first], i[m - last:]])
+        want = torch.full((keep,), -1, device="cuda")
+        want[:stay.numel()] = stay
+        assert (kept[s].long() == want).all()
+        for a, b in zip(old, (k, v, w.transpose(1, 2)[..., None])):
+            a, b = R.gather(a, table[s], m, page), R.gather(b, table[s], m, page)
+            assert torch.equal(b[:stay.numel()], a[stay])
+        if m > keep:
+            assert not b[keep:].any()
