@@ -501,8 +501,9 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
   __shared__ __align__(16) float2 s_row[2 * AW_TILE];  // factor and summand of a row's exponents
   __shared__ __align__(16) float s_inv[2 * AW_TILE];   // factor of its weights
   __shared__ __align__(16) int s_see[2 * AW_TILE];     // tokens that it sees
-  // of two units: a thread may still read its token's when another fetches the next unit's
-  __shared__ float s_scale[2][AW_TILE], s_sum[AW_TILE];
+  // of two units: a thread may still read its token's when another fetches the next unit's, or has
+  // added it up (a head's last unit comes without a barrier before its sums)
+  __shared__ float s_scale[2][AW_TILE], s_sum[2][AW_TILE];
   __shared__ uint64_t bar[2];
   __shared__ uint32_t holder;
   const CacheView& c = a.c;
@@ -693,7 +694,7 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
       if (live[1]) add(1, a1.count, start, mine);
     }
     const float sum = (col[0] + col[1]) + (col[2] + col[3]);
-    if (warp >= 4) s_sum[r] = sum;
+    if (warp >= 4) s_sum[t & 1][r] = sum;
     // and the second tile's columns are read
     ok = __syncthreads_and(ok);
     if (!ok) {
@@ -702,7 +703,7 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
     }
     if (same) issue(1, w, r1, key0);
     begin = !same;
-    if (to) *to = was + (sum + s_sum[r]);
+    if (to) *to = was + (sum + s_sum[t & 1][r]);
   }
   aw_free<2 * AW_TILE>(tmem);
 }

@@ -260,3 +260,27 @@ def test_evict_to_the_first_and_last(sls, lengths, first, last):
             assert torch.equal(b[:stay.numel()], a[stay])
         if m > keep:
             assert not b[keep:].any()
+
+
+# ---------------------------------------------------------------------------
+# weights
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("code", [None] + CODES)
+def test_weights_repeat_themselves(sls, code):
+    """CTAs that go through several tiles of tokens, of one tile of rows or two, and over the ends of
+    heads: right, and the same bits a hundred times."""
+    new, m, Hq, Hkv, hd, page = [24, 40, 20], [14000, 9000, 5000], 16, 4, 64, 64
+    b = R.make_batch(new, m, Hq, Hkv, hd, page, torch.bfloat16, seed=51)
+    p, scale = b, None
+    if code is not None:
+        b = S.codes_of(b, code, 32, seed=51)
+        p, scale = S.plain(b), b["k_scale"]
+    zero = torch.zeros(b["k"].shape[0], Hkv, page, device="cuda")
+    want, bound = S.weights(p, zero)
+    sums = []
+    for _ in range(100):
+        sums.append(sls.attention_weights(b["q"], b["k"], b["table"], b["kv_lens"], zero.clone(),
+                                          cu_seqlens=b["cu"], k_scale=scale))
+    S.check(sums[0], want, bound, "weights")
+    assert all(torch.equal(sums[0], w) for w in sums[1:])
