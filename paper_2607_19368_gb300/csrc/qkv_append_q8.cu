@@ -381,9 +381,10 @@ SLS_DEV void q8_many(const Q8Lane<E, L, MODE>& me, const Q8Block& b, int j, bool
   float* const sp = b.scales + j * b.scale_head;
   const float was = live && b.lo > 0 ? *sp : 0.f;
   if (share > 1) {
-    // the old scale is read in front of the barrier, behind which it is written
+    // A barrier of the head's warps alone: another's may be at values, whose code is a copy of its own.
+    // The old scale is read in front of it, and written behind it.
     if (lane == 0) s_most[parity][warp] = most;
-    __syncthreads();
+    named_sync(1 + warp / share, 32 * share);
     const float each = s_most[parity][(warp & ~(share - 1)) + (lane & (share - 1))];
     most = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(each)));
     parity ^= 1;

@@ -104,6 +104,28 @@ def test_append_of_the_smallest_keys_behind_a_norm(sls, n, code):
              1e-6)
 
 
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("block", [16, 64, 128])
+@pytest.mark.parametrize("H,hd", [(1, 128), (3, 64), (5, 128), (7, 64)])
+def test_append_where_keys_and_values_share_a_block_of_threads(sls, H, hd, block, code):
+    """Few blocks, so that several warps have a head: the last key head's beside the first value
+    head's, some without a head at the end.  Right, and the same bits twenty times."""
+    new, m = [150, 70], [150, 211]
+    b = only_earlier(new, m, H, hd, 128, block, torch.bfloat16, code, seed=61)
+    g = torch.Generator("cuda").manual_seed(5)
+    qkv = torch.randn(sum(new), 3 * H, hd, generator=g, device="cuda").bfloat16()
+    norm = (1 + 0.2 * torch.randn(hd, generator=g, device="cuda")).bfloat16()
+    rope = sls.Rope.make(hd)
+    names = ("k", "v", "k_scale", "v_scale")
+    before = {x: b[x].clone() for x in names}
+    appended(sls, b, qkv, H, norm, rope, rope.inv_freq, False, 1e-6)
+    for _ in range(20):
+        c = dict(b, **{x: before[x].clone() for x in names})
+        sls.qkv_append_q8(qkv[:, :H], qkv[:, H:2 * H], qkv[:, 2 * H:], *cache(c), cu_seqlens=b["cu"],
+                          q_weight=norm, k_weight=norm, eps=1e-6, rope=rope)
+        assert all(torch.equal(c[x].view(torch.uint8), b[x].view(torch.uint8)) for x in names)
+
+
 # ---------------------------------------------------------------------------
 # scales of either sign
 # ---------------------------------------------------------------------------
