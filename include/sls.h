@@ -651,6 +651,10 @@ int sls_attention_decode_q8(const sls_rows_t* q, int q_heads, const sls_kv_cache
  * fixed order.  A page must belong to one sequence; weights of a page outside
  * the cache are dropped.  A row with a score that is NaN or +infinity leaves NaN in
  * the sums of the tokens that it sees; a score of -infinity is a weight of 0.
+ * Workspace: up to 32 rows (tokens times query heads of a key head) a sequence on
+ * average, 4 bytes for every row, key head and token that the page table has room for,
+ * where that is at most 1 GiB; else 8 bytes a row and key head, and less than 2 MiB.
+ * So a smaller T may want more than a larger one.
  * Errors: as sls_attention_prefill, and INVALID_ARG for weights.
  */
 size_t sls_attention_weights_workspace_size(int64_t T, int q_heads, const sls_kv_cache_t* cache,

@@ -4,7 +4,8 @@
 // Bound by HBM bandwidth.  The first launch is decode without values: a warp owns a key head of a
 // part of all sequences' steps of 32 tokens, keys are the 16-row operands and rows (token, query
 // head) the 8 columns, and scores go to the workspace, 4 bytes a row and token (four rows': a
-// sixteenth of a 16-bit key of 128 elements), with maximum and sum of every piece.  A sequence of
+// sixteenth of a 16-bit key of 128 elements; places for as many tokens as the page table holds), with
+// maximum and sum of every piece.  A sequence of
 // more rows is gone through again for each AF_ROWS of them.  The second launch has a thread for each
 // token: it joins the pieces of every row in order and adds up the row's weights.  32 sequences to
 // 4096 tokens, 32 + 8 heads of 128, bfloat16: 39.4 us, 3.9 TB/s of keys (31 us for the scores, in
@@ -21,6 +22,7 @@ namespace {
 constexpr int AF_SUM_T = 256;
 constexpr int AF_UNIT = 4 * AF_SUM_T;  // tokens of a CTA of the second launch
 constexpr int AF_AHEAD = 4;            // rows whose scores it fetches first
+constexpr int64_t AF_MOST_SCORES = (int64_t)1 << 28;
 
 // SIZE: bytes of an element of keys
 template <int HD, int SIZE>
@@ -512,11 +514,17 @@ int launch(const AttnArgs& a, const ScaleView& s, const WeightView& w, int code,
 
 // Up to 32 rows a sequence on average.  8 sequences to 8192 tokens, 8 key heads of 128, 4 / 8 / 16 /
 // 32 / 64 rows: bfloat16 keys 19 / 22 / 30 / 47 / 87 us here, 60 / 60 / 61 / 60 / 64 in two passes;
-// e4m3 15 / 19 / 27 / 45 / 80 and 52 / 52 / 53 / 50 / 55.
+// e4m3 15 / 19 / 27 / 45 / 80 and 52 / 52 / 53 / 50 / 55.  The average does for ragged rows too: 400
+// tokens of 32 + 8 heads in one sequence beside 63 single ones, 4096 cached each, 1316 us here (200
+// times through the one's keys), 2175 in two passes.
+//
+// Scores have places for all that the page table can hold, so that their room is what a wide table
+// costs: up to 1 GiB of them.  256 single tokens of 32 heads over up to 2048, a table of 131072: 359 us
+// here with 4 GiB, 558 in two passes without.
 bool attention_weights_few(const CacheView& c, int64_t T, int q_heads) {
-  const int64_t room = ((int64_t)c.max_pages << c.page_shift) / AF_UNIT + 1;
+  const int64_t room = (((int64_t)c.max_pages << c.page_shift) + AF_UNIT - 1) / AF_UNIT;
   return T * (q_heads / c.kv_heads) <= 32 * (int64_t)c.B && c.B * room <= 0x7fffffff &&
-         c.kv_heads <= 65535;
+         c.kv_heads <= 65535 && T * q_heads <= AF_MOST_SCORES / (room * AF_UNIT);
 }
 
 size_t attention_weights_few_workspace(const CacheView& c, int64_t T, int q_heads) {

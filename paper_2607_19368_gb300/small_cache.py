@@ -218,7 +218,8 @@ def attention_weights(q: torch.Tensor, cache_k: torch.Tensor, page_table: torch.
     queries (T x q_heads x head_dim, packed by cu_seqlens; None: one token per sequence) place
     on it, summed over the tokens and the head's query heads.  Rows see what they see in
     ``attention_prefill``: give the last few tokens of a prompt to let them alone vote.
-    cache_k is of q's type, or codes with k_scale.  Returns `weights`."""
+    cache_k is of q's type, or codes with k_scale.  For few rows the workspace goes by the
+    page table's width, up to 1 GiB.  Returns `weights`."""
     dtype = _query(q)
     c, (n, ps, H, hd), dt, dev, B, cols = _cache(cache_k, cache_k, page_table, kv_lens,
                                                  _ANY if k_scale is not None else _at._CODES)

@@ -306,3 +306,28 @@ def test_weights_repeat_themselves(sls, code):
                                           cu_seqlens=b["cu"], k_scale=scale))
     S.check(sums[0], want, bound, "weights")
     assert all(torch.equal(sums[0], w) for w in sums[1:])
+
+
+def test_workspace_of_weights_is_bounded(sls):
+    """A wide page table does not make a call of short sequences ask for gigabytes."""
+    from paper_2607_19368_gb300 import small_cache as C
+    for B, Hq, Hkv, hd, page, cols in [(256, 32, 8, 128, 64, 2048), (64, 12, 12, 64, 16, 8192),
+                                       (4096, 128, 1, 128, 128, 1024), (1, 40, 8, 128, 1024, 2 ** 20),
+                                       (65536, 128, 128, 64, 1024, 2 ** 20)]:
+        for T in (B, 2 * B, 32 * B):
+            size = C._bytes("weights", 0, 1, 0, (T, Hq, 1), (Hkv, hd, page, 1000, B, cols))
+            assert 0 < size <= 2 ** 30 + 2 ** 24 + 8 * T * Hq, (B, Hq, cols, T)
+
+
+@pytest.mark.parametrize("width", [1024, 131072])
+def test_weights_of_single_tokens_behind_a_wide_table(sls, width):
+    """The same sums whichever way the table's width sends the call."""
+    B, Hq, Hkv, hd, page = 40, 64, 2, 64, 32
+    m = [(37 * i) % 900 + 1 for i in range(B)]
+    b = R.make_batch([1] * B, m, Hq, Hkv, hd, page, torch.float16, seed=52)
+    table = torch.full((B, width // page), 1 << 29, dtype=torch.int32, device="cuda")
+    table[:, :b["table"].shape[1]] = b["table"][:, :table.shape[1]]
+    zero = torch.zeros(b["k"].shape[0], Hkv, page, device="cuda")
+    want, bound = S.weights(b, zero)
+    got = sls.attention_weights(b["q"], b["k"], table, b["kv_lens"], zero.clone())
+    S.check(got, want, bound, "weights")
