@@ -676,6 +676,10 @@ int sls_attention_weights(const sls_rows_t* q, int64_t T, int q_heads,
  * scales that its tokens come from, s', and their codes become round(c s / s').
  * kept: B x kv_heads x keep int32, the indices that stayed, ascending; of a
  * shorter sequence, which is left alone, all of its own and then -1.
+ * kv_lens is cut with the cache that it belongs to: where several caches (a model's
+ * layers) share their lengths, each call takes a copy of them as they were before the
+ * first.  Over lengths that are cut already the call leaves a cache as it is, longer than
+ * its lengths say, without an error.
  * Rotated keys keep their angles: give sls_qkv_append the positions of later
  * tokens, which kv_lens no longer tells.  A page must belong to one sequence.  A
  * page outside the cache reads as zeros (weights too) and is not written.

@@ -256,7 +256,9 @@ def cache_evict(cache_k: torch.Tensor, cache_v: torch.Tensor, page_table: torch.
     lowest index) and move to the front in their order: keys, values, weights and, for codes,
     scales.  kv_lens is cut too, weights behind it are zeroed.  Returns the indices that
     stayed (B x kv_heads x keep int32, ascending, -1 past a shorter sequence's end).  Give
-    later calls of ``qkv_append`` their positions: lengths no longer tell them."""
+    later calls of ``qkv_append`` their positions: lengths no longer tell them.
+    Layers that share kv_lens each want a copy of the lengths before the cut: over lengths
+    that are cut already the call leaves a layer's cache as it is."""
     eight = k_scale is not None
     c, (n, ps, H, _), _, dev, B, _ = _cache(cache_k, cache_v, page_table, kv_lens,
                                             _CODES8 if eight else _at._CODES)

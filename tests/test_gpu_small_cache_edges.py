@@ -331,3 +331,30 @@ def test_weights_of_single_tokens_behind_a_wide_table(sls, width):
     want, bound = S.weights(b, zero)
     got = sls.attention_weights(b["q"], b["k"], table, b["kv_lens"], zero.clone())
     S.check(got, want, bound, "weights")
+
+
+# ---------------------------------------------------------------------------
+# layers
+# ---------------------------------------------------------------------------
+
+def test_layers_that_share_their_lengths(sls):
+    """Each layer's cut takes a copy of the lengths before it; the lengths that are left are one."""
+    m, page, Hkv, hd, keep = [90, 12, 300], 16, 2, 32, 40
+    layers = [R.make_batch([1] * 3, m, Hkv, Hkv, hd, page, torch.float16, seed=7) for _ in range(3)]
+    lens, table = layers[0]["kv_lens"], layers[0]["table"]
+    after = None
+    for i, b in enumerate(layers):
+        g = torch.Generator("cpu").manual_seed(i)
+        w = torch.rand(b["k"].shape[0], Hkv, page, generator=g)
+        host = {k: (v.cpu() if torch.is_tensor(v) else v) for k, v in b.items()}
+        want = S.evict(host, w, keep, 2, 8)
+        w, after = w.cuda(), lens.clone()
+        kept = sls.cache_evict(b["k"], b["v"], table, after, w, keep, first=2, last=8)
+        assert torch.equal(kept.cpu(), want["kept"]) and torch.equal(w.cpu(), want["w"])
+        assert torch.equal(b["k"].cpu().view(torch.int16), want["k"])
+        assert after.tolist() == [40, 12, 40]
+    # over lengths that are cut already a layer is left alone
+    before = layers[0]["k"].clone()
+    kept = sls.cache_evict(layers[0]["k"], layers[0]["v"], table, after, w, keep, first=2, last=8)
+    assert torch.equal(layers[0]["k"].view(torch.int16), before.view(torch.int16))
+    assert after.tolist() == [40, 12, 40] and kept[0, 0].tolist() == list(range(40))
