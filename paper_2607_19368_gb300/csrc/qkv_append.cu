@@ -39,8 +39,9 @@ struct QaFactors {
   f32x2_t c0[4], s0[4], c1[4], s1[4];
 };
 
-// L lanes per row; heads of one token are shared by QA_T / (L tokens) groups of lanes
-template <typename E, int L, int MODE>
+// L lanes per row; heads of one token are shared by QA_T / (L tokens) groups of lanes.  BESIDE: queries
+// alone, see AppendArgs (as a condition at run time it cost the other form 0.6 us of 10717 tokens' 14.3).
+template <typename E, int L, int MODE, bool BESIDE>
 __global__ void __launch_bounds__(QA_T, 6)
 qkv_append_kernel(const __grid_constant__ AppendArgs a, int tokens, int heads_per_cta) {
   __shared__ float2 s_turn[QA_MAX_TOKENS][QA_MAX_PAIRS];  // (cos, sin) * scale
@@ -92,7 +93,7 @@ qkv_append_kernel(const __grid_constant__ AppendArgs a, int tokens, int heads_pe
     }
   };
   at_go();
-  if (!a.beside) at_wait_ahead();
+  if constexpr (!BESIDE) at_wait_ahead();
   const char* q_src = a.q.data + t * a.q.token_b;
   load(q_src, a.q.head_b, sq.first, tok < nt ? sq.end : 0);  // while the tokens are looked up
 
@@ -258,19 +259,21 @@ qkv_append_kernel(const __grid_constant__ AppendArgs a, int tokens, int heads_pe
   };
   turned(q_src, a.q.head_b, a.out.data + t * a.out.token_b, a.out.head_b, sq,
          reinterpret_cast<const E*>(a.q_weight), true);
-  if (slot >= 0) {
-    turned(a.k.data + t * a.k.token_b, a.k.head_b, c.k + slot, c.head_b, sk,
-           reinterpret_cast<const E*>(a.k_weight), false);
-    for (int h0 = sv.first; h0 < sv.end; h0 += stride) {
-      load(a.v.data + t * a.v.token_b, a.v.head_b, h0, sv.end);
-      store(c.v + slot, c.head_b, h0, sv.end);
-    }
+  if constexpr (BESIDE) {
+    // what follows waits for this launch, and so for the one beside it
+    at_wait_ahead();
+    return;
   }
-  // what follows waits for this launch, and so for the one beside it
-  if (a.beside) at_wait_ahead();
+  if (slot < 0) return;
+  turned(a.k.data + t * a.k.token_b, a.k.head_b, c.k + slot, c.head_b, sk,
+         reinterpret_cast<const E*>(a.k_weight), false);
+  for (int h0 = sv.first; h0 < sv.end; h0 += stride) {
+    load(a.v.data + t * a.v.token_b, a.v.head_b, h0, sv.end);
+    store(c.v + slot, c.head_b, h0, sv.end);
+  }
 }
 
-template <typename E>
+template <typename E, bool BESIDE>
 int launch(const AppendArgs& a, cudaStream_t stream) {
   const int heads = a.q_heads + 2 * a.c.kv_heads;
   const bool narrow = a.c.head_dim <= 64;
@@ -287,7 +290,7 @@ int launch(const AppendArgs& a, cudaStream_t stream) {
   const dim3 grid((unsigned)tiles, (unsigned)((heads + per - 1) / per));
   const int mode = a.interleaved ? QA_INTERLEAVED : (a.pairs & 7) ? QA_ODD : QA_PAIRED;
 #define QA_LAUNCH(L, MODE) \
-  return at_launch(qkv_append_kernel<E, L, MODE>, grid, QA_T, 0, 1, stream, a, tokens, per)
+  return at_launch(qkv_append_kernel<E, L, MODE, BESIDE>, grid, QA_T, 0, 1, stream, a, tokens, per)
   if (narrow) {
     if (mode == QA_PAIRED) QA_LAUNCH(4, QA_PAIRED);
     else if (mode == QA_INTERLEAVED) QA_LAUNCH(4, QA_INTERLEAVED);
@@ -304,7 +307,9 @@ int launch(const AppendArgs& a, cudaStream_t stream) {
 
 int launch_qkv_append(const AppendArgs& a, int dtype, cudaStream_t stream) {
   if (a.T == 0) return SLS_OK;
-  return dtype == SLS_BF16 ? launch<__nv_bfloat16>(a, stream) : launch<__half>(a, stream);
+  if (a.beside)
+    return dtype == SLS_BF16 ? launch<__nv_bfloat16, true>(a, stream) : launch<__half, true>(a, stream);
+  return dtype == SLS_BF16 ? launch<__nv_bfloat16, false>(a, stream) : launch<__half, false>(a, stream);
 }
 
 }  // namespace sls
