@@ -407,6 +407,8 @@ attention_weights_rows_kernel(const __grid_constant__ AttnArgs a,
     ok = __syncthreads_and(ok);
     if (!ok) {
       if (threadIdx.x == 0) atomicExch(status, SLS_ERR_TIMEOUT);
+      // the last products of both barriers end, or run out of time too, before their columns are freed
+      for (unsigned k = 1; k <= min(turn, 2u); ++k) mbar_wait(&bar[(turn - k) & 1], ((turn - k) >> 1) & 1);
       break;
     }
     if (warp >= 4) s_ml[r] = make_float2(m, l);
@@ -699,6 +701,9 @@ attention_weights_sum_kernel(const __grid_constant__ AttnArgs a, const __grid_co
     ok = __syncthreads_and(ok);
     if (!ok) {
       if (threadIdx.x == 0) atomicExch(status, SLS_ERR_TIMEOUT);
+      // as in the first pass; the next unit's first products are issued where it is the same head's
+      for (int i = 0; i < 2; ++i) mbar_wait(&bar[i], phase[i] ^ 1);
+      if (same && live[0]) mbar_wait(&bar[0], phase[0]);
       break;
     }
     if (same) issue(1, w, r1, key0);
