@@ -126,6 +126,38 @@ def test_append_where_keys_and_values_share_a_block_of_threads(sls, H, hd, block
         assert all(torch.equal(c[x].view(torch.uint8), b[x].view(torch.uint8)) for x in names)
 
 
+@pytest.mark.parametrize("code", CODES)
+def test_append_and_decode_of_a_padded_batch(sls, code):
+    """Places of a batch without a sequence (length 0, a table row of any numbers) take and change
+    nothing; the others are as without them."""
+    m, H, hd, page, block = [9, 40, 17], 4, 64, 32, 16
+    b = only_earlier([1] * 3, m, H, hd, page, block, torch.bfloat16, code, seed=71)
+    g = torch.Generator("cuda").manual_seed(8)
+    qkv = torch.randn(7, 3 * H, hd, generator=g, device="cuda").bfloat16()
+    real = torch.tensor([1, 2, 5], device="cuda")
+    table = torch.randint(-9, 99, (7, b["table"].shape[1]), device="cuda").int()
+    table[real] = b["table"]
+    lens = torch.zeros(7, dtype=torch.int32, device="cuda")
+    lens[real] = b["kv_lens"]
+    names = ("k", "v", "k_scale", "v_scale")
+    c = dict(b, table=table, kv_lens=lens, **{x: b[x].clone() for x in names})
+    rope = sls.Rope.make(hd)
+    out = []
+    for d, x in ((b, qkv[real]), (c, qkv)):
+        q = sls.qkv_append_q8(x[:, :H], x[:, H:2 * H], x[:, 2 * H:], *cache(d), rope=rope)
+        w = torch.zeros(b["k"].shape[0], H, page, device="cuda")
+        sls.attention_weights(q, d["k"], d["table"], d["kv_lens"], w, k_scale=d["k_scale"])
+        out.append((q, sls.attention_decode_q8(q, *cache(d)), w))
+    assert all(torch.equal(b[x].view(torch.uint8), c[x].view(torch.uint8)) for x in names)
+    assert torch.equal(out[0][0], out[1][0][real])
+    rest = torch.tensor([0, 3, 4, 6], device="cuda")
+    assert not out[1][1][rest].any()
+    want, bound = R.attention(dict(S.plain(b), q=out[0][0]), causal=False)
+    S.check(out[1][1][real], want, bound, "decode")
+    sums, err = S.weights(dict(S.plain(b), q=out[0][0]), torch.zeros_like(out[1][2]))
+    S.check(out[1][2], sums, err, "weights")
+
+
 # ---------------------------------------------------------------------------
 # scales of either sign
 # ---------------------------------------------------------------------------
