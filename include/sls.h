@@ -633,6 +633,8 @@ int sls_attention_prefill_q8(const sls_rows_t* q, int64_t T, int q_heads,
  * sls_attention_decode over a cache of codes; q and out are of `dtype`.  Scales of values may be
  * at most 2^126 in size.  Weights times values' scales are held in float16: to 11 bits, or to 2^-40 of a
  * unit that is less than 32 times the largest of them of the query head.
+ * bfloat16 queries are taken to float16 by a power of two of each row, here and in
+ * sls_attention_weights over codes: what is below 2^-39 of a row's largest element is lost.
  */
 size_t sls_attention_decode_q8_workspace_size(int q_heads, const sls_kv_cache_t* cache,
                                               const sls_kv_scales_t* scales, int dtype);

@@ -3,12 +3,13 @@
 //
 // Bound by HBM bandwidth: 2 hd bytes a cached token and key head, against some 500 instructions
 // of a warp for each 32 tokens of a head, which take half of the issue slots.  64 streams to 8192
-// tokens, 32 + 8 heads of 128, int8 in pages of 16: 92.1 us, 5.5 TB/s; 3 to 131072, 40 + 8, e4m3:
-// 103.8 us, 5.8 TB/s; one of 2061 tokens 8.0 us, latency.  A warp owns a (sequence, key head) at a time, its parts
+// tokens, 32 + 8 heads of 128, int8 in pages of 16: 92.0 us, 5.5 TB/s; 3 to 131072, 40 + 8, e4m3:
+// 103.2 us, 5.8 TB/s; one of 2061 tokens 7.7 us, latency.  A warp owns a (sequence, key head) at a time, its parts
 // and pieces as in the 16-bit kernel, and multiplies float16 (every code is one exactly) by
 // mma.sync.  What the 8 bits change:
 //  * The scale of a block of tokens multiplies finished scores, and weights instead of values.  Weights
-//    are then in units of their own for each head, to stay in float16's range: see q8_unit.
+//    are then in units of their own for each head, to stay in float16's range: see q8_unit (64 streams
+//    91.9 us; with one unit for all heads, the largest scale so far, 90.9, but wrong for values far apart).
 //  * bfloat16 queries become float16 times a power of two for each row, which scores take back:
 //    exact down to 2^-31 of the row's largest element, and to 2^-39 of it below.
 //  * Keys and values are the 16-row operands, query heads the 8 columns (S^T = K Q^T, O^T = V^T

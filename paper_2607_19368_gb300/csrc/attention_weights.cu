@@ -18,7 +18,7 @@
 // bytes are below either from some ten rows on.  A CTA goes through phases in step (keys to shared
 // memory, codes to float16 on the way; products; scores), with the next keys on their way in
 // registers; two CTAs an SM fill each other's gaps.  32 rows (tokens) of 7 heads over 32768
-// tokens of 4 key heads, e4m3: 58.3 us, 24.0 the first pass and 34.5 the second (86 us with mma.sync,
+// tokens of 4 key heads, e4m3: 57.8 us, 24.0 the first pass and 34.5 the second (86 us with mma.sync,
 // whose products took the time); 58.7 million exponentials are 12 us at 16 a cycle and SM.  A CTA has
 // 7 tiles of a row tile, then 3.4 units of two: in a trace 9000 to 15000 of its 36000 and 46000
 // cycles go until the first scores (lengths, pages, rows), a tile's scores take 1700 to 2400.

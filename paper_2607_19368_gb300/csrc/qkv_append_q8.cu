@@ -16,9 +16,9 @@
 // this launch.
 //
 // Bound by memory in the limit; keys and values are held up by latency and instructions instead (16
-// warps an SM, 42% of issue slots, 19% of DRAM's rate in a profile of them alone), which the queries'
-// launch makes up for in part.  21345 tokens of 32 + 8 heads of 128, e4m3: 117.4 us, 4.1 TB/s; 10717
-// tokens of 25 + 5 heads of 64, int8: 20.4 us, 2.7 TB/s; 4 single tokens 4.2 us, latency.  In a trace
+// warps an SM, 41% of issue slots, 20% of DRAM's rate in a profile of them alone), which the queries'
+// launch makes up for in part.  21345 tokens of 32 + 8 heads of 128, e4m3: 113.9 us, 4.2 TB/s; 10717
+// tokens of 25 + 5 heads of 64, int8: 18.6 us, 2.9 TB/s; 4 single tokens 3.9 us, latency.  In a trace
 // of the first a CTA of keys forms its factors in 9000 cycles and goes over its rows in 31000 and
 // 15000, one of values in 16000 and 9000.
 #include <algorithm>
